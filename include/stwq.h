@@ -9,6 +9,7 @@
  *   online    stwq_quantize    X -> int8 codes with the static scales     (Eq. 1, Eq. 2, Section 4.2)
  *   online    qlinear          quantize -> int8 GEMM -> dequantize (+bias, +GELU)
  *   online    qlinear_q        the same from precomputed codes
+ *   serving   page_plan, kv_append_paged, paged_attention, sample_tokens   (a decoder's step over a paged cache)
  * and, beside the path: chained layers, bf16 activations, the asymmetric quantizer, the dynamic
  * token-wise baseline, packed 4-bit weights, quantized attention with a quantized KV cache, and the
  * selection of calibration samples (each documented at its declaration below).
@@ -60,8 +61,10 @@ enum {
     STWQ_ERR_POS_RANGE = -8,      /* a pos_id was outside [0,P); that row was written as 0   */
     STWQ_ERR_NONFINITE = -9,      /* calibration saw NaN or Inf                              */
     STWQ_ERR_NOMEM = -10,         /* workspace allocation failed                             */
-    STWQ_ERR_CAPTURE = -11        /* the call would have to (re)allocate workspace while its stream is being
+    STWQ_ERR_CAPTURE = -11,       /* the call would have to (re)allocate workspace while its stream is being
                                      captured into a CUDA graph; reserve the workspace before capturing */
+    STWQ_ERR_PAGES = -12          /* page bookkeeping saw a length, page id, slot or table entry out of range
+                                     (the call's description says what it did instead)      */
 };
 
 /*
@@ -357,6 +360,81 @@ int qattn_pv(stwq_ctx* ctx, const uint8_t* Pq, int G, int Tq, int Tk_pad, int d,
              const float* s_v, const float* delta_p, int out_dtype, void* O, void* stream);
 
 /*
+ * Serving a batch of requests over a paged KV cache: page_plan -> (qkv linear) -> kv_append_paged ->
+ * paged_attention -> ... -> (head linear) -> sample_tokens. (The paper evaluates autoregressive decoding with a KV
+ * cache, Appendix C, one contiguous cache per sample; pages let requests of different lengths share one pool.)
+ * Layout: a pool of n_pages pages of page_size token slots, per page one block per key head:
+ *     Kp, Vp [n_pages, Hkv, page_size, d], bf16 (STWQ_KV_BF16) or int8 codes (STWQ_KV_INT8) with the scales
+ *     s_k [P] (one per token position, as in kv_append) and s_v [Hkv, d] (one per value channel): k = code * s_k[pos],
+ *     v = code * s_v[head, channel].
+ * Slot = page id * page_size + offset. block_table [B, W]: entry (b, i) is the page of tokens i * page_size .. of
+ * request b. Tokens of a step are packed: request b owns rows cu_new[b] .. cu_new[b+1] - 1.
+ */
+enum { STWQ_KV_BF16 = 0, STWQ_KV_INT8 = 1 };
+/* norm of a head vector x: none; x / sqrt(mean x^2 + eps) * w; x / max(|x|, eps) * w (no weights: w = 1) */
+enum { STWQ_NORM_NONE = 0, STWQ_NORM_RMS = 1, STWQ_NORM_L2 = 2 };
+/* which channels a rotation pairs: (i, i + rot/2) or (2i, 2i + 1), i < rot/2 */
+enum { STWQ_ROPE_HALF = 0, STWQ_ROPE_PAIRS = 1 };
+
+/*
+ * Block tables, slots and positions of a step, built on the GPU from the requests' lengths.
+ * cached_lens [B] tokens in the cache, new_lens [B] tokens of this step, free_pages [n_free] ids of free pages.
+ *  - block_table [B, W] in/out: pages that request b needs beyond ceil(cached / page_size) are taken from free_pages in
+ *    order (request 0 first) and entered behind the existing ones; other entries are left as they are.
+ *  - cu_new [B+1], kv_lens [B] (cached + new), slot_map [T], pos_ids [T] out: where token t of the packed step goes, and
+ *    its position in its request. T is the capacity of the two lists: entries behind the last token become -1.
+ *  - pages_used [1] out: how many entries of free_pages were taken.
+ * B <= 4096, W * page_size < 2^31. STWQ_ERR_PAGES is recorded, and the outputs stay consistent, when a length is
+ * negative (taken as 0) or longer than a row of the table, when T or free_pages is too small (tokens beyond T are
+ * dropped, cu_new ends at T; tokens without a page get slot -1, kv_lens counts those that have one), or when a needed
+ * entry is a negative page id. Slots do not check ids against a pool size (kv_append_paged does).
+ */
+int page_plan(stwq_ctx* ctx, const int32_t* cached_lens, const int32_t* new_lens, int B, const int32_t* free_pages, int n_free,
+              int page_size, int32_t* block_table, int W, int32_t* cu_new, int32_t* kv_lens, int32_t* slot_map, int32_t* pos_ids,
+              int64_t T, int32_t* pages_used, void* stream);
+
+/*
+ * Norms of queries and keys per head and the position rotation, in one pass over the output of the qkv linear.
+ * QKV: T rows of (Hq + 2 Hkv) head vectors of d channels (queries, keys, values), fp32 or bf16 (x_dtype), rows ld elements
+ * apart (16-byte multiples). w_q / w_k: NULL with *_heads 0, or [d] (heads = 1: shared), or [Hq, d] / [Hkv, d]; used by the
+ * norm only. cs [P, rot] fp32: rot/2 cosines, then rot/2 sines, for each position (any angles: 1-D or 2-D grids);
+ * NULL with rot = 0 for no rotation. rot <= d; channels from rot on are not turned. d a multiple of 16, <= 256; rot a
+ * multiple of 16. fp32 arithmetic, one rounding at the store.
+ *  - qk_norm_rope: Qo [T, Hq, d] and Ko [T, Hkv, d] of out_dtype (fp32 or bf16), element (t, h, c) at
+ *    t * ts + h * hs + c (strides in elements, 16-byte multiples: a head-major [H, T, d] output feeds kv_append and
+ *    qattention). Values are not touched.
+ *  - kv_append_paged: queries to Qo (bf16, strides as above), keys (normed, rotated) and values to slot slot_map[t] of the
+ *    pool; int8 codes are those of kv_append: clamp(round(x * (1 / s))), bits in {8, 6}. Slot -1: nothing is appended for
+ *    the row. A slot beyond the pool is not written and records STWQ_ERR_PAGES. Two rows with one slot: unspecified which stays.
+ * pos_ids -1 marks a padding row, of which nothing is written. With a rotation or key scales, any other position
+ * outside [0, P) writes zeros to Qo (and Ko), appends nothing, and records STWQ_ERR_POS_RANGE.
+ */
+int qk_norm_rope(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, const int32_t* pos_ids, int64_t T, int Hq, int Hkv,
+                 int d, const float* w_q, int w_q_heads, const float* w_k, int w_k_heads, int norm, float eps, const float* cs,
+                 int rot, int rope, int P, void* Qo, int64_t q_ts, int64_t q_hs, void* Ko, int64_t k_ts, int64_t k_hs,
+                 int out_dtype, void* stream);
+int kv_append_paged(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, const int32_t* pos_ids, const int32_t* slot_map,
+                    int64_t T, int Hq, int Hkv, int d, const float* w_q, int w_q_heads, const float* w_k, int w_k_heads, int norm,
+                    float eps, const float* cs, int rot, int rope, int P, const float* s_k, const float* s_v, int bits, void* Qo,
+                    int64_t q_ts, int64_t q_hs, void* Kp, void* Vp, int n_pages, int page_size, int kv_dtype, void* stream);
+
+/*
+ * Token sampling with temperature, top-k, top-p and min-p from given uniform numbers.
+ * logits: B rows of V (fp32 or bf16, x_dtype), rows ld elements apart; NaN counts as -Inf and a token at -Inf is never
+ * drawn. Per row (a NULL vector switches its limit off): w_i = exp((x_i - max) / temperature); temperature <= 0 is
+ * greedy (the largest, lowest index first). Order: larger x first, equal x by lower index.
+ *   top_k > 0 keeps the first top_k; top_p < 1 then keeps the shortest prefix of those whose mass reaches top_p of theirs
+ *   (at least one); min_p keeps w_i >= min_p. u in [0, 1): the token is the first kept index whose running sum of kept weights,
+ *   in index order, exceeds u times their total.
+ * tokens [B]; probs [B] (weight of the token / total of the kept; may be NULL), kept [B] (number of kept tokens; may be NULL).
+ * A row without any token to draw gives token -1, probability 0, kept 0. Weights are 2^-43 fixed point summed in 64-bit
+ * integers, so results repeat bit for bit. V <= 409600.
+ */
+int sample_tokens(stwq_ctx* ctx, const void* logits, int x_dtype, int64_t ld, int B, int V, const float* temperature,
+                  const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tokens, float* probs,
+                  int32_t* kept, void* stream);
+
+/*
  * qlinear without any allocation. (The paper has no counterpart to this call; it exists for the
  * way the library gets embedded.) qlinear needs a context, whose creation allocates, and keeps
  * the int8 copy of X in workspace that may be (re)allocated during a call. Hosts that cannot
@@ -385,7 +463,8 @@ int qlinear_static(const float* X, const int32_t* pos_ids, int64_t M, int K, int
 
 /*
  * Synchronise `stream`, then return and clear the status recorded by device code since the
- * last call: STWQ_OK, STWQ_ERR_POS_RANGE, STWQ_ERR_NONFINITE or STWQ_ERR_DEVICE_TIMEOUT.
+ * last call: STWQ_OK, STWQ_ERR_POS_RANGE, STWQ_ERR_NONFINITE, STWQ_ERR_PAGES or
+ * STWQ_ERR_DEVICE_TIMEOUT.
  */
 int stwq_device_status(stwq_ctx* ctx, void* stream);
 

@@ -17,6 +17,9 @@ ACT_NONE, ACT_GELU_ERF, ACT_GELU_TANH, ACT_GELU_FAST = 0, 1, 2, 3
 OUT_F32, OUT_BF16, OUT_INT32 = 0, 1, 2
 OPT_GEMM_PATH, OPT_WAIT_LIMIT_MS = 1, 2
 OPT_TILE_N, OPT_VARIANT, OPT_KSPLIT = 100, 101, 102
+KV_BF16, KV_INT8 = 0, 1
+NORM_NONE, NORM_RMS, NORM_L2 = 0, 1, 2
+ROPE_HALF, ROPE_PAIRS = 0, 1
 STATIC_MAX_CODES = 4 * 1024 * 1024
 
 _SYMBOLS = ["stwq_create", "stwq_destroy", "stwq_reserve", "stwq_calibrate", "gps_fold", "stwq_quantize",
@@ -25,7 +28,7 @@ _SYMBOLS = ["stwq_create", "stwq_destroy", "stwq_reserve", "stwq_calibrate", "gp
             "stwq_quantize_asym", "qlinear_asym", "gps_scales", "qlinear_bf16", "stwq_reserve_layer",
             "stwq_workspace_generation", "stwq_selftest_wait_expiry", "stwq_probe_int8_peak", "gps_fold_packed4", "stwq_unpack4",
             "qlinear_w4", "kv_append", "qattention", "stwq_reserve_attention", "qattn_softmax_quantize", "qattn_pv",
-            "dgc_select"]
+            "dgc_select", "page_plan", "qk_norm_rope", "kv_append_paged", "sample_tokens"]
 
 _lib = None
 
@@ -91,6 +94,13 @@ def load_library():
     L.qlinear_chain_q.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, i32, vp, vp]
     L.dtwq_quantize.argtypes = [vp, vp, i64, i32, vp, i32, vp, vp, vp]
     L.qlinear_dtwq.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp]
+    f32 = C.c_float
+    L.page_plan.argtypes = [vp, vp, vp, i32, vp, i32, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp]
+    nr = [vp, vp, i64, i32, vp]
+    heads = [i64, i32, i32, i32, vp, i32, vp, i32, i32, f32, vp, i32, i32, i32]
+    L.qk_norm_rope.argtypes = nr + heads + [vp, i64, i64, vp, i64, i64, i32, vp]
+    L.kv_append_paged.argtypes = nr + [vp] + heads + [vp, vp, i32, vp, i64, i64, vp, vp, i32, i32, i32, vp]
+    L.sample_tokens.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.stwq_device_status.argtypes = [vp, vp]
     L.stwq_set_option.argtypes = [vp, i32, i32]
     L.stwq_launch_count.argtypes = [vp]
@@ -135,6 +145,33 @@ def check_args(where, device, *specs):
             raise StwqError(ERR_DIM, where, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
         if not t.is_contiguous():
             raise StwqError(ERR_ALIGN, where, f"{name} is not contiguous (row-major dense storage is required)")
+
+
+def check_rows(where, device, name, t, dtypes, shape, inner):
+    """Host-side check of a strided operand: element type among `dtypes`, exact shape, the last `inner` dimensions dense,
+    the leading strides non-negative and large enough that no two elements share storage order with a shorter buffer
+    (the sizes and strides are torch's own, so every element lies inside the tensor's storage)."""
+    if t is None:
+        raise StwqError(ERR_NULL, where, f"{name} is None")
+    if not getattr(t, "is_cuda", False):
+        raise StwqError(ERR_CUDA, where, f"{name} is not a CUDA tensor")
+    idx = t.device.index
+    if device is not None and idx is not None and idx != device:
+        raise StwqError(ERR_CUDA, where, f"{name} lives on cuda:{idx}, the call runs on cuda:{device}")
+    if str(t.dtype) not in dtypes:
+        raise StwqError(ERR_BITS, where, f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+    if len(t.shape) != len(shape) or any(w is not None and int(g) != w for g, w in zip(t.shape, shape)):
+        raise StwqError(ERR_DIM, where, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    step = 1
+    for k in range(1, inner + 1):
+        if int(t.shape[-k]) != 1 and int(t.stride(-k)) != step:
+            raise StwqError(ERR_ALIGN, where, f"{name}: its last {inner} dimension(s) must be dense")
+        step *= int(t.shape[-k])
+
+
+def _dense(t, dtype, shape, device):
+    """The quick form of check_args for one tensor (True: nothing to complain about)."""
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and t.device.index == device
 
 
 def _mk(X, what="X"):
@@ -320,6 +357,100 @@ class Context:
                    ("O", O, _out_dtype("qattn_pv", out_dtype), (G, Tq, d), False))
         self._check(self._L.qattn_pv(self._h, _p(Pq), G, Tq, Tk_pad, d, Tmax, _p(Vt), _p(s_v), _p(delta_p), out_dtype,
                                      _p(O), self._stream(stream)), "qattn_pv")
+
+    # ---- serving over a paged KV cache
+    def _fast(self, where, *specs):
+        """check_args in a form that costs little when all is well: the step calls of a decode loop are short."""
+        dev = self.device
+        T = self._torch
+        kinds = {_F32: T.float32, _BF16: T.bfloat16, _I8: T.int8, _I32: T.int32}
+        for name, t, dtype, shape, optional in specs:
+            if t is None and optional:
+                continue
+            if t is None or not hasattr(t, "is_contiguous") or not _dense(t, kinds[dtype], shape, dev):
+                check_args(where, dev, *specs)
+                return
+
+    def _raw_stream(self, stream):
+        return self._torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
+
+    def page_plan(self, cached_lens, new_lens, free_pages, page_size, block_table, cu_new, kv_lens, slot_map, pos_ids,
+                  pages_used, stream=None):
+        B, W = _mk(block_table, "block_table")
+        T, F = int(slot_map.numel()), int(free_pages.numel())
+        self._fast("page_plan", ("cached_lens", cached_lens, _I32, (B,), False), ("new_lens", new_lens, _I32, (B,), False),
+                   ("free_pages", free_pages, _I32, (F,), False), ("block_table", block_table, _I32, (B, W), False),
+                   ("cu_new", cu_new, _I32, (B + 1,), False), ("kv_lens", kv_lens, _I32, (B,), False),
+                   ("slot_map", slot_map, _I32, (T,), False), ("pos_ids", pos_ids, _I32, (T,), False),
+                   ("pages_used", pages_used, _I32, (1,), False))
+        self._check(self._L.page_plan(self._h, cached_lens.data_ptr(), new_lens.data_ptr(), B, free_pages.data_ptr() or None, F,
+                                      page_size, block_table.data_ptr(), W, cu_new.data_ptr(), kv_lens.data_ptr(),
+                                      slot_map.data_ptr(), pos_ids.data_ptr(), T, pages_used.data_ptr(), self._raw_stream(stream)),
+                    "page_plan")
+
+    def _head_args(self, where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k=None):
+        """Checks of the operands that qk_norm_rope and kv_append_paged share; returns T, x_dtype, weights' heads, rot, P."""
+        check_rows(where, self.device, "QKV", QKV, (_F32, _BF16), (None, (Hq + 2 * Hkv) * d), 1)
+        T = int(QKV.shape[0])
+        P = int(cs.shape[0]) if cs is not None else int(s_k.numel()) if s_k is not None else 1
+        rot = int(cs.shape[1]) if cs is not None else 0
+        nq = 0 if w_q is None else 1 if len(w_q.shape) == 1 else Hq
+        nk = 0 if w_k is None else 1 if len(w_k.shape) == 1 else Hkv
+        self._fast(where, ("pos_ids", pos_ids, _I32, (T,), False),
+                   ("w_q", w_q, _F32, (d,) if nq == 1 and len(w_q.shape) == 1 else (Hq, d), True),
+                   ("w_k", w_k, _F32, (d,) if nk == 1 and len(w_k.shape) == 1 else (Hkv, d), True),
+                   ("cs", cs, _F32, (P, rot), True), ("s_k", s_k, _F32, (P,), True))
+        return T, OUT_BF16 if QKV.dtype is self._torch.bfloat16 else OUT_F32, nq, nk, rot, P
+
+    def qk_norm_rope(self, QKV, pos_ids, Hq, Hkv, w_q, w_k, norm, eps, cs, rope, Qo, Ko, stream=None):
+        d = int(Qo.shape[-1])
+        T, x_dtype, nq, nk, rot, P = self._head_args("qk_norm_rope", QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs)
+        check_rows("qk_norm_rope", self.device, "Qo", Qo, (_F32, _BF16), (T, Hq, d), 1)
+        check_rows("qk_norm_rope", self.device, "Ko", Ko, (str(Qo.dtype),), (T, Hkv, d), 1)
+        out = OUT_BF16 if Qo.dtype is self._torch.bfloat16 else OUT_F32
+        self._check(self._L.qk_norm_rope(self._h, QKV.data_ptr(), QKV.stride(0), x_dtype, pos_ids.data_ptr(), T, Hq, Hkv, d,
+                                         w_q.data_ptr() if nq else None, nq, w_k.data_ptr() if nk else None, nk, norm, eps,
+                                         None if cs is None else cs.data_ptr(), rot, rope, P, Qo.data_ptr(), Qo.stride(0),
+                                         Qo.stride(1), Ko.data_ptr(), Ko.stride(0), Ko.stride(1), out, self._raw_stream(stream)),
+                    "qk_norm_rope")
+
+    def _pool(self, where, Kp, Vp):
+        """Checks the two pools; returns n_pages, Hkv, page_size, d, kv_dtype."""
+        if Kp is None or Vp is None or len(Kp.shape) != 4:
+            raise StwqError(ERR_DIM, where, "Kp and Vp are [n_pages, Hkv, page_size, d]")
+        shape = tuple(int(v) for v in Kp.shape)
+        i8 = Kp.dtype is self._torch.int8
+        self._fast(where, ("Kp", Kp, _I8 if i8 else _BF16, shape, False), ("Vp", Vp, _I8 if i8 else _BF16, shape, False))
+        return (*shape, KV_INT8 if i8 else KV_BF16)
+
+    def kv_append_paged(self, QKV, pos_ids, slot_map, Hq, Hkv, w_q, w_k, norm, eps, cs, rope, s_k, s_v, bits, Qo, Kp, Vp,
+                        stream=None):
+        where = "kv_append_paged"
+        NP, hk, S, d, kv = self._pool(where, Kp, Vp)
+        if hk != Hkv:
+            raise StwqError(ERR_DIM, where, f"the pool has {hk} key heads, the call {Hkv}")
+        T, x_dtype, nq, nk, rot, P = self._head_args(where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k)
+        check_rows(where, self.device, "Qo", Qo, (_BF16,), (T, Hq, d), 1)
+        self._fast(where, ("slot_map", slot_map, _I32, (T,), False), ("s_k", s_k, _F32, (P,), kv == KV_BF16),
+                   ("s_v", s_v, _F32, (Hkv, d), kv == KV_BF16))
+        self._check(self._L.kv_append_paged(self._h, QKV.data_ptr(), QKV.stride(0), x_dtype, pos_ids.data_ptr(),
+                                            slot_map.data_ptr(), T, Hq, Hkv, d, w_q.data_ptr() if nq else None, nq,
+                                            w_k.data_ptr() if nk else None, nk, norm, eps, None if cs is None else cs.data_ptr(),
+                                            rot, rope, P, None if s_k is None else s_k.data_ptr(),
+                                            None if s_v is None else s_v.data_ptr(), bits, Qo.data_ptr(), Qo.stride(0),
+                                            Qo.stride(1), Kp.data_ptr(), Vp.data_ptr(), NP, S, kv, self._raw_stream(stream)), where)
+
+    def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, probs=None, kept=None, stream=None):
+        check_rows("sample_tokens", self.device, "logits", logits, (_F32, _BF16), (None, None), 1)
+        B, V = int(logits.shape[0]), int(logits.shape[1])
+        self._fast("sample_tokens", ("temperature", temperature, _F32, (B,), True), ("top_k", top_k, _I32, (B,), True),
+                   ("top_p", top_p, _F32, (B,), True), ("min_p", min_p, _F32, (B,), True), ("u", u, _F32, (B,), False),
+                   ("tokens", tokens, _I32, (B,), False), ("probs", probs, _F32, (B,), True), ("kept", kept, _I32, (B,), True))
+        q = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._check(self._L.sample_tokens(self._h, logits.data_ptr(), OUT_BF16 if logits.dtype is self._torch.bfloat16 else OUT_F32,
+                                          max(logits.stride(0), V) if B == 1 else logits.stride(0), B, V, q(temperature), q(top_k),
+                                          q(top_p), q(min_p), u.data_ptr(), tokens.data_ptr(), q(probs), q(kept),
+                                          self._raw_stream(stream)), "sample_tokens")
 
     def _quantize_specs(self, X, x_dtype, pos_ids, s_ch, s_tok, Xq):
         M, K = _mk(X)

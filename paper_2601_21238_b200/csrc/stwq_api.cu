@@ -573,6 +573,7 @@ int stwq_device_status(stwq_ctx* ctx, void* stream)
     if (h & STWQ_DEV_TIMEOUT) return STWQ_ERR_DEVICE_TIMEOUT;
     if (h & STWQ_DEV_POS_RANGE) return STWQ_ERR_POS_RANGE;
     if (h & STWQ_DEV_NONFINITE) return STWQ_ERR_NONFINITE;
+    if (h & STWQ_DEV_PAGES) return STWQ_ERR_PAGES;
     return STWQ_OK;
 }
 
@@ -597,6 +598,7 @@ const char* stwq_strerror(int status)
         case STWQ_ERR_NONFINITE: return "calibration input contains NaN or Inf";
         case STWQ_ERR_NOMEM: return "workspace allocation failed";
         case STWQ_ERR_CAPTURE: return "workspace would have to grow during stream capture (reserve it first)";
+        case STWQ_ERR_PAGES: return "a length, page id, slot or block-table entry was out of range";
         default: return "unknown status";
     }
 }

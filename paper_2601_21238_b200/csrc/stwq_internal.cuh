@@ -10,6 +10,7 @@
 #define STWQ_DEV_POS_RANGE 1u
 #define STWQ_DEV_NONFINITE 2u
 #define STWQ_DEV_TIMEOUT 4u
+#define STWQ_DEV_PAGES 8u
 
 struct stwq_ctx {
     int device;
