@@ -419,6 +419,27 @@ int kv_append_paged(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, con
                     int64_t q_ts, int64_t q_hs, void* Kp, void* Vp, int n_pages, int page_size, int kv_dtype, void* stream);
 
 /*
+ * Attention of the new tokens of a step over the paged cache (their keys and values are in the cache already):
+ *     O[t, h] = sum_j softmax_j(scale * q[t, h] . k[j, h / (Hq / Hkv)]) v[j, h / (Hq / Hkv)]
+ * For request b with n = cu_new[b+1] - cu_new[b] new tokens and L = kv_lens[b] keys, its token i sees keys j < L - n + i + 1
+ * (causal != 0) or all j < L. A row that sees no key gives zeros. Rows of O outside every request are left as they were.
+ * Q, O: element (t, h, c) at t * ts + h * hs + c (strides in elements, 16-byte multiples); Q bf16, O out_dtype (fp32 or
+ * bf16). max_new: no request of the step has more new tokens (host-side bound, at most T). Hq a multiple of Hkv; d a
+ * multiple of 16, <= 128; page_size a multiple of 16; B <= 4096; scale > 0. Token slots at or beyond L are never read, so
+ * stale pages may hold anything; values of visible keys must be finite (a masked key has weight 0, and 0 * Inf is NaN).
+ * fp32 scores, softmax and sums; probabilities are rounded to bf16 (bf16 cache) or fp16 (codes) for the second product;
+ * codes enter both products exactly. Results do not depend on how the work is split over the GPU's SMs at run time.
+ * STWQ_ERR_PAGES is recorded for lengths outside the table, the scales' P positions, T or max_new (clamped), and for a
+ * needed page id outside [0, n_pages) (page 0 is read instead).
+ * Workspace: partial results and arrival counters, at most 20 MB; stwq_reserve_paged_attention sizes it ahead of time.
+ */
+int paged_attention(stwq_ctx* ctx, const void* Q, int64_t q_ts, int64_t q_hs, const int32_t* cu_new, int64_t T, int max_new, int B,
+                    int Hq, int Hkv, int d, const int32_t* block_table, int W, const int32_t* kv_lens, const void* Kp, const void* Vp,
+                    int n_pages, int page_size, int kv_dtype, const float* s_k, int P, const float* s_v, float scale, int causal,
+                    int out_dtype, void* O, int64_t o_ts, int64_t o_hs, void* stream);
+int stwq_reserve_paged_attention(stwq_ctx* ctx, int B, int Hq, int Hkv, int d);
+
+/*
  * Token sampling with temperature, top-k, top-p and min-p from given uniform numbers.
  * logits: B rows of V (fp32 or bf16, x_dtype), rows ld elements apart; NaN counts as -Inf and a token at -Inf is never
  * drawn. Per row (a NULL vector switches its limit off): w_i = exp((x_i - max) / temperature); temperature <= 0 is

@@ -28,7 +28,8 @@ _SYMBOLS = ["stwq_create", "stwq_destroy", "stwq_reserve", "stwq_calibrate", "gp
             "stwq_quantize_asym", "qlinear_asym", "gps_scales", "qlinear_bf16", "stwq_reserve_layer",
             "stwq_workspace_generation", "stwq_selftest_wait_expiry", "stwq_probe_int8_peak", "gps_fold_packed4", "stwq_unpack4",
             "qlinear_w4", "kv_append", "qattention", "stwq_reserve_attention", "qattn_softmax_quantize", "qattn_pv",
-            "dgc_select", "page_plan", "qk_norm_rope", "kv_append_paged", "sample_tokens"]
+            "dgc_select", "page_plan", "qk_norm_rope", "kv_append_paged", "sample_tokens",
+            "paged_attention", "stwq_reserve_paged_attention"]
 
 _lib = None
 
@@ -100,6 +101,9 @@ def load_library():
     heads = [i64, i32, i32, i32, vp, i32, vp, i32, i32, f32, vp, i32, i32, i32]
     L.qk_norm_rope.argtypes = nr + heads + [vp, i64, i64, vp, i64, i64, i32, vp]
     L.kv_append_paged.argtypes = nr + [vp] + heads + [vp, vp, i32, vp, i64, i64, vp, vp, i32, i32, i32, vp]
+    L.paged_attention.argtypes = [vp, vp, i64, i64, vp, i64, i32, i32, i32, i32, i32, vp, i32, vp, vp, vp, i32, i32, i32, vp, i32, vp,
+                                  f32, i32, i32, vp, i64, i64, vp]
+    L.stwq_reserve_paged_attention.argtypes = [vp, i32, i32, i32, i32]
     L.sample_tokens.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.stwq_device_status.argtypes = [vp, vp]
     L.stwq_set_option.argtypes = [vp, i32, i32]
@@ -439,6 +443,28 @@ class Context:
                                             rot, rope, P, None if s_k is None else s_k.data_ptr(),
                                             None if s_v is None else s_v.data_ptr(), bits, Qo.data_ptr(), Qo.stride(0),
                                             Qo.stride(1), Kp.data_ptr(), Vp.data_ptr(), NP, S, kv, self._raw_stream(stream)), where)
+
+    def paged_attention(self, Q, cu_new, max_new, block_table, kv_lens, Kp, Vp, s_k, s_v, scale, causal, out_dtype, O, stream=None):
+        where = "paged_attention"
+        NP, Hkv, S, d, kv = self._pool(where, Kp, Vp)
+        check_rows(where, self.device, "Q", Q, (_BF16,), (None, None, d), 1)
+        T, Hq = int(Q.shape[0]), int(Q.shape[1])
+        if out_dtype not in (OUT_F32, OUT_BF16):
+            raise StwqError(ERR_BITS, where, f"out_dtype {out_dtype} is not OUT_F32 / OUT_BF16")
+        check_rows(where, self.device, "O", O, (_OUT_DTYPES[out_dtype],), (T, Hq, d), 1)
+        B, W = _mk(block_table, "block_table")
+        P = int(s_k.numel()) if s_k is not None else 1
+        self._fast(where, ("cu_new", cu_new, _I32, (B + 1,), False), ("block_table", block_table, _I32, (B, W), False),
+                   ("kv_lens", kv_lens, _I32, (B,), False), ("s_k", s_k, _F32, (P,), kv == KV_BF16),
+                   ("s_v", s_v, _F32, (Hkv, d), kv == KV_BF16))
+        self._check(self._L.paged_attention(self._h, Q.data_ptr(), Q.stride(0), Q.stride(1), cu_new.data_ptr(), T, max_new, B, Hq, Hkv,
+                                            d, block_table.data_ptr(), W, kv_lens.data_ptr(), Kp.data_ptr(), Vp.data_ptr(), NP, S, kv,
+                                            None if s_k is None else s_k.data_ptr(), P, None if s_v is None else s_v.data_ptr(),
+                                            scale, int(bool(causal)), out_dtype, O.data_ptr(), O.stride(0), O.stride(1),
+                                            self._raw_stream(stream)), where)
+
+    def stwq_reserve_paged_attention(self, B, Hq, Hkv, d):
+        self._check(self._L.stwq_reserve_paged_attention(self._h, B, Hq, Hkv, d), "stwq_reserve_paged_attention")
 
     def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, probs=None, kept=None, stream=None):
         check_rows("sample_tokens", self.device, "logits", logits, (_F32, _BF16), (None, None), 1)

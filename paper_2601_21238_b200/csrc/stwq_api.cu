@@ -171,6 +171,8 @@ void stwq_destroy(stwq_ctx* ctx)
     if (ctx->ws_dyn) cudaFree(ctx->ws_dyn);
     if (ctx->ws_w4) cudaFree(ctx->ws_w4);
     if (ctx->ws_attn) cudaFree(ctx->ws_attn);
+    if (ctx->ws_pattn) cudaFree(ctx->ws_pattn);
+    if (ctx->ws_pcnt) cudaFree(ctx->ws_pcnt);
     if (ctx->d_status) cudaFree(ctx->d_status);
     delete ctx;
 }

@@ -40,6 +40,10 @@ struct stwq_ctx {
     uint64_t configured_decode;
     void* ws_attn;             // workspace of qattention: codes of Q, scores, probability codes
     size_t ws_attn_bytes;
+    void* ws_pattn;            // workspace of paged_attention: partial results of units that several CTAs share
+    size_t ws_pattn_bytes;
+    void* ws_pcnt;             // and their arrival counters, zero between calls
+    size_t ws_pcnt_bytes;
     int8_t* ws_w4;             // workspace: int8 copy of packed 4-bit weights (qlinear_w4 on the tiled route)
     size_t ws_w4_bytes;
     int force_ksplit;          // tuning: 0 = choose, else the number of K ranges of the few-row path

@@ -1,0 +1,620 @@
+// Paged attention for few rows (a decode step, a few speculative tokens): at most 16 query rows per key head and request,
+// rows being the new tokens times the query heads that share the key head.
+//     S[j, r] = scale * k_j . q_r,   O[r] = sum_j softmax_j(S[., r]) v_j,   j below the row's visible length
+// Reads the request's keys and values once and is bound by that: HBM bytes, 0.5 to 16 flops per byte.
+//
+//  * Split: all (request, key head) units are laid end to end as 64-key blocks and cut into equal contiguous ranges, one
+//    per CTA, whatever the lengths. A CTA has at most two units that it shares with neighbours; their partial
+//    (max, sum, O) go to workspace and the last CTA to arrive adds them up in the order of the keys (so the result does
+//    not depend on who was last).
+//  * A warp takes 16 keys at a time, whole: S^T = K Q^T by mma m16n8k16 with the KEYS as the 16 rows and up to 8 query
+//    rows as columns, then O^T = V^T P^T with 16 CHANNELS as rows. The channel order inside the first product and the key
+//    and channel order inside the second are free, and are chosen so that every operand register pair comes out of
+//    16 consecutive bytes that the thread itself loaded: no shared-memory exchange, no barrier in the loop. P^T is the
+//    transpose of the S^T fragment: one movmatrix per 8 keys.
+//  * Loads: each thread copies its own pieces with cp.async into a ring that only it reads, so a stage is complete when the
+//    thread's own groups are. Enough stages for 100 KB and more in flight per SM.
+//  * The running maximum is a reference, not the maximum: it moves only when a score exceeds it by more than 2^10 (a vote
+//    per block instead of six shuffles). fp32 sums; P in bf16, or in fp16 over the code cache.
+//  * Codes (int8) become fp16, exactly: byte ^ 0x80 under the exponent of 1024, minus 1152. Queries are scaled by a power of
+//    two per row so that their largest lies in [2^13, 2^14): bf16 -> fp16 is then exact down to 2^-37 of that
+//    largest. Key scales multiply S (fp32), value scales multiply O at the end.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "stwq_paged.cuh"
+#include "stwq_pattn.cuh"
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kBlk = 16 * kWarps;            // keys per CTA block: 16 per warp
+constexpr int kMaxParts = 64;                // CTAs that share one unit
+constexpr float kSlack = 10.0f;              // log2: how far a score may exceed the running reference
+
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <int BYTES>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool live)
+{
+    const int n = live ? BYTES : 0;          // fewer source bytes: the rest is zero-filled, the source is not read
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else if (BYTES == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds16(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t a)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float lds4f(uint32_t a)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+// two codes (already ^ 0x80) at bytes lo, hi of w -> half2, exact
+__device__ __forceinline__ uint32_t codes_half2(uint32_t w, uint32_t sel)
+{
+    const uint32_t x = prmt(w, 0x64646464u, sel), k = 0x64806480u;
+    __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
+    return *reinterpret_cast<uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+template <bool F16>
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    if (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    if (F16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+template <bool I8, int DP>
+struct Ring {
+    static constexpr int es = I8 ? 1 : 2;
+    static constexpr int npk = DP * es / 64;              // 16-byte key pieces per thread and key (4 threads share a key)
+    static constexpr int vbytes = DP * es / 8;            // value bytes per thread and key (8 threads share a key)
+    static constexpr int koff = 0;
+    static constexpr int voff = 2 * npk * 512;
+    static constexpr int soff = voff + 4 * vbytes * 32;   // key scales
+    static constexpr int stage = soff + (I8 ? 256 : 0);   // bytes per warp and 16 keys
+    static constexpr int stages = DP * es >= 256 ? 2 : (DP * es >= 128 ? 4 : 6);
+    static constexpr int smem = kWarps * stages * stage;
+};
+
+template <bool I8, int DP, int NR>
+__global__ void __launch_bounds__(kThreads, 3) pattn_few_kernel(const PaParams p, const int min_blocks)
+{
+    using R = Ring<I8, DP>;
+    constexpr int NT = DP / 16;                           // channel tiles of O^T
+    constexpr int NK = DP / 16;                           // steps of S^T
+    extern __shared__ __align__(16) uint8_t smem[];
+    // after the ring: first block of each request
+    long long* pre = reinterpret_cast<long long*>(smem + R::smem);        // [B + 1]
+    __shared__ long long wsum[kWarps];
+    __shared__ float sm_m[kWarps][8 * NR], sm_l[kWarps][8 * NR];
+    __shared__ uint32_t sm_last;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int r = lane >> 2, t = lane & 3;
+    bool bad = false;
+
+    // ---- the blocks of every request, end to end
+    auto blocks_of = [&](const PaReq& q) -> long long {   // a request with rows but no keys still writes zeros
+        if (q.n <= 0 || (int64_t)q.n * p.g > 8 * NR) return 0;
+        return (long long)p.Hkv * max(1, (q.kv + kBlk - 1) / kBlk);
+    };
+    {
+        const int per = (p.B + kThreads - 1) / kThreads;
+        const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
+        long long sum = 0;
+        for (int b = b0; b < b1; ++b) sum += blocks_of(pa_request(p, b, bad));
+        long long s = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, s, o);
+            if (lane >= o) s += u;
+        }
+        if (lane == 31) wsum[warp] = s;
+        __syncthreads();
+        long long at = s - sum;
+        for (int w = 0; w < warp; ++w) at += wsum[w];
+        for (int b = b0; b < b1; ++b) {
+            pre[b] = at;
+            at += blocks_of(pa_request(p, b, bad));
+        }
+        if (tid == kThreads - 1) pre[p.B] = at;
+        __syncthreads();
+    }
+    if (bad && blockIdx.x == 0) atomicOr(p.status, STWQ_DEV_PAGES);
+    const long long N = pre[p.B];
+    if (N == 0) return;
+    // ranges of at least min_blocks: a range costs a set-up and, when it splits a unit, a trip through workspace
+    const long long G = max(1ll, min((long long)gridDim.x, (N + min_blocks - 1) / min_blocks));
+    if (blockIdx.x >= G) return;
+    const long long lo = N * blockIdx.x / G, hi = N * (blockIdx.x + 1) / G;
+    if (lo >= hi) return;
+
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * R::stages * R::stage;
+    const int d = p.d, S = p.S, per_page = S / 16;
+    const int64_t row_bytes = (int64_t)d * R::es;
+
+    long long at = lo;
+    int b = 0;
+    {
+        int x0 = 0, x1 = p.B;                             // last b with pre[b] <= at
+        while (x1 - x0 > 1) {
+            const int m = (x0 + x1) >> 1;
+            if (pre[m] <= at) x0 = m;
+            else x1 = m;
+        }
+        b = x0;
+    }
+    while (at < hi) {
+        while (pre[b + 1] <= at) ++b;
+        bool dummy = false;
+        const PaReq q = pa_request(p, b, dummy);
+        const int nb = max(1, (q.kv + kBlk - 1) / kBlk);
+        const int hk = (int)((at - pre[b]) / nb);
+        const long long unit0 = pre[b] + (long long)hk * nb;
+        const int blk0 = (int)(at - unit0);
+        const int blk1 = (int)min((long long)nb, hi - unit0);
+        const int rows = q.n * p.g;
+
+        // ---- queries: B operand, row r (and r + 8), this thread's channels
+        uint32_t qf[NR][NK][2];
+        float qscale[NR][2];                              // for rows 2t, 2t + 1: softmax scale, log2(e), inverse power of two
+        int limit[NR][2];                                 // visible keys of rows 2t, 2t + 1
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+            const int row = nr * 8 + r;
+            const bool live = row < rows;
+            const int ti = live ? row / p.g : 0;
+            const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.Q) + (int64_t)(q.t0 + ti) * p.q_ts +
+                                       (int64_t)(hk * p.g + (live ? row - ti * p.g : 0)) * p.q_hs;
+            float inv = 1.0f;
+            if (!I8) {
+#pragma unroll
+                for (int j = 0; j < R::npk; ++j) {
+                    const int ch = (t + 4 * j) * 8;
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (live && ch < d) v = __ldg(reinterpret_cast<const uint4*>(src + ch));
+                    qf[nr][2 * j][0] = v.x;
+                    qf[nr][2 * j][1] = v.y;
+                    qf[nr][2 * j + 1][0] = v.z;
+                    qf[nr][2 * j + 1][1] = v.w;
+                }
+            } else {
+                uint32_t raw[R::npk][8];
+                float mx = 0.0f;
+#pragma unroll
+                for (int j = 0; j < R::npk; ++j) {
+                    const int ch = (t + 4 * j) * 16;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                        if (live && ch < d) v = __ldg(reinterpret_cast<const uint4*>(src + ch) + h);
+                        raw[j][4 * h] = v.x; raw[j][4 * h + 1] = v.y; raw[j][4 * h + 2] = v.z; raw[j][4 * h + 3] = v.w;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(raw[j][k] << 16)), fabsf(__uint_as_float(raw[j][k] & 0xffff0000u))));
+                }
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                // 2^(13 - e), e the exponent of the row's largest; both powers stay normal numbers
+                int e = (int)(__float_as_uint(mx) >> 23) - 127;
+                e = mx > 0.0f && mx < INFINITY ? max(e, -100) : 13;
+                const float up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
+                inv = __uint_as_float((uint32_t)(e - 13 + 127) << 23);
+#pragma unroll
+                for (int j = 0; j < R::npk; ++j)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        qf[nr][4 * j + k / 2][k & 1] = pack2<true>(__uint_as_float(raw[j][k] << 16) * up, __uint_as_float(raw[j][k] & 0xffff0000u) * up);
+            }
+#pragma unroll
+            for (int e2 = 0; e2 < 2; ++e2) {
+                const int rr = nr * 8 + 2 * t + e2;
+                qscale[nr][e2] = p.scale * kPaLog2e * __shfl_sync(0xffffffffu, inv, (2 * t + e2) * 4);
+                limit[nr][e2] = rr >= rows ? 0 : (p.causal ? q.kv - q.n + rr / p.g + 1 : q.kv);
+            }
+        }
+        const int min_limit = p.causal ? q.kv - q.n + 1 : q.kv;           // the shortest row that exists
+
+        float o[NR][NT][4];
+        float m[NR][2], l[NR][2];
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[nr][i][k] = 0.0f;
+            m[nr][0] = m[nr][1] = -INFINITY;
+            l[nr][0] = l[nr][1] = 0.0f;
+        }
+
+        // ---- the 16-key blocks of this warp: first + 4 i
+        const int first = blk0 * kWarps + warp;
+        const int end16 = min(blk1 * kWarps, (q.kv + 15) / 16);
+        const int n16 = first < end16 ? (end16 - first + kWarps - 1) / kWarps : 0;
+        const int32_t* trow = p.table + (int64_t)b * p.W;
+        int ids = 0, ids_next = 0;                        // page of block it0 + lane, of block it0 + 32 + lane
+        auto load_ids = [&](int it0) -> int {
+            const int it = it0 + lane;
+            int id = 0;
+            if (it < n16) {
+                id = __ldg(trow + (first + kWarps * it) / per_page);
+                if (id < 0 || id >= p.n_pages) {
+                    atomicOr(p.status, STWQ_DEV_PAGES);
+                    id = 0;
+                }
+            }
+            return id;
+        };
+        ids = load_ids(0);
+        ids_next = load_ids(32);
+        auto issue = [&](int it) {
+            if (it < n16) {
+                if ((it & 31) == 0 && it > 0) {
+                    ids = ids_next;
+                    ids_next = load_ids(it + 32);
+                }
+                const int id = __shfl_sync(0xffffffffu, ids, it & 31);
+                const int b16 = first + kWarps * it;
+                const int64_t base = (((int64_t)id * p.Hkv + hk) * S + (b16 % per_page) * 16) * row_bytes;
+                const int j0 = b16 * 16;                  // first key
+                const uint32_t dst = ring + (it % R::stages) * R::stage + lane * 16;
+                const uint8_t* kp = reinterpret_cast<const uint8_t*>(p.Kp) + base;
+                const uint8_t* vp = reinterpret_cast<const uint8_t*>(p.Vp) + base;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < R::npk; ++j) {
+                        const int byte = (t + 4 * j) * 16;
+                        cp_async<16>(dst + R::koff + (h * R::npk + j) * 512, kp + (byte < row_bytes ? (8 * h + r) * row_bytes + byte : 0),
+                                     j0 + 8 * h + r < q.kv && byte < row_bytes);
+                    }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int key = 2 * t + (k & 1) + 8 * (k >> 1);
+                    const bool seen = j0 + key < q.kv;
+                    if (I8) {
+                        constexpr int nv = R::vbytes < 16 ? 8 : 16;
+                        const int byte = r * R::vbytes;
+                        const bool in = byte < row_bytes;
+                        cp_async<nv>(dst - lane * 16 + lane * nv + R::voff + k * R::vbytes * 32, vp + (in ? key * row_bytes + byte : 0), seen && in);
+                    } else {
+#pragma unroll
+                        for (int hh = 0; hh < R::vbytes / 16; ++hh) {
+                            const int byte = hh * 128 + r * 16;
+                            const bool in = byte < row_bytes;
+                            cp_async<16>(dst + R::voff + (k * (R::vbytes / 16) + hh) * 512, vp + (in ? key * row_bytes + byte : 0), seen && in);
+                        }
+                    }
+                }
+                if (I8) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int key = j0 + 8 * h + r;
+                        cp_async<4>(dst - lane * 16 + lane * 4 + R::soff + h * 128, p.s_k + min(key, p.P - 1), key < q.kv);
+                    }
+                }
+            }
+            cp_commit();                                  // also when empty: the count of groups stays the stage count
+        };
+#pragma unroll
+        for (int s = 0; s < R::stages; ++s) issue(s);
+
+        for (int it = 0; it < n16; ++it) {
+            cp_wait<R::stages - 1>();
+            const uint32_t st = ring + (it % R::stages) * R::stage + lane * 16;
+            const int j0 = (first + kWarps * it) * 16;
+            // ---- S^T: keys r, r + 8 x rows 2t, 2t + 1
+            float s[NR][4];
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) s[nr][0] = s[nr][1] = s[nr][2] = s[nr][3] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < R::npk; ++j) {
+                const uint4 ka = lds16(st + R::koff + j * 512), kb = lds16(st + R::koff + (R::npk + j) * 512);
+                if (!I8) {
+#pragma unroll
+                    for (int nr = 0; nr < NR; ++nr) {
+                        mma<false>(s[nr], ka.x, kb.x, ka.y, kb.y, qf[nr][2 * j][0], qf[nr][2 * j][1]);
+                        mma<false>(s[nr], ka.z, kb.z, ka.w, kb.w, qf[nr][2 * j + 1][0], qf[nr][2 * j + 1][1]);
+                    }
+                } else {
+                    const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t xa = wa[k] ^ 0x80808080u, xb = wb[k] ^ 0x80808080u;
+                        const uint32_t a0 = codes_half2(xa, 0x4140u), a2 = codes_half2(xa, 0x4342u);
+                        const uint32_t a1 = codes_half2(xb, 0x4140u), a3 = codes_half2(xb, 0x4342u);
+#pragma unroll
+                        for (int nr = 0; nr < NR; ++nr) mma<true>(s[nr], a0, a1, a2, a3, qf[nr][4 * j + k][0], qf[nr][4 * j + k][1]);
+                    }
+                }
+            }
+            float ska = 1.0f, skb = 1.0f;
+            if (I8) {
+                ska = lds4f(st - lane * 16 + lane * 4 + R::soff);
+                skb = lds4f(st - lane * 16 + lane * 4 + R::soff + 128);
+            }
+            const bool masked = j0 + 16 > min_limit;      // uniform
+            bool over = false;
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    s[nr][e] *= qscale[nr][e] * ska;
+                    s[nr][2 + e] *= qscale[nr][e] * skb;
+                    if (masked) {
+                        if (j0 + r >= limit[nr][e]) s[nr][e] = -INFINITY;
+                        if (j0 + 8 + r >= limit[nr][e]) s[nr][2 + e] = -INFINITY;
+                    }
+                    over |= fmaxf(s[nr][e], s[nr][2 + e]) > m[nr][e] + kSlack;
+                }
+            }
+            if (__any_sync(0xffffffffu, over)) {          // the reference moves to the maximum so far
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(s[nr][e], s[nr][2 + e]);
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                        const float mn = fmaxf(m[nr][e], mx);
+                        const float f = mn == -INFINITY ? 1.0f : ex2(m[nr][e] - mn);
+                        m[nr][e] = mn;
+                        l[nr][e] *= f;
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) {
+                            o[nr][i][e] *= f;
+                            o[nr][i][2 + e] *= f;
+                        }
+                    }
+            }
+            uint32_t pf[NR][2];
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+                float pv[4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    // over the code cache P is fp16: four octaves up, so that small probabilities keep their bits
+                    const float mm = m[nr][e] == -INFINITY ? 0.0f : m[nr][e] - (I8 ? 4.0f : 0.0f);
+                    pv[e] = ex2(s[nr][e] - mm);
+                    pv[2 + e] = ex2(s[nr][2 + e] - mm);
+                    l[nr][e] += pv[e] + pv[2 + e];
+                }
+                pf[nr][0] = transpose8x8(pack2<I8>(pv[0], pv[1]));
+                pf[nr][1] = transpose8x8(pack2<I8>(pv[2], pv[3]));
+            }
+            // ---- O^T += V^T P^T
+            if (!I8) {
+#pragma unroll
+                for (int hh = 0; hh < (R::vbytes >= 16 ? R::vbytes / 16 : 1); ++hh) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = lds16(st + R::voff + (k * (R::vbytes / 16) + hh) * 512);
+                    const uint32_t w[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w},
+                                              {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t a0 = prmt(w[0][i], w[1][i], 0x5410u), a1 = prmt(w[0][i], w[1][i], 0x7632u);
+                        const uint32_t a2 = prmt(w[2][i], w[3][i], 0x5410u), a3 = prmt(w[2][i], w[3][i], 0x7632u);
+#pragma unroll
+                        for (int nr = 0; nr < NR; ++nr) mma<false>(o[nr][hh * 4 + i], a0, a1, a2, a3, pf[nr][0], pf[nr][1]);
+                    }
+                }
+            } else {
+                constexpr int nw = R::vbytes / 4;
+                uint32_t w[4][nw];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (nw == 4) {
+                        const uint4 v = lds16(st + R::voff + k * 512);
+                        w[k][0] = v.x; w[k][1] = v.y; w[k][nw > 2 ? 2 : 0] = v.z; w[k][nw > 2 ? 3 : 1] = v.w;
+                    } else {
+                        const uint2 v = lds8(st - lane * 16 + lane * 8 + R::voff + k * 256);
+                        w[k][0] = v.x; w[k][1] = v.y;
+                    }
+#pragma unroll
+                    for (int i = 0; i < nw; ++i) w[k][i] ^= 0x80808080u;
+                }
+#pragma unroll
+                for (int i = 0; i < nw; ++i) {
+                    // bytes of channels 0, 1 (2, 3) of two keys side by side
+                    const uint32_t x01 = prmt(w[0][i], w[1][i], 0x5140u), y01 = prmt(w[0][i], w[1][i], 0x7362u);
+                    const uint32_t x23 = prmt(w[2][i], w[3][i], 0x5140u), y23 = prmt(w[2][i], w[3][i], 0x7362u);
+                    const uint32_t a0 = codes_half2(x01, 0x4140u), a1 = codes_half2(x01, 0x4342u);
+                    const uint32_t a2 = codes_half2(x23, 0x4140u), a3 = codes_half2(x23, 0x4342u);
+                    const uint32_t c0 = codes_half2(y01, 0x4140u), c1 = codes_half2(y01, 0x4342u);
+                    const uint32_t c2 = codes_half2(y23, 0x4140u), c3 = codes_half2(y23, 0x4342u);
+#pragma unroll
+                    for (int nr = 0; nr < NR; ++nr) {
+                        mma<true>(o[nr][2 * i], a0, a1, a2, a3, pf[nr][0], pf[nr][1]);
+                        mma<true>(o[nr][2 * i + 1], c0, c1, c2, c3, pf[nr][0], pf[nr][1]);
+                    }
+                }
+            }
+            issue(it + R::stages);                        // the stage's bytes are in registers: refill it
+        }
+        cp_wait<0>();
+        __syncthreads();                                  // every warp is done with its ring: it becomes the exchange buffer
+
+        // ---- the four warps' parts
+        float* ex = reinterpret_cast<float*>(smem);       // [kWarps][8 NR][DP]
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float s = l[nr][e];
+                s += __shfl_xor_sync(0xffffffffu, s, 4);
+                s += __shfl_xor_sync(0xffffffffu, s, 8);
+                s += __shfl_xor_sync(0xffffffffu, s, 16);
+                const int row = nr * 8 + 2 * t + e;
+                if (r == 0) {
+                    sm_m[warp][row] = m[nr][e];
+                    sm_l[warp][row] = s;
+                }
+                if (row < rows) {
+                    float* dst = ex + (warp * 8 * NR + row) * DP;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        const int ch = I8 ? r * (DP / 8) + 2 * i : (i >> 2) * 64 + r * 8 + (i & 3) * 2;
+                        *reinterpret_cast<float2*>(dst + ch) = make_float2(o[nr][i][e], o[nr][i][2 + e]);
+                    }
+                }
+            }
+        __syncthreads();
+        const bool whole = blk0 == 0 && blk1 == nb;
+        const int slots = 8 * NR * (DP + 2);              // floats of a partial result: O, then (max, sum) per row
+        float* part = p.part + ((int64_t)blockIdx.x * 2 + (blk0 == 0 ? 1 : 0)) * slots;
+        auto write_out = [&](int row, int ch, float a, float b2, float lsum) {       // two channels of a row
+            const float inv = lsum > 0.0f ? __fdividef(1.0f, lsum) : 0.0f;           // no visible key: zeros
+            a = lsum > 0.0f ? a * inv : 0.0f;
+            b2 = lsum > 0.0f ? b2 * inv : 0.0f;
+            if (I8) {
+                const float2 sv = *reinterpret_cast<const float2*>(p.s_v + (int64_t)hk * d + ch);
+                a *= sv.x;
+                b2 *= sv.y;
+            }
+            const int ti = row / p.g;
+            const int64_t at_o = (int64_t)(q.t0 + ti) * p.o_ts + (int64_t)(hk * p.g + row - ti * p.g) * p.o_hs + ch;
+            if (p.out_bf16) *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.O) + at_o) = pack2<false>(a, b2);
+            else *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.O) + at_o) = make_float2(a, b2);
+        };
+        for (int x = tid; x < rows * (DP / 2); x += kThreads) {
+            const int row = x / (DP / 2), ch = (x - row * (DP / 2)) * 2;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm_m[w][row]);
+            float a = 0.0f, b2 = 0.0f, L = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = M == -INFINITY ? 0.0f : ex2(sm_m[w][row] - M);
+                const float2 v = *reinterpret_cast<const float2*>(ex + (w * 8 * NR + row) * DP + ch);
+                a = fmaf(f, v.x, a);
+                b2 = fmaf(f, v.y, b2);
+                L = fmaf(f, sm_l[w][row], L);
+            }
+            if (whole) {
+                if (ch < d) write_out(row, ch, a, b2, L);
+            } else {
+                __stcg(reinterpret_cast<float2*>(part + row * DP + ch), make_float2(a, b2));
+                if (ch == 0) __stcg(reinterpret_cast<float2*>(part + 8 * NR * DP + 2 * row), make_float2(M, L));
+            }
+        }
+        if (!whole) {
+            // CTA c owns blocks c N / G .. (c + 1) N / G: the unit's first and last block give its CTAs
+            const long long c0 = ((unit0 + 1) * G - 1) / N, c1 = ((unit0 + nb) * G - 1) / N;
+            __threadfence();
+            __syncthreads();
+            uint32_t* cnt = p.counters + ((int64_t)b * p.Hkv + hk);
+            if (tid == 0) {
+                const uint32_t n = atomicAdd(cnt, 1u);
+                sm_last = n == (uint32_t)(c1 - c0) ? 1u : 0u;
+                if (sm_last) *cnt = 0u;                   // zero again for the next call
+                __threadfence();
+            }
+            __syncthreads();
+            if (sm_last) {
+                auto part_of = [&](long long c) { return p.part + (c * 2 + (c == c0 ? 1 : 0)) * slots; };
+                for (int x = tid; x < rows * (DP / 2); x += kThreads) {
+                    const int row = x / (DP / 2), ch = (x - row * (DP / 2)) * 2;
+                    float M = -INFINITY, a = 0.0f, b2 = 0.0f, L = 0.0f;
+                    for (long long c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(part_of(c) + 8 * NR * DP + 2 * row));
+                    for (long long c = c0; c <= c1; ++c) {
+                        const float* src = part_of(c);
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 8 * NR * DP + 2 * row));
+                        const float f = M == -INFINITY ? 0.0f : ex2(ml.x - M);
+                        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + row * DP + ch));
+                        a = fmaf(f, v.x, a);
+                        b2 = fmaf(f, v.y, b2);
+                        L = fmaf(f, ml.y, L);
+                    }
+                    if (ch < d) write_out(row, ch, a, b2, L);
+                }
+            }
+        }
+        __syncthreads();                                  // the exchange buffer is a ring again
+        at = unit0 + blk1;
+    }
+}
+
+template <bool I8, int DP, int NR>
+int launch(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
+{
+    auto kern = pattn_few_kernel<I8, DP, NR>;
+    const int smem = Ring<I8, DP>::smem + (p.B + 1) * 8;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem > 48 * 1024 ? 112 * 1024 : 48 * 1024);
+    if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
+    int64_t grid = (int64_t)ctx->sm_count * 3;
+    if (grid > (int64_t)p.B * p.Hkv * kMaxParts) grid = (int64_t)p.B * p.Hkv * kMaxParts;
+    kern<<<(unsigned)grid, kThreads, smem, st>>>(p, 2);
+    ctx->launches += 1;
+    e = cudaGetLastError();
+    return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
+}
+
+}  // namespace
+
+size_t stwq_pattn_few_part_bytes(const stwq_ctx* ctx, int B, int Hkv, int d)
+{
+    (void)B; (void)Hkv;
+    const int DP = d <= 64 ? 64 : 128;
+    return (size_t)ctx->sm_count * 3 * 2 * 16 * (DP + 2) * 4;
+}
+
+int stwq_launch_pattn_few(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
+{
+    const bool i8 = p.s_k != nullptr;
+    const bool two = (int64_t)p.max_new * p.g > 8;
+    if (p.d <= 64) {
+        if (i8) return two ? launch<true, 64, 2>(ctx, p, st) : launch<true, 64, 1>(ctx, p, st);
+        return two ? launch<false, 64, 2>(ctx, p, st) : launch<false, 64, 1>(ctx, p, st);
+    }
+    if (i8) return two ? launch<true, 128, 2>(ctx, p, st) : launch<true, 128, 1>(ctx, p, st);
+    return two ? launch<false, 128, 2>(ctx, p, st) : launch<false, 128, 1>(ctx, p, st);
+}

@@ -1,0 +1,726 @@
+// Paged attention for many rows (a prefill chunk, a scale of an image pyramid): 256 query rows of one key head against
+// 128 keys at a time on the tensor cores. Rows are (new token, query head of the key head), token-major, so shared
+// key heads fill a tile with fewer tokens.
+//     S = Q K^T (fp32 in tensor memory),  P = 2^(S c - m),  O += P V,  O / l at the end
+//
+//  * Two tiles of 128 rows (A, B) share every K and V tile. Each has a group of 128 threads, one per row; while one group
+//    computes its probabilities the tensor core works for the other. The bound is the tensor core for d = 128 (2048 cycles
+//    per 256 x 128 tile) and the ex2 unit (16 per clock: 2048 cycles) for both d = 64 and d = 128.
+//  * S, P, O live in tensor memory: S_A, S_B 128 columns each, O_A, O_B d columns each. P (16-bit) is written over the S
+//    columns already read and is the A operand of the second product straight from there: no trip through shared memory.
+//  * K and V tiles are gathered page by page by four loader warps with cp.async into the 128-byte-swizzled layouts: K rows as
+//    K-major, V rows as they are (MN-major B operand: no transpose). Codes pass through registers and become fp16.
+//  * The running maximum is a reference that moves only when a row exceeds it by 2^10 (see the few-row kernel): the
+//    rescale of O in tensor memory is rare, and each score is read once.
+//  * With fewer units than SMs the keys of a unit are cut into equal ranges; partial (m, l, O) go to workspace and the
+//    last CTA adds them in key order.
+// 16-bit operands: bf16 for a bf16 cache (P rounded to bf16); fp16 for codes (exact), with queries scaled per row by a
+// power of two as in the few-row kernel. Sums, maxima and O in fp32.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "stwq_paged.cuh"
+#include "stwq_pattn.cuh"
+#include "stwq_ptx.cuh"
+
+using namespace stwq_ptx;
+
+namespace {
+
+constexpr int kRowWarps = 8, kLoadWarps = 4;
+constexpr int kThreads = 32 * (kRowWarps + kLoadWarps + 1);
+constexpr int kKT = 128;                     // keys per tile
+constexpr int kHalf = 128 * 128;             // bytes of 128 rows of 128 bytes
+constexpr int kMaxStages = 4;
+constexpr int kLag = 2;                      // loads in flight behind the one being issued
+constexpr int kMaxSplit = 32;
+constexpr float kSlack = 10.0f;
+constexpr int kTmemCols = 512, kColS = 0, kColO = 256;
+
+template <int NH>
+struct Smem {
+    static constexpr int stages = NH == 1 ? 4 : 2;
+    static constexpr int tile = NH * kHalf;              // one Q, K or V tile
+    static constexpr int offQ = 0;
+    static constexpr int offV = 2 * tile;
+    static constexpr int offK = offV + stages * tile;
+    static constexpr int offBars = offK + stages * tile;
+    static constexpr int offScale = offBars + 512;       // key scales: 4 slots of 128
+    static constexpr int offPre = offScale + 4 * 512;    // first unit of each request [B + 1]
+};
+
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t codes_half2(uint32_t w, uint32_t sel)      // w: codes ^ 0x80
+{
+    const uint32_t x = prmt(w, 0x64646464u, sel), k = 0x64806480u;
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+// D[128 x N] (+)= A B, kind::f16, fp32 accumulators; A from shared memory or from tensor memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// MN-major operand, 128-byte swizzle: rows (the contraction index) of 64 elements, 8-row groups 1024 bytes apart,
+// the next 64 elements of a row kHalf bytes further
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr)
+{
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)(kHalf >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// D fp32, A and B bf16 (1) or fp16 (0); bmn: B is MN-major
+__device__ __forceinline__ uint32_t idesc_f16(int n, bool bf16, bool bmn)
+{
+    const uint32_t f = bf16 ? 1u : 0u;
+    return (1u << 4) | (f << 7) | (f << 10) | ((bmn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+                   "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void rows_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+template <bool I8, int NH>
+__global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams p, const int sm_count)
+{
+    using L = Smem<NH>;
+    constexpr int NST = L::stages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t* smem = smem_raw + (base - raw);
+    const uint32_t bars = base + L::offBars;
+    auto bar_q = [&](int x) { return bars + 8u * x; };
+    auto bar_kfull = [&](int s) { return bars + 8u * (2 + s); };
+    auto bar_kempty = [&](int s) { return bars + 8u * (2 + kMaxStages + s); };
+    auto bar_vfull = [&](int s) { return bars + 8u * (2 + 2 * kMaxStages + s); };
+    auto bar_vempty = [&](int s) { return bars + 8u * (2 + 3 * kMaxStages + s); };
+    auto bar_s = [&](int x) { return bars + 8u * (2 + 4 * kMaxStages + x); };
+    auto bar_p = [&](int x) { return bars + 8u * (4 + 4 * kMaxStages + x); };
+    auto bar_o = [&](int x) { return bars + 8u * (6 + 4 * kMaxStages + x); };
+    const uint32_t bar_drain = bars + 8u * (8 + 4 * kMaxStages);
+    uint32_t* misc = reinterpret_cast<uint32_t*>(smem + L::offBars + 256);
+    uint32_t* tmem_slot = misc;
+    volatile uint32_t* abort_flag = misc + 1;
+    uint32_t* sm_last = misc + 2;
+    int* wsum = reinterpret_cast<int*>(misc + 8);         // [13]
+    int* pre = reinterpret_cast<int*>(smem + L::offPre);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // ---- units of every request: key heads x tiles of 256 rows
+    bool bad = false;
+    auto units_of = [&](int b) -> int {
+        const PaReq q = pa_request(p, b, bad);
+        const int rows = q.n * p.g;
+        return rows <= p.few_max || q.n <= 0 ? 0 : p.Hkv * ((rows + 255) / 256);
+    };
+    {
+        const int per = (p.B + kThreads - 1) / kThreads;
+        const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
+        int sum = 0;
+        for (int b = b0; b < b1; ++b) sum += units_of(b);
+        int s = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, s, o);
+            if (lane >= o) s += u;
+        }
+        if (lane == 31) wsum[warp] = s;
+        __syncthreads();
+        int at = s - sum;
+        for (int w = 0; w < warp; ++w) at += wsum[w];
+        for (int b = b0; b < b1; ++b) {
+            pre[b] = at;
+            at += units_of(b);
+        }
+        if (tid == kThreads - 1) pre[p.B] = at;
+    }
+    if (bad && blockIdx.x == 0) atomicOr(p.status, STWQ_DEV_PAGES);
+    __syncthreads();
+    const int U = pre[p.B];
+    if (U == 0) return;
+    const int nS = min(max(sm_count / U, 1), kMaxSplit);  // ranges of keys per unit
+    if ((int)blockIdx.x >= U * nS) return;
+    const int unit = blockIdx.x / nS, split = blockIdx.x - unit * nS;
+    int b = 0;
+    {
+        int x0 = 0, x1 = p.B;
+        while (x1 - x0 > 1) {
+            const int m = (x0 + x1) >> 1;
+            if (pre[m] <= unit) x0 = m;
+            else x1 = m;
+        }
+        b = x0;                                           // requests without units share their start with the next one
+    }
+    const PaReq q = pa_request(p, b, bad);
+    const int rows = q.n * p.g;
+    const int nqt = (rows + 255) / 256;
+    const int ul = unit - pre[b];
+    const int qt = nqt - 1 - ul / p.Hkv, hk = ul % p.Hkv; // late rows first: under a causal mask they see the most keys
+    const int row0 = qt * 256;
+    // keys that the last row of tile x sees, and tiles of keys
+    auto last_limit = [&](int x) -> int {
+        const int last = min(rows, row0 + 128 * (x + 1)) - 1;
+        if (last < row0 + 128 * x) return 0;
+        return max(0, p.causal ? q.kv - q.n + last / p.g + 1 : q.kv);
+    };
+    const int tiles0 = (last_limit(0) + kKT - 1) / kKT, tiles1 = (last_limit(1) + kKT - 1) / kKT;
+    const int tiles = max(tiles0, tiles1);
+    const int eS = min(nS, max(1, (tiles + 1) / 2));      // ranges of at least two tiles
+    if (split >= eS) return;
+    const int t0 = (int)((long long)tiles * split / eS), t1 = (int)((long long)tiles * (split + 1) / eS);
+    const int nt0 = max(0, min(tiles0, t1) - t0), nt1 = max(0, min(tiles1, t1) - t0);
+    const int n = max(nt0, nt1);
+
+    if (tid == 0) {
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(bar_q(x), 4);
+            mbar_init(bar_s(x), 1);
+            mbar_init(bar_p(x), 4);
+            mbar_init(bar_o(x), 1);
+        }
+        for (int s = 0; s < NST; ++s) {
+            mbar_init(bar_kfull(s), kLoadWarps);
+            mbar_init(bar_kempty(s), 1);
+            mbar_init(bar_vfull(s), kLoadWarps);
+            mbar_init(bar_vempty(s), 1);
+        }
+        mbar_init(bar_drain, 1);
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_smem();
+    }
+    if (warp == kRowWarps + kLoadWarps) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const unsigned long long limit_ns = p.wait_limit_ns;
+    const int d = p.d;
+
+    if (warp == kRowWarps + kLoadWarps) {
+        // ------------------------------------------------------------------------------------ MMA issuer
+        if (lane == 0 && n > 0) {
+            const uint32_t id_s = idesc_f16(kKT, !I8, false), id_o = idesc_f16(d, !I8, true);
+            const int ksteps = d / 16;
+            auto qk = [&](int x, int s) {
+#pragma unroll
+                for (int k = 0; k < NH * 4; ++k)
+                    if (k < ksteps) {
+                        const uint32_t off = (uint32_t)((k >> 2) * kHalf + (k & 3) * 32);
+                        mma_ss(tmem + kColS + 128 * x, make_smem_desc(base + L::offQ + x * L::tile + off),
+                               make_smem_desc(base + L::offK + s * L::tile + off), id_s, k > 0 ? 1u : 0u);
+                    }
+            };
+            auto pv = [&](int x, int s, uint32_t acc) {
+#pragma unroll
+                for (int k = 0; k < kKT / 16; ++k)
+                    mma_ts(tmem + kColO + 128 * x, tmem + kColS + 128 * x + 8 * k, desc_mn(base + L::offV + s * L::tile + k * 2048), id_o,
+                           k > 0 ? 1u : acc);
+            };
+            bool ok = true;
+            const int nt[2] = {nt0, nt1};
+            for (int x = 0; ok && x < 2; ++x)
+                if (nt[x] > 0) ok = mbar_wait(bar_q(x), 0u, abort_flag, limit_ns);
+            ok = ok && mbar_wait(bar_kfull(0), 0u, abort_flag, limit_ns);
+            if (ok) {
+                tc_fence_after();
+                for (int x = 0; x < 2; ++x)
+                    if (nt[x] > 0) {
+                        qk(x, 0);
+                        tc_commit(bar_s(x));
+                    }
+                tc_commit(bar_kempty(0));
+            }
+            for (int j = 0; ok && j < n; ++j) {
+                const int sv = j % NST, sk = (j + 1) % NST;
+                ok = mbar_wait(bar_vfull(sv), (uint32_t)(j / NST) & 1u, abort_flag, limit_ns);
+                if (ok && j + 1 < n) ok = mbar_wait(bar_kfull(sk), (uint32_t)((j + 1) / NST) & 1u, abort_flag, limit_ns);
+                for (int x = 0; ok && x < 2; ++x) {
+                    if (j >= nt[x]) continue;
+                    ok = mbar_wait(bar_p(x), (uint32_t)j & 1u, abort_flag, limit_ns);
+                    if (!ok) break;
+                    tc_fence_after();
+                    pv(x, sv, j > 0 ? 1u : 0u);
+                    if (j + 1 < nt[x]) {
+                        qk(x, sk);                        // over S and P, behind the product that reads P
+                        tc_commit(bar_s(x));
+                    } else tc_commit(bar_o(x));
+                }
+                if (ok) {
+                    tc_commit(bar_vempty(sv));
+                    if (j + 1 < n) tc_commit(bar_kempty(sk));
+                }
+            }
+            if (!ok) {                                    // giving up: products already issued must not outlive the tensor memory
+                tc_commit(bar_drain);
+                const unsigned long long w0 = globaltimer_ns();
+                while (!mbar_try_wait(bar_drain, 0u))
+                    if (globaltimer_ns() - w0 > limit_ns) break;
+            }
+        }
+    } else if (warp >= kRowWarps) {
+        // ------------------------------------------------------------------------------------ loaders
+        const int lt = tid - 32 * kRowWarps;              // 0 .. 127
+        const int es = I8 ? 1 : 2;
+        const int ppk = d * es / 16;                      // 16-byte pieces per key
+        const int per_page = p.S / 16;
+        const int64_t row_bytes = (int64_t)d * es, page_bytes = row_bytes * p.S;
+        const int32_t* trow = p.table + (int64_t)b * p.W;
+        const int kstep = 128 / ppk, cstep = 128 - kstep * ppk;
+        const int key00 = lt / ppk, c00 = lt - key00 * ppk;
+        bool ok = true;
+        int id = 0;                                       // lane 0 .. 7: page of that 16-key block of the tile
+        auto load_ids = [&](int j) {
+            const int b16 = (t0 + j) * 8 + (lane & 7);
+            int v = 0;
+            if (b16 * 16 < q.kv) {
+                v = __ldg(trow + b16 / per_page);
+                if (v < 0 || v >= p.n_pages) {
+                    atomicOr(p.status, STWQ_DEV_PAGES);
+                    v = 0;
+                }
+            }
+            return v;
+        };
+        // element offset (bytes) of a key's row, inside the pool
+        auto key_at = [&](int j, int key, int ids) -> int64_t {
+            const int page = __shfl_sync(0xffffffffu, ids, (key >> 4) & 7);
+            const int b16 = (t0 + j) * 8 + (key >> 4);
+            return ((int64_t)page * p.Hkv + hk) * page_bytes + ((b16 % per_page) * 16 + (key & 15)) * row_bytes;
+        };
+        auto wait_stage = [&](bool is_v, int j) -> bool {
+            if (j < NST) return true;
+            const int s = j % NST;
+            return mbar_wait(is_v ? bar_vempty(s) : bar_kempty(s), (uint32_t)(j / NST + 1) & 1u, abort_flag, limit_ns);
+        };
+        auto publish = [&](int i) {                       // load i: key tile i / 2 (even) or value tile i / 2 (odd)
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive((i & 1) ? bar_vfull((i >> 1) % NST) : bar_kfull((i >> 1) % NST));
+        };
+        if (n > 0) id = load_ids(0);
+        if (!I8) {
+            int i = 0;
+            for (; i < 2 * n; ++i) {
+                const int j = i >> 1;
+                const bool is_v = i & 1;
+                ok = wait_stage(is_v, j);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t dst0 = base + (is_v ? L::offV : L::offK) + (j % NST) * L::tile;
+                const uint8_t* pool = reinterpret_cast<const uint8_t*>(is_v ? p.Vp : p.Kp);
+                int key = key00, c = c00;
+                for (int k = 0; k < ppk; ++k) {
+                    const int64_t off = key_at(j, key, id);
+                    const uint32_t dst = dst0 + (c >> 3) * kHalf + key * 128 + (((c & 7) ^ (key & 7)) << 4);
+                    cp_async16(dst, pool + off + c * 16, (t0 + j) * kKT + key < q.kv);
+                    key += kstep;
+                    c += cstep;
+                    if (c >= ppk) {
+                        c -= ppk;
+                        ++key;
+                    }
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (is_v) id = j + 1 < n ? load_ids(j + 1) : 0;
+                if (i >= kLag) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+                    publish(i - kLag);
+                }
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if (ok)
+                for (int k = max(0, 2 * n - kLag); k < 2 * n; ++k) publish(k);
+        } else {
+            // codes: the next tile's bytes are on their way in registers while this one is widened
+            constexpr int kMaxP = NH == 1 ? 4 : 8;
+            uint4 buf[kMaxP];
+            float sk = 0.0f;
+            auto fetch = [&](int i) {
+                const int j = i >> 1;
+                const uint8_t* pool = reinterpret_cast<const uint8_t*>((i & 1) ? p.Vp : p.Kp);
+                int key = key00, c = c00;
+#pragma unroll
+                for (int k = 0; k < kMaxP; ++k)
+                    if (k < ppk) {
+                        const int64_t off = key_at(j, key, id);
+                        buf[k] = make_uint4(0u, 0u, 0u, 0u);
+                        if ((t0 + j) * kKT + key < q.kv) buf[k] = __ldg(reinterpret_cast<const uint4*>(pool + off + c * 16));
+                        key += kstep;
+                        c += cstep;
+                        if (c >= ppk) {
+                            c -= ppk;
+                            ++key;
+                        }
+                    }
+                if (!(i & 1)) {
+                    const int kj = (t0 + j) * kKT + lt;
+                    sk = kj < q.kv ? __ldg(p.s_k + kj) : 0.0f;
+                } else id = j + 1 < n ? load_ids(j + 1) : 0;
+            };
+            if (n > 0) fetch(0);
+            for (int i = 0; i < 2 * n; ++i) {
+                const int j = i >> 1;
+                const bool is_v = i & 1;
+                ok = wait_stage(is_v, j);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t dst0 = base + (is_v ? L::offV : L::offK) + (j % NST) * L::tile;
+                uint4 cur[kMaxP];
+#pragma unroll
+                for (int k = 0; k < kMaxP; ++k) cur[k] = buf[k];
+                if (!is_v) reinterpret_cast<float*>(smem + L::offScale)[(j & 3) * 128 + lt] = sk;
+                if (i + 1 < 2 * n) fetch(i + 1);
+                int key = key00, c = c00;
+#pragma unroll
+                for (int k = 0; k < kMaxP; ++k)
+                    if (k < ppk) {
+                        const bool live = (t0 + j) * kKT + key < q.kv;
+                        const uint32_t w[4] = {cur[k].x, cur[k].y, cur[k].z, cur[k].w};
+                        uint32_t h[8];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t u = live ? w[e] ^ 0x80808080u : 0x80808080u;
+                            h[2 * e] = codes_half2(u, 0x4140u);
+                            h[2 * e + 1] = codes_half2(u, 0x4342u);
+                        }
+                        const int cc = 2 * c;             // 16-byte pieces of the widened row
+                        const uint32_t dst = dst0 + (cc >> 3) * kHalf + key * 128;
+                        st_shared_v4(dst + (((cc & 7) ^ (key & 7)) << 4), h[0], h[1], h[2], h[3]);
+                        st_shared_v4(dst + ((((cc + 1) & 7) ^ (key & 7)) << 4), h[4], h[5], h[6], h[7]);
+                        key += kstep;
+                        c += cstep;
+                        if (c >= ppk) {
+                            c -= ppk;
+                            ++key;
+                        }
+                    }
+                publish(i);
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------------------------ one thread per row
+        const int x = warp >> 2;                          // tile
+        const int rl = tid & 127;                         // row of the tile
+        const int row = row0 + 128 * x + rl;
+        const bool live = row < rows;
+        const int ti = live ? row / p.g : 0, hd = hk * p.g + (live ? row - ti * p.g : 0);
+        const int nt = x == 0 ? nt0 : nt1;
+        const int vis = !live ? 0 : max(0, p.causal ? q.kv - q.n + ti + 1 : q.kv);        // keys this row sees
+        float inv = 1.0f;
+        if (nt > 0) {
+            // ---- the row of Q, swizzled
+            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.Q) + (int64_t)(q.t0 + ti) * p.q_ts +
+                                                              (int64_t)hd * p.q_hs);
+            const uint32_t dst = base + L::offQ + x * L::tile + rl * 128;
+            float up = 1.0f;
+            if (I8) {
+                float mx = 0.0f;
+                for (int c = 0; c < d / 8; ++c) {
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (live) v = __ldg(src + c);
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u))));
+                }
+                int e = (int)(__float_as_uint(mx) >> 23) - 127;
+                e = mx > 0.0f && mx < INFINITY ? max(e, -100) : 13;
+                up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
+                inv = __uint_as_float((uint32_t)(e - 13 + 127) << 23);
+            }
+#pragma unroll
+            for (int c = 0; c < NH * 8; ++c)
+                if (c < d / 8) {
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (live) v = __ldg(src + c);
+                    if (I8) {
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = pack_f16(__uint_as_float(w[e] << 16) * up, __uint_as_float(w[e] & 0xffff0000u) * up);
+                        v = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    st_shared_v4(dst + (c >> 3) * kHalf + (((c & 7) ^ (rl & 7)) << 4), v.x, v.y, v.z, v.w);
+                }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_q(x));
+        }
+        const float cc = p.scale * kPaLog2e * inv;        // scores in units of log2
+        const uint64_t cc2 = dup_f2(cc);
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t ts = tmem + kColS + 128 * x + lanes, to = tmem + kColO + 128 * x + lanes;
+        const int min_vis = __reduce_min_sync(0xffffffffu, live ? vis : 0x7fffffff);
+        float m = -INFINITY, l = 0.0f;
+        bool ok = true;
+        for (int j = 0; j < nt; ++j) {
+            ok = mbar_wait(bar_s(x), (uint32_t)j & 1u, abort_flag, limit_ns);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const int key0 = (t0 + j) * kKT;
+            const bool masked = key0 + kKT > min_vis;     // uniform over the warp
+            const float4* sks = reinterpret_cast<const float4*>(smem + L::offScale) + (j & 3) * 32;
+            uint32_t v[32];
+            tmem_ld32(ts, v);
+#pragma unroll
+            for (int qd = 0; qd < 4; ++qd) {
+                tmem_ld_wait();
+                uint64_t s2[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) s2[k] = pack_f2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
+                if (I8) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float4 f = sks[qd * 8 + k];
+                        s2[2 * k] = mul_f2(s2[2 * k], pack_f2(f.x, f.y));
+                        s2[2 * k + 1] = mul_f2(s2[2 * k + 1], pack_f2(f.z, f.w));
+                    }
+                }
+                if (qd < 3) tmem_ld32(ts + 32 * (qd + 1), v);
+                if (masked) {
+                    const int seen = vis - key0 - 32 * qd;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float a, c;
+                        unpack_f2(s2[k], a, c);
+                        s2[k] = pack_f2(2 * k < seen ? a : -INFINITY, 2 * k + 1 < seen ? c : -INFINITY);
+                    }
+                }
+                float mx = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    float a, c;
+                    unpack_f2(s2[k], a, c);
+                    mx = fmaxf(mx, fmaxf(a, c));
+                }
+                mx *= cc;                                 // cc > 0
+                if (__any_sync(0xffffffffu, mx > m + kSlack)) {
+                    // the reference moves: what was summed, written and accumulated so far is scaled down to it
+                    const float mn = fmaxf(m, mx);
+                    const float f = mn == -INFINITY ? 1.0f : ex2_approx(m - mn);
+                    m = mn;
+                    l *= f;
+                    uint32_t w[16];
+                    if (qd < 3) tmem_ld_wait();
+                    if (j > 0)
+                        for (int cb = 0; cb < d; cb += 16) {
+                            tmem_ld16(to + cb, w);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
+                            tmem_st16(to + cb, w);
+                        }
+                    for (int pb = 0; pb < qd; ++pb) {
+                        tmem_ld16(ts + 16 * pb, w);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            if (I8) {
+                                const float2 pv = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                                w[k] = pack_f16(pv.x * f, pv.y * f);
+                            } else w[k] = pack_bf16(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xffff0000u) * f);
+                        }
+                        tmem_st16(ts + 16 * pb, w);
+                    }
+                    tmem_st_wait();
+                }
+                const float mm = m == -INFINITY ? 0.0f : m - (I8 ? 4.0f : 0.0f);       // fp16: four octaves up keep small probabilities' bits
+                const uint64_t negm2 = dup_f2(-mm);
+                uint32_t w[16];
+                uint64_t l2 = 0ull;                       // (0, 0)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    float a, c;
+                    unpack_f2(fma_f2(s2[k], cc2, negm2), a, c);
+                    a = ex2_approx(a);
+                    c = ex2_approx(c);
+                    l2 = add_f2(l2, pack_f2(a, c));
+                    w[k] = I8 ? pack_f16(a, c) : pack_bf16(a, c);
+                }
+                float la, lb;
+                unpack_f2(l2, la, lb);
+                l += la + lb;
+                tmem_st16(ts + 16 * qd, w);               // columns whose scores have been read
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_p(x));
+        }
+        // ---- O
+        if (ok && nt > 0) {
+            ok = mbar_wait(bar_o(x), 0u, abort_flag, limit_ns);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+        }
+        auto write16 = [&](int cb, float (&o)[16], float rl_sum) {       // 16 channels of the row
+            const float inv_l = rl_sum > 0.0f ? __fdividef(1.0f, rl_sum) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                o[k] = rl_sum != 0.0f ? o[k] * inv_l : 0.0f;             // no visible key: zeros
+                if (I8) o[k] *= __ldg(p.s_v + (int64_t)hk * d + cb + k);
+            }
+            const int64_t at = (int64_t)(q.t0 + ti) * p.o_ts + (int64_t)hd * p.o_hs + cb;
+            if (p.out_bf16) {
+                uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.O) + at);
+                dst[0] = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
+                dst[1] = make_uint4(pack_bf16(o[8], o[9]), pack_bf16(o[10], o[11]), pack_bf16(o[12], o[13]), pack_bf16(o[14], o[15]));
+            } else {
+                float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.O) + at);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) dst[k] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            }
+        };
+        constexpr int DP = NH * 64;
+        const int64_t part_f4 = (int64_t)(DP / 4) * 256 + 128;           // float4s of a partial result: O, then (m, l)
+        float4* part = reinterpret_cast<float4*>(p.part) + ((int64_t)unit * nS + split) * part_f4;
+        const int pr = 128 * x + rl;
+        if (ok) {
+            for (int cb = 0; cb < d; cb += 16) {
+                uint32_t w[16];
+                float o[16];
+                if (nt > 0) {
+                    tmem_ld16(to + cb, w);
+                    tmem_ld_wait();
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[k] = nt > 0 ? __uint_as_float(w[k]) : 0.0f;
+                if (eS == 1) {
+                    if (live) write16(cb, o, l);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) __stcg(part + (cb / 4 + k) * 256 + pr, make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
+                }
+            }
+        }
+        if (eS > 1) {
+            float2* ml = reinterpret_cast<float2*>(part + (DP / 4) * 256);
+            __stcg(ml + pr, make_float2(m, l));
+            __threadfence();
+            rows_barrier();
+            if (tid == 0) {
+                const uint32_t k = atomicAdd(p.counters + unit, 1u);
+                *sm_last = k == (uint32_t)(eS - 1) ? 1u : 0u;
+                if (*sm_last) p.counters[unit] = 0u;      // zero again for the next call
+                __threadfence();
+            }
+            rows_barrier();
+            if (*sm_last && live) {
+                const float4* p0 = reinterpret_cast<const float4*>(p.part) + (int64_t)unit * nS * part_f4;
+                float M = -INFINITY, Ls = 0.0f;
+                float* fs = reinterpret_cast<float*>(smem);              // [eS][256]: the operand tiles are no longer needed
+                for (int s = 0; s < eS; ++s) {
+                    const float2 v = __ldcg(reinterpret_cast<const float2*>(p0 + s * part_f4 + (DP / 4) * 256) + pr);
+                    M = fmaxf(M, v.x);
+                }
+                for (int s = 0; s < eS; ++s) {
+                    const float2 v = __ldcg(reinterpret_cast<const float2*>(p0 + s * part_f4 + (DP / 4) * 256) + pr);
+                    const float f = M == -INFINITY ? 0.0f : ex2_approx(v.x - M);
+                    fs[s * 256 + pr] = f;
+                    Ls = fmaf(f, v.y, Ls);
+                }
+                for (int cb = 0; cb < d; cb += 16) {
+                    float o[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) o[k] = 0.0f;
+                    for (int s = 0; s < eS; ++s) {
+                        const float f = fs[s * 256 + pr];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float4 v = __ldcg(p0 + s * part_f4 + (cb / 4 + k) * 256 + pr);
+                            o[4 * k] = fmaf(f, v.x, o[4 * k]);
+                            o[4 * k + 1] = fmaf(f, v.y, o[4 * k + 1]);
+                            o[4 * k + 2] = fmaf(f, v.z, o[4 * k + 2]);
+                            o[4 * k + 3] = fmaf(f, v.w, o[4 * k + 3]);
+                        }
+                    }
+                    write16(cb, o, Ls);
+                }
+            }
+        }
+    }
+    // ---- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (tid == 0 && *abort_flag) atomicOr(p.status, STWQ_DEV_TIMEOUT);
+    tc_fence_after();
+    if (warp == kRowWarps + kLoadWarps) {
+        __syncwarp();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+template <bool I8, int NH>
+int launch(stwq_ctx* ctx, const PaParams& p, unsigned grid, cudaStream_t st)
+{
+    auto kern = pattn_tiled_kernel<I8, NH>;
+    int smem = Smem<NH>::offPre + (p.B + 1) * 4 + 1024;
+    if (smem < 116 * 1024) smem = 116 * 1024;             // all of tensor memory: one CTA per SM
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
+    if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
+    kern<<<grid, kThreads, smem, st>>>(p, ctx->sm_count);
+    ctx->launches += 1;
+    e = cudaGetLastError();
+    return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
+}
+
+}  // namespace
+
+size_t stwq_pattn_tiled_part_bytes(const stwq_ctx* ctx, int d)
+{
+    const int DP = d <= 64 ? 64 : 128;
+    return (size_t)ctx->sm_count * ((size_t)(DP / 4) * 256 + 128) * 16;      // only with units x ranges <= SMs
+}
+
+int stwq_launch_pattn_tiled(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
+{
+    // units: at most ceil(rows / 256) per request and key head, rows adding up to T g
+    int64_t grid = (int64_t)p.Hkv * ((p.T * p.g + 255) / 256 + p.B);
+    if (grid < ctx->sm_count) grid = ctx->sm_count;
+    if (grid > 0x7fffffff) return STWQ_ERR_DIM;
+    const unsigned gx = (unsigned)grid;
+    if (p.d <= 64) return p.s_k ? launch<true, 1>(ctx, p, gx, st) : launch<false, 1>(ctx, p, gx, st);
+    return p.s_k ? launch<true, 2>(ctx, p, gx, st) : launch<false, 2>(ctx, p, gx, st);
+}
