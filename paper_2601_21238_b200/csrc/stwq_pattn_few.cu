@@ -16,6 +16,9 @@
 //    thread's own groups are. Enough stages for 100 KB and more in flight per SM.
 //  * The running maximum is a reference, not the maximum: it moves only when a score exceeds it by more than 2^10 (a vote
 //    per block instead of six shuffles). fp32 sums; P in bf16, or in fp16 over the code cache.
+//  * fp32 output: P goes in as a sum of 16-bit terms (bf16: three, fp16: two; 22 to 24 significant bits), and each block's
+//    product is added to O by fp32 instructions: the tensor core truncates its running sums, which over thousands of keys
+//    would show in an fp32 result (1e-5 over 5000 keys). For bf16 output P is one term, an error like that of the store.
 //  * Codes (int8) become fp16, exactly: byte ^ 0x80 under the exponent of 1024, minus 1152. Queries are scaled by a power of
 //    two per row so that their largest lies in [2^13, 2^14): bf16 -> fp16 is then exact down to 2^-37 of that
 //    largest. Key scales multiply S (fp32), value scales multiply O at the end.
@@ -123,8 +126,15 @@ struct Ring {
     static constexpr int smem = kWarps * stages * stage;
 };
 
-template <bool I8, int DP, int NR>
-__global__ void __launch_bounds__(kThreads, 3) pattn_few_kernel(const PaParams p, const int min_blocks)
+template <bool F16>
+__device__ __forceinline__ float2 unpack2(uint32_t w)
+{
+    if (F16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+template <bool I8, int DP, int NR, bool F32>
+__global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const PaParams p, const int min_blocks)
 {
     using R = Ring<I8, DP>;
     constexpr int NT = DP / 16;                           // channel tiles of O^T
@@ -415,7 +425,8 @@ __global__ void __launch_bounds__(kThreads, 3) pattn_few_kernel(const PaParams p
                         }
                     }
             }
-            uint32_t pf[NR][2];
+            constexpr int kTerms = !F32 ? 1 : (I8 ? 2 : 3);
+            uint32_t pf[kTerms][NR][2];                   // P^T fragments: the value, then what rounding it left over
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr) {
                 float pv[4];
@@ -427,9 +438,28 @@ __global__ void __launch_bounds__(kThreads, 3) pattn_few_kernel(const PaParams p
                     pv[2 + e] = ex2(s[nr][2 + e] - mm);
                     l[nr][e] += pv[e] + pv[2 + e];
                 }
-                pf[nr][0] = transpose8x8(pack2<I8>(pv[0], pv[1]));
-                pf[nr][1] = transpose8x8(pack2<I8>(pv[2], pv[3]));
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float a = pv[2 * e], c = pv[2 * e + 1];
+#pragma unroll
+                    for (int k = 0; k < kTerms; ++k) {
+                        const uint32_t h = pack2<I8>(a, c);
+                        pf[k][nr][e] = transpose8x8(h);
+                        const float2 v = unpack2<I8>(h);
+                        a -= v.x;
+                        c -= v.y;
+                    }
+                }
             }
+            auto pv_mma = [&](int nr, int i, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+                if (F32) {
+                    float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int k = kTerms - 1; k >= 0; --k) mma<I8>(c, a0, a1, a2, a3, pf[k][nr][0], pf[k][nr][1]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[nr][i][k] += c[k];
+                } else mma<I8>(o[nr][i], a0, a1, a2, a3, pf[0][nr][0], pf[0][nr][1]);
+            };
             // ---- O^T += V^T P^T
             if (!I8) {
 #pragma unroll
@@ -444,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 3) pattn_few_kernel(const PaParams p
                         const uint32_t a0 = prmt(w[0][i], w[1][i], 0x5410u), a1 = prmt(w[0][i], w[1][i], 0x7632u);
                         const uint32_t a2 = prmt(w[2][i], w[3][i], 0x5410u), a3 = prmt(w[2][i], w[3][i], 0x7632u);
 #pragma unroll
-                        for (int nr = 0; nr < NR; ++nr) mma<false>(o[nr][hh * 4 + i], a0, a1, a2, a3, pf[nr][0], pf[nr][1]);
+                        for (int nr = 0; nr < NR; ++nr) pv_mma(nr, hh * 4 + i, a0, a1, a2, a3);
                     }
                 }
             } else {
@@ -473,8 +503,8 @@ __global__ void __launch_bounds__(kThreads, 3) pattn_few_kernel(const PaParams p
                     const uint32_t c2 = codes_half2(y23, 0x4140u), c3 = codes_half2(y23, 0x4342u);
 #pragma unroll
                     for (int nr = 0; nr < NR; ++nr) {
-                        mma<true>(o[nr][2 * i], a0, a1, a2, a3, pf[nr][0], pf[nr][1]);
-                        mma<true>(o[nr][2 * i + 1], c0, c1, c2, c3, pf[nr][0], pf[nr][1]);
+                        pv_mma(nr, 2 * i, a0, a1, a2, a3);
+                        pv_mma(nr, 2 * i + 1, c0, c1, c2, c3);
                     }
                 }
             }
@@ -522,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 3) pattn_few_kernel(const PaParams p
             }
             const int ti = row / p.g;
             const int64_t at_o = (int64_t)(q.t0 + ti) * p.o_ts + (int64_t)(hk * p.g + row - ti * p.g) * p.o_hs + ch;
-            if (p.out_bf16) *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.O) + at_o) = pack2<false>(a, b2);
+            if (!F32) *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.O) + at_o) = pack2<false>(a, b2);
             else *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.O) + at_o) = make_float2(a, b2);
         };
         for (int x = tid; x < rows * (DP / 2); x += kThreads) {
@@ -583,10 +613,10 @@ __global__ void __launch_bounds__(kThreads, 3) pattn_few_kernel(const PaParams p
     }
 }
 
-template <bool I8, int DP, int NR>
-int launch(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
+template <bool I8, int DP, int NR, bool F32>
+int launch_as(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
 {
-    auto kern = pattn_few_kernel<I8, DP, NR>;
+    auto kern = pattn_few_kernel<I8, DP, NR, F32>;
     const int smem = Ring<I8, DP>::smem + (p.B + 1) * 8;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem > 48 * 1024 ? 112 * 1024 : 48 * 1024);
     if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
@@ -596,6 +626,12 @@ int launch(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
     ctx->launches += 1;
     e = cudaGetLastError();
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
+}
+
+template <bool I8, int DP, int NR>
+int launch(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
+{
+    return p.out_bf16 ? launch_as<I8, DP, NR, false>(ctx, p, st) : launch_as<I8, DP, NR, true>(ctx, p, st);
 }
 
 }  // namespace

@@ -14,6 +14,9 @@
 //    rescale of O in tensor memory is rare, and each score is read once.
 //  * With fewer units than SMs the keys of a unit are cut into equal ranges; partial (m, l, O) go to workspace and the
 //    last CTA adds them in key order.
+//  * fp32 output: P is kept as a sum of 16-bit terms (bf16: three, fp16: two; 22 to 24 significant bits), all multiplied by V.
+//    The tensor core truncates its running sums (1e-5 over 5000 keys), so the row threads add each tile's product to an
+//    fp32 sum beside it. Both want tensor memory: a CTA then has one tile of rows, not two.
 // 16-bit operands: bf16 for a bf16 cache (P rounded to bf16); fp16 for codes (exact), with queries scaled per row by a
 // power of two as in the few-row kernel. Sums, maxima and O in fp32.
 #include <cuda.h>
@@ -33,10 +36,10 @@ constexpr int kThreads = 32 * (kRowWarps + kLoadWarps + 1);
 constexpr int kKT = 128;                     // keys per tile
 constexpr int kHalf = 128 * 128;             // bytes of 128 rows of 128 bytes
 constexpr int kMaxStages = 4;
-constexpr int kLag = 2;                      // loads in flight behind the one being issued
 constexpr int kMaxSplit = 32;
 constexpr float kSlack = 10.0f;
 constexpr int kTmemCols = 512, kColS = 0, kColO = 256;
+constexpr int kColMore = 128, kColSum = 384; // fp32 output: further terms of P (64 columns each), the fp32 sum of O
 
 template <int NH>
 struct Smem {
@@ -46,8 +49,12 @@ struct Smem {
     static constexpr int offV = 2 * tile;
     static constexpr int offK = offV + stages * tile;
     static constexpr int offBars = offK + stages * tile;
-    static constexpr int offScale = offBars + 512;       // key scales: 4 slots of 128
-    static constexpr int offPre = offScale + 4 * 512;    // first unit of each request [B + 1]
+    // Key scales, a slot of 128 per tile. The loaders write slot j once the first product of tile j - stages is done, when
+    // the row threads may still be reading that tile's: stages + 1 slots are alive at once.
+    static constexpr int offScale = offBars + 512;
+    static constexpr int slots = 8;
+    static constexpr int offPre = offScale + slots * 512;               // first unit of each request [B + 1]
+    static_assert(stages + 1 <= slots, "key-scale slots");
 };
 
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
@@ -117,11 +124,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void rows_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-template <bool I8, int NH>
+template <bool I8, int NH, bool F32>
 __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams p, const int sm_count)
 {
     using L = Smem<NH>;
     constexpr int NST = L::stages;
+    constexpr int kX = F32 ? 1 : 2;                       // tiles of 128 rows
+    constexpr int kRows = 128 * kX;
+    constexpr int kTerms = !F32 ? 1 : (I8 ? 2 : 3);       // 16-bit terms of P
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -149,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     auto units_of = [&](int b) -> int {
         const PaReq q = pa_request(p, b, bad);
         const int rows = q.n * p.g;
-        return rows <= p.few_max || q.n <= 0 ? 0 : p.Hkv * ((rows + 255) / 256);
+        return rows <= p.few_max || q.n <= 0 ? 0 : p.Hkv * ((rows + kRows - 1) / kRows);
     };
     {
         const int per = (p.B + kThreads - 1) / kThreads;
@@ -191,17 +201,17 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     }
     const PaReq q = pa_request(p, b, bad);
     const int rows = q.n * p.g;
-    const int nqt = (rows + 255) / 256;
+    const int nqt = (rows + kRows - 1) / kRows;
     const int ul = unit - pre[b];
     const int qt = nqt - 1 - ul / p.Hkv, hk = ul % p.Hkv; // late rows first: under a causal mask they see the most keys
-    const int row0 = qt * 256;
+    const int row0 = qt * kRows;
     // keys that the last row of tile x sees, and tiles of keys
     auto last_limit = [&](int x) -> int {
         const int last = min(rows, row0 + 128 * (x + 1)) - 1;
         if (last < row0 + 128 * x) return 0;
         return max(0, p.causal ? q.kv - q.n + last / p.g + 1 : q.kv);
     };
-    const int tiles0 = (last_limit(0) + kKT - 1) / kKT, tiles1 = (last_limit(1) + kKT - 1) / kKT;
+    const int tiles0 = (last_limit(0) + kKT - 1) / kKT, tiles1 = kX == 1 ? 0 : (last_limit(1) + kKT - 1) / kKT;
     const int tiles = max(tiles0, tiles1);
     const int eS = min(nS, max(1, (tiles + 1) / 2));      // ranges of at least two tiles
     if (split >= eS) return;
@@ -217,9 +227,9 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             mbar_init(bar_o(x), 1);
         }
         for (int s = 0; s < NST; ++s) {
-            mbar_init(bar_kfull(s), kLoadWarps);
+            mbar_init(bar_kfull(s), I8 ? kLoadWarps : 32 * kLoadWarps);
             mbar_init(bar_kempty(s), 1);
-            mbar_init(bar_vfull(s), kLoadWarps);
+            mbar_init(bar_vfull(s), I8 ? kLoadWarps : 32 * kLoadWarps);
             mbar_init(bar_vempty(s), 1);
         }
         mbar_init(bar_drain, 1);
@@ -243,20 +253,29 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         if (lane == 0 && n > 0) {
             const uint32_t id_s = idesc_f16(kKT, !I8, false), id_o = idesc_f16(d, !I8, true);
             const int ksteps = d / 16;
+            // descriptors count in 16 bytes: steps are plain additions to the low word
+            const uint64_t dq = make_smem_desc(base + L::offQ), dk = make_smem_desc(base + L::offK), dv = desc_mn(base + L::offV);
             auto qk = [&](int x, int s) {
+                const uint64_t a = dq + (uint32_t)(x * (L::tile >> 4)), c = dk + (uint32_t)(s * (L::tile >> 4));
+                const uint32_t to = tmem + kColS + 128 * x;
+                auto step = [&](int k) { const uint32_t off = (uint32_t)((k >> 2) * kHalf + (k & 3) * 32) >> 4; mma_ss(to, a + off, c + off, id_s, k > 0 ? 1u : 0u); };
+                if (ksteps == NH * 4) {
 #pragma unroll
-                for (int k = 0; k < NH * 4; ++k)
-                    if (k < ksteps) {
-                        const uint32_t off = (uint32_t)((k >> 2) * kHalf + (k & 3) * 32);
-                        mma_ss(tmem + kColS + 128 * x, make_smem_desc(base + L::offQ + x * L::tile + off),
-                               make_smem_desc(base + L::offK + s * L::tile + off), id_s, k > 0 ? 1u : 0u);
-                    }
+                    for (int k = 0; k < NH * 4; ++k) step(k);
+                } else {
+#pragma unroll 1
+                    for (int k = 0; k < ksteps; ++k) step(k);
+                }
             };
             auto pv = [&](int x, int s, uint32_t acc) {
+                const uint64_t c = dv + (uint32_t)(s * (L::tile >> 4));
+                const uint32_t to = tmem + kColO + 128 * x, a = tmem + kColS + 128 * x;
 #pragma unroll
-                for (int k = 0; k < kKT / 16; ++k)
-                    mma_ts(tmem + kColO + 128 * x, tmem + kColS + 128 * x + 8 * k, desc_mn(base + L::offV + s * L::tile + k * 2048), id_o,
-                           k > 0 ? 1u : acc);
+                for (int k = 0; k < kKT / 16; ++k) mma_ts(to, a + 8 * k, c + k * 128, id_o, k > 0 ? 1u : acc);
+#pragma unroll
+                for (int e = 1; e < kTerms; ++e)
+#pragma unroll
+                    for (int k = 0; k < kKT / 16; ++k) mma_ts(to, tmem + kColMore + 64 * (e - 1) + 8 * k, c + k * 128, id_o, 1u);
             };
             bool ok = true;
             const int nt[2] = {nt0, nt1};
@@ -265,6 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             ok = ok && mbar_wait(bar_kfull(0), 0u, abort_flag, limit_ns);
             if (ok) {
                 tc_fence_after();
+                fence_async_smem();                       // what the loaders' copies wrote, for the tensor core's reads
                 for (int x = 0; x < 2; ++x)
                     if (nt[x] > 0) {
                         qk(x, 0);
@@ -276,12 +296,13 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 const int sv = j % NST, sk = (j + 1) % NST;
                 ok = mbar_wait(bar_vfull(sv), (uint32_t)(j / NST) & 1u, abort_flag, limit_ns);
                 if (ok && j + 1 < n) ok = mbar_wait(bar_kfull(sk), (uint32_t)((j + 1) / NST) & 1u, abort_flag, limit_ns);
+                fence_async_smem();
                 for (int x = 0; ok && x < 2; ++x) {
                     if (j >= nt[x]) continue;
                     ok = mbar_wait(bar_p(x), (uint32_t)j & 1u, abort_flag, limit_ns);
                     if (!ok) break;
                     tc_fence_after();
-                    pv(x, sv, j > 0 ? 1u : 0u);
+                    pv(x, sv, !F32 && j > 0 ? 1u : 0u);
                     if (j + 1 < nt[x]) {
                         qk(x, sk);                        // over S and P, behind the product that reads P
                         tc_commit(bar_s(x));
@@ -301,33 +322,39 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         }
     } else if (warp >= kRowWarps) {
         // ------------------------------------------------------------------------------------ loaders
-        const int lt = tid - 32 * kRowWarps;              // 0 .. 127
-        const int es = I8 ? 1 : 2;
-        const int ppk = d * es / 16;                      // 16-byte pieces per key
+        // Warp w copies the 16-key blocks w and w + 4 of a tile. A block lies in one page and is contiguous there: 16 d
+        // elements, taken 16 bytes per lane; the swizzled destinations inside a block are the same for every block and
+        // stay in registers. Page lookups: every 16 tiles a lane finds the address of one (tile, block) pair.
+        const int lw = warp - kRowWarps;
+        constexpr int es = I8 ? 1 : 2;
+        constexpr int kP = NH * 4 * es;                   // pieces per lane and block
+        const int ppk = d * es / 16, pieces = 16 * ppk;
         const int per_page = p.S / 16;
         const int64_t row_bytes = (int64_t)d * es, page_bytes = row_bytes * p.S;
         const int32_t* trow = p.table + (int64_t)b * p.W;
-        const int kstep = 128 / ppk, cstep = 128 - kstep * ppk;
-        const int key00 = lt / ppk, c00 = lt - key00 * ppk;
+        uint32_t dsto[kP];                                // destination of the lane's pieces, from the block's first row
+        int keyo[kP];                                     // their key in the block
+#pragma unroll
+        for (int k = 0; k < kP; ++k) {
+            const int x = lane + 32 * k, key = x / ppk, c = (x - key * ppk) * (I8 ? 2 : 1);
+            keyo[k] = x < pieces ? key : 1 << 20;
+            dsto[k] = (uint32_t)((c >> 3) * kHalf + key * 128 + (((c & 7) ^ (key & 7)) << 4));
+        }
         bool ok = true;
-        int id = 0;                                       // lane 0 .. 7: page of that 16-key block of the tile
-        auto load_ids = [&](int j) {
-            const int b16 = (t0 + j) * 8 + (lane & 7);
-            int v = 0;
-            if (b16 * 16 < q.kv) {
-                v = __ldg(trow + b16 / per_page);
-                if (v < 0 || v >= p.n_pages) {
+        // byte offset in the pool of block lw + 4 (lane & 1) of tile j0 + lane / 2
+        auto find_blocks = [&](int j0) -> int64_t {
+            const int b16 = (t0 + j0 + (lane >> 1)) * 8 + lw + 4 * (lane & 1);
+            int id = 0, off = 0;
+            if (j0 + (lane >> 1) < n && b16 * 16 < q.kv) {
+                const int pg = b16 / per_page;
+                off = b16 - pg * per_page;
+                id = __ldg(trow + pg);
+                if (id < 0 || id >= p.n_pages) {
                     atomicOr(p.status, STWQ_DEV_PAGES);
-                    v = 0;
+                    id = 0;
                 }
             }
-            return v;
-        };
-        // element offset (bytes) of a key's row, inside the pool
-        auto key_at = [&](int j, int key, int ids) -> int64_t {
-            const int page = __shfl_sync(0xffffffffu, ids, (key >> 4) & 7);
-            const int b16 = (t0 + j) * 8 + (key >> 4);
-            return ((int64_t)page * p.Hkv + hk) * page_bytes + ((b16 % per_page) * 16 + (key & 15)) * row_bytes;
+            return ((int64_t)id * p.Hkv + hk) * page_bytes + off * 16 * row_bytes;
         };
         auto wait_stage = [&](bool is_v, int j) -> bool {
             if (j < NST) return true;
@@ -339,65 +366,65 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             __syncwarp();
             if (lane == 0) mbar_arrive((i & 1) ? bar_vfull((i >> 1) % NST) : bar_kfull((i >> 1) % NST));
         };
-        if (n > 0) id = load_ids(0);
+        int64_t blocks = find_blocks(0), blocks_next = find_blocks(16);
+        auto block_at = [&](int j, int h) -> int64_t { return __shfl_sync(0xffffffffu, blocks, 2 * (j & 15) + h); };
+        auto advance = [&](int j) {                       // before the first use of tile j
+            if ((j & 15) == 0 && j > 0) {
+                blocks = blocks_next;
+                blocks_next = find_blocks(j + 16);
+            }
+        };
         if (!I8) {
-            int i = 0;
-            for (; i < 2 * n; ++i) {
+            for (int i = 0; i < 2 * n; ++i) {
                 const int j = i >> 1;
                 const bool is_v = i & 1;
+                if (!is_v) advance(j);
                 ok = wait_stage(is_v, j);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const uint32_t dst0 = base + (is_v ? L::offV : L::offK) + (j % NST) * L::tile;
                 const uint8_t* pool = reinterpret_cast<const uint8_t*>(is_v ? p.Vp : p.Kp);
-                int key = key00, c = c00;
-                for (int k = 0; k < ppk; ++k) {
-                    const int64_t off = key_at(j, key, id);
-                    const uint32_t dst = dst0 + (c >> 3) * kHalf + key * 128 + (((c & 7) ^ (key & 7)) << 4);
-                    cp_async16(dst, pool + off + c * 16, (t0 + j) * kKT + key < q.kv);
-                    key += kstep;
-                    c += cstep;
-                    if (c >= ppk) {
-                        c -= ppk;
-                        ++key;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint8_t* src = pool + block_at(j, h) + lane * 16;
+                    const int first = (lw + 4 * h) * 16;
+                    const int left = q.kv - (t0 + j) * kKT - first;       // keys of the block that exist
+                    const uint32_t dst = dst0 + first * 128;
+                    if (left >= 16 && pieces == 32 * kP) {
+#pragma unroll
+                        for (int k = 0; k < kP; ++k) cp_async16(dst + dsto[k], src + k * 512, true);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < kP; ++k)
+                            if (keyo[k] < 16) cp_async16(dst + dsto[k], keyo[k] < left ? src + k * 512 : pool, keyo[k] < left);
                     }
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (is_v) id = j + 1 < n ? load_ids(j + 1) : 0;
-                if (i >= kLag) {
-                    asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-                    publish(i - kLag);
-                }
+                // the lane's arrival on the stage's barrier comes when its copies have landed
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(is_v ? bar_vfull(j % NST) : bar_kfull(j % NST)) : "memory");
             }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            if (ok)
-                for (int k = max(0, 2 * n - kLag); k < 2 * n; ++k) publish(k);
+            asm volatile("cp.async.wait_all;" ::: "memory");       // nothing lands after the CTA has given up
         } else {
             // codes: the next tile's bytes are on their way in registers while this one is widened
-            constexpr int kMaxP = NH == 1 ? 4 : 8;
-            uint4 buf[kMaxP];
+            uint4 buf[2][kP];
             float sk = 0.0f;
             auto fetch = [&](int i) {
                 const int j = i >> 1;
+                if (!(i & 1)) advance(j);
                 const uint8_t* pool = reinterpret_cast<const uint8_t*>((i & 1) ? p.Vp : p.Kp);
-                int key = key00, c = c00;
 #pragma unroll
-                for (int k = 0; k < kMaxP; ++k)
-                    if (k < ppk) {
-                        const int64_t off = key_at(j, key, id);
-                        buf[k] = make_uint4(0u, 0u, 0u, 0u);
-                        if ((t0 + j) * kKT + key < q.kv) buf[k] = __ldg(reinterpret_cast<const uint4*>(pool + off + c * 16));
-                        key += kstep;
-                        c += cstep;
-                        if (c >= ppk) {
-                            c -= ppk;
-                            ++key;
-                        }
+                for (int h = 0; h < 2; ++h) {
+                    const uint8_t* src = pool + block_at(j, h) + lane * 16;
+                    const int left = q.kv - (t0 + j) * kKT - (lw + 4 * h) * 16;
+#pragma unroll
+                    for (int k = 0; k < kP; ++k) {
+                        buf[h][k] = make_uint4(0u, 0u, 0u, 0u);
+                        if (keyo[k] < min(left, 16)) buf[h][k] = __ldg(reinterpret_cast<const uint4*>(src + k * 512));
                     }
+                }
                 if (!(i & 1)) {
-                    const int kj = (t0 + j) * kKT + lt;
+                    const int kj = (t0 + j) * kKT + lw * 32 + lane;
                     sk = kj < q.kv ? __ldg(p.s_k + kj) : 0.0f;
-                } else id = j + 1 < n ? load_ids(j + 1) : 0;
+                }
             };
             if (n > 0) fetch(0);
             for (int i = 0; i < 2 * n; ++i) {
@@ -407,35 +434,31 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const uint32_t dst0 = base + (is_v ? L::offV : L::offK) + (j % NST) * L::tile;
-                uint4 cur[kMaxP];
+                uint4 cur[2][kP];
 #pragma unroll
-                for (int k = 0; k < kMaxP; ++k) cur[k] = buf[k];
-                if (!is_v) reinterpret_cast<float*>(smem + L::offScale)[(j & 3) * 128 + lt] = sk;
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < kP; ++k) cur[h][k] = buf[h][k];
+                if (!is_v) reinterpret_cast<float*>(smem + L::offScale)[(j & (L::slots - 1)) * 128 + lw * 32 + lane] = sk;
                 if (i + 1 < 2 * n) fetch(i + 1);
-                int key = key00, c = c00;
 #pragma unroll
-                for (int k = 0; k < kMaxP; ++k)
-                    if (k < ppk) {
-                        const bool live = (t0 + j) * kKT + key < q.kv;
-                        const uint32_t w[4] = {cur[k].x, cur[k].y, cur[k].z, cur[k].w};
-                        uint32_t h[8];
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t dst = dst0 + (lw + 4 * h) * 16 * 128;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t u = live ? w[e] ^ 0x80808080u : 0x80808080u;
-                            h[2 * e] = codes_half2(u, 0x4140u);
-                            h[2 * e + 1] = codes_half2(u, 0x4342u);
+                    for (int k = 0; k < kP; ++k)
+                        if (keyo[k] < 16) {
+                            const uint32_t w[4] = {cur[h][k].x, cur[h][k].y, cur[h][k].z, cur[h][k].w};
+                            uint32_t v[8];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const uint32_t u = w[e] ^ 0x80808080u;
+                                v[2 * e] = codes_half2(u, 0x4140u);
+                                v[2 * e + 1] = codes_half2(u, 0x4342u);
+                            }
+                            st_shared_v4(dst + dsto[k], v[0], v[1], v[2], v[3]);
+                            st_shared_v4(dst + (dsto[k] ^ 16u), v[4], v[5], v[6], v[7]);     // the neighbouring piece of the swizzled row
                         }
-                        const int cc = 2 * c;             // 16-byte pieces of the widened row
-                        const uint32_t dst = dst0 + (cc >> 3) * kHalf + key * 128;
-                        st_shared_v4(dst + (((cc & 7) ^ (key & 7)) << 4), h[0], h[1], h[2], h[3]);
-                        st_shared_v4(dst + ((((cc + 1) & 7) ^ (key & 7)) << 4), h[4], h[5], h[6], h[7]);
-                        key += kstep;
-                        c += cstep;
-                        if (c >= ppk) {
-                            c -= ppk;
-                            ++key;
-                        }
-                    }
+                }
                 publish(i);
             }
         }
@@ -444,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         const int x = warp >> 2;                          // tile
         const int rl = tid & 127;                         // row of the tile
         const int row = row0 + 128 * x + rl;
-        const bool live = row < rows;
+        const bool live = x < kX && row < rows;
         const int ti = live ? row / p.g : 0, hd = hk * p.g + (live ? row - ti * p.g : 0);
         const int nt = x == 0 ? nt0 : nt1;
         const int vis = !live ? 0 : max(0, p.causal ? q.kv - q.n + ti + 1 : q.kv);        // keys this row sees
@@ -493,6 +516,22 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         const uint32_t ts = tmem + kColS + 128 * x + lanes, to = tmem + kColO + 128 * x + lanes;
         const int min_vis = __reduce_min_sync(0xffffffffu, live ? vis : 0x7fffffff);
         float m = -INFINITY, l = 0.0f;
+        float m_sum = -INFINITY;                          // the reference that the fp32 sum of O stands against
+        auto add_up = [&](bool more) {                     // sum = sum 2^(m_sum - m) + O
+            const float f = more && m > -INFINITY ? ex2_approx(m_sum - m) : 0.0f;
+            for (int cb = 0; cb < d; cb += 16) {
+                uint32_t w[16], a[16];
+                tmem_ld16(to + cb, w);
+                if (more) tmem_ld16(tmem + kColSum + lanes + cb, a);
+                tmem_ld_wait();
+                if (more) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(fmaf(__uint_as_float(a[k]), f, __uint_as_float(w[k])));
+                }
+                tmem_st16(tmem + kColSum + lanes + cb, w);
+            }
+            tmem_st_wait();
+        };
         bool ok = true;
         for (int j = 0; j < nt; ++j) {
             ok = mbar_wait(bar_s(x), (uint32_t)j & 1u, abort_flag, limit_ns);
@@ -501,13 +540,11 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             tc_fence_after();
             const int key0 = (t0 + j) * kKT;
             const bool masked = key0 + kKT > min_vis;     // uniform over the warp
-            const float4* sks = reinterpret_cast<const float4*>(smem + L::offScale) + (j & 3) * 32;
+            const float4* sks = reinterpret_cast<const float4*>(smem + L::offScale) + (j & (L::slots - 1)) * 32;
             uint32_t v[32];
-            tmem_ld32(ts, v);
-#pragma unroll
-            for (int qd = 0; qd < 4; ++qd) {
-                tmem_ld_wait();
-                uint64_t s2[16];
+            uint64_t s2[16];
+            // 32 scores from v: key scales, mask
+            auto scores = [&](int qd) {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) s2[k] = pack_f2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
                 if (I8) {
@@ -518,7 +555,8 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                         s2[2 * k + 1] = mul_f2(s2[2 * k + 1], pack_f2(f.z, f.w));
                     }
                 }
-                if (qd < 3) tmem_ld32(ts + 32 * (qd + 1), v);
+            };
+            auto mask = [&](int qd) {
                 if (masked) {
                     const int seen = vis - key0 - 32 * qd;
 #pragma unroll
@@ -528,6 +566,8 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                         s2[k] = pack_f2(2 * k < seen ? a : -INFINITY, 2 * k + 1 < seen ? c : -INFINITY);
                     }
                 }
+            };
+            auto maximum = [&]() -> float {
                 float mx = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
@@ -535,8 +575,32 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     unpack_f2(s2[k], a, c);
                     mx = fmaxf(mx, fmaxf(a, c));
                 }
-                mx *= cc;                                 // cc > 0
-                if (__any_sync(0xffffffffu, mx > m + kSlack)) {
+                return mx * cc;                           // cc > 0
+            };
+            if (F32 && j > 0) {                           // the product of the tile before is done
+                add_up(j > 1);
+                m_sum = m;
+            }
+            float tile_max = -INFINITY;                   // fp32 output: known before the first exponential, so no term is rescaled
+            if (F32) {
+#pragma unroll 1
+                for (int qd = 0; qd < 4; ++qd) {
+                    tmem_ld32(ts + 32 * qd, v);
+                    tmem_ld_wait();
+                    scores(qd);
+                    mask(qd);
+                    tile_max = fmaxf(tile_max, maximum());
+                }
+            }
+            tmem_ld32(ts, v);
+#pragma unroll
+            for (int qd = 0; qd < 4; ++qd) {
+                tmem_ld_wait();
+                scores(qd);
+                if (qd < 3) tmem_ld32(ts + 32 * (qd + 1), v);
+                mask(qd);
+                const float mx = F32 ? tile_max : maximum();
+                if ((!F32 || qd == 0) && __any_sync(0xffffffffu, mx > m + kSlack)) {
                     // the reference moves: what was summed, written and accumulated so far is scaled down to it
                     const float mn = fmaxf(m, mx);
                     const float f = mn == -INFINITY ? 1.0f : ex2_approx(m - mn);
@@ -544,7 +608,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     l *= f;
                     uint32_t w[16];
                     if (qd < 3) tmem_ld_wait();
-                    if (j > 0)
+                    if (!F32 && j > 0)
                         for (int cb = 0; cb < d; cb += 16) {
                             tmem_ld16(to + cb, w);
                             tmem_ld_wait();
@@ -552,7 +616,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                             for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
                             tmem_st16(to + cb, w);
                         }
-                    for (int pb = 0; pb < qd; ++pb) {
+                    for (int pb = 0; !F32 && pb < qd; ++pb) {
                         tmem_ld16(ts + 16 * pb, w);
                         tmem_ld_wait();
 #pragma unroll
@@ -568,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 }
                 const float mm = m == -INFINITY ? 0.0f : m - (I8 ? 4.0f : 0.0f);       // fp16: four octaves up keep small probabilities' bits
                 const uint64_t negm2 = dup_f2(-mm);
-                uint32_t w[16];
+                uint32_t w[kTerms][16];
                 uint64_t l2 = 0ull;                       // (0, 0)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
@@ -577,12 +641,23 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     a = ex2_approx(a);
                     c = ex2_approx(c);
                     l2 = add_f2(l2, pack_f2(a, c));
-                    w[k] = I8 ? pack_f16(a, c) : pack_bf16(a, c);
+#pragma unroll
+                    for (int e = 0; e < kTerms; ++e) {
+                        w[e][k] = I8 ? pack_f16(a, c) : pack_bf16(a, c);
+                        if (e + 1 < kTerms) {
+                            const float2 h = I8 ? __half22float2(*reinterpret_cast<const __half2*>(&w[e][k]))
+                                                : make_float2(__uint_as_float(w[e][k] << 16), __uint_as_float(w[e][k] & 0xffff0000u));
+                            a -= h.x;
+                            c -= h.y;
+                        }
+                    }
                 }
                 float la, lb;
                 unpack_f2(l2, la, lb);
                 l += la + lb;
-                tmem_st16(ts + 16 * qd, w);               // columns whose scores have been read
+                tmem_st16(ts + 16 * qd, w[0]);            // columns whose scores have been read
+#pragma unroll
+                for (int e = 1; e < kTerms; ++e) tmem_st16(tmem + kColMore + lanes + 64 * (e - 1) + 16 * qd, w[e]);
             }
             tmem_st_wait();
             tc_fence_before();
@@ -603,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 if (I8) o[k] *= __ldg(p.s_v + (int64_t)hk * d + cb + k);
             }
             const int64_t at = (int64_t)(q.t0 + ti) * p.o_ts + (int64_t)hd * p.o_hs + cb;
-            if (p.out_bf16) {
+            if (!F32) {
                 uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.O) + at);
                 dst[0] = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
                 dst[1] = make_uint4(pack_bf16(o[8], o[9]), pack_bf16(o[10], o[11]), pack_bf16(o[12], o[13]), pack_bf16(o[14], o[15]));
@@ -627,6 +702,13 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 }
 #pragma unroll
                 for (int k = 0; k < 16; ++k) o[k] = nt > 0 ? __uint_as_float(w[k]) : 0.0f;
+                if (F32 && nt > 1) {
+                    const float f = m > -INFINITY ? ex2_approx(m_sum - m) : 0.0f;
+                    tmem_ld16(tmem + kColSum + lanes + cb, w);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) o[k] = fmaf(__uint_as_float(w[k]), f, o[k]);
+                }
                 if (eS == 1) {
                     if (live) write16(cb, o, l);
                 } else {
@@ -692,10 +774,10 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     }
 }
 
-template <bool I8, int NH>
-int launch(stwq_ctx* ctx, const PaParams& p, unsigned grid, cudaStream_t st)
+template <bool I8, int NH, bool F32>
+int launch_as(stwq_ctx* ctx, const PaParams& p, unsigned grid, cudaStream_t st)
 {
-    auto kern = pattn_tiled_kernel<I8, NH>;
+    auto kern = pattn_tiled_kernel<I8, NH, F32>;
     int smem = Smem<NH>::offPre + (p.B + 1) * 4 + 1024;
     if (smem < 116 * 1024) smem = 116 * 1024;             // all of tensor memory: one CTA per SM
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
@@ -704,6 +786,12 @@ int launch(stwq_ctx* ctx, const PaParams& p, unsigned grid, cudaStream_t st)
     ctx->launches += 1;
     e = cudaGetLastError();
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
+}
+
+template <bool I8, int NH>
+int launch(stwq_ctx* ctx, const PaParams& p, unsigned grid, cudaStream_t st)
+{
+    return p.out_bf16 ? launch_as<I8, NH, false>(ctx, p, grid, st) : launch_as<I8, NH, true>(ctx, p, grid, st);
 }
 
 }  // namespace
@@ -716,8 +804,8 @@ size_t stwq_pattn_tiled_part_bytes(const stwq_ctx* ctx, int d)
 
 int stwq_launch_pattn_tiled(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
 {
-    // units: at most ceil(rows / 256) per request and key head, rows adding up to T g
-    int64_t grid = (int64_t)p.Hkv * ((p.T * p.g + 255) / 256 + p.B);
+    // units: at most ceil(rows / unit) per request and key head, rows adding up to T g
+    int64_t grid = (int64_t)p.Hkv * ((p.T * p.g + (p.out_bf16 ? 255 : 127)) / (p.out_bf16 ? 256 : 128) + p.B);
     if (grid < ctx->sm_count) grid = ctx->sm_count;
     if (grid > 0x7fffffff) return STWQ_ERR_DIM;
     const unsigned gx = (unsigned)grid;
