@@ -31,13 +31,14 @@ using namespace stwq_ptx;
 
 namespace {
 
-constexpr int kRowWarps = 8, kLoadWarps = 4;
+constexpr int kRowWarps = 8, kLoadWarps = 3;   // and one that issues the products: 12 warps leave a thread 168 registers
 constexpr int kThreads = 32 * (kRowWarps + kLoadWarps + 1);
 constexpr int kKT = 128;                     // keys per tile
 constexpr int kHalf = 128 * 128;             // bytes of 128 rows of 128 bytes
 constexpr int kMaxStages = 4;
 constexpr int kMaxSplit = 32;
 constexpr float kSlack = 10.0f;
+constexpr int kPolyEvery = 4;                // one pair of exponentials in so many goes through the fma pipe instead of the ex2 unit
 constexpr int kTmemCols = 512, kColS = 0, kColO = 256;
 constexpr int kColMore = 128, kColSum = 384; // fp32 output: further terms of P (64 columns each), the fp32 sum of O
 
@@ -122,6 +123,51 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                  : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint64_t pack_u2(uint32_t lo, uint32_t hi) { return pack_f2(__uint_as_float(lo), __uint_as_float(hi)); }
+__device__ __forceinline__ void unpack_u2(uint64_t v, uint32_t& lo, uint32_t& hi)
+{
+    float a, b;
+    unpack_f2(v, a, b);
+    lo = __float_as_uint(a);
+    hi = __float_as_uint(b);
+}
+// 2^x on a pair without the ex2 unit: x = n + r with |r| <= 1/2 (adding 1.5 2^23 rounds to the integer), a cubic for 2^r
+// (least maximum relative error, 7.5e-5: a quarter of fp16's half step), n added to the exponent. x is cut at -126.
+__device__ __forceinline__ uint64_t exp2_poly(uint64_t x2)
+{
+    float x0, x1;
+    unpack_f2(x2, x0, x1);
+    const uint64_t x = pack_f2(fmaxf(x0, -126.0f), fmaxf(x1, -126.0f));
+    const uint64_t t = add_f2(x, dup_f2(12582912.0f));
+    const uint64_t r = fma_f2(add_f2(t, dup_f2(-12582912.0f)), dup_f2(-1.0f), x);
+    uint64_t q = fma_f2(r, dup_f2(0.05517167f), dup_f2(0.24261113f));
+    q = fma_f2(q, r, dup_f2(0.69326099f));
+    q = fma_f2(q, r, dup_f2(0.99992807f));
+    uint32_t t0, t1, q0, q1;
+    unpack_u2(t, t0, t1);
+    unpack_u2(q, q0, q1);
+    return pack_u2((t0 << 23) + q0, (t1 << 23) + q1);
+}
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// The bounded wait of the GEMM kernels behind a few polls that do not read the timer.
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, unsigned long long limit_ns)
+{
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait(bar, parity, abort_flag, limit_ns);
+}
 __device__ __forceinline__ void rows_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 template <bool I8, int NH, bool F32>
@@ -154,6 +200,30 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     int* pre = reinterpret_cast<int*>(smem + L::offPre);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
+    // barriers and tensor memory, while the lengths are on their way
+    if (tid == 0) {
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(bar_q(x), 4);
+            mbar_init(bar_s(x), 1);
+            mbar_init(bar_p(x), 4);
+            mbar_init(bar_o(x), 1);
+        }
+        for (int s = 0; s < NST; ++s) {
+            mbar_init(bar_kfull(s), I8 ? kLoadWarps : 32 * kLoadWarps);
+            mbar_init(bar_kempty(s), 1);
+            mbar_init(bar_vfull(s), I8 ? kLoadWarps : 32 * kLoadWarps);
+            mbar_init(bar_vempty(s), 1);
+        }
+        mbar_init(bar_drain, 1);
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_smem();
+    }
+    if (warp == kRowWarps + kLoadWarps) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        tc_fence_before();
+    }
     // ---- units of every request: key heads x tiles of 256 rows
     bool bad = false;
     auto units_of = [&](int b) -> int {
@@ -166,6 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
         int sum = 0;
         for (int b = b0; b < b1; ++b) sum += units_of(b);
+        const int units0 = sum;                           // of the only request, where a thread has one
         int s = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -175,19 +246,30 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         if (lane == 31) wsum[warp] = s;
         __syncthreads();
         int at = s - sum;
-        for (int w = 0; w < warp; ++w) at += wsum[w];
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) at += w < warp ? wsum[w] : 0;
         for (int b = b0; b < b1; ++b) {
             pre[b] = at;
-            at += units_of(b);
+            at += per == 1 ? units0 : units_of(b);
         }
         if (tid == kThreads - 1) pre[p.B] = at;
     }
     if (bad && blockIdx.x == 0) atomicOr(p.status, STWQ_DEV_PAGES);
     __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    auto free_tmem = [&]() {
+        if (warp == kRowWarps + kLoadWarps) {
+            __syncwarp();
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        }
+    };
     const int U = pre[p.B];
-    if (U == 0) return;
-    const int nS = min(max(sm_count / U, 1), kMaxSplit);  // ranges of keys per unit
-    if ((int)blockIdx.x >= U * nS) return;
+    const int nS = min(max(sm_count / max(U, 1), 1), kMaxSplit);        // ranges of keys per unit
+    if ((int)blockIdx.x >= U * nS) {
+        free_tmem();
+        return;
+    }
     const int unit = blockIdx.x / nS, split = blockIdx.x - unit * nS;
     int b = 0;
     {
@@ -214,37 +296,14 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     const int tiles0 = (last_limit(0) + kKT - 1) / kKT, tiles1 = kX == 1 ? 0 : (last_limit(1) + kKT - 1) / kKT;
     const int tiles = max(tiles0, tiles1);
     const int eS = min(nS, max(1, (tiles + 1) / 2));      // ranges of at least two tiles
-    if (split >= eS) return;
-    const int t0 = (int)((long long)tiles * split / eS), t1 = (int)((long long)tiles * (split + 1) / eS);
+    if (split >= eS) {
+        free_tmem();
+        return;
+    }
+    const int t0 = (int)((uint32_t)tiles * (uint32_t)split / (uint32_t)eS), t1 = (int)((uint32_t)tiles * (uint32_t)(split + 1) / (uint32_t)eS);   // tiles < 2^24, eS <= 32
     const int nt0 = max(0, min(tiles0, t1) - t0), nt1 = max(0, min(tiles1, t1) - t0);
     const int n = max(nt0, nt1);
 
-    if (tid == 0) {
-        for (int x = 0; x < 2; ++x) {
-            mbar_init(bar_q(x), 4);
-            mbar_init(bar_s(x), 1);
-            mbar_init(bar_p(x), 4);
-            mbar_init(bar_o(x), 1);
-        }
-        for (int s = 0; s < NST; ++s) {
-            mbar_init(bar_kfull(s), I8 ? kLoadWarps : 32 * kLoadWarps);
-            mbar_init(bar_kempty(s), 1);
-            mbar_init(bar_vfull(s), I8 ? kLoadWarps : 32 * kLoadWarps);
-            mbar_init(bar_vempty(s), 1);
-        }
-        mbar_init(bar_drain, 1);
-        *abort_flag = 0u;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        fence_async_smem();
-    }
-    if (warp == kRowWarps + kLoadWarps) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        tc_fence_before();
-    }
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
     const unsigned long long limit_ns = p.wait_limit_ns;
     const int d = p.d;
 
@@ -280,8 +339,8 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             bool ok = true;
             const int nt[2] = {nt0, nt1};
             for (int x = 0; ok && x < 2; ++x)
-                if (nt[x] > 0) ok = mbar_wait(bar_q(x), 0u, abort_flag, limit_ns);
-            ok = ok && mbar_wait(bar_kfull(0), 0u, abort_flag, limit_ns);
+                if (nt[x] > 0) ok = wait_bar(bar_q(x), 0u, abort_flag, limit_ns);
+            ok = ok && wait_bar(bar_kfull(0), 0u, abort_flag, limit_ns);
             if (ok) {
                 tc_fence_after();
                 fence_async_smem();                       // what the loaders' copies wrote, for the tensor core's reads
@@ -294,12 +353,12 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             }
             for (int j = 0; ok && j < n; ++j) {
                 const int sv = j % NST, sk = (j + 1) % NST;
-                ok = mbar_wait(bar_vfull(sv), (uint32_t)(j / NST) & 1u, abort_flag, limit_ns);
-                if (ok && j + 1 < n) ok = mbar_wait(bar_kfull(sk), (uint32_t)((j + 1) / NST) & 1u, abort_flag, limit_ns);
+                ok = wait_bar(bar_vfull(sv), (uint32_t)(j / NST) & 1u, abort_flag, limit_ns);
+                if (ok && j + 1 < n) ok = wait_bar(bar_kfull(sk), (uint32_t)((j + 1) / NST) & 1u, abort_flag, limit_ns);
                 fence_async_smem();
                 for (int x = 0; ok && x < 2; ++x) {
                     if (j >= nt[x]) continue;
-                    ok = mbar_wait(bar_p(x), (uint32_t)j & 1u, abort_flag, limit_ns);
+                    ok = wait_bar(bar_p(x), (uint32_t)j & 1u, abort_flag, limit_ns);
                     if (!ok) break;
                     tc_fence_after();
                     pv(x, sv, !F32 && j > 0 ? 1u : 0u);
@@ -322,12 +381,13 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         }
     } else if (warp >= kRowWarps) {
         // ------------------------------------------------------------------------------------ loaders
-        // Warp w copies the 16-key blocks w and w + 4 of a tile. A block lies in one page and is contiguous there: 16 d
+        // Warp w copies the 16-key blocks w, w + 3 and w + 6 of a tile. A block lies in one page and is contiguous there: 16 d
         // elements, taken 16 bytes per lane; the swizzled destinations inside a block are the same for every block and
-        // stay in registers. Page lookups: every 16 tiles a lane finds the address of one (tile, block) pair.
+        // stay in registers. Page lookups: every 8 tiles a lane finds the address of one (tile, block) pair.
         const int lw = warp - kRowWarps;
         constexpr int es = I8 ? 1 : 2;
-        constexpr int kP = NH * 4 * es;                   // pieces per lane and block
+        constexpr int kP = NH * 2 * es;                   // pieces per lane and block
+        const int nb = lw < 2 ? 3 : 2;                    // blocks of a tile
         const int ppk = d * es / 16, pieces = 16 * ppk;
         const int per_page = p.S / 16;
         const int64_t row_bytes = (int64_t)d * es, page_bytes = row_bytes * p.S;
@@ -341,11 +401,11 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             dsto[k] = (uint32_t)((c >> 3) * kHalf + key * 128 + (((c & 7) ^ (key & 7)) << 4));
         }
         bool ok = true;
-        // byte offset in the pool of block lw + 4 (lane & 1) of tile j0 + lane / 2
+        // byte offset in the pool of block lw + 3 (lane & 3) of tile j0 + lane / 4
         auto find_blocks = [&](int j0) -> int64_t {
-            const int b16 = (t0 + j0 + (lane >> 1)) * 8 + lw + 4 * (lane & 1);
+            const int b16 = (t0 + j0 + (lane >> 2)) * 8 + lw + 3 * (lane & 3);
             int id = 0, off = 0;
-            if (j0 + (lane >> 1) < n && b16 * 16 < q.kv) {
+            if (j0 + (lane >> 2) < n && (lane & 3) < nb && b16 * 16 < q.kv) {
                 const int pg = b16 / per_page;
                 off = b16 - pg * per_page;
                 id = __ldg(trow + pg);
@@ -359,19 +419,19 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         auto wait_stage = [&](bool is_v, int j) -> bool {
             if (j < NST) return true;
             const int s = j % NST;
-            return mbar_wait(is_v ? bar_vempty(s) : bar_kempty(s), (uint32_t)(j / NST + 1) & 1u, abort_flag, limit_ns);
+            return wait_bar(is_v ? bar_vempty(s) : bar_kempty(s), (uint32_t)(j / NST + 1) & 1u, abort_flag, limit_ns);
         };
         auto publish = [&](int i) {                       // load i: key tile i / 2 (even) or value tile i / 2 (odd)
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive((i & 1) ? bar_vfull((i >> 1) % NST) : bar_kfull((i >> 1) % NST));
         };
-        int64_t blocks = find_blocks(0), blocks_next = find_blocks(16);
-        auto block_at = [&](int j, int h) -> int64_t { return __shfl_sync(0xffffffffu, blocks, 2 * (j & 15) + h); };
+        int64_t blocks = find_blocks(0), blocks_next = find_blocks(8);
+        auto block_at = [&](int j, int h) -> int64_t { return __shfl_sync(0xffffffffu, blocks, 4 * (j & 7) + h); };
         auto advance = [&](int j) {                       // before the first use of tile j
-            if ((j & 15) == 0 && j > 0) {
+            if ((j & 7) == 0 && j > 0) {
                 blocks = blocks_next;
-                blocks_next = find_blocks(j + 16);
+                blocks_next = find_blocks(j + 8);
             }
         };
         if (!I8) {
@@ -385,9 +445,10 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 const uint32_t dst0 = base + (is_v ? L::offV : L::offK) + (j % NST) * L::tile;
                 const uint8_t* pool = reinterpret_cast<const uint8_t*>(is_v ? p.Vp : p.Kp);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < 3; ++h) {
+                    if (h == nb) break;
                     const uint8_t* src = pool + block_at(j, h) + lane * 16;
-                    const int first = (lw + 4 * h) * 16;
+                    const int first = (lw + 3 * h) * 16;
                     const int left = q.kv - (t0 + j) * kKT - first;       // keys of the block that exist
                     const uint32_t dst = dst0 + first * 128;
                     if (left >= 16 && pieces == 32 * kP) {
@@ -405,16 +466,17 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             asm volatile("cp.async.wait_all;" ::: "memory");       // nothing lands after the CTA has given up
         } else {
             // codes: the next tile's bytes are on their way in registers while this one is widened
-            uint4 buf[2][kP];
-            float sk = 0.0f;
+            uint4 buf[3][kP];
+            float sk[2] = {0.0f, 0.0f};
             auto fetch = [&](int i) {
                 const int j = i >> 1;
                 if (!(i & 1)) advance(j);
                 const uint8_t* pool = reinterpret_cast<const uint8_t*>((i & 1) ? p.Vp : p.Kp);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < 3; ++h) {
+                    if (h == nb) break;
                     const uint8_t* src = pool + block_at(j, h) + lane * 16;
-                    const int left = q.kv - (t0 + j) * kKT - (lw + 4 * h) * 16;
+                    const int left = q.kv - (t0 + j) * kKT - (lw + 3 * h) * 16;
 #pragma unroll
                     for (int k = 0; k < kP; ++k) {
                         buf[h][k] = make_uint4(0u, 0u, 0u, 0u);
@@ -422,8 +484,11 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     }
                 }
                 if (!(i & 1)) {
-                    const int kj = (t0 + j) * kKT + lw * 32 + lane;
-                    sk = kj < q.kv ? __ldg(p.s_k + kj) : 0.0f;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int kl = (lw + 3 * h) * 32 + lane, kj = (t0 + j) * kKT + kl;
+                        sk[h] = kl < kKT && kj < q.kv ? __ldg(p.s_k + kj) : 0.0f;
+                    }
                 }
             };
             if (n > 0) fetch(0);
@@ -434,16 +499,21 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const uint32_t dst0 = base + (is_v ? L::offV : L::offK) + (j % NST) * L::tile;
-                uint4 cur[2][kP];
+                uint4 cur[3][kP];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 3; ++h)
 #pragma unroll
                     for (int k = 0; k < kP; ++k) cur[h][k] = buf[h][k];
-                if (!is_v) reinterpret_cast<float*>(smem + L::offScale)[(j & (L::slots - 1)) * 128 + lw * 32 + lane] = sk;
+                if (!is_v) {
+                    float* dst = reinterpret_cast<float*>(smem + L::offScale) + (j & (L::slots - 1)) * 128 + lw * 32 + lane;
+                    dst[0] = sk[0];
+                    if (lw == 0) dst[96] = sk[1];
+                }
                 if (i + 1 < 2 * n) fetch(i + 1);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t dst = dst0 + (lw + 4 * h) * 16 * 128;
+                for (int h = 0; h < 3; ++h) {
+                    if (h == nb) break;
+                    const uint32_t dst = dst0 + (lw + 3 * h) * 16 * 128;
 #pragma unroll
                     for (int k = 0; k < kP; ++k)
                         if (keyo[k] < 16) {
@@ -472,17 +542,44 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         const int nt = x == 0 ? nt0 : nt1;
         const int vis = !live ? 0 : max(0, p.causal ? q.kv - q.n + ti + 1 : q.kv);        // keys this row sees
         float inv = 1.0f;
+        // the 16-byte pieces of the warp's 32 rows of d 16-bit elements, in the order of the rows: body(row, piece)
+        const int ppr = d / 8;
+        auto walk_rows = [&](auto&& body) {
+            if (ppr == NH * 8) {
+#pragma unroll
+                for (int k = 0; k < NH * 8; ++k) body(lane / (NH * 8) + k * (4 / NH), lane % (NH * 8));
+                return;
+            }
+            int rw = lane / ppr, c = lane - rw * ppr;
+            const int dr = 32 / ppr, dc = 32 - dr * ppr;
+            for (int k = 0; k < ppr; ++k) {               // 32 ppr pieces over 32 lanes
+                body(rw, c);
+                rw += dr;
+                c += dc;
+                if (c >= ppr) {
+                    c -= ppr;
+                    ++rw;
+                }
+            }
+        };
         if (nt > 0) {
-            // ---- the row of Q, swizzled
-            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.Q) + (int64_t)(q.t0 + ti) * p.q_ts +
-                                                              (int64_t)hd * p.q_hs);
-            const uint32_t dst = base + L::offQ + x * L::tile + rl * 128;
-            float up = 1.0f;
+            // ---- the warp's 32 rows of Q, swizzled: lanes walk along the rows
+            const int64_t qoff = live ? (int64_t)(q.t0 + ti) * p.q_ts + (int64_t)hd * p.q_hs : -1;
+            const uint32_t qrow = base + L::offQ + x * L::tile + (rl & ~31) * 128;
+            walk_rows([&](int rw, int c) {
+                const int64_t off = __shfl_sync(0xffffffffu, qoff, rw);
+                cp_async16(qrow + (c >> 3) * kHalf + rw * 128 + (((c & 7) ^ (rw & 7)) << 4),
+                           reinterpret_cast<const __nv_bfloat16*>(p.Q) + max(off, (int64_t)0) + c * 8, off >= 0);
+            });
+            asm volatile("cp.async.wait_all;" ::: "memory");
             if (I8) {
+                // each thread turns its own row into fp16 under a power of two
+                __syncwarp();
+                const uint32_t mine = qrow + lane * 128;
+                auto piece = [&](int c) { return mine + (c >> 3) * kHalf + (((c & 7) ^ (lane & 7)) << 4); };
                 float mx = 0.0f;
                 for (int c = 0; c < d / 8; ++c) {
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (live) v = __ldg(src + c);
+                    const uint4 v = ld_shared_v4(piece(c));
                     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -490,22 +587,16 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 }
                 int e = (int)(__float_as_uint(mx) >> 23) - 127;
                 e = mx > 0.0f && mx < INFINITY ? max(e, -100) : 13;
-                up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
+                const float up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
                 inv = __uint_as_float((uint32_t)(e - 13 + 127) << 23);
-            }
+                for (int c = 0; c < d / 8; ++c) {
+                    const uint4 v = ld_shared_v4(piece(c));
+                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int c = 0; c < NH * 8; ++c)
-                if (c < d / 8) {
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (live) v = __ldg(src + c);
-                    if (I8) {
-                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = pack_f16(__uint_as_float(w[e] << 16) * up, __uint_as_float(w[e] & 0xffff0000u) * up);
-                        v = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                    st_shared_v4(dst + (c >> 3) * kHalf + (((c & 7) ^ (rl & 7)) << 4), v.x, v.y, v.z, v.w);
+                    for (int k = 0; k < 4; ++k) w[k] = pack_f16(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xffff0000u) * up);
+                    st_shared_v4(piece(c), w[0], w[1], w[2], w[3]);
                 }
+            }
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_q(x));
@@ -514,6 +605,10 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         const uint64_t cc2 = dup_f2(cc);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + kColS + 128 * x + lanes, to = tmem + kColO + 128 * x + lanes;
+        auto pack_p = [](float a, float c) { return I8 ? pack_f16(a, c) : pack_bf16(a, c); };
+        auto unpack_p = [](uint32_t w) {
+            return I8 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        };
         const int min_vis = __reduce_min_sync(0xffffffffu, live ? vis : 0x7fffffff);
         float m = -INFINITY, l = 0.0f;
         float m_sum = -INFINITY;                          // the reference that the fp32 sum of O stands against
@@ -534,48 +629,36 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         };
         bool ok = true;
         for (int j = 0; j < nt; ++j) {
-            ok = mbar_wait(bar_s(x), (uint32_t)j & 1u, abort_flag, limit_ns);
+            ok = wait_bar(bar_s(x), (uint32_t)j & 1u, abort_flag, limit_ns);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
             const int key0 = (t0 + j) * kKT;
             const bool masked = key0 + kKT > min_vis;     // uniform over the warp
             const float4* sks = reinterpret_cast<const float4*>(smem + L::offScale) + (j & (L::slots - 1)) * 32;
-            uint32_t v[32];
-            uint64_t s2[16];
-            // 32 scores from v: key scales, mask
-            auto scores = [&](int qd) {
-#pragma unroll
-                for (int k = 0; k < 16; ++k) s2[k] = pack_f2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
+            uint32_t v[2][32];                            // 64 scores at a time
+            // key scales and mask on the 32 scores h of part qd
+            auto scores = [&](int qd, int h) {
                 if (I8) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const float4 f = sks[qd * 8 + k];
-                        s2[2 * k] = mul_f2(s2[2 * k], pack_f2(f.x, f.y));
-                        s2[2 * k + 1] = mul_f2(s2[2 * k + 1], pack_f2(f.z, f.w));
+                        const float4 f = sks[qd * 16 + h * 8 + k];
+                        unpack_u2(mul_f2(pack_u2(v[h][4 * k], v[h][4 * k + 1]), pack_f2(f.x, f.y)), v[h][4 * k], v[h][4 * k + 1]);
+                        unpack_u2(mul_f2(pack_u2(v[h][4 * k + 2], v[h][4 * k + 3]), pack_f2(f.z, f.w)), v[h][4 * k + 2], v[h][4 * k + 3]);
                     }
                 }
-            };
-            auto mask = [&](int qd) {
                 if (masked) {
-                    const int seen = vis - key0 - 32 * qd;
+                    const int seen = vis - key0 - 64 * qd - 32 * h;
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        float a, c;
-                        unpack_f2(s2[k], a, c);
-                        s2[k] = pack_f2(2 * k < seen ? a : -INFINITY, 2 * k + 1 < seen ? c : -INFINITY);
-                    }
+                    for (int k = 0; k < 32; ++k)
+                        if (k >= seen) v[h][k] = 0xff800000u;             // -Inf
                 }
             };
-            auto maximum = [&]() -> float {
-                float mx = -INFINITY;
+            auto maximum = [&](int h) -> float {
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    float a, c;
-                    unpack_f2(s2[k], a, c);
-                    mx = fmaxf(mx, fmaxf(a, c));
-                }
-                return mx * cc;                           // cc > 0
+                for (int k = 0; k < 32; k += 2) mx[(k >> 1) & 3] = max3(mx[(k >> 1) & 3], __uint_as_float(v[h][k]), __uint_as_float(v[h][k + 1]));
+                return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
             };
             if (F32 && j > 0) {                           // the product of the tile before is done
                 add_up(j > 1);
@@ -584,22 +667,23 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             float tile_max = -INFINITY;                   // fp32 output: known before the first exponential, so no term is rescaled
             if (F32) {
 #pragma unroll 1
-                for (int qd = 0; qd < 4; ++qd) {
-                    tmem_ld32(ts + 32 * qd, v);
+                for (int qd = 0; qd < 2; ++qd) {
+                    tmem_ld32(ts + 64 * qd, v[0]);
+                    tmem_ld32(ts + 64 * qd + 32, v[1]);
                     tmem_ld_wait();
-                    scores(qd);
-                    mask(qd);
-                    tile_max = fmaxf(tile_max, maximum());
+                    scores(qd, 0);
+                    scores(qd, 1);
+                    tile_max = max3(tile_max, maximum(0), maximum(1));
                 }
             }
-            tmem_ld32(ts, v);
+            tmem_ld32(ts, v[0]);
+            tmem_ld32(ts + 32, v[1]);
 #pragma unroll
-            for (int qd = 0; qd < 4; ++qd) {
+            for (int qd = 0; qd < 2; ++qd) {
                 tmem_ld_wait();
-                scores(qd);
-                if (qd < 3) tmem_ld32(ts + 32 * (qd + 1), v);
-                mask(qd);
-                const float mx = F32 ? tile_max : maximum();
+                scores(qd, 0);
+                scores(qd, 1);
+                const float mx = cc * (F32 ? tile_max : fmaxf(maximum(0), maximum(1)));      // cc > 0
                 if ((!F32 || qd == 0) && __any_sync(0xffffffffu, mx > m + kSlack)) {
                     // the reference moves: what was summed, written and accumulated so far is scaled down to it
                     const float mn = fmaxf(m, mx);
@@ -607,8 +691,8 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     m = mn;
                     l *= f;
                     uint32_t w[16];
-                    if (qd < 3) tmem_ld_wait();
                     if (!F32 && j > 0)
+#pragma unroll 1
                         for (int cb = 0; cb < d; cb += 16) {
                             tmem_ld16(to + cb, w);
                             tmem_ld_wait();
@@ -616,15 +700,14 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                             for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
                             tmem_st16(to + cb, w);
                         }
-                    for (int pb = 0; !F32 && pb < qd; ++pb) {
+#pragma unroll 1
+                    for (int pb = 0; !F32 && pb < 2 * qd; ++pb) {
                         tmem_ld16(ts + 16 * pb, w);
                         tmem_ld_wait();
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            if (I8) {
-                                const float2 pv = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
-                                w[k] = pack_f16(pv.x * f, pv.y * f);
-                            } else w[k] = pack_bf16(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xffff0000u) * f);
+                            const float2 pv = unpack_p(w[k]);
+                            w[k] = pack_p(pv.x * f, pv.y * f);
                         }
                         tmem_st16(ts + 16 * pb, w);
                     }
@@ -632,32 +715,39 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 }
                 const float mm = m == -INFINITY ? 0.0f : m - (I8 ? 4.0f : 0.0f);       // fp16: four octaves up keep small probabilities' bits
                 const uint64_t negm2 = dup_f2(-mm);
-                uint32_t w[kTerms][16];
-                uint64_t l2 = 0ull;                       // (0, 0)
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    float a, c;
-                    unpack_f2(fma_f2(s2[k], cc2, negm2), a, c);
-                    a = ex2_approx(a);
-                    c = ex2_approx(c);
-                    l2 = add_f2(l2, pack_f2(a, c));
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[kTerms][16];
+                    uint64_t l2[2] = {0ull, 0ull};        // (0, 0)
 #pragma unroll
-                    for (int e = 0; e < kTerms; ++e) {
-                        w[e][k] = I8 ? pack_f16(a, c) : pack_bf16(a, c);
-                        if (e + 1 < kTerms) {
-                            const float2 h = I8 ? __half22float2(*reinterpret_cast<const __half2*>(&w[e][k]))
-                                                : make_float2(__uint_as_float(w[e][k] << 16), __uint_as_float(w[e][k] & 0xffff0000u));
-                            a -= h.x;
-                            c -= h.y;
+                    for (int k = 0; k < 16; ++k) {
+                        const uint64_t e2 = fma_f2(pack_u2(v[h][2 * k], v[h][2 * k + 1]), cc2, negm2);
+                        float a, c;
+                        if (!F32 && k % kPolyEvery == kPolyEvery - 1) unpack_f2(exp2_poly(e2), a, c);
+                        else {
+                            unpack_f2(e2, a, c);
+                            a = ex2_approx(a);
+                            c = ex2_approx(c);
+                        }
+                        l2[k & 1] = add_f2(l2[k & 1], pack_f2(a, c));
+#pragma unroll
+                        for (int e = 0; e < kTerms; ++e) {
+                            w[e][k] = pack_p(a, c);
+                            if (e + 1 < kTerms) {
+                                const float2 r = unpack_p(w[e][k]);
+                                a -= r.x;
+                                c -= r.y;
+                            }
                         }
                     }
-                }
-                float la, lb;
-                unpack_f2(l2, la, lb);
-                l += la + lb;
-                tmem_st16(ts + 16 * qd, w[0]);            // columns whose scores have been read
+                    if (qd == 0) tmem_ld32(ts + 64 + 32 * h, v[h]);        // the next scores into the registers just used up
+                    float la, lb;
+                    unpack_f2(add_f2(l2[0], l2[1]), la, lb);
+                    l += la + lb;
+                    tmem_st16(ts + 32 * qd + 16 * h, w[0]);                // columns whose scores have been read
 #pragma unroll
-                for (int e = 1; e < kTerms; ++e) tmem_st16(tmem + kColMore + lanes + 64 * (e - 1) + 16 * qd, w[e]);
+                    for (int e = 1; e < kTerms; ++e) tmem_st16(tmem + kColMore + lanes + 64 * (e - 1) + 32 * qd + 16 * h, w[e]);
+                }
             }
             tmem_st_wait();
             tc_fence_before();
@@ -666,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         }
         // ---- O
         if (ok && nt > 0) {
-            ok = mbar_wait(bar_o(x), 0u, abort_flag, limit_ns);
+            ok = wait_bar(bar_o(x), 0u, abort_flag, limit_ns);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
         }
@@ -675,18 +765,37 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
                 o[k] = rl_sum != 0.0f ? o[k] * inv_l : 0.0f;             // no visible key: zeros
-                if (I8) o[k] *= __ldg(p.s_v + (int64_t)hk * d + cb + k);
+            }
+            if (I8) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float4 f = __ldg(reinterpret_cast<const float4*>(p.s_v + (int64_t)hk * d + cb) + k);
+                    o[4 * k] *= f.x; o[4 * k + 1] *= f.y; o[4 * k + 2] *= f.z; o[4 * k + 3] *= f.w;
+                }
             }
             const int64_t at = (int64_t)(q.t0 + ti) * p.o_ts + (int64_t)hd * p.o_hs + cb;
-            if (!F32) {
-                uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.O) + at);
-                dst[0] = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
-                dst[1] = make_uint4(pack_bf16(o[8], o[9]), pack_bf16(o[10], o[11]), pack_bf16(o[12], o[13]), pack_bf16(o[14], o[15]));
+            if (!F32) {                                   // into the row's place in the Q tile, which no product reads any more
+                const uint32_t mine = base + L::offQ + x * L::tile + rl * 128 + (cb >> 6) * kHalf;
+                const int c = (cb >> 3) & 7;
+                st_shared_v4(mine + ((c ^ (rl & 7)) << 4), pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
+                st_shared_v4(mine + (((c + 1) ^ (rl & 7)) << 4), pack_bf16(o[8], o[9]), pack_bf16(o[10], o[11]), pack_bf16(o[12], o[13]),
+                             pack_bf16(o[14], o[15]));
             } else {
                 float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.O) + at);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) dst[k] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
             }
+        };
+        auto store_rows = [&]() {                         // bf16 output: from there to memory, lanes walking along the rows
+            if (F32) return;
+            __syncwarp();
+            const int64_t ooff = live ? (int64_t)(q.t0 + ti) * p.o_ts + (int64_t)hd * p.o_hs : -1;
+            const uint32_t orow = base + L::offQ + x * L::tile + (rl & ~31) * 128;
+            walk_rows([&](int rw, int c) {
+                const int64_t off = __shfl_sync(0xffffffffu, ooff, rw);
+                const uint4 v = ld_shared_v4(orow + (c >> 3) * kHalf + rw * 128 + (((c & 7) ^ (rw & 7)) << 4));
+                if (off >= 0) *(reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.O) + off) + c) = v;
+            });
         };
         constexpr int DP = NH * 64;
         const int64_t part_f4 = (int64_t)(DP / 4) * 256 + 128;           // float4s of a partial result: O, then (m, l)
@@ -710,12 +819,13 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     for (int k = 0; k < 16; ++k) o[k] = fmaf(__uint_as_float(w[k]), f, o[k]);
                 }
                 if (eS == 1) {
-                    if (live) write16(cb, o, l);
+                    if (live || !F32) write16(cb, o, l);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) __stcg(part + (cb / 4 + k) * 256 + pr, make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
                 }
             }
+            if (eS == 1) store_rows();
         }
         if (eS > 1) {
             float2* ml = reinterpret_cast<float2*>(part + (DP / 4) * 256);
@@ -729,10 +839,10 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 __threadfence();
             }
             rows_barrier();
-            if (*sm_last && live) {
+            if (*sm_last && x < kX) {
                 const float4* p0 = reinterpret_cast<const float4*>(p.part) + (int64_t)unit * nS * part_f4;
                 float M = -INFINITY, Ls = 0.0f;
-                float* fs = reinterpret_cast<float*>(smem);              // [eS][256]: the operand tiles are no longer needed
+                float* fs = reinterpret_cast<float*>(smem + L::offV);    // [eS][256]: the operand tiles are no longer needed
                 for (int s = 0; s < eS; ++s) {
                     const float2 v = __ldcg(reinterpret_cast<const float2*>(p0 + s * part_f4 + (DP / 4) * 256) + pr);
                     M = fmaxf(M, v.x);
@@ -758,8 +868,9 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                             o[4 * k + 3] = fmaf(f, v.w, o[4 * k + 3]);
                         }
                     }
-                    write16(cb, o, Ls);
+                    if (live || !F32) write16(cb, o, Ls);
                 }
+                store_rows();
             }
         }
     }
@@ -768,10 +879,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     __syncthreads();
     if (tid == 0 && *abort_flag) atomicOr(p.status, STWQ_DEV_TIMEOUT);
     tc_fence_after();
-    if (warp == kRowWarps + kLoadWarps) {
-        __syncwarp();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
-    }
+    free_tmem();
 }
 
 template <bool I8, int NH, bool F32>
