@@ -170,6 +170,40 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
 }
 __device__ __forceinline__ void rows_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
+template <bool I8>
+__device__ __forceinline__ uint32_t pack_p(float a, float c) { return I8 ? pack_f16(a, c) : pack_bf16(a, c); }
+template <bool I8>
+__device__ __forceinline__ float2 unpack_p(uint32_t w)
+{
+    return I8 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+// O (d columns) and the blocks of P already written for this tile, times f. Rare, so kept out of the loop's code.
+template <bool I8>
+__device__ __noinline__ void rescale(uint32_t to, int d, uint32_t tp, int blocks, float f)
+{
+    uint32_t w[16];
+#pragma unroll 1
+    for (int cb = 0; cb < d; cb += 16) {
+        tmem_ld16(to + cb, w);
+        tmem_ld_wait();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
+        tmem_st16(to + cb, w);
+    }
+#pragma unroll 1
+    for (int pb = 0; pb < blocks; ++pb) {
+        tmem_ld16(tp + 16 * pb, w);
+        tmem_ld_wait();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const float2 v = unpack_p<I8>(w[k]);
+            w[k] = pack_p<I8>(v.x * f, v.y * f);
+        }
+        tmem_st16(tp + 16 * pb, w);
+    }
+    tmem_st_wait();
+}
+
 template <bool I8, int NH, bool F32>
 __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams p, const int sm_count)
 {
@@ -177,6 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     constexpr int NST = L::stages;
     constexpr int kX = F32 ? 1 : 2;                       // tiles of 128 rows
     constexpr int kRows = 128 * kX;
+    constexpr int kUnroll = I8 || F32 ? 1 : 2;            // the loops of all roles have to stay in the instruction cache together
     constexpr int kTerms = !F32 ? 1 : (I8 ? 2 : 3);       // 16-bit terms of P
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -421,11 +456,6 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             const int s = j % NST;
             return wait_bar(is_v ? bar_vempty(s) : bar_kempty(s), (uint32_t)(j / NST + 1) & 1u, abort_flag, limit_ns);
         };
-        auto publish = [&](int i) {                       // load i: key tile i / 2 (even) or value tile i / 2 (odd)
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive((i & 1) ? bar_vfull((i >> 1) % NST) : bar_kfull((i >> 1) % NST));
-        };
         int64_t blocks = find_blocks(0), blocks_next = find_blocks(8);
         auto block_at = [&](int j, int h) -> int64_t { return __shfl_sync(0xffffffffu, blocks, 4 * (j & 7) + h); };
         auto advance = [&](int j) {                       // before the first use of tile j
@@ -465,10 +495,14 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             }
             asm volatile("cp.async.wait_all;" ::: "memory");       // nothing lands after the CTA has given up
         } else {
-            // codes: the next tile's bytes are on their way in registers while this one is widened
-            uint4 buf[3][kP];
-            float sk[2] = {0.0f, 0.0f};
-            auto fetch = [&](int i) {
+            // codes: the bytes of the next loads are on their way in registers while this one is widened (kDeep loads of
+            // 8 or 16 KB per CTA cover the latency of HBM)
+            constexpr int kDeep = 2;
+            const bool whole = pieces == 32 * kP;         // d fills the lanes
+            const int n_full = q.kv / kKT - t0;           // tiles before this one have all their keys
+            uint4 buf[kDeep][3][kP];
+            float sk[kDeep][2];
+            auto fetch = [&](int i, uint4 (&to)[3][kP], float (&sc)[2]) {
                 const int j = i >> 1;
                 if (!(i & 1)) advance(j);
                 const uint8_t* pool = reinterpret_cast<const uint8_t*>((i & 1) ? p.Vp : p.Kp);
@@ -476,60 +510,71 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 for (int h = 0; h < 3; ++h) {
                     if (h == nb) break;
                     const uint8_t* src = pool + block_at(j, h) + lane * 16;
-                    const int left = q.kv - (t0 + j) * kKT - (lw + 3 * h) * 16;
+                    if (whole && j < n_full) {
 #pragma unroll
-                    for (int k = 0; k < kP; ++k) {
-                        buf[h][k] = make_uint4(0u, 0u, 0u, 0u);
-                        if (keyo[k] < min(left, 16)) buf[h][k] = __ldg(reinterpret_cast<const uint4*>(src + k * 512));
+                        for (int k = 0; k < kP; ++k) to[h][k] = __ldg(reinterpret_cast<const uint4*>(src + k * 512));
+                    } else {
+                        const int left = min(q.kv - (t0 + j) * kKT - (lw + 3 * h) * 16, 16);
+#pragma unroll
+                        for (int k = 0; k < kP; ++k) {
+                            to[h][k] = make_uint4(0u, 0u, 0u, 0u);
+                            if (keyo[k] < left) to[h][k] = __ldg(reinterpret_cast<const uint4*>(src + k * 512));
+                        }
                     }
                 }
                 if (!(i & 1)) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int kl = (lw + 3 * h) * 32 + lane, kj = (t0 + j) * kKT + kl;
-                        sk[h] = kl < kKT && kj < q.kv ? __ldg(p.s_k + kj) : 0.0f;
-                    }
+                    const int kj = (t0 + j) * kKT + lw * 32 + lane;
+                    sc[0] = kj < q.kv ? __ldg(p.s_k + kj) : 0.0f;
+                    if (lw == 0) sc[1] = kj + 96 < q.kv ? __ldg(p.s_k + kj + 96) : 0.0f;
                 }
             };
-            if (n > 0) fetch(0);
-            for (int i = 0; i < 2 * n; ++i) {
-                const int j = i >> 1;
-                const bool is_v = i & 1;
-                ok = wait_stage(is_v, j);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                const uint32_t dst0 = base + (is_v ? L::offV : L::offK) + (j % NST) * L::tile;
-                uint4 cur[3][kP];
+            auto widen = [&](const uint4& x, uint32_t at) {
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                uint32_t v[8];
 #pragma unroll
-                for (int h = 0; h < 3; ++h)
-#pragma unroll
-                    for (int k = 0; k < kP; ++k) cur[h][k] = buf[h][k];
-                if (!is_v) {
-                    float* dst = reinterpret_cast<float*>(smem + L::offScale) + (j & (L::slots - 1)) * 128 + lw * 32 + lane;
-                    dst[0] = sk[0];
-                    if (lw == 0) dst[96] = sk[1];
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t c = w[e] ^ 0x80808080u;
+                    v[2 * e] = codes_half2(c, 0x4140u);
+                    v[2 * e + 1] = codes_half2(c, 0x4342u);
                 }
-                if (i + 1 < 2 * n) fetch(i + 1);
+                st_shared_v4(at, v[0], v[1], v[2], v[3]);
+                st_shared_v4(at ^ 16u, v[4], v[5], v[6], v[7]);            // the neighbouring piece of the swizzled row
+            };
 #pragma unroll
-                for (int h = 0; h < 3; ++h) {
-                    if (h == nb) break;
-                    const uint32_t dst = dst0 + (lw + 3 * h) * 16 * 128;
+            for (int u = 0; u < kDeep; ++u)
+                if (u < 2 * n) fetch(u, buf[u], sk[u]);
+            for (int i0 = 0; ok && i0 < 2 * n; i0 += kDeep) {
 #pragma unroll
-                    for (int k = 0; k < kP; ++k)
-                        if (keyo[k] < 16) {
-                            const uint32_t w[4] = {cur[h][k].x, cur[h][k].y, cur[h][k].z, cur[h][k].w};
-                            uint32_t v[8];
+                for (int u = 0; u < kDeep; ++u) {
+                    const int i = i0 + u, j = i >> 1;
+                    const bool is_v = i & 1;
+                    if (i >= 2 * n) break;
+                    ok = wait_stage(is_v, j);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    const uint32_t dst0 = base + (is_v ? L::offV : L::offK) + (j % NST) * L::tile;
+                    if (!is_v) {
+                        float* dst = reinterpret_cast<float*>(smem + L::offScale) + (j & (L::slots - 1)) * 128 + lw * 32 + lane;
+                        dst[0] = sk[u][0];
+                        if (lw == 0) dst[96] = sk[u][1];
+                    }
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const uint32_t u = w[e] ^ 0x80808080u;
-                                v[2 * e] = codes_half2(u, 0x4140u);
-                                v[2 * e + 1] = codes_half2(u, 0x4342u);
-                            }
-                            st_shared_v4(dst + dsto[k], v[0], v[1], v[2], v[3]);
-                            st_shared_v4(dst + (dsto[k] ^ 16u), v[4], v[5], v[6], v[7]);     // the neighbouring piece of the swizzled row
+                    for (int h = 0; h < 3; ++h) {
+                        if (h == nb) break;
+                        const uint32_t dst = dst0 + (lw + 3 * h) * 16 * 128;
+                        if (whole) {
+#pragma unroll
+                            for (int k = 0; k < kP; ++k) widen(buf[u][h][k], dst + dsto[k]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < kP; ++k)
+                                if (keyo[k] < 16) widen(buf[u][h][k], dst + dsto[k]);
                         }
+                    }
+                    __syncwarp();                         // the proxy fence is the issuer's: here it would also wait for the loads in flight
+                    if (lane == 0) mbar_arrive(is_v ? bar_vfull(j % NST) : bar_kfull(j % NST));
+                    if (i + kDeep < 2 * n) fetch(i + kDeep, buf[u], sk[u]);
                 }
-                publish(i);
             }
         }
     } else {
@@ -605,10 +650,6 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         const uint64_t cc2 = dup_f2(cc);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + kColS + 128 * x + lanes, to = tmem + kColO + 128 * x + lanes;
-        auto pack_p = [](float a, float c) { return I8 ? pack_f16(a, c) : pack_bf16(a, c); };
-        auto unpack_p = [](uint32_t w) {
-            return I8 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-        };
         const int min_vis = __reduce_min_sync(0xffffffffu, live ? vis : 0x7fffffff);
         float m = -INFINITY, l = 0.0f;
         float m_sum = -INFINITY;                          // the reference that the fp32 sum of O stands against
@@ -678,7 +719,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             }
             tmem_ld32(ts, v[0]);
             tmem_ld32(ts + 32, v[1]);
-#pragma unroll
+#pragma unroll(kUnroll)
             for (int qd = 0; qd < 2; ++qd) {
                 tmem_ld_wait();
                 scores(qd, 0);
@@ -690,28 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     const float f = mn == -INFINITY ? 1.0f : ex2_approx(m - mn);
                     m = mn;
                     l *= f;
-                    uint32_t w[16];
-                    if (!F32 && j > 0)
-#pragma unroll 1
-                        for (int cb = 0; cb < d; cb += 16) {
-                            tmem_ld16(to + cb, w);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
-                            tmem_st16(to + cb, w);
-                        }
-#pragma unroll 1
-                    for (int pb = 0; !F32 && pb < 2 * qd; ++pb) {
-                        tmem_ld16(ts + 16 * pb, w);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const float2 pv = unpack_p(w[k]);
-                            w[k] = pack_p(pv.x * f, pv.y * f);
-                        }
-                        tmem_st16(ts + 16 * pb, w);
-                    }
-                    tmem_st_wait();
+                    if (!F32) rescale<I8>(to, j > 0 ? d : 0, ts, 2 * qd, f);
                 }
                 const float mm = m == -INFINITY ? 0.0f : m - (I8 ? 4.0f : 0.0f);       // fp16: four octaves up keep small probabilities' bits
                 const uint64_t negm2 = dup_f2(-mm);
@@ -732,9 +752,9 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                         l2[k & 1] = add_f2(l2[k & 1], pack_f2(a, c));
 #pragma unroll
                         for (int e = 0; e < kTerms; ++e) {
-                            w[e][k] = pack_p(a, c);
+                            w[e][k] = pack_p<I8>(a, c);
                             if (e + 1 < kTerms) {
-                                const float2 r = unpack_p(w[e][k]);
+                                const float2 r = unpack_p<I8>(w[e][k]);
                                 a -= r.x;
                                 c -= r.y;
                             }
