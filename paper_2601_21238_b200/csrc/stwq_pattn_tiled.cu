@@ -85,16 +85,22 @@ __device__ __forceinline__ uint32_t codes_half2(uint32_t w, uint32_t sel)      /
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&k));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
-// D[128 x N] (+)= A B, kind::f16, fp32 accumulators; A from shared memory or from tensor memory
+// D[128 x N] (+)= A B, kind::f16, fp32 accumulators; A from shared memory or from tensor memory. The whole warp comes here
+// with the same values (they then live in uniform registers) and one elected lane issues.
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+    asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+    asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void commit_one(uint32_t bar)
+{
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+                 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 // MN-major operand, 128-byte swizzle: rows (the contraction index) of 64 elements, 8-row groups 1024 bytes apart,
 // the next 64 elements of a row kHalf bytes further
@@ -233,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     uint32_t* sm_last = misc + 2;
     int* wsum = reinterpret_cast<int*>(misc + 8);         // [13]
     int* pre = reinterpret_cast<int*>(smem + L::offPre);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;      // warp: uniform
 
     // barriers and tensor memory, while the lengths are on their way
     if (tid == 0) {
@@ -292,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     if (bad && blockIdx.x == 0) atomicOr(p.status, STWQ_DEV_PAGES);
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     auto free_tmem = [&]() {
         if (warp == kRowWarps + kLoadWarps) {
             __syncwarp();
@@ -344,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
 
     if (warp == kRowWarps + kLoadWarps) {
         // ------------------------------------------------------------------------------------ MMA issuer
-        if (lane == 0 && n > 0) {
+        if (n > 0) {
             const uint32_t id_s = idesc_f16(kKT, !I8, false), id_o = idesc_f16(d, !I8, true);
             const int ksteps = d / 16;
             // descriptors count in 16 bytes: steps are plain additions to the low word
@@ -374,41 +380,41 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             bool ok = true;
             const int nt[2] = {nt0, nt1};
             for (int x = 0; ok && x < 2; ++x)
-                if (nt[x] > 0) ok = wait_bar(bar_q(x), 0u, abort_flag, limit_ns);
-            ok = ok && wait_bar(bar_kfull(0), 0u, abort_flag, limit_ns);
+                if (nt[x] > 0) ok = __all_sync(0xffffffffu, wait_bar(bar_q(x), 0u, abort_flag, limit_ns));
+            ok = ok && __all_sync(0xffffffffu, wait_bar(bar_kfull(0), 0u, abort_flag, limit_ns));
             if (ok) {
                 tc_fence_after();
                 fence_async_smem();                       // what the loaders' copies wrote, for the tensor core's reads
                 for (int x = 0; x < 2; ++x)
                     if (nt[x] > 0) {
                         qk(x, 0);
-                        tc_commit(bar_s(x));
+                        commit_one(bar_s(x));
                     }
-                tc_commit(bar_kempty(0));
+                commit_one(bar_kempty(0));
             }
             for (int j = 0; ok && j < n; ++j) {
                 const int sv = j % NST, sk = (j + 1) % NST;
-                ok = wait_bar(bar_vfull(sv), (uint32_t)(j / NST) & 1u, abort_flag, limit_ns);
-                if (ok && j + 1 < n) ok = wait_bar(bar_kfull(sk), (uint32_t)((j + 1) / NST) & 1u, abort_flag, limit_ns);
+                ok = __all_sync(0xffffffffu, wait_bar(bar_vfull(sv), (uint32_t)(j / NST) & 1u, abort_flag, limit_ns));
+                if (ok && j + 1 < n) ok = __all_sync(0xffffffffu, wait_bar(bar_kfull(sk), (uint32_t)((j + 1) / NST) & 1u, abort_flag, limit_ns));
                 fence_async_smem();
                 for (int x = 0; ok && x < 2; ++x) {
                     if (j >= nt[x]) continue;
-                    ok = wait_bar(bar_p(x), (uint32_t)j & 1u, abort_flag, limit_ns);
+                    ok = __all_sync(0xffffffffu, wait_bar(bar_p(x), (uint32_t)j & 1u, abort_flag, limit_ns));
                     if (!ok) break;
                     tc_fence_after();
                     pv(x, sv, !F32 && j > 0 ? 1u : 0u);
                     if (j + 1 < nt[x]) {
                         qk(x, sk);                        // over S and P, behind the product that reads P
-                        tc_commit(bar_s(x));
-                    } else tc_commit(bar_o(x));
+                        commit_one(bar_s(x));
+                    } else commit_one(bar_o(x));
                 }
                 if (ok) {
-                    tc_commit(bar_vempty(sv));
-                    if (j + 1 < n) tc_commit(bar_kempty(sk));
+                    commit_one(bar_vempty(sv));
+                    if (j + 1 < n) commit_one(bar_kempty(sk));
                 }
             }
             if (!ok) {                                    // giving up: products already issued must not outlive the tensor memory
-                tc_commit(bar_drain);
+                commit_one(bar_drain);
                 const unsigned long long w0 = globaltimer_ns();
                 while (!mbar_try_wait(bar_drain, 0u))
                     if (globaltimer_ns() - w0 > limit_ns) break;
