@@ -173,9 +173,8 @@ def check_rows(where, device, name, t, dtypes, shape, inner):
         step *= int(t.shape[-k])
 
 
-def _dense(t, dtype, shape, device):
-    """The quick form of check_args for one tensor (True: nothing to complain about)."""
-    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and t.device.index == device
+def _kinds(torch):
+    return {_F32: torch.float32, _BF16: torch.bfloat16, _I8: torch.int8, _I32: torch.int32}
 
 
 def _mk(X, what="X"):
@@ -229,6 +228,8 @@ class Context:
         self._torch = torch
         self._L = load_library()
         self.device = device
+        self._kinds = _kinds(torch)
+        self._row_kinds = {d: tuple(self._kinds[x] for x in d) for d in ((_F32,), (_BF16,), (_F32, _BF16))}
         h = C.c_void_p()
         self._check(self._L.stwq_create(C.byref(h), device), "stwq_create")
         self._h = h
@@ -365,15 +366,35 @@ class Context:
     # ---- serving over a paged KV cache
     def _fast(self, where, *specs):
         """check_args in a form that costs little when all is well: the step calls of a decode loop are short."""
-        dev = self.device
-        T = self._torch
-        kinds = {_F32: T.float32, _BF16: T.bfloat16, _I8: T.int8, _I32: T.int32}
-        for name, t, dtype, shape, optional in specs:
-            if t is None and optional:
-                continue
-            if t is None or not hasattr(t, "is_contiguous") or not _dense(t, kinds[dtype], shape, dev):
-                check_args(where, dev, *specs)
+        dev, kinds = self.device, self._kinds
+        try:
+            for _, t, dtype, shape, optional in specs:
+                if t is None:
+                    if optional:
+                        continue
+                    break
+                if t.dtype is not kinds[dtype] or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+                    break
+            else:
                 return
+        except (AttributeError, TypeError):
+            pass
+        check_args(where, dev, *specs)
+
+    def _rows(self, where, name, t, dtypes, shape):
+        """check_rows for operands whose last dimension is dense, in the quick form. Returns the strides."""
+        try:
+            st = t.stride()
+            if t.get_device() == self.device and t.dtype in self._row_kinds[dtypes] and st[-1] == 1 and len(st) == len(shape):
+                for a, b in zip(t.shape, shape):
+                    if a != b and b is not None:
+                        break
+                else:
+                    return st
+        except (AttributeError, TypeError):
+            pass
+        check_rows(where, self.device, name, t, dtypes, shape, 1)
+        return t.stride()
 
     def _raw_stream(self, stream):
         return self._torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
@@ -392,37 +413,36 @@ class Context:
                                       slot_map.data_ptr(), pos_ids.data_ptr(), T, pages_used.data_ptr(), self._raw_stream(stream)),
                     "page_plan")
 
-    def _head_args(self, where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k=None):
-        """Checks of the operands that qk_norm_rope and kv_append_paged share; returns T, x_dtype, weights' heads, rot, P."""
-        check_rows(where, self.device, "QKV", QKV, (_F32, _BF16), (None, (Hq + 2 * Hkv) * d), 1)
-        T = int(QKV.shape[0])
-        P = int(cs.shape[0]) if cs is not None else int(s_k.numel()) if s_k is not None else 1
-        rot = int(cs.shape[1]) if cs is not None else 0
-        nq = 0 if w_q is None else 1 if len(w_q.shape) == 1 else Hq
-        nk = 0 if w_k is None else 1 if len(w_k.shape) == 1 else Hkv
-        self._fast(where, ("pos_ids", pos_ids, _I32, (T,), False),
-                   ("w_q", w_q, _F32, (d,) if nq == 1 and len(w_q.shape) == 1 else (Hq, d), True),
-                   ("w_k", w_k, _F32, (d,) if nk == 1 and len(w_k.shape) == 1 else (Hkv, d), True),
-                   ("cs", cs, _F32, (P, rot), True), ("s_k", s_k, _F32, (P,), True))
-        return T, OUT_BF16 if QKV.dtype is self._torch.bfloat16 else OUT_F32, nq, nk, rot, P
+    def _head_args(self, where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k, *more):
+        """Checks of the operands that qk_norm_rope and kv_append_paged share; returns T, ld, x_dtype, weights' heads, rot, P."""
+        ld = self._rows(where, "QKV", QKV, (_F32, _BF16), (None, (Hq + 2 * Hkv) * d))[0]
+        T = QKV.shape[0]
+        P, rot = (cs.shape if cs is not None and len(cs.shape) == 2 else (s_k.numel() if s_k is not None else 1, 0))
+        flat_q, flat_k = w_q is not None and len(w_q.shape) == 1, w_k is not None and len(w_k.shape) == 1
+        self._fast(where, ("pos_ids", pos_ids, _I32, (T,), False), ("w_q", w_q, _F32, (d,) if flat_q else (Hq, d), True),
+                   ("w_k", w_k, _F32, (d,) if flat_k else (Hkv, d), True), ("cs", cs, _F32, (P, rot), True),
+                   ("s_k", s_k, _F32, (P,), True), *more)
+        return (T, ld if T > 1 else max(ld, (Hq + 2 * Hkv) * d), OUT_BF16 if QKV.dtype is self._torch.bfloat16 else OUT_F32,
+                0 if w_q is None else 1 if flat_q else Hq, 0 if w_k is None else 1 if flat_k else Hkv, rot, P)
 
     def qk_norm_rope(self, QKV, pos_ids, Hq, Hkv, w_q, w_k, norm, eps, cs, rope, Qo, Ko, stream=None):
         d = int(Qo.shape[-1])
-        T, x_dtype, nq, nk, rot, P = self._head_args("qk_norm_rope", QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs)
-        check_rows("qk_norm_rope", self.device, "Qo", Qo, (_F32, _BF16), (T, Hq, d), 1)
-        check_rows("qk_norm_rope", self.device, "Ko", Ko, (str(Qo.dtype),), (T, Hkv, d), 1)
-        out = OUT_BF16 if Qo.dtype is self._torch.bfloat16 else OUT_F32
-        self._check(self._L.qk_norm_rope(self._h, QKV.data_ptr(), QKV.stride(0), x_dtype, pos_ids.data_ptr(), T, Hq, Hkv, d,
+        T, ld, x_dtype, nq, nk, rot, P = self._head_args("qk_norm_rope", QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, None)
+        qs = self._rows("qk_norm_rope", "Qo", Qo, (_F32, _BF16), (T, Hq, d))
+        bf = Qo.dtype is self._torch.bfloat16
+        ks = self._rows("qk_norm_rope", "Ko", Ko, (_BF16,) if bf else (_F32,), (T, Hkv, d))
+        out = OUT_BF16 if bf else OUT_F32
+        self._check(self._L.qk_norm_rope(self._h, QKV.data_ptr(), ld, x_dtype, pos_ids.data_ptr(), T, Hq, Hkv, d,
                                          w_q.data_ptr() if nq else None, nq, w_k.data_ptr() if nk else None, nk, norm, eps,
-                                         None if cs is None else cs.data_ptr(), rot, rope, P, Qo.data_ptr(), Qo.stride(0),
-                                         Qo.stride(1), Ko.data_ptr(), Ko.stride(0), Ko.stride(1), out, self._raw_stream(stream)),
+                                         None if cs is None else cs.data_ptr(), rot, rope, P, Qo.data_ptr(), qs[0],
+                                         qs[1], Ko.data_ptr(), ks[0], ks[1], out, self._raw_stream(stream)),
                     "qk_norm_rope")
 
     def _pool(self, where, Kp, Vp):
         """Checks the two pools; returns n_pages, Hkv, page_size, d, kv_dtype."""
         if Kp is None or Vp is None or len(Kp.shape) != 4:
             raise StwqError(ERR_DIM, where, "Kp and Vp are [n_pages, Hkv, page_size, d]")
-        shape = tuple(int(v) for v in Kp.shape)
+        shape = tuple(Kp.shape)
         i8 = Kp.dtype is self._torch.int8
         self._fast(where, ("Kp", Kp, _I8 if i8 else _BF16, shape, False), ("Vp", Vp, _I8 if i8 else _BF16, shape, False))
         return (*shape, KV_INT8 if i8 else KV_BF16)
@@ -433,48 +453,50 @@ class Context:
         NP, hk, S, d, kv = self._pool(where, Kp, Vp)
         if hk != Hkv:
             raise StwqError(ERR_DIM, where, f"the pool has {hk} key heads, the call {Hkv}")
-        T, x_dtype, nq, nk, rot, P = self._head_args(where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k)
-        check_rows(where, self.device, "Qo", Qo, (_BF16,), (T, Hq, d), 1)
-        self._fast(where, ("slot_map", slot_map, _I32, (T,), False), ("s_k", s_k, _F32, (P,), kv == KV_BF16),
-                   ("s_v", s_v, _F32, (Hkv, d), kv == KV_BF16))
-        self._check(self._L.kv_append_paged(self._h, QKV.data_ptr(), QKV.stride(0), x_dtype, pos_ids.data_ptr(),
+        if kv == KV_INT8 and s_k is None:
+            raise StwqError(ERR_NULL, where, "s_k is None")
+        T, ld, x_dtype, nq, nk, rot, P = self._head_args(where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k,
+                                                         ("slot_map", slot_map, _I32, tuple(QKV.shape[:1]), False),
+                                                         ("s_v", s_v, _F32, (Hkv, d), kv == KV_BF16))
+        qs = self._rows(where, "Qo", Qo, (_BF16,), (T, Hq, d))
+        self._check(self._L.kv_append_paged(self._h, QKV.data_ptr(), ld, x_dtype, pos_ids.data_ptr(),
                                             slot_map.data_ptr(), T, Hq, Hkv, d, w_q.data_ptr() if nq else None, nq,
                                             w_k.data_ptr() if nk else None, nk, norm, eps, None if cs is None else cs.data_ptr(),
                                             rot, rope, P, None if s_k is None else s_k.data_ptr(),
-                                            None if s_v is None else s_v.data_ptr(), bits, Qo.data_ptr(), Qo.stride(0),
-                                            Qo.stride(1), Kp.data_ptr(), Vp.data_ptr(), NP, S, kv, self._raw_stream(stream)), where)
+                                            None if s_v is None else s_v.data_ptr(), bits, Qo.data_ptr(), qs[0],
+                                            qs[1], Kp.data_ptr(), Vp.data_ptr(), NP, S, kv, self._raw_stream(stream)), where)
 
     def paged_attention(self, Q, cu_new, max_new, block_table, kv_lens, Kp, Vp, s_k, s_v, scale, causal, out_dtype, O, stream=None):
         where = "paged_attention"
         NP, Hkv, S, d, kv = self._pool(where, Kp, Vp)
-        check_rows(where, self.device, "Q", Q, (_BF16,), (None, None, d), 1)
-        T, Hq = int(Q.shape[0]), int(Q.shape[1])
+        qs = self._rows(where, "Q", Q, (_BF16,), (None, None, d))
+        T, Hq = Q.shape[0], Q.shape[1]
         if out_dtype not in (OUT_F32, OUT_BF16):
             raise StwqError(ERR_BITS, where, f"out_dtype {out_dtype} is not OUT_F32 / OUT_BF16")
-        check_rows(where, self.device, "O", O, (_OUT_DTYPES[out_dtype],), (T, Hq, d), 1)
+        os_ = self._rows(where, "O", O, (_OUT_DTYPES[out_dtype],), (T, Hq, d))
         B, W = _mk(block_table, "block_table")
         P = int(s_k.numel()) if s_k is not None else 1
         self._fast(where, ("cu_new", cu_new, _I32, (B + 1,), False), ("block_table", block_table, _I32, (B, W), False),
                    ("kv_lens", kv_lens, _I32, (B,), False), ("s_k", s_k, _F32, (P,), kv == KV_BF16),
                    ("s_v", s_v, _F32, (Hkv, d), kv == KV_BF16))
-        self._check(self._L.paged_attention(self._h, Q.data_ptr(), Q.stride(0), Q.stride(1), cu_new.data_ptr(), T, max_new, B, Hq, Hkv,
+        self._check(self._L.paged_attention(self._h, Q.data_ptr(), qs[0], qs[1], cu_new.data_ptr(), T, max_new, B, Hq, Hkv,
                                             d, block_table.data_ptr(), W, kv_lens.data_ptr(), Kp.data_ptr(), Vp.data_ptr(), NP, S, kv,
                                             None if s_k is None else s_k.data_ptr(), P, None if s_v is None else s_v.data_ptr(),
-                                            scale, int(bool(causal)), out_dtype, O.data_ptr(), O.stride(0), O.stride(1),
+                                            scale, int(bool(causal)), out_dtype, O.data_ptr(), os_[0], os_[1],
                                             self._raw_stream(stream)), where)
 
     def stwq_reserve_paged_attention(self, B, Hq, Hkv, d):
         self._check(self._L.stwq_reserve_paged_attention(self._h, B, Hq, Hkv, d), "stwq_reserve_paged_attention")
 
     def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, probs=None, kept=None, stream=None):
-        check_rows("sample_tokens", self.device, "logits", logits, (_F32, _BF16), (None, None), 1)
-        B, V = int(logits.shape[0]), int(logits.shape[1])
+        ld = self._rows("sample_tokens", "logits", logits, (_F32, _BF16), (None, None))[0]
+        B, V = logits.shape
         self._fast("sample_tokens", ("temperature", temperature, _F32, (B,), True), ("top_k", top_k, _I32, (B,), True),
                    ("top_p", top_p, _F32, (B,), True), ("min_p", min_p, _F32, (B,), True), ("u", u, _F32, (B,), False),
                    ("tokens", tokens, _I32, (B,), False), ("probs", probs, _F32, (B,), True), ("kept", kept, _I32, (B,), True))
         q = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         self._check(self._L.sample_tokens(self._h, logits.data_ptr(), OUT_BF16 if logits.dtype is self._torch.bfloat16 else OUT_F32,
-                                          max(logits.stride(0), V) if B == 1 else logits.stride(0), B, V, q(temperature), q(top_k),
+                                          max(ld, V) if B == 1 else ld, B, V, q(temperature), q(top_k),
                                           q(top_p), q(min_p), u.data_ptr(), tokens.data_ptr(), q(probs), q(kept),
                                           self._raw_stream(stream)), "sample_tokens")
 

@@ -15,8 +15,8 @@
 //     (a c - b s, b c + a s), channels from rot on as they are.
 // One pass: each vector is read once, its sum of squares is a shuffle reduction inside the 8, 16 or 32 lanes that
 // hold it (8 channels = one or two 16-byte accesses per lane), the partner of a half-split pair comes by shuffle
-// from the lane rot/16 further. Bound by HBM. A lane group takes up to kHeads heads of one token: their loads are in
-// flight together and the angles are read once for all of them.
+// from the lane rot/16 further. Bound by HBM. A lane group takes up to kHeads heads of one kind of one token: their
+// loads are in flight together, and weights and angles are read once for all of them.
 #include <cuda_bf16.h>
 
 #include "stwq_internal.cuh"
@@ -172,8 +172,8 @@ struct NrParams {
     const void* X;
     int64_t ld;                    // elements between rows of X
     const int32_t *pos, *slots;
-    int64_t T, items;
-    int Hq, Hkv, NH, chunks, d, norm, rot, pairs, P, need_pos;
+    int64_t T;
+    int Hq, Hkv, d, norm, rot, pairs, P, need_pos;
     float eps;
     const float *wq, *wk;
     int wq_hs, wk_hs;              // elements between the weights of two heads (0 = shared)
@@ -230,151 +230,177 @@ __device__ __forceinline__ void store8_codes(int8_t* p, const float (&v)[8], con
 
 // LPV lanes hold a head vector. XT: element type of X; QT: of the queries (and of the keys when DEST is 0).
 // DEST 0: keys to a dense tensor, values untouched; 1: bf16 pages; 2: pages of codes.
+// blockIdx.y selects a chunk of kHeads heads of one kind (queries, then keys, then values), so that the kind, its weights
+// and its destination are the same for the whole block; a lane group takes one token.
 template <int LPV, typename XT, typename QT, int DEST>
 __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(const NrParams p)
 {
     const int l = threadIdx.x % LPV;
-    const int64_t item = (int64_t)blockIdx.x * (kNrThreads / LPV) + threadIdx.x / LPV;
+    const int64_t t = (int64_t)blockIdx.x * (kNrThreads / LPV) + threadIdx.x / LPV;
     const int e0 = 8 * l;
-    const bool in = item < p.items && e0 < p.d;
-    const int64_t t = item < p.items ? item / p.chunks : 0;
-    const int h0 = item < p.items ? (int)(item - t * p.chunks) * kHeads : 0;
-    const int pos = p.pos[t];
-    bool row = in && pos != -1;                           // position -1 marks a padding row: nothing is written for it
-    const bool pos_ok = pos >= 0 && pos < p.P;
-    const bool zero = p.need_pos && !pos_ok;              // no angle, no key scale: the query row becomes zeros
-    if (row && zero && l == 0) atomicOr(p.status, STWQ_DEV_POS_RANGE);
-    int64_t slot = -1;
-    if (DEST != 0 && row) {
-        slot = p.slots[t];
-        if (slot < -1 || slot >= p.n_slots) {
-            if (l == 0) atomicOr(p.status, STWQ_DEV_PAGES);
-            slot = -1;
-        }
-        if (zero) slot = -1;
-    }
+    const int nq = (p.Hq + kHeads - 1) / kHeads, nk = (p.Hkv + kHeads - 1) / kHeads;
+    int y = blockIdx.y;
+    const int kind = y < nq ? 0 : (y < nq + nk ? 1 : 2);
+    y -= kind == 0 ? 0 : (kind == 1 ? nq : nq + nk);
+    const int h0 = y * kHeads;                            // first head, counted within its kind
+    const int heads = min(kHeads, (kind == 0 ? p.Hq : p.Hkv) - h0);
+    const int hx = h0 + (kind == 0 ? 0 : (kind == 1 ? p.Hq : p.Hq + p.Hkv));              // and in the row of X
+    const bool in = t < p.T && e0 < p.d;
+    const int pos = t < p.T ? p.pos[t] : -1;
+    const bool row = in && pos != -1;                     // position -1 marks a padding row: nothing is written for it
+    const bool zero = p.need_pos && !(pos >= 0 && pos < p.P);     // no angle, no key scale: the query row becomes zeros
+    if (row && zero && l == 0 && blockIdx.y == 0) atomicOr(p.status, STWQ_DEV_POS_RANGE);
 
     float x[kHeads][8];
-    const XT* src = reinterpret_cast<const XT*>(p.X) + t * p.ld + (int64_t)h0 * p.d + e0;
+    const XT* src = reinterpret_cast<const XT*>(p.X) + t * p.ld + (int64_t)hx * p.d + e0;
 #pragma unroll
     for (int k = 0; k < kHeads; ++k) {
-        if (row && h0 + k < p.NH) load8(src + (int64_t)k * p.d, x[k]);
+        if (row && k < heads) load8(src + k * p.d, x[k]);
         else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[k][i] = 0.0f;
         }
     }
-    // the angles of this lane's channels: one per channel (half-split) or one per pair
-    float c[8], s[8];
-    const int half = p.rot >> 1;
-    const bool turns = e0 < p.rot;
+    // ---- where the vectors go
+    int64_t dst = -1, dst_step = 0;                       // of the first head, elements to the next; -1: nowhere
+    if (DEST != 0 && kind != 0) {
+        if (row) {
+            int slot = p.slots[t];
+            if (slot < -1 || slot >= p.n_slots) {
+                if (l == 0 && kind == 1 && h0 == 0) atomicOr(p.status, STWQ_DEV_PAGES);
+                slot = -1;
+            }
+            if (slot >= 0 && !zero) {
+                const int page = slot / p.S;
+                dst = (((int64_t)page * p.Hkv + h0) * p.S + (slot - page * p.S)) * p.d + e0;
+                dst_step = (int64_t)p.S * p.d;
+            }
+        }
+    } else if (row) {
+        dst = t * (kind == 0 ? p.q_ts : p.k_ts) + h0 * (kind == 0 ? p.q_hs : p.k_hs) + e0;
+        dst_step = kind == 0 ? p.q_hs : p.k_hs;
+    }
+
+    if (kind != 2) {
+        const unsigned lanes = LPV == 32 ? 0xffffffffu : ((1u << (LPV & 31)) - 1u) << (threadIdx.x & 31 & ~(LPV - 1));
+        if (p.norm != STWQ_NORM_NONE) {
+            const float* wp = kind == 0 ? p.wq : p.wk;
+            const int whs = kind == 0 ? p.wq_hs : p.wk_hs;
+            float w[8];
+            if (wp != nullptr && e0 < p.d) load8(wp + (int64_t)h0 * whs + e0, w);
+            else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
-    if (row && turns && !zero) {
-        const float* cs = p.cs + (int64_t)pos * p.rot;
-        if (p.pairs) {
-            const float4 a = __ldg(reinterpret_cast<const float4*>(cs + e0 / 2)), b = __ldg(reinterpret_cast<const float4*>(cs + half + e0 / 2));
-            c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w;
-            s[0] = b.x; s[1] = b.y; s[2] = b.z; s[3] = b.w;
-        } else {
-            const int i0 = e0 < half ? e0 : e0 - half;
-            load8(cs + i0, c);
-            load8(cs + half + i0, s);
+                for (int i = 0; i < 8; ++i) w[i] = 1.0f;
+            }
+            float ss[kHeads];
+#pragma unroll
+            for (int k = 0; k < kHeads; ++k) {
+                ss[k] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ss[k] = fmaf(x[k][i], x[k][i], ss[k]);
+            }
+#pragma unroll
+            for (int o = LPV / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int k = 0; k < kHeads; ++k) ss[k] += __shfl_xor_sync(lanes, ss[k], o);
+            const float inv_d = 1.0f / (float)p.d;
+#pragma unroll
+            for (int k = 0; k < kHeads; ++k) {
+                // sqrt and reciprocal as IEEE operations: a huge or tiny sum of squares behaves as in the formula
+                const float r = p.norm == STWQ_NORM_RMS ? __frcp_rn(__fsqrt_rn(fmaf(ss[k], inv_d, p.eps))) : __frcp_rn(fmaxf(__fsqrt_rn(ss[k]), p.eps));
+                if (k > 0 && whs != 0 && wp != nullptr && k < heads && e0 < p.d) load8(wp + (int64_t)(h0 + k) * whs + e0, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[k][i] = x[k][i] * r * w[i];
+            }
+        }
+        if (p.rot > 0) {
+            // the angles of this lane's channels: one per channel (half-split) or one per pair
+            const int half = p.rot >> 1;
+            const bool turns = e0 < p.rot;
+            float c[8], s[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
+            if (row && turns && !zero) {
+                const float* cs = p.cs + (int64_t)pos * p.rot;
+                if (p.pairs) {
+                    const float4 a = __ldg(reinterpret_cast<const float4*>(cs + e0 / 2)), b = __ldg(reinterpret_cast<const float4*>(cs + half + e0 / 2));
+                    c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w;
+                    s[0] = b.x; s[1] = b.y; s[2] = b.z; s[3] = b.w;
+                } else {
+                    const int i0 = e0 < half ? e0 : e0 - half;
+                    load8(cs + i0, c);
+                    load8(cs + half + i0, s);
+                }
+            }
+            if (p.pairs) {
+                if (turns) {
+#pragma unroll
+                    for (int k = 0; k < kHeads; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float a = x[k][2 * i], b = x[k][2 * i + 1];
+                            x[k][2 * i] = a * c[i] - b * s[i];
+                            x[k][2 * i + 1] = b * c[i] + a * s[i];
+                        }
+                }
+            } else {
+                const bool lower = e0 < half;
+                const int from = turns ? (lower ? l + half / 8 : l - half / 8) : l;
+                if (turns && lower) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[i] = -s[i];
+                }
+#pragma unroll
+                for (int k = 0; k < kHeads; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[k][i] = fmaf(__shfl_sync(lanes, x[k][i], from, LPV), s[i], x[k][i] * c[i]);
+            }
+        }
+        if (zero) {
+#pragma unroll
+            for (int k = 0; k < kHeads; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[k][i] = 0.0f;
         }
     }
-    const float rk = DEST == 2 && row && !zero ? __frcp_rn(p.s_k[pos]) : 1.0f;
-
+    if (dst < 0) return;
+    if (DEST == 2 && kind != 0) {
+        const float rk = kind == 1 ? __frcp_rn(p.s_k[pos]) : 1.0f;
+        int8_t* out = reinterpret_cast<int8_t*>(kind == 1 ? p.Kp : p.Vp) + dst;
 #pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-        const int h = h0 + k;
-        if (DEST == 0 && h >= p.Hq + p.Hkv) break;        // uniform for the lanes of a vector; no shuffle follows for them
-        const bool live = row && h < p.NH;
-        const bool is_q = h < p.Hq, is_k = !is_q && h < p.Hq + p.Hkv;
-        float y[8];
+        for (int k = 0; k < kHeads; ++k) {
+            if (k >= heads) break;
+            float r[8];
+            if (kind == 1) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[k][i];
-        if (is_q || is_k) {
-            const unsigned lanes = LPV == 32 ? 0xffffffffu : ((1u << (LPV & 31)) - 1u) << (threadIdx.x & 31 & ~(LPV - 1));
-            if (p.norm != STWQ_NORM_NONE) {
-                float ss = 0.0f;
+                for (int i = 0; i < 8; ++i) r[i] = rk;
+            } else {
+                load8(p.s_v + (int64_t)(h0 + k) * p.d + e0, r);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(y[i], y[i], ss);
-#pragma unroll
-                for (int o = LPV / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(lanes, ss, o);
-                const float r = p.norm == STWQ_NORM_RMS ? __frcp_rn(__fsqrt_rn(__fdiv_rn(ss, (float)p.d) + p.eps))
-                                                        : __frcp_rn(fmaxf(__fsqrt_rn(ss), p.eps));
-                float w[8];
-                const float* wp = is_q ? p.wq : p.wk;
-                if (wp != nullptr && live) load8(wp + (int64_t)(is_q ? h * p.wq_hs : (h - p.Hq) * p.wk_hs) + e0, w);
-                else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = 1.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = y[i] * r * w[i];
+                for (int i = 0; i < 8; ++i) r[i] = __frcp_rn(r[i]);
             }
-            if (p.rot > 0) {
-                if (p.pairs) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = y[2 * i], b = y[2 * i + 1];
-                        if (turns) {
-                            y[2 * i] = a * c[i] - b * s[i];
-                            y[2 * i + 1] = b * c[i] + a * s[i];
-                        }
-                    }
-                } else {
-                    const bool lower = e0 < half;
-                    const int from = turns ? (lower ? l + half / 8 : l - half / 8) : l;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float o = __shfl_sync(lanes, y[i], from, LPV);
-                        if (turns) y[i] = lower ? y[i] * c[i] - o * s[i] : y[i] * c[i] + o * s[i];
-                    }
-                }
-            }
+            store8_codes(out + k * dst_step, x[k], r, p.qmin, p.qmax);
         }
-        if (!live) continue;
-        if (is_q) {
-            if (zero) {
+    } else if (DEST != 0 && kind != 0) {
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(kind == 1 ? p.Kp : p.Vp) + dst;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = 0.0f;
-            }
-            store8(reinterpret_cast<QT*>(p.Qo) + t * p.q_ts + h * p.q_hs + e0, y);
-        } else if (DEST == 0) {
-            if (zero) {
+        for (int k = 0; k < kHeads; ++k)
+            if (k < heads) store8(out + k * dst_step, x[k]);
+    } else {
+        QT* out = reinterpret_cast<QT*>(kind == 0 ? p.Qo : p.Ko) + dst;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = 0.0f;
-            }
-            store8(reinterpret_cast<QT*>(p.Ko) + t * p.k_ts + (h - p.Hq) * p.k_hs + e0, y);
-        } else if (slot >= 0) {
-            const int kh = is_k ? h - p.Hq : h - p.Hq - p.Hkv;
-            const int64_t page = slot / p.S;
-            const int64_t at = ((page * p.Hkv + kh) * p.S + (slot - page * p.S)) * p.d + e0;
-            void* pool = is_k ? p.Kp : p.Vp;
-            if (DEST == 1) store8(reinterpret_cast<__nv_bfloat16*>(pool) + at, y);
-            else {
-                float r[8];
-                if (is_k) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) r[i] = rk;
-                } else {
-                    load8(p.s_v + (int64_t)kh * p.d + e0, r);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) r[i] = __frcp_rn(r[i]);
-                }
-                store8_codes(reinterpret_cast<int8_t*>(pool) + at, y, r, p.qmin, p.qmax);
-            }
-        }
+        for (int k = 0; k < kHeads; ++k)
+            if (k < heads) store8(out + k * dst_step, x[k]);
     }
 }
 
 template <int LPV, typename XT>
 int launch_nr(stwq_ctx* ctx, const NrParams& p, int q_f32, int dest, cudaStream_t st)
 {
-    const int64_t blocks = (p.items + kNrThreads / LPV - 1) / (kNrThreads / LPV);
-    if (blocks > 0x7fffffff) return STWQ_ERR_DIM;
-    const unsigned gx = (unsigned)blocks;
+    const int64_t blocks = (p.T + kNrThreads / LPV - 1) / (kNrThreads / LPV);
+    const int nq = (p.Hq + kHeads - 1) / kHeads, nk = (p.Hkv + kHeads - 1) / kHeads;
+    if (blocks > 0x7fffffff || nq + 2 * nk > 65535) return STWQ_ERR_DIM;
+    const dim3 gx((unsigned)blocks, (unsigned)(nq + (dest == 0 ? nk : 2 * nk)));
     if (dest == 0) {
         if (q_f32) norm_rope_kernel<LPV, XT, float, 0><<<gx, kNrThreads, 0, st>>>(p);
         else norm_rope_kernel<LPV, XT, __nv_bfloat16, 0><<<gx, kNrThreads, 0, st>>>(p);
@@ -473,9 +499,6 @@ int qk_norm_rope(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, const 
     if (!stwq_disjoint(T, Hkv, d, k_ts, k_hs)) return STWQ_ERR_DIM;
     if (!stwq_aligned16(Ko) || k_ts % elem16 != 0 || k_hs % elem16 != 0) return STWQ_ERR_ALIGN;
     p.Ko = Ko; p.k_ts = k_ts; p.k_hs = k_hs;
-    p.NH = Hq + Hkv;
-    p.chunks = (p.NH + kHeads - 1) / kHeads;
-    p.items = T * p.chunks;
     p.status = ctx->d_status;
     StwqDevGuard g(ctx->device);
     return launch_nr_any(ctx, p, x_dtype == STWQ_OUT_BF16, out_dtype == STWQ_OUT_F32, 0, static_cast<cudaStream_t>(stream));
@@ -504,9 +527,6 @@ int kv_append_paged(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, con
     p.slots = slot_map;
     p.Kp = Kp; p.Vp = Vp; p.S = page_size; p.n_slots = (int64_t)n_pages * page_size;
     p.s_k = s_k; p.s_v = s_v;
-    p.NH = Hq + 2 * Hkv;
-    p.chunks = (p.NH + kHeads - 1) / kHeads;
-    p.items = T * p.chunks;
     p.status = ctx->d_status;
     StwqDevGuard g(ctx->device);
     return launch_nr_any(ctx, p, x_dtype == STWQ_OUT_BF16, 0, kv_dtype == STWQ_KV_INT8 ? 2 : 1, static_cast<cudaStream_t>(stream));
