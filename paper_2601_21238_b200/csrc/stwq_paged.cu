@@ -21,6 +21,9 @@
 
 #include "stwq_internal.cuh"
 #include "stwq_paged.cuh"
+#include "stwq_ptx.cuh"
+
+using namespace stwq_ptx;       // packed fp32 arithmetic
 
 namespace {
 
@@ -166,7 +169,7 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanParam
 
 // ------------------------------------------------------------------------------------------ norm + rotation + append
 constexpr int kHeads = 4;          // heads of one token that a lane group takes
-constexpr int kNrThreads = 256;
+constexpr int kNrThreads = 128;
 
 struct NrParams {
     const void* X;
@@ -233,7 +236,7 @@ __device__ __forceinline__ void store8_codes(int8_t* p, const float (&v)[8], con
 // blockIdx.y selects a chunk of kHeads heads of one kind (queries, then keys, then values), so that the kind, its weights
 // and its destination are the same for the whole block; a lane group takes one token.
 template <int LPV, typename XT, typename QT, int DEST>
-__global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(const NrParams p)
+__global__ void __launch_bounds__(kNrThreads, 8) norm_rope_kernel(const NrParams p)
 {
     const int l = threadIdx.x % LPV;
     const int64_t t = (int64_t)blockIdx.x * (kNrThreads / LPV) + threadIdx.x / LPV;
@@ -295,22 +298,26 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(const NrParams p)
             float ss[kHeads];
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
-                ss[k] = 0.0f;
+                uint64_t s2 = mul_f2(pack_f2(x[k][0], x[k][1]), pack_f2(x[k][0], x[k][1]));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss[k] = fmaf(x[k][i], x[k][i], ss[k]);
+                for (int i = 2; i < 8; i += 2) s2 = fma_f2(pack_f2(x[k][i], x[k][i + 1]), pack_f2(x[k][i], x[k][i + 1]), s2);
+                float a, b;
+                unpack_f2(s2, a, b);
+                ss[k] = a + b;
             }
 #pragma unroll
             for (int o = LPV / 2; o > 0; o >>= 1)
 #pragma unroll
                 for (int k = 0; k < kHeads; ++k) ss[k] += __shfl_xor_sync(lanes, ss[k], o);
-            const float inv_d = 1.0f / (float)p.d;
+            const float inv_d = 1.0f / (float)p.d, inv_eps = 1.0f / p.eps;
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
-                // sqrt and reciprocal as IEEE operations: a huge or tiny sum of squares behaves as in the formula
-                const float r = p.norm == STWQ_NORM_RMS ? __frcp_rn(__fsqrt_rn(fmaf(ss[k], inv_d, p.eps))) : __frcp_rn(fmaxf(__fsqrt_rn(ss[k]), p.eps));
+                // 1 / max(|x|, eps) = min(rsqrt(x.x), 1 / eps); rsqrtf is good to 2 ulp, and takes 0 and Inf as the formula does
+                const float r = p.norm == STWQ_NORM_RMS ? rsqrtf(fmaf(ss[k], inv_d, p.eps)) : fminf(rsqrtf(ss[k]), inv_eps);
                 if (k > 0 && whs != 0 && wp != nullptr && k < heads && e0 < p.d) load8(wp + (int64_t)(h0 + k) * whs + e0, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[k][i] = x[k][i] * r * w[i];
+                for (int i = 0; i < 8; i += 2)
+                    unpack_f2(mul_f2(mul_f2(pack_f2(x[k][i], x[k][i + 1]), dup_f2(r)), pack_f2(w[i], w[i + 1])), x[k][i], x[k][i + 1]);
             }
         }
         if (p.rot > 0) {
@@ -339,8 +346,7 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(const NrParams p)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float a = x[k][2 * i], b = x[k][2 * i + 1];
-                            x[k][2 * i] = a * c[i] - b * s[i];
-                            x[k][2 * i + 1] = b * c[i] + a * s[i];
+                            unpack_f2(fma_f2(pack_f2(b, a), pack_f2(-s[i], s[i]), mul_f2(pack_f2(a, b), dup_f2(c[i]))), x[k][2 * i], x[k][2 * i + 1]);
                         }
                 }
             } else {
@@ -353,7 +359,10 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(const NrParams p)
 #pragma unroll
                 for (int k = 0; k < kHeads; ++k)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[k][i] = fmaf(__shfl_sync(lanes, x[k][i], from, LPV), s[i], x[k][i] * c[i]);
+                    for (int i = 0; i < 8; i += 2) {
+                        const uint64_t o = pack_f2(__shfl_sync(lanes, x[k][i], from, LPV), __shfl_sync(lanes, x[k][i + 1], from, LPV));
+                        unpack_f2(fma_f2(o, pack_f2(s[i], s[i + 1]), mul_f2(pack_f2(x[k][i], x[k][i + 1]), pack_f2(c[i], c[i + 1]))), x[k][i], x[k][i + 1]);
+                    }
             }
         }
         if (zero) {
