@@ -448,8 +448,8 @@ int stwq_reserve_paged_attention(stwq_ctx* ctx, int B, int Hq, int Hkv, int d);
  *   (at least one); min_p keeps w_i >= min_p. u in [0, 1): the token is the first kept index whose running sum of kept weights,
  *   in index order, exceeds u times their total.
  * tokens [B]; probs [B] (weight of the token / total of the kept; may be NULL), kept [B] (number of kept tokens; may be NULL).
- * A row without any token to draw gives token -1, probability 0, kept 0. Weights are 2^-43 fixed point summed in 64-bit
- * integers, so results repeat bit for bit. V <= 409600.
+ * A row without any token to draw gives token -1, probability 0, kept 0. Weights are 2^-42 fixed point summed in 64-bit
+ * integers, so results repeat bit for bit. V <= 360448.
  */
 int sample_tokens(stwq_ctx* ctx, const void* logits, int x_dtype, int64_t ld, int B, int V, const float* temperature,
                   const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tokens, float* probs,

@@ -7,18 +7,22 @@
 //     min-p keeps the w_i >= min_p (w of the largest is 1)
 //     token = first kept index i, in index order, with  sum_{j <= i, kept} w_j > u * sum_{kept} w_j
 // No sort: a kept set is "every key above K, and the first r tokens (by index) whose key equals K", so both limits
-// are order statistics, found by radix selection over the monotone 32-bit image of the logits (11 + 11 + 10
-// bits, one histogram per digit): counts for top-k, masses for top-p.
+// are order statistics over the monotone 32-bit image of the logits. Each is found in two steps: 64 coarse bins (by
+// distance from the maximum; counts for top-k, masses for top-p) give the bin that holds the border, and a radix
+// selection (up to 11 bits a pass) over that bin's few members gives K. A coarse bin has a counter per lane, so that the
+// atomics of a warp never meet, however the logits cluster. What top-k keeps, if it is at most kList tokens, is
+// compacted in index order, and everything after it works on that list.
 //
-// Weights are integers, round(w 2^43), summed in 64 bits: sums do not depend on the order of the atomics that form
-// them, so the same call gives the same token every time, and p W and u W are compared exactly. 2^43 leaves room for
-// 2^20 tokens and puts the rounding of a weight (2^-44 of the largest) far below the fp64 rounding of a long sum;
-// with fp32 weights one row in some ten thousand would fall on the other side of a border. exp is table-driven
-// (2^(j/64) from a table, a degree-4 polynomial for the rest; the method of Tang, "Table-driven implementation of
-// the exponential function", 1989), in fp64: 11 fp64 operations per weight, error below 5e-14.
+// Weights are integers, round(w 2^42), summed in 64 bits: sums do not depend on the order of the atomics that form
+// them, so the same call gives the same token every time, and p W and u W are compared exactly. 2^42 leaves room for
+// the sums of 2^19 tokens and puts the rounding of a weight (2^-43 of the largest) far below what could move a border;
+// with fp32 weights one row in some ten thousand would fall on the other side of one. exp is table-driven (2^(j/256) from
+// a table, a cubic for the rest; the method of Tang, "Table-driven implementation of the exponential function", 1989),
+// in fp64: 9 fp64 operations per weight, error below 2e-13.
 //
-// A row is read from HBM once, into the shared memory of one CTA or of a cluster of up to 8 (the histograms are then
-// added up over distributed shared memory); every later pass runs on shared memory.
+// A row is read from HBM once, into the shared memory of one CTA or of a cluster of up to 8 (the bins are then
+// added up over distributed shared memory); every later pass runs on shared memory. What bounds it: the passes' latency
+// for few rows, the fp64 weights of top-p without top-k (every token needs one).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
@@ -29,10 +33,14 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int kBins = 2048;
+constexpr int kBins = 2048;                 // of a radix digit
+constexpr int kCoarse = 64;                 // coarse bins, a counter per lane each
+constexpr int kList = 2048;                 // tokens of a compacted list
 constexpr int kMaxCluster = 8;
-constexpr int kMaxSlice = 50 * 1024;         // logits per CTA: 200 KB of shared memory
-constexpr int kFrac = 43;                    // fraction bits of a weight
+constexpr int kMaxSlice = 44 * 1024;         // logits per CTA: 176 KB of shared memory
+constexpr int kPairSlice = 17 * 1024;        // two CTAs fit an SM
+constexpr int kFrac = 42;                    // fraction bits of a weight
+constexpr int kLow = 21;                     // a coarse counter holds the low bits, another the rest: 44 K / 32 adds fit both
 
 struct SmpParams {
     const void* X;
@@ -46,15 +54,21 @@ struct SmpParams {
 };
 
 struct SmpShared {
-    double table[64];
-    unsigned long long warp_a[32], warp_b[32];
+    double table[256];
+    unsigned long long warp_a[32];
+    uint32_t warp_n[32];
     unsigned long long total;                // of this CTA: exchanged inside a cluster
-    unsigned long long sel_above;
-    uint32_t maxkey;
+    unsigned long long tot[kCoarse];
+    unsigned long long sel_above, sel_total;
+    uint32_t maxkey, kmin, kmax;
     uint32_t sel_bin;
-    uint32_t cnt_total, ties;
-    uint32_t hist_lo[kBins], hist_hi[kBins];
+    uint32_t cnt_total, n_in;
+    uint32_t hist_lo[kBins], hist_hi[kBins]; // radix digits; or kCoarse x 32 lanes
+    uint32_t list_key[kList], list_idx[kList];                             // what top-k keeps, in index order
+    uint32_t in_key[kList];                  // members of the border bin (3 kList of them where the list above is not in use)
 };
+static_assert(kMaxSlice <= 65536, "16-bit offsets");
+static_assert(kCoarse * 32 <= kBins, "coarse counters share the radix histograms");
 
 // fp32 -> unsigned key, larger logit = larger key, -0 = +0; 0 for NaN and -Inf (never drawn)
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -69,36 +83,37 @@ __device__ __forceinline__ float value_of(uint32_t k)
 }
 
 struct Weigher {
-    double m, c;                             // row maximum, 64 log2(e) / temperature
+    double c, mc;                            // 256 log2(e) / temperature, and the row maximum times it
+    double m;
+    float low;                               // below this logit a weight rounds to zero
     uint32_t maxkey;
     const double* table;
-    // round(exp((x - m) / t) 2^43); w_out gets the unrounded weight
+    // round(exp((x - m) / t) 2^42); w_out gets the unrounded weight (0 below 2^-46)
     __device__ __forceinline__ unsigned long long fixed(uint32_t key, double& w_out) const
     {
-        if (key == maxkey) {
-            w_out = 1.0;
-            return 1ull << kFrac;
+        const float x = value_of(key);
+        if (key == maxkey || !(x > low)) {               // the maximum itself (also at +Inf), or rounds to zero
+            w_out = key == maxkey ? 1.0 : 0.0;
+            return key == maxkey ? 1ull << kFrac : 0ull;
         }
-        const double z = ((double)value_of(key) - m) * c;
-        if (!(z > -64.0 * 46.0)) {           // below 2^-46: rounds to zero (also x - m = -Inf)
-            w_out = z > -64.0 * 1000.0 ? exp2(z * 0.015625) : 0.0;
-            return 0ull;
-        }
-        const double magic = 6755399441055744.0;                       // 1.5 * 2^52: the integer part lands in the low word
-        const double s = z + magic;
+        const double xd = (double)x, magic = 6755399441055744.0;       // 1.5 * 2^52: the integer part lands in the low word
+        const double z = fma(xd, c, -mc), s = z + magic;
         const int n = __double2loint(s);
-        const double f = z - (s - magic);                              // |f| <= 1/2, in 64ths of an octave
-        // 2^(f/64) - 1 = sum (f ln2/64)^k / k!
-        double q = 5.732851688640402e-10;                             // (ln2/64)^4 / 24
-        q = fma(q, f, 2.1173137155464774e-07);                         // (ln2/64)^3 / 6
-        q = fma(q, f, 5.864904955056169e-05);                           // (ln2/64)^2 / 2
-        q = fma(q, f, 0.010830424696249145);                           // ln2 / 64
-        const double t = table[n & 63];
-        const double ts = __hiloint2double(__double2hiint(t) + ((n >> 6) << 20), __double2loint(t));
+        const double f = z - (s - magic);                              // |f| <= 1/2, in 256ths of an octave
+        // 2^(f/256) - 1 = sum (f ln2/256)^k / k!, the next term is below 1.4e-13
+        double q = fma(f, 3.308302680541371e-09, 3.665565596910106e-06);
+        q = fma(q, f, 0.0027076061740622863);
+        const double t = table[n & 255];
+        const double ts = __hiloint2double(__double2hiint(t) + ((n >> 8) << 20), __double2loint(t));
         const double w = fma(ts, f * q, ts);
         w_out = w;
         const double fx = fma(w, (double)(1ull << kFrac), 4503599627370496.0);   // + 2^52
         return (unsigned long long)__double_as_longlong(fx) & 0xfffffffffffffull;
+    }
+    // the weight itself, however small (for a min-p below 2^-46)
+    __device__ __noinline__ double exact(uint32_t key) const
+    {
+        return key == maxkey ? 1.0 : exp2(((double)value_of(key) - m) * c * 0.00390625);
     }
 };
 
@@ -138,7 +153,7 @@ __device__ __forceinline__ unsigned long long block_scan_u64(unsigned long long 
 }
 
 template <int NT, bool CL, typename XT>
-__global__ void __launch_bounds__(NT) sample_kernel(const SmpParams p)
+__global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p)
 {
     extern __shared__ __align__(16) uint32_t keys[];
     __shared__ SmpShared sh;
@@ -154,9 +169,8 @@ __global__ void __launch_bounds__(NT) sample_kernel(const SmpParams p)
 
     const int i0 = rank * p.chunk;
     const int n = max(0, min(p.V - i0, p.chunk));
-    const int run = ((n + NT - 1) / NT) | 1;              // consecutive tokens per thread: odd, so that no two lanes share a bank
 
-    if (tid < 64) sh.table[tid] = exp2((double)tid * 0.015625);
+    if (tid < 256) sh.table[tid] = exp2((double)tid * 0.00390625);
     // ---- the row, once
     uint32_t mx = 0u;
     {
@@ -217,184 +231,450 @@ __global__ void __launch_bounds__(NT) sample_kernel(const SmpParams p)
     const double min_p = min_pf > 0.0f ? fmin((double)min_pf, 1.0) : 0.0;
     Weigher wg;
     wg.m = (double)value_of(maxkey);
-    wg.c = greedy ? 64.0 : 92.33248261689366 / (double)temp;      // 64 log2(e)
+    wg.c = greedy ? 256.0 : 369.3299304675746 / (double)temp;      // 256 log2(e)
+    wg.mc = wg.m * wg.c;
+    wg.low = (float)fmax(wg.m - 46.0 * 256.0 / wg.c, -3.4028234663852886e38);      // 46 octaves below (an infinite maximum leaves the others at 0)
     wg.maxkey = maxkey;
     wg.table = sh.table;
+    const bool tiny_min_p = min_p > 0.0 && min_p < 1.5e-14;
 
-    // The bin (from the top) in which the running sum of the histograms, on top of `above`, reaches `target`;
-    // `total` receives the sum over all bins. False if the target is not reached.
-    auto find_bin = [&](unsigned long long above, unsigned long long target, bool mass, unsigned long long& total, uint32_t& bin,
-                        unsigned long long& above_out) -> bool {
-        constexpr int kPerT = kBins / NT;
-        unsigned long long b[kPerT], sum = 0;
-#pragma unroll
-        for (int k = 0; k < kPerT; ++k) {
-            const int i = kBins - 1 - (tid * kPerT + k);  // from the top
-            unsigned long long v = 0;
-            for (int r = 0; r < C; ++r) {
-                v += *peer(&sh.hist_lo[i], r);
-                if (mass) v += (unsigned long long)*peer(&sh.hist_hi[i], r) << 32;
-            }
-            b[k] = v;
-            sum += v;
-        }
-        unsigned long long at = above + block_scan_u64<NT>(sum, sh.warp_a, total);
-        if (tid == 0) sh.sel_bin = 0xffffffffu;
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kPerT; ++k) {
-            if (at < target && at + b[k] >= target) {
-                sh.sel_bin = kBins - 1 - (tid * kPerT + k);
-                sh.sel_above = at;
-            }
-            at += b[k];
-        }
-        __syncthreads();
-        bin = sh.sel_bin;
-        above_out = sh.sel_above;
-        return bin != 0xffffffffu;
-    };
+    const int lane = tid & 31, warp = tid >> 5;
     auto clear_hist = [&]() {
         for (int i = tid; i < kBins; i += NT) {
             sh.hist_lo[i] = 0u;
             sh.hist_hi[i] = 0u;
         }
+        if (tid == 0) {
+            sh.n_in = 0u;
+            sh.kmin = 0xffffffffu;
+            sh.kmax = 0u;
+        }
         __syncthreads();
     };
-    const int shift_of[3] = {21, 10, 0}, bins_of[3] = {2048, 2048, 1024};
+    // The first coarse bin in which the running sum reaches `target(total)`; sets sel_bin, sel_above, sel_total.
+    auto find_coarse = [&](bool mass, auto&& target) {
+        __syncthreads();
+        for (int b = warp; b < kCoarse; b += NT / 32) {
+            unsigned long long v = sh.hist_lo[b * 32 + lane];
+            if (mass) v += (unsigned long long)sh.hist_hi[b * 32 + lane] << kLow;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (lane == 0) sh.tot[b] = v;
+        }
+        sync_all();                                       // the sums of every CTA are complete
+        unsigned long long all_bins = 0;
+        if (tid < kCoarse)
+            for (int r = 0; r < C; ++r) all_bins += *peer(&sh.tot[tid], r);
+        if (CL) {
+            sync_all();                                   // and have been read
+            if (tid < kCoarse) sh.tot[tid] = all_bins;
+            __syncthreads();
+        }
+        if (warp == 0) {
+            static_assert(kCoarse == 64, "two bins per lane");
+            const unsigned long long a = sh.tot[2 * lane], b = sh.tot[2 * lane + 1];
+            unsigned long long s = a + b;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned long long t = __shfl_up_sync(0xffffffffu, s, o);
+                if (lane >= o) s += t;
+            }
+            const unsigned long long total = __shfl_sync(0xffffffffu, s, 31), tg = target(total);
+            const unsigned long long before = s - a - b;
+            if (lane == 0) {
+                sh.sel_bin = 0xffffffffu;
+                sh.sel_total = total;
+            }
+            __syncwarp();
+            if (before < tg && before + a + b >= tg) {
+                const bool second = before + a < tg;
+                sh.sel_bin = 2 * lane + (second ? 1 : 0);
+                sh.sel_above = before + (second ? a : 0ull);
+            }
+        }
+        __syncthreads();
+    };
+    // K of the border inside a coarse bin: on top of `above`, the running sum (counts or masses) over the bin's keys, from
+    // the largest, first reaches `target` at K. member(key): the key is in the bin. Leaves the sum above K in `above`.
+    // *whole is set if every token at K is part of it.
+    auto select_in_bin = [&](const uint32_t* src, int ns, auto&& member, bool mass, unsigned long long& above, unsigned long long target,
+                             bool& whole) -> uint32_t {
+        clear_hist();
+        // the members, gathered from every CTA of the row into each: from here on no CTA waits for another
+        const int cap = src == sh.list_key ? kList : 3 * kList;
+        uint32_t* members = src == sh.list_key ? sh.in_key : sh.list_key;
+        auto gather = [&](uint32_t k, bool in, uint32_t& at) {
+            const unsigned ins = __ballot_sync(0xffffffffu, in);
+            if (in && at + __popc(ins & ((1u << lane) - 1u)) < (uint32_t)cap) members[at + __popc(ins & ((1u << lane) - 1u))] = k;
+            at += __popc(ins);
+        };
+        uint32_t kmin = 0xffffffffu, kmax = 0u, mine = 0u;
+        for (int i = tid; i < ns; i += NT) {
+            const uint32_t k = src[i];
+            if (member(k)) {
+                ++mine;
+                kmin = min(kmin, k);
+                kmax = max(kmax, k);
+            }
+        }
+        const uint32_t warp_members = __reduce_add_sync(0xffffffffu, mine);
+        kmin = __reduce_min_sync(0xffffffffu, kmin);
+        kmax = __reduce_max_sync(0xffffffffu, kmax);
+        uint32_t at = 0u;
+        if (lane == 0 && warp_members > 0u) {
+            at = atomicAdd(&sh.n_in, warp_members);
+            atomicMin(&sh.kmin, kmin);
+            atomicMax(&sh.kmax, kmax);
+        }
+        at = __shfl_sync(0xffffffffu, at, 0);
+        sync_all();
+        uint32_t lo = 0xffffffffu, hi = 0u, n_all = 0u, n_before = 0u;
+        for (int r = 0; r < C; ++r) {
+            lo = min(lo, *peer(&sh.kmin, r));
+            hi = max(hi, *peer(&sh.kmax, r));
+            const uint32_t v = *peer(&sh.n_in, r);
+            n_all += v;
+            n_before += r < rank ? v : 0u;
+        }
+        const bool listed = n_all <= (uint32_t)cap;       // else the members are looked up in the source again, CTA by CTA
+        if (listed) {
+            at += n_before;
+            if (warp_members > 0u)
+                for (int i = tid; i - lane < ns; i += NT) {
+                    const uint32_t k = i < ns ? src[i] : 0u;
+                    gather(k, i < ns && member(k), at);
+                }
+            sync_all();
+            if (CL) {
+                // CTA r wrote the members from its n_before on; copy the others'
+                uint32_t from = 0u;
+                for (int r = 0; r < C; ++r) {
+                    const uint32_t v = *peer(&sh.n_in, r);
+                    if (r != rank)
+                        for (uint32_t i = from + tid; i < from + v; i += NT) members[i] = *peer(&members[i], r);
+                    from += v;
+                }
+                sync_all();
+            }
+        }
+        const uint32_t* from = listed ? members : src;
+        const int nf = listed ? (int)n_all : ns;
+        auto sync_sel = [&]() {
+            if (listed) __syncthreads();
+            else sync_all();
+        };
+        int rem = hi > lo ? 32 - __clz(hi - lo) : 0;      // bits of a key above the bin's lowest that are still open
+        uint32_t prefix = 0u;
+        unsigned long long at_k = 0ull;
+        bool first = true;
+        do {
+            const int width = min(rem, 11), shift = rem - width;
+            const uint32_t open = rem >= 32 ? 0u : prefix >> rem;
+            if (!first) {
+                for (int i = tid; i < kBins; i += NT) {
+                    sh.hist_lo[i] = 0u;
+                    sh.hist_hi[i] = 0u;
+                }
+                __syncthreads();
+            }
+            first = false;
+            for (int i = tid; i < nf; i += NT) {
+                const uint32_t k = from[i];
+                if (!listed && !member(k)) continue;
+                const uint32_t x = k - lo;
+                if (rem < 32 && (x >> rem) != open) continue;
+                const uint32_t d = (x >> shift) & ((1u << width) - 1u);
+                if (mass) {
+                    double wd;
+                    const unsigned long long w = wg.fixed(k, wd);
+                    const uint32_t old = atomicAdd(&sh.hist_lo[d], (uint32_t)w);
+                    const uint32_t up = (uint32_t)(w >> 32) + (old + (uint32_t)w < old ? 1u : 0u);
+                    if (up != 0u) atomicAdd(&sh.hist_hi[d], up);
+                } else atomicAdd(&sh.hist_lo[d], 1u);
+            }
+            sync_sel();
+            constexpr int kPerT = kBins / NT;
+            unsigned long long b[kPerT], sum = 0, total;
+#pragma unroll
+            for (int k = 0; k < kPerT; ++k) {
+                const int i = kBins - 1 - (tid * kPerT + k);               // from the top
+                unsigned long long v = 0;
+                if (listed) v = (unsigned long long)sh.hist_lo[i] + ((unsigned long long)sh.hist_hi[i] << 32);
+                else
+                    for (int r = 0; r < C; ++r) v += (unsigned long long)*peer(&sh.hist_lo[i], r) + ((unsigned long long)*peer(&sh.hist_hi[i], r) << 32);
+                b[k] = v;
+                sum += v;
+            }
+            unsigned long long run = above + block_scan_u64<NT>(sum, sh.warp_a, total);
+#pragma unroll
+            for (int k = 0; k < kPerT; ++k) {
+                if (run < target && run + b[k] >= target) {
+                    sh.sel_bin = kBins - 1 - (tid * kPerT + k);
+                    sh.sel_above = run;
+                    sh.sel_total = b[k];
+                }
+                run += b[k];
+            }
+            sync_sel();                                   // chosen, and the histograms read by every CTA
+            above = sh.sel_above;
+            at_k = sh.sel_total;
+            prefix |= sh.sel_bin << shift;
+            rem = shift;
+            __syncthreads();
+        } while (rem > 0);
+        whole = above + at_k == target;
+        return lo + prefix;
+    };
+    // Coarse bins, both monotone in the key. For counts: the distance below the maximum, four bins per octave from 2^-6 on.
+    // For masses: half octaves of the weight (fp32: only the grouping depends on it).
+    const float fmax_ = value_of(maxkey);
+    auto distance_bin = [&](uint32_t key) -> int {
+        if (key == maxkey) return 0;
+        const int e = (int)(__float_as_uint(__fsub_rn(fmax_, value_of(key))) >> 21) - (121 << 2);
+        return min(max(e, 0), kCoarse - 1);
+    };
+    const float half_octaves = greedy ? 1.0f : 2.885390082f / temp;
+    auto weight_bin = [&](uint32_t key) -> int {
+        if (key == maxkey) return 0;
+        return (int)fminf(__fmul_rn(__fsub_rn(fmax_, value_of(key)), half_octaves), (float)(kCoarse - 1));
+    };
 
-    // kept set: key > K, and the first r tokens with key == K
+    // kept set: key > K, and the first r tokens with key == K. src: the slice, or a list of it (then all of it is kept so far).
+    const uint32_t* src = keys;
+    const uint32_t* src_idx = nullptr;
+    int ns = n;
     uint32_t K = 0u;
     unsigned long long r_keep = 0ull;
     if (top_k == 1) {                                     // greedy, or top-1: no selection needed
         K = maxkey;
         r_keep = 1ull;
     } else if (top_k > 1 && top_k < p.V) {
-        unsigned long long above = 0ull;
-        uint32_t prefix = 0u;
-        bool found = true;
-#pragma unroll
-        for (int ps = 0; ps < 3 && found; ++ps) {
-            clear_hist();
-            const int sh_hi = ps == 0 ? 32 : shift_of[ps - 1];
-            for (int i = tid; i < n; i += NT) {
-                const uint32_t k = keys[i];
-                if (k != 0u && (ps == 0 || ((k ^ prefix) >> (sh_hi & 31)) == 0u))
-                    atomicAdd(&sh.hist_lo[(k >> shift_of[ps]) & (bins_of[ps] - 1)], 1u);
-            }
-            sync_all();
-            unsigned long long total, ab;
-            uint32_t bin;
-            found = find_bin(above, (unsigned long long)top_k, false, total, bin, ab);
-            if (found) {
-                above = ab;
-                prefix |= bin << shift_of[ps];
-            }
-            sync_all();                                   // the histograms have been read by every CTA
+        clear_hist();
+        for (int i = tid; i < n; i += NT) {
+            const uint32_t k = keys[i];
+            if (k != 0u) atomicAdd(&sh.hist_lo[distance_bin(k) * 32 + lane], 1u);
         }
-        if (found) {                                      // else fewer than k tokens can be drawn: no limit
-            K = prefix;
+        find_coarse(false, [&](unsigned long long) { return (unsigned long long)top_k; });
+        if (sh.sel_bin != 0xffffffffu) {                  // else fewer than k tokens can be drawn: no limit
+            const int border = (int)sh.sel_bin;
+            unsigned long long above = sh.sel_above;
+            __syncthreads();
+            bool whole;
+            K = select_in_bin(keys, n, [&](uint32_t k) { return k != 0u && distance_bin(k) == border; }, false, above, (unsigned long long)top_k, whole);
             r_keep = (unsigned long long)top_k - above;
+            if (whole) {                                  // every token at K is kept: no ranks needed
+                K -= 1u;
+                r_keep = 0ull;
+            }
         }
+    }
+    // Index order: a warp has a contiguous segment of the source and walks it 32 tokens at a time, so ranks are ballots.
+    constexpr int kW = NT / 32;
+    int seg = ((ns + kW - 1) / kW + 31) & ~31;
+    int s0 = min(ns, warp * seg), s1 = min(ns, s0 + seg);
+    // sum over the warps before this one (and the CTAs before this one) of a value that all lanes of a warp hold
+    auto warps_before = [&](uint32_t v) -> uint32_t {
+        __syncthreads();
+        if (lane == 0) sh.warp_n[warp] = v;
+        __syncthreads();
+        uint32_t mine = lane < kW ? sh.warp_n[lane] : 0u, before = 0u;
+        const uint32_t all = __reduce_add_sync(0xffffffffu, mine);
+        before = __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0u);
+        if (CL) {
+            if (tid == 0) sh.cnt_total = all;
+            sync_all();
+            for (int r = 0; r < rank; ++r) before += *peer(&sh.cnt_total, r);
+            sync_all();
+        }
+        return before;
+    };
+    // number of tokens before the segment whose key equals K
+    auto ties_before = [&]() -> uint32_t {
+        uint32_t c = 0;
+#pragma unroll 4
+        for (int j = s0 + lane; j < s1; j += 32) c += src[j] == K;
+        return warps_before(__reduce_add_sync(0xffffffffu, c));
+    };
+    const unsigned below = (1u << lane) - 1u;
+    if (K != 0u && top_k > 1 && top_k <= kList) {
+        // at most kList tokens are left: list them in index order
+        const uint32_t tie0 = r_keep > 0 ? ties_before() : 0u;
+        uint32_t mine = 0, tie = tie0;
+        auto walk = [&](bool write, uint32_t at) {
+            tie = tie0;
+            mine = 0;
+#pragma unroll 4
+            for (int j = s0; j < s1; j += 32) {
+                const uint32_t k = j + lane < s1 ? keys[j + lane] : 0u;
+                bool in = k > K;
+                if (r_keep > 0) {
+                    const unsigned eq = __ballot_sync(0xffffffffu, k == K);              // K > 0
+                    in |= k == K && tie + __popc(eq & below) < r_keep;
+                    tie += __popc(eq);
+                }
+                const unsigned ins = __ballot_sync(0xffffffffu, in);
+                if (write && in) {
+                    const uint32_t to = at + mine + __popc(ins & below);
+                    sh.list_key[to] = k;
+                    sh.list_idx[to] = (uint32_t)(i0 + j + lane);
+                }
+                mine += __popc(ins);
+            }
+        };
+        walk(false, 0u);
+        __syncthreads();
+        if (lane == 0) sh.warp_n[warp] = mine;
+        __syncthreads();
+        const uint32_t v = lane < kW ? sh.warp_n[lane] : 0u;
+        const uint32_t listed = __reduce_add_sync(0xffffffffu, v);
+        walk(true, __reduce_add_sync(0xffffffffu, lane < warp ? v : 0u));
+        __syncthreads();
+        src = sh.list_key;
+        src_idx = sh.list_idx;
+        ns = (int)listed;
+        K = 0u;
+        r_keep = 0ull;
+        seg = ((ns + kW - 1) / kW + 31) & ~31;
+        s0 = min(ns, warp * seg);
+        s1 = min(ns, s0 + seg);
     }
     if (top_p < 1.0f && top_k != 1) {
         double wd;
         const unsigned long long wk = r_keep > 0 ? wg.fixed(K, wd) : 0ull;
         const unsigned long long pfx = frac64(top_p);
-        unsigned long long above = 0ull, target = 0ull;
-        uint32_t prefix = 0u;
-        bool inside = true;
-#pragma unroll
-        for (int ps = 0; ps < 3 && inside; ++ps) {
-            clear_hist();
-            const int sh_hi = ps == 0 ? 32 : shift_of[ps - 1];
-            for (int i = tid; i < n; i += NT) {
-                const uint32_t k = keys[i];
-                if (k > K && (ps == 0 || ((k ^ prefix) >> (sh_hi & 31)) == 0u)) {
-                    const unsigned long long w = wg.fixed(k, wd);
-                    const uint32_t bin = (k >> shift_of[ps]) & (bins_of[ps] - 1);
-                    const uint32_t lo = (uint32_t)w;
-                    const uint32_t old = atomicAdd(&sh.hist_lo[bin], lo);
-                    const uint32_t hi = (uint32_t)(w >> 32) + (old + lo < old ? 1u : 0u);
-                    if (hi != 0u) atomicAdd(&sh.hist_hi[bin], hi);
-                }
+        unsigned long long W = 0ull, target = 0ull;
+        clear_hist();
+        for (int i = tid; i < ns; i += NT) {
+            const uint32_t k = src[i];
+            if (k > K) {
+                const unsigned long long w = wg.fixed(k, wd);
+                const int bn = weight_bin(k);
+                const uint32_t low = (uint32_t)w & ((1u << kLow) - 1u), up = (uint32_t)(w >> kLow);
+                if (low != 0u) atomicAdd(&sh.hist_lo[bn * 32 + lane], low);
+                if (up != 0u) atomicAdd(&sh.hist_hi[bn * 32 + lane], up);
             }
-            sync_all();
-            unsigned long long total, ab;
-            uint32_t bin;
-            if (ps == 0) {
-                // the mass first: the target is p times it
-                unsigned long long sum = 0;
-                for (int i = tid; i < kBins; i += NT)
-                    for (int r = 0; r < C; ++r)
-                        sum += (unsigned long long)*peer(&sh.hist_lo[i], r) + ((unsigned long long)*peer(&sh.hist_hi[i], r) << 32);
-                unsigned long long mass;
-                block_scan_u64<NT>(sum, sh.warp_b, mass);
-                const unsigned long long W = mass + r_keep * wk;
-                target = __umul64hi(pfx, W) + (pfx * W != 0ull ? 1ull : 0ull);         // ceil(p W)
-                if (target == 0ull) target = 1ull;
-                if (mass < target) {                      // every key above K, and some of those equal to K
-                    inside = false;
-                    const unsigned long long want = wk > 0 ? (target - mass + wk - 1) / wk : r_keep;
-                    r_keep = min(r_keep, want);
-                    sync_all();
-                    break;
-                }
-            }
-            find_bin(above, target, true, total, bin, ab);
-            above = ab;
-            prefix |= bin << shift_of[ps];
-            sync_all();
         }
-        if (inside) {
-            K = prefix;
+        auto goal = [&](unsigned long long mass) {
+            W = mass + r_keep * wk;
+            const unsigned long long t = __umul64hi(pfx, W) + (pfx * W != 0ull ? 1ull : 0ull);     // ceil(p W)
+            return t == 0ull ? 1ull : t;
+        };
+        find_coarse(true, goal);
+        const unsigned long long mass = sh.sel_total;
+        target = goal(mass);
+        if (sh.sel_bin == 0xffffffffu) {                  // every key above K, and some of those equal to K
+            const unsigned long long want = wk > 0 ? (target - mass + wk - 1) / wk : r_keep;
+            r_keep = min(r_keep, want);
+        } else {
+            const int border = (int)sh.sel_bin;
+            unsigned long long above = sh.sel_above;
+            const uint32_t K0 = K;
+            bool whole;
+            __syncthreads();
+            K = select_in_bin(src, ns, [&](uint32_t k) { return k > K0 && weight_bin(k) == border; }, true, above, target, whole);
             const unsigned long long wp = wg.fixed(K, wd);
             r_keep = wp > 0 ? (target - above + wp - 1) / wp : 1ull;
         }
+        __syncthreads();
     }
 
-    // ---- ranks of the tokens whose key equals K, in index order
-    const int j0 = min(n, tid * run), j1 = min(n, j0 + run);
-    unsigned long long tie_at = 0ull;
-    if (r_keep > 0) {
-        unsigned long long ties = 0, tot;
-        for (int j = j0; j < j1; ++j) ties += keys[j] == K;
-        tie_at = block_scan_u64<NT>(ties, sh.warp_a, tot);
-        if (CL) {
-            if (tid == 0) sh.total = tot;
-            sync_all();
-            for (int r = 0; r < rank; ++r) tie_at += *peer(&sh.total, r);
-            sync_all();
-        }
-    }
-    // ---- mass and number of the kept tokens
-    unsigned long long sum = 0, tie = tie_at;
-    uint32_t cnt = 0;
-    for (int j = j0; j < j1; ++j) {
-        const uint32_t k = keys[j];
-        const bool eq = k == K && r_keep > 0;
-        if ((k > K) || (eq && tie < r_keep)) {
-            double w;
-            const unsigned long long f = wg.fixed(k, w);
-            if (w >= min_p) {
-                sum += f;
-                ++cnt;
+    // ---- mass and number of the kept tokens. Over the whole slice the kept ones are listed first (16-bit offsets), so
+    // that the fp64 weights run on full warps.
+    uint32_t tie_at = r_keep > 0 ? ties_before() : 0u;
+    uint16_t* offs = reinterpret_cast<uint16_t*>(sh.list_key);             // 6 kList of them, behind one another
+    bool by_offset = false;
+    if (src == keys && top_k != 1) {
+        __syncthreads();
+        uint32_t mine = 0;
+        auto walk = [&](bool write, uint32_t at) {
+            uint32_t tie = tie_at;
+            mine = 0;
+#pragma unroll 4
+            for (int j = s0; j < s1; j += 32) {
+                const uint32_t k = j + lane < s1 ? keys[j + lane] : 0u;
+                bool in = k > K;
+                if (r_keep > 0) {
+                    const unsigned eq = __ballot_sync(0xffffffffu, k == K);
+                    in |= k == K && tie + __popc(eq & below) < r_keep;
+                    tie += __popc(eq);
+                }
+                const unsigned ins = __ballot_sync(0xffffffffu, in);
+                if (write && in) offs[at + mine + __popc(ins & below)] = (uint16_t)(j + lane);
+                mine += __popc(ins);
             }
+        };
+        walk(false, 0u);
+        if (lane == 0) sh.warp_n[warp] = mine;
+        __syncthreads();
+        const uint32_t v = lane < kW ? sh.warp_n[lane] : 0u;
+        const uint32_t listed = __reduce_add_sync(0xffffffffu, v);
+        by_offset = listed <= 6 * kList;                  // uniform over the CTA; the slice is shorter than 2^16
+        if (by_offset) {
+            walk(true, __reduce_add_sync(0xffffffffu, lane < warp ? v : 0u));
+            ns = (int)listed;
+            K = 0u;
+            r_keep = 0ull;
+            tie_at = 0u;
+            seg = ((ns + kW - 1) / kW + 31) & ~31;
+            s0 = min(ns, warp * seg);
+            s1 = min(ns, s0 + seg);
         }
-        tie += eq;
+        __syncthreads();
     }
-    unsigned long long mine, kept_cnt;
-    const unsigned long long before_cta = block_scan_u64<NT>(sum, sh.warp_a, mine);
-    block_scan_u64<NT>((unsigned long long)cnt, sh.warp_b, kept_cnt);
-    unsigned long long all = mine, base = 0ull;
+    const int quarter = ((seg / 4) + 31) & ~31;
+    unsigned long long part[4] = {0ull, 0ull, 0ull, 0ull};
+    uint32_t tie_q[4], tie = tie_at, cnt = 0;
+    auto weight_at = [&](int j, uint32_t& tie_now, bool& kept) -> unsigned long long {     // of token j + lane; counts the ties passed
+        const uint32_t k = j + lane < s1 ? (by_offset ? keys[offs[j + lane]] : src[j + lane]) : 0u;
+        bool in = k > K;
+        if (r_keep > 0) {                                 // uniform
+            const unsigned eq = __ballot_sync(0xffffffffu, k == K);
+            in |= k == K && tie_now + __popc(eq & below) < r_keep;
+            tie_now += __popc(eq);
+        }
+        kept = false;
+        if (!in) return 0ull;
+        double w;
+        const unsigned long long f = wg.fixed(k, w);
+        if (tiny_min_p && w == 0.0) w = wg.exact(k);
+        kept = w >= min_p;
+        return kept ? f : 0ull;
+    };
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        tie_q[q] = tie;
+        for (int j = s0 + q * quarter; j < min(s1, s0 + (q + 1) * quarter); j += 32) {
+            bool kept;
+            part[q] += weight_at(j, tie, kept);
+            cnt += kept;
+        }
+    }
+    unsigned long long sum = part[0] + part[1] + part[2] + part[3];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    cnt = __reduce_add_sync(0xffffffffu, cnt);
+    __syncthreads();
+    if (lane == 0) {
+        sh.warp_a[warp] = sum;
+        sh.warp_n[warp] = cnt;
+    }
+    __syncthreads();
+    unsigned long long all = 0ull, base = 0ull;           // of the row; before this warp
+    uint32_t kept_cnt = __reduce_add_sync(0xffffffffu, lane < kW ? sh.warp_n[lane] : 0u);
+#pragma unroll 4
+    for (int w = 0; w < kW; ++w) {
+        const unsigned long long v = sh.warp_a[w];
+        all += v;
+        base += w < warp ? v : 0ull;
+    }
     if (CL) {
         if (tid == 0) {
-            sh.total = mine;
-            sh.cnt_total = (uint32_t)kept_cnt;
+            sh.total = all;
+            sh.cnt_total = kept_cnt;
         }
         sync_all();
         all = 0ull;
-        kept_cnt = 0ull;
+        kept_cnt = 0u;
         for (int r = 0; r < C; ++r) {
             const unsigned long long t = *peer(&sh.total, r);
             if (r < rank) base += t;
@@ -403,24 +683,24 @@ __global__ void __launch_bounds__(NT) sample_kernel(const SmpParams p)
         }
     }
     const unsigned long long thr = __umul64hi(frac64(p.u[row]), all);  // floor(u W) < W
-    const unsigned long long from = base + before_cta;
-    const bool owner = from <= thr && thr < from + sum;
-    const unsigned own = __ballot_sync(0xffffffffu, owner);
-    if (own != 0u) {
-        // the warp of the thread whose run holds the token walks that run 32 tokens at a time
-        const int src = __ffs(own) - 1, lane = tid & 31;
-        const int a0 = __shfl_sync(0xffffffffu, j0, src), a1 = __shfl_sync(0xffffffffu, j1, src);
-        unsigned long long at = __shfl_sync(0xffffffffu, from, src), tr = __shfl_sync(0xffffffffu, tie_at, src);
-        for (int j = a0; j < a1; j += 32) {
-            const uint32_t k = j + lane < a1 ? keys[j + lane] : 0u;
-            const bool eq = j + lane < a1 && k == K && r_keep > 0;
-            const unsigned eqs = __ballot_sync(0xffffffffu, eq);
-            unsigned long long f = 0ull;
-            if (j + lane < a1 && (k > K || (eq && tr + __popc(eqs & ((1u << lane) - 1u)) < r_keep))) {
-                double w;
-                f = wg.fixed(k, w);
-                if (!(w >= min_p)) f = 0ull;
-            }
+    if (base <= thr && thr < base + sum) {                // the warp whose segment holds the token finds the quarter, then walks it
+        unsigned long long at = base;
+        int j = s0;
+        uint32_t tr = tie_at;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            unsigned long long v = part[q];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (at <= thr && thr >= at + v && q < 3) {
+                at += v;
+                j = s0 + (q + 1) * quarter;
+                tr = tie_q[q + 1];
+            } else break;
+        }
+        for (; j < s1 && at <= thr; j += 32) {
+            bool kept;
+            const unsigned long long f = weight_at(j, tr, kept);
             unsigned long long s = f;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -428,12 +708,11 @@ __global__ void __launch_bounds__(NT) sample_kernel(const SmpParams p)
                 if (lane >= o) s += t;
             }
             if (f > 0ull && at + s > thr && at + s - f <= thr) {
-                p.tokens[row] = i0 + j + lane;
+                p.tokens[row] = src_idx != nullptr ? (int32_t)src_idx[j + lane] : i0 + (by_offset ? (int)offs[j + lane] : j + lane);
                 if (p.probs) p.probs[row] = (float)((double)f / (double)all);
                 if (p.kept) p.kept[row] = (int32_t)kept_cnt;
             }
             at += __shfl_sync(0xffffffffu, s, 31);
-            tr += __popc(eqs);
         }
     }
     if (CL) sync_all();                                   // no CTA leaves while another reads its shared memory
@@ -477,7 +756,9 @@ extern "C" int sample_tokens(stwq_ctx* ctx, const void* logits, int x_dtype, int
     if ((reinterpret_cast<uintptr_t>(logits) & (x_dtype == STWQ_OUT_F32 ? 3u : 1u)) != 0) return STWQ_ERR_ALIGN;
     StwqDevGuard g(ctx->device);
     int C = 1;
-    while ((V + C - 1) / C > kMaxSlice || (C < kMaxCluster && B * C * 2 <= ctx->sm_count && V / C >= 4096)) C *= 2;
+    // slices that leave room for two CTAs per SM, if a cluster of 8 gets there; more CTAs per row while SMs would idle
+    while (C < kMaxCluster && ((V + C - 1) / C > kPairSlice || (B * C * 2 <= ctx->sm_count && V / C >= 4096))) C *= 2;
+    if ((V + C - 1) / C > kMaxSlice) return STWQ_ERR_DIM;
     SmpParams p;
     p.X = logits; p.ld = ld; p.V = V;
     p.chunk = ((V + C - 1) / C + 31) & ~31;
@@ -486,6 +767,6 @@ extern "C" int sample_tokens(stwq_ctx* ctx, const void* logits, int x_dtype, int
     const size_t smem = (size_t)p.chunk * 4;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool bf = x_dtype == STWQ_OUT_BF16;
-    if (C > 1) return bf ? launch_sample<1024, true, __nv_bfloat16>(ctx, p, B, C, smem, st) : launch_sample<1024, true, float>(ctx, p, B, C, smem, st);
-    return bf ? launch_sample<1024, false, __nv_bfloat16>(ctx, p, B, C, smem, st) : launch_sample<1024, false, float>(ctx, p, B, C, smem, st);
+    if (C > 1) return bf ? launch_sample<512, true, __nv_bfloat16>(ctx, p, B, C, smem, st) : launch_sample<512, true, float>(ctx, p, B, C, smem, st);
+    return bf ? launch_sample<512, false, __nv_bfloat16>(ctx, p, B, C, smem, st) : launch_sample<512, false, float>(ctx, p, B, C, smem, st);
 }
