@@ -180,21 +180,28 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
         const int head = mis == 0 ? 0 : min(n, kPer - mis);
         const int nvec = (n - head) / kPer;
         const uint4* vsrc = reinterpret_cast<const uint4*>(src + head);
-        for (int i = tid; i < nvec; i += NT) {
-            const uint4 v = __ldcs(vsrc + i);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            const int at = head + i * kPer;
+        for (int i0v = tid; i0v < nvec; i0v += 4 * NT) {                   // four 16-byte loads in flight per thread
+            uint4 v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (sizeof(XT) == 4) {
-                    const uint32_t a = key_of(__uint_as_float(w[k]));
-                    keys[at + k] = a;
-                    mx = max(mx, a);
-                } else {
-                    const uint32_t a = key_of(__uint_as_float(w[k] << 16)), b = key_of(__uint_as_float(w[k] & 0xffff0000u));
-                    keys[at + 2 * k] = a;
-                    keys[at + 2 * k + 1] = b;
-                    mx = max(mx, max(a, b));
+            for (int q = 0; q < 4; ++q)
+                if (i0v + q * NT < nvec) v[q] = __ldcs(vsrc + i0v + q * NT);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (i0v + q * NT >= nvec) break;
+                const uint32_t w[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+                const int at = head + (i0v + q * NT) * kPer;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (sizeof(XT) == 4) {
+                        const uint32_t a = key_of(__uint_as_float(w[k]));
+                        keys[at + k] = a;
+                        mx = max(mx, a);
+                    } else {
+                        const uint32_t a = key_of(__uint_as_float(w[k] << 16)), b = key_of(__uint_as_float(w[k] & 0xffff0000u));
+                        keys[at + 2 * k] = a;
+                        keys[at + 2 * k + 1] = b;
+                        mx = max(mx, max(a, b));
+                    }
                 }
             }
         }
@@ -251,6 +258,45 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
         }
         __syncthreads();
     };
+    // A thread owns a run of consecutive tokens of the source: odd length, so that no two lanes share a bank. What it picks
+    // from its run it holds as bits, up to kMasks words of them.
+    constexpr int kMasks = 3;
+    static_assert((kMaxSlice / NT | 1) <= 32 * kMasks, "bits for a run");
+    auto pick = [&](const uint32_t* from, int j0, int j1, uint32_t (&m)[kMasks], auto&& pred) {
+#pragma unroll
+        for (int q = 0; q < kMasks; ++q) {
+            m[q] = 0u;
+            const int c = min(32, j1 - j0 - 32 * q);
+#pragma unroll 4
+            for (int t = 0; t < c; ++t) m[q] |= (pred(from[j0 + 32 * q + t]) ? 1u : 0u) << t;
+        }
+    };
+    auto picked = [&](const uint32_t (&m)[kMasks]) -> uint32_t { return __popc(m[0]) + __popc(m[1]) + __popc(m[2]); };
+    auto each = [&](int j0, const uint32_t (&m)[kMasks], auto&& body) {
+#pragma unroll
+        for (int q = 0; q < kMasks; ++q)
+            for (uint32_t x = m[q]; x != 0u; x &= x - 1u) body(j0 + 32 * q + __ffs(x) - 1);
+    };
+    // sum of v over the threads before this one; total: over the CTA
+    auto scan_u32 = [&](uint32_t v, uint32_t& total) -> uint32_t {
+        uint32_t x = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t t = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += t;
+        }
+        __syncthreads();
+        if (lane == 31) sh.warp_n[warp] = x;
+        __syncthreads();
+        const uint32_t w = lane < NT / 32 ? sh.warp_n[lane] : 0u;
+        total = __reduce_add_sync(0xffffffffu, w);
+        return __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u) + x - v;
+    };
+    auto run_of = [&](int ns, int& j0, int& j1) {
+        const int run = ((ns + NT - 1) / NT) | 1;
+        j0 = min(ns, tid * run);
+        j1 = min(ns, j0 + run);
+    };
     // The first coarse bin in which the running sum reaches `target(total)`; sets sel_bin, sel_above, sel_total.
     auto find_coarse = [&](bool mass, auto&& target) {
         __syncthreads();
@@ -303,30 +349,22 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
         // the members, gathered from every CTA of the row into each: from here on no CTA waits for another
         const int cap = src == sh.list_key ? kList : 3 * kList;
         uint32_t* members = src == sh.list_key ? sh.in_key : sh.list_key;
-        auto gather = [&](uint32_t k, bool in, uint32_t& at) {
-            const unsigned ins = __ballot_sync(0xffffffffu, in);
-            if (in && at + __popc(ins & ((1u << lane) - 1u)) < (uint32_t)cap) members[at + __popc(ins & ((1u << lane) - 1u))] = k;
-            at += __popc(ins);
-        };
-        uint32_t kmin = 0xffffffffu, kmax = 0u, mine = 0u;
-        for (int i = tid; i < ns; i += NT) {
-            const uint32_t k = src[i];
-            if (member(k)) {
-                ++mine;
-                kmin = min(kmin, k);
-                kmax = max(kmax, k);
-            }
-        }
-        const uint32_t warp_members = __reduce_add_sync(0xffffffffu, mine);
+        int j0, j1;
+        run_of(ns, j0, j1);
+        uint32_t m[kMasks], kmin = 0xffffffffu, kmax = 0u, n_mine;
+        pick(src, j0, j1, m, member);
+        each(j0, m, [&](int j) {
+            kmin = min(kmin, src[j]);
+            kmax = max(kmax, src[j]);
+        });
+        const uint32_t at0 = scan_u32(picked(m), n_mine);
         kmin = __reduce_min_sync(0xffffffffu, kmin);
         kmax = __reduce_max_sync(0xffffffffu, kmax);
-        uint32_t at = 0u;
-        if (lane == 0 && warp_members > 0u) {
-            at = atomicAdd(&sh.n_in, warp_members);
+        if (lane == 0 && kmax != 0u) {
             atomicMin(&sh.kmin, kmin);
             atomicMax(&sh.kmax, kmax);
         }
-        at = __shfl_sync(0xffffffffu, at, 0);
+        if (tid == 0) sh.n_in = n_mine;
         sync_all();
         uint32_t lo = 0xffffffffu, hi = 0u, n_all = 0u, n_before = 0u;
         for (int r = 0; r < C; ++r) {
@@ -338,12 +376,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
         }
         const bool listed = n_all <= (uint32_t)cap;       // else the members are looked up in the source again, CTA by CTA
         if (listed) {
-            at += n_before;
-            if (warp_members > 0u)
-                for (int i = tid; i - lane < ns; i += NT) {
-                    const uint32_t k = i < ns ? src[i] : 0u;
-                    gather(k, i < ns && member(k), at);
-                }
+            uint32_t at = n_before + at0;
+            each(j0, m, [&](int j) { members[at++] = src[j]; });
             sync_all();
             if (CL) {
                 // CTA r wrote the members from its n_before on; copy the others'
@@ -450,6 +484,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
         r_keep = 1ull;
     } else if (top_k > 1 && top_k < p.V) {
         clear_hist();
+#pragma unroll 4
         for (int i = tid; i < n; i += NT) {
             const uint32_t k = keys[i];
             if (k != 0u) atomicAdd(&sh.hist_lo[distance_bin(k) * 32 + lane], 1u);
@@ -468,75 +503,41 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
             }
         }
     }
-    // Index order: a warp has a contiguous segment of the source and walks it 32 tokens at a time, so ranks are ballots.
-    constexpr int kW = NT / 32;
-    int seg = ((ns + kW - 1) / kW + 31) & ~31;
-    int s0 = min(ns, warp * seg), s1 = min(ns, s0 + seg);
-    // sum over the warps before this one (and the CTAs before this one) of a value that all lanes of a warp hold
-    auto warps_before = [&](uint32_t v) -> uint32_t {
-        __syncthreads();
-        if (lane == 0) sh.warp_n[warp] = v;
-        __syncthreads();
-        uint32_t mine = lane < kW ? sh.warp_n[lane] : 0u, before = 0u;
-        const uint32_t all = __reduce_add_sync(0xffffffffu, mine);
-        before = __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0u);
-        if (CL) {
-            if (tid == 0) sh.cnt_total = all;
-            sync_all();
-            for (int r = 0; r < rank; ++r) before += *peer(&sh.cnt_total, r);
-            sync_all();
+    // bits of the tokens of the thread's run that are kept: above K, and the ties whose rank, in index order, is below r
+    int j0, j1;
+    auto kept_bits = [&](uint32_t (&m)[kMasks]) {
+        run_of(ns, j0, j1);
+        pick(src, j0, j1, m, [&](uint32_t k) { return k > K; });
+        if (r_keep > 0) {                                 // uniform
+            uint32_t e[kMasks], total;
+            pick(src, j0, j1, e, [&](uint32_t k) { return k == K; });
+            unsigned long long rank_at = scan_u32(picked(e), total);
+            if (CL) {
+                if (tid == 0) sh.cnt_total = total;
+                sync_all();
+                for (int r = 0; r < rank; ++r) rank_at += *peer(&sh.cnt_total, r);
+                sync_all();
+            }
+#pragma unroll
+            for (int q = 0; q < kMasks; ++q)
+                for (uint32_t x = e[q]; x != 0u && rank_at < r_keep; x &= x - 1u, ++rank_at) m[q] |= x & (0u - x);
         }
-        return before;
     };
-    // number of tokens before the segment whose key equals K
-    auto ties_before = [&]() -> uint32_t {
-        uint32_t c = 0;
-#pragma unroll 4
-        for (int j = s0 + lane; j < s1; j += 32) c += src[j] == K;
-        return warps_before(__reduce_add_sync(0xffffffffu, c));
-    };
-    const unsigned below = (1u << lane) - 1u;
     if (K != 0u && top_k > 1 && top_k <= kList) {
         // at most kList tokens are left: list them in index order
-        const uint32_t tie0 = r_keep > 0 ? ties_before() : 0u;
-        uint32_t mine = 0, tie = tie0;
-        auto walk = [&](bool write, uint32_t at) {
-            tie = tie0;
-            mine = 0;
-#pragma unroll 4
-            for (int j = s0; j < s1; j += 32) {
-                const uint32_t k = j + lane < s1 ? keys[j + lane] : 0u;
-                bool in = k > K;
-                if (r_keep > 0) {
-                    const unsigned eq = __ballot_sync(0xffffffffu, k == K);              // K > 0
-                    in |= k == K && tie + __popc(eq & below) < r_keep;
-                    tie += __popc(eq);
-                }
-                const unsigned ins = __ballot_sync(0xffffffffu, in);
-                if (write && in) {
-                    const uint32_t to = at + mine + __popc(ins & below);
-                    sh.list_key[to] = k;
-                    sh.list_idx[to] = (uint32_t)(i0 + j + lane);
-                }
-                mine += __popc(ins);
-            }
-        };
-        walk(false, 0u);
-        __syncthreads();
-        if (lane == 0) sh.warp_n[warp] = mine;
-        __syncthreads();
-        const uint32_t v = lane < kW ? sh.warp_n[lane] : 0u;
-        const uint32_t listed = __reduce_add_sync(0xffffffffu, v);
-        walk(true, __reduce_add_sync(0xffffffffu, lane < warp ? v : 0u));
+        uint32_t m[kMasks], listed;
+        kept_bits(m);
+        uint32_t at = scan_u32(picked(m), listed);
+        each(j0, m, [&](int j) {
+            sh.list_key[at] = keys[j];
+            sh.list_idx[at++] = (uint32_t)(i0 + j);
+        });
         __syncthreads();
         src = sh.list_key;
         src_idx = sh.list_idx;
         ns = (int)listed;
         K = 0u;
         r_keep = 0ull;
-        seg = ((ns + kW - 1) / kW + 31) & ~31;
-        s0 = min(ns, warp * seg);
-        s1 = min(ns, s0 + seg);
     }
     if (top_p < 1.0f && top_k != 1) {
         double wd;
@@ -578,62 +579,43 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
         __syncthreads();
     }
 
-    // ---- mass and number of the kept tokens. Over the whole slice the kept ones are listed first (16-bit offsets), so
-    // that the fp64 weights run on full warps.
-    uint32_t tie_at = r_keep > 0 ? ties_before() : 0u;
+    // ---- mass and number of the kept tokens. Over a slice the kept ones are listed first (16-bit offsets), so that the fp64
+    // weights run on full warps; then a warp takes a contiguous segment and a lane sums each quarter of it.
     uint16_t* offs = reinterpret_cast<uint16_t*>(sh.list_key);             // 6 kList of them, behind one another
     bool by_offset = false;
-    if (src == keys && top_k != 1) {
-        __syncthreads();
-        uint32_t mine = 0;
-        auto walk = [&](bool write, uint32_t at) {
-            uint32_t tie = tie_at;
-            mine = 0;
-#pragma unroll 4
-            for (int j = s0; j < s1; j += 32) {
-                const uint32_t k = j + lane < s1 ? keys[j + lane] : 0u;
-                bool in = k > K;
-                if (r_keep > 0) {
-                    const unsigned eq = __ballot_sync(0xffffffffu, k == K);
-                    in |= k == K && tie + __popc(eq & below) < r_keep;
-                    tie += __popc(eq);
-                }
-                const unsigned ins = __ballot_sync(0xffffffffu, in);
-                if (write && in) offs[at + mine + __popc(ins & below)] = (uint16_t)(j + lane);
-                mine += __popc(ins);
-            }
-        };
-        walk(false, 0u);
-        if (lane == 0) sh.warp_n[warp] = mine;
-        __syncthreads();
-        const uint32_t v = lane < kW ? sh.warp_n[lane] : 0u;
-        const uint32_t listed = __reduce_add_sync(0xffffffffu, v);
+    if (src == keys) {
+        uint32_t m[kMasks], listed;
+        kept_bits(m);
+        uint32_t at = scan_u32(picked(m), listed);
         by_offset = listed <= 6 * kList;                  // uniform over the CTA; the slice is shorter than 2^16
         if (by_offset) {
-            walk(true, __reduce_add_sync(0xffffffffu, lane < warp ? v : 0u));
+            each(j0, m, [&](int j) { offs[at++] = (uint16_t)j; });
             ns = (int)listed;
-            K = 0u;
-            r_keep = 0ull;
-            tie_at = 0u;
-            seg = ((ns + kW - 1) / kW + 31) & ~31;
-            s0 = min(ns, warp * seg);
-            s1 = min(ns, s0 + seg);
+        } else {
+            // too many for the list: mark the others in place (their keys are not needed any more)
+            for (int q = 0; q < kMasks; ++q)
+                for (int t = 0; t < 32 && j0 + 32 * q + t < j1; ++t)
+                    if (((m[q] >> t) & 1u) == 0u) keys[j0 + 32 * q + t] = 0u;
         }
         __syncthreads();
+    } else if (K != 0u || r_keep > 0) {
+        uint32_t m[kMasks];
+        kept_bits(m);
+        __syncthreads();
+        for (int q = 0; q < kMasks; ++q)
+            for (int t = 0; t < 32 && j0 + 32 * q + t < j1; ++t)
+                if (((m[q] >> t) & 1u) == 0u) sh.list_key[j0 + 32 * q + t] = 0u;
+        __syncthreads();
     }
-    const int quarter = ((seg / 4) + 31) & ~31;
+    constexpr int kW = NT / 32;
+    const int seg = ((ns + kW - 1) / kW + 31) & ~31, quarter = ((seg / 4) + 31) & ~31;
+    const int s0 = min(ns, warp * seg), s1 = min(ns, s0 + seg);
     unsigned long long part[4] = {0ull, 0ull, 0ull, 0ull};
-    uint32_t tie_q[4], tie = tie_at, cnt = 0;
-    auto weight_at = [&](int j, uint32_t& tie_now, bool& kept) -> unsigned long long {     // of token j + lane; counts the ties passed
+    uint32_t cnt = 0;
+    auto weight_at = [&](int j, bool& kept) -> unsigned long long {        // of token j + lane (key 0: not kept)
         const uint32_t k = j + lane < s1 ? (by_offset ? keys[offs[j + lane]] : src[j + lane]) : 0u;
-        bool in = k > K;
-        if (r_keep > 0) {                                 // uniform
-            const unsigned eq = __ballot_sync(0xffffffffu, k == K);
-            in |= k == K && tie_now + __popc(eq & below) < r_keep;
-            tie_now += __popc(eq);
-        }
         kept = false;
-        if (!in) return 0ull;
+        if (k == 0u) return 0ull;
         double w;
         const unsigned long long f = wg.fixed(k, w);
         if (tiny_min_p && w == 0.0) w = wg.exact(k);
@@ -641,14 +623,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
         return kept ? f : 0ull;
     };
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        tie_q[q] = tie;
+    for (int q = 0; q < 4; ++q)
         for (int j = s0 + q * quarter; j < min(s1, s0 + (q + 1) * quarter); j += 32) {
             bool kept;
-            part[q] += weight_at(j, tie, kept);
+            part[q] += weight_at(j, kept);
             cnt += kept;
         }
-    }
     unsigned long long sum = part[0] + part[1] + part[2] + part[3];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -686,7 +666,6 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
     if (base <= thr && thr < base + sum) {                // the warp whose segment holds the token finds the quarter, then walks it
         unsigned long long at = base;
         int j = s0;
-        uint32_t tr = tie_at;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             unsigned long long v = part[q];
@@ -695,12 +674,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
             if (at <= thr && thr >= at + v && q < 3) {
                 at += v;
                 j = s0 + (q + 1) * quarter;
-                tr = tie_q[q + 1];
             } else break;
         }
         for (; j < s1 && at <= thr; j += 32) {
             bool kept;
-            const unsigned long long f = weight_at(j, tr, kept);
+            const unsigned long long f = weight_at(j, kept);
             unsigned long long s = f;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
