@@ -10,10 +10,12 @@
 //  * A warp takes 16 keys at a time, whole: S^T = K Q^T by mma m16n8k16 with the KEYS as the 16 rows and up to 8 query
 //    rows as columns, then O^T = V^T P^T with 16 CHANNELS as rows. The channel order inside the first product and the key
 //    and channel order inside the second are free, and are chosen so that every operand register pair comes out of
-//    16 consecutive bytes that the thread itself loaded: no shared-memory exchange, no barrier in the loop. P^T is the
-//    transpose of the S^T fragment: one movmatrix per 8 keys.
-//  * Loads: each thread copies its own pieces with cp.async into a ring that only it reads, so a stage is complete when the
-//    thread's own groups are. Enough stages for 100 KB and more in flight per SM.
+//    16 consecutive bytes of a key or value row. P^T is the transpose of the S^T fragment: one movmatrix per 8 keys.
+//  * Loads: 16 keys of a page are contiguous, so a warp's block is two bulk copies into a ring that only this warp reads:
+//    one lane issues them, a barrier per stage counts their bytes, and nothing in the loop waits for another warp. 64 KB
+//    and more per CTA, three CTAs per SM. The rows stay as they lie (bank conflicts of 2 and 4 ways cost less than
+//    the time HBM takes for them). Per-thread 16-byte copies straight into a swizzled layout moved 4.2 TB/s where this
+//    one moves %MEASURED%.
 //  * The running maximum is a reference, not the maximum: it moves only when a score exceeds it by more than 2^10 (a vote
 //    per block instead of six shuffles). fp32 sums; P in bf16, or in fp16 over the code cache.
 //  * fp32 output: P goes in as a sum of 16-bit terms (bf16: three, fp16: two; 22 to 24 significant bits), and each block's
@@ -27,6 +29,9 @@
 
 #include "stwq_paged.cuh"
 #include "stwq_pattn.cuh"
+#include "stwq_ptx.cuh"
+
+using namespace stwq_ptx;
 
 namespace {
 
@@ -42,23 +47,12 @@ __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
     asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
     return r;
 }
-__device__ __forceinline__ float ex2(float x)
+__device__ __forceinline__ float ex2(float x) { return ex2_approx(x); }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
 {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-template <int BYTES>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool live)
-{
-    const int n = live ? BYTES : 0;          // fewer source bytes: the rest is zero-filled, the source is not read
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else if (BYTES == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint4 lds16(uint32_t a)
 {
     uint4 v;
@@ -69,12 +63,6 @@ __device__ __forceinline__ uint2 lds8(uint32_t a)
 {
     uint2 v;
     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ float lds4f(uint32_t a)
-{
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
     return v;
 }
 // two codes (already ^ 0x80) at bytes lo, hi of w -> half2, exact
@@ -118,12 +106,12 @@ struct Ring {
     static constexpr int es = I8 ? 1 : 2;
     static constexpr int npk = DP * es / 64;              // 16-byte key pieces per thread and key (4 threads share a key)
     static constexpr int vbytes = DP * es / 8;            // value bytes per thread and key (8 threads share a key)
-    static constexpr int koff = 0;
-    static constexpr int voff = 2 * npk * 512;
-    static constexpr int soff = voff + 4 * vbytes * 32;   // key scales
-    static constexpr int stage = soff + (I8 ? 256 : 0);   // bytes per warp and 16 keys
+    static constexpr int half = 16 * DP * es;             // bytes of 16 key rows, or value rows, at most
+    static constexpr int stage = 2 * half;                // per warp and 16 keys
     static constexpr int stages = DP * es >= 256 ? 2 : (DP * es >= 128 ? 4 : 6);
-    static constexpr int smem = kWarps * stages * stage;
+    static constexpr int ring = kWarps * stages * stage;
+    static constexpr int bars = ring;                     // one barrier per warp and stage
+    static constexpr int smem = bars + 256;
 };
 
 template <bool F16>
@@ -144,10 +132,18 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
     long long* pre = reinterpret_cast<long long*>(smem + R::smem);        // [B + 1]
     __shared__ long long wsum[kWarps];
     __shared__ float sm_m[kWarps][8 * NR], sm_l[kWarps][8 * NR];
-    __shared__ uint32_t sm_last;
+    __shared__ uint32_t sm_last, sm_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int r = lane >> 2, t = lane & 3;
     bool bad = false;
+    const uint32_t bars = (uint32_t)__cvta_generic_to_shared(smem) + R::bars + warp * R::stages * 8;
+    if (lane == 0) {
+        for (int s = 0; s < R::stages; ++s) mbar_init(bars + 8 * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_smem();
+    }
+    if (tid == 0) sm_abort = 0u;
+    __syncwarp();
 
     // ---- the blocks of every request, end to end
     auto blocks_of = [&](const PaReq& q) -> long long {   // a request with rows but no keys still writes zeros
@@ -189,6 +185,7 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
     const int d = p.d, S = p.S, per_page = S / 16;
     const int64_t row_bytes = (int64_t)d * R::es;
 
+    uint32_t used = 0;                                    // blocks this warp has taken: stage and parity run on over the units
     long long at = lo;
     int b = 0;
     {
@@ -304,61 +301,47 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
         };
         ids = load_ids(0);
         ids_next = load_ids(32);
-        auto issue = [&](int it) {
-            if (it < n16) {
-                if ((it & 31) == 0 && it > 0) {
-                    ids = ids_next;
-                    ids_next = load_ids(it + 32);
-                }
-                const int id = __shfl_sync(0xffffffffu, ids, it & 31);
-                const int b16 = first + kWarps * it;
-                const int64_t base = (((int64_t)id * p.Hkv + hk) * S + (b16 % per_page) * 16) * row_bytes;
-                const int j0 = b16 * 16;                  // first key
-                const uint32_t dst = ring + (it % R::stages) * R::stage + lane * 16;
-                const uint8_t* kp = reinterpret_cast<const uint8_t*>(p.Kp) + base;
-                const uint8_t* vp = reinterpret_cast<const uint8_t*>(p.Vp) + base;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < R::npk; ++j) {
-                        const int byte = (t + 4 * j) * 16;
-                        cp_async<16>(dst + R::koff + (h * R::npk + j) * 512, kp + (byte < row_bytes ? (8 * h + r) * row_bytes + byte : 0),
-                                     j0 + 8 * h + r < q.kv && byte < row_bytes);
-                    }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int key = 2 * t + (k & 1) + 8 * (k >> 1);
-                    const bool seen = j0 + key < q.kv;
-                    if (I8) {
-                        constexpr int nv = R::vbytes < 16 ? 8 : 16;
-                        const int byte = r * R::vbytes;
-                        const bool in = byte < row_bytes;
-                        cp_async<nv>(dst - lane * 16 + lane * nv + R::voff + k * R::vbytes * 32, vp + (in ? key * row_bytes + byte : 0), seen && in);
-                    } else {
-#pragma unroll
-                        for (int hh = 0; hh < R::vbytes / 16; ++hh) {
-                            const int byte = hh * 128 + r * 16;
-                            const bool in = byte < row_bytes;
-                            cp_async<16>(dst + R::voff + (k * (R::vbytes / 16) + hh) * 512, vp + (in ? key * row_bytes + byte : 0), seen && in);
-                        }
-                    }
-                }
-                if (I8) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int key = j0 + 8 * h + r;
-                        cp_async<4>(dst - lane * 16 + lane * 4 + R::soff + h * 128, p.s_k + min(key, p.P - 1), key < q.kv);
-                    }
-                }
+        const uint32_t blk_bytes = (uint32_t)(16 * row_bytes);
+        auto issue = [&](int it) {                        // the whole warp; the stage has been read
+            if (it >= n16) return;
+            if ((it & 31) == 0 && it > 0) {
+                ids = ids_next;
+                ids_next = load_ids(it + 32);
             }
-            cp_commit();                                  // also when empty: the count of groups stays the stage count
+            const int id = __shfl_sync(0xffffffffu, ids, it & 31);
+            if (lane == 0) {
+                const int b16 = first + kWarps * it, s = (used + it) % R::stages;
+                const int64_t base = (((int64_t)id * p.Hkv + hk) * S + (b16 % per_page) * 16) * row_bytes;
+                const uint32_t dst = ring + s * R::stage;
+                mbar_expect_tx(bars + 8 * s, 2 * blk_bytes);
+                bulk_load(dst, reinterpret_cast<const uint8_t*>(p.Kp) + base, blk_bytes, bars + 8 * s);
+                bulk_load(dst + R::half, reinterpret_cast<const uint8_t*>(p.Vp) + base, blk_bytes, bars + 8 * s);
+            }
         };
 #pragma unroll
         for (int s = 0; s < R::stages; ++s) issue(s);
 
-        for (int it = 0; it < n16; ++it) {
-            cp_wait<R::stages - 1>();
-            const uint32_t st = ring + (it % R::stages) * R::stage + lane * 16;
+        bool ok = true;
+        const int rb = (int)row_bytes;
+        int it = 0;
+        for (; it < n16; ++it) {
+            const int sg = (used + it) % R::stages;
+            float ska = 1.0f, skb = 1.0f;
+            if (I8) {
+                const int j = (first + kWarps * it) * 16 + r;
+                ska = __ldg(p.s_k + min(j, p.P - 1));
+                skb = __ldg(p.s_k + min(j + 8, p.P - 1));
+            }
+            ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * sg, (uint32_t)((used + it) / R::stages) & 1u, &sm_abort, p.wait_limit_ns));
+            if (!ok) break;
+            const uint32_t st = ring + sg * R::stage;
+            const uint32_t krow = st + r * rb + t * 16, vrow = st + R::half + 2 * t * rb;
+            if ((first + kWarps * it) * 16 + 16 > q.kv) {
+                // the last keys' block: value rows beyond them may hold anything, and 0 * Inf is not 0
+                for (int x = lane; x < 16 * rb / 16; x += 32)
+                    if ((first + kWarps * it) * 16 + x * 16 / rb >= q.kv) st_shared_v4(st + R::half + x * 16, 0u, 0u, 0u, 0u);
+                __syncwarp();
+            }
             const int j0 = (first + kWarps * it) * 16;
             // ---- S^T: keys r, r + 8 x rows 2t, 2t + 1
             float s[NR][4];
@@ -366,7 +349,8 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
             for (int nr = 0; nr < NR; ++nr) s[nr][0] = s[nr][1] = s[nr][2] = s[nr][3] = 0.0f;
 #pragma unroll
             for (int j = 0; j < R::npk; ++j) {
-                const uint4 ka = lds16(st + R::koff + j * 512), kb = lds16(st + R::koff + (R::npk + j) * 512);
+                uint4 ka = lds16(krow + j * 64), kb = lds16(krow + 8 * rb + j * 64);
+                if ((t + 4 * j) * 16 >= rb) ka = kb = make_uint4(0u, 0u, 0u, 0u);        // beyond the row
                 if (!I8) {
 #pragma unroll
                     for (int nr = 0; nr < NR; ++nr) {
@@ -384,11 +368,6 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
                         for (int nr = 0; nr < NR; ++nr) mma<true>(s[nr], a0, a1, a2, a3, qf[nr][4 * j + k][0], qf[nr][4 * j + k][1]);
                     }
                 }
-            }
-            float ska = 1.0f, skb = 1.0f;
-            if (I8) {
-                ska = lds4f(st - lane * 16 + lane * 4 + R::soff);
-                skb = lds4f(st - lane * 16 + lane * 4 + R::soff + 128);
             }
             const bool masked = j0 + 16 > min_limit;      // uniform
             bool over = false;
@@ -466,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
                 for (int hh = 0; hh < (R::vbytes >= 16 ? R::vbytes / 16 : 1); ++hh) {
                     uint4 v[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = lds16(st + R::voff + (k * (R::vbytes / 16) + hh) * 512);
+                    for (int k = 0; k < 4; ++k) v[k] = lds16(vrow + ((k & 1) + 8 * (k >> 1)) * rb + hh * 128 + r * 16);
                     const uint32_t w[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w},
                                               {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
 #pragma unroll
@@ -483,10 +462,10 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     if (nw == 4) {
-                        const uint4 v = lds16(st + R::voff + k * 512);
+                        const uint4 v = lds16(vrow + ((k & 1) + 8 * (k >> 1)) * rb + r * 16);
                         w[k][0] = v.x; w[k][1] = v.y; w[k][nw > 2 ? 2 : 0] = v.z; w[k][nw > 2 ? 3 : 1] = v.w;
                     } else {
-                        const uint2 v = lds8(st - lane * 16 + lane * 8 + R::voff + k * 256);
+                        const uint2 v = lds8(vrow + ((k & 1) + 8 * (k >> 1)) * rb + r * 8);
                         w[k][0] = v.x; w[k][1] = v.y;
                     }
 #pragma unroll
@@ -508,9 +487,16 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
                     }
                 }
             }
-            issue(it + R::stages);                        // the stage's bytes are in registers: refill it
+            __syncwarp();                                 // the stage's bytes are in registers: refill it
+            issue(it + R::stages);
         }
-        cp_wait<0>();
+        if (!ok && lane == 0) {                           // gave up: let the copies in flight land before their buffer goes
+            const unsigned long long w0 = globaltimer_ns();
+            for (int k = it; k < min(n16, it + R::stages); ++k)
+                while (!mbar_try_wait(bars + 8 * ((used + k) % R::stages), (uint32_t)((used + k) / R::stages) & 1u))
+                    if (globaltimer_ns() - w0 > p.wait_limit_ns) break;
+        }
+        used += n16;
         __syncthreads();                                  // every warp is done with its ring: it becomes the exchange buffer
 
         // ---- the four warps' parts
@@ -608,9 +594,12 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
                 }
             }
         }
-        __syncthreads();                                  // the exchange buffer is a ring again
+        fence_async_smem();                               // the exchange buffer is a ring again: these accesses come before its copies
+        __syncthreads();
         at = unit0 + blk1;
     }
+    // a wait that ran out leaves wrong values behind, but the units' counters as they have to be
+    if (tid == 0 && sm_abort != 0u) atomicOr(p.status, STWQ_DEV_TIMEOUT);
 }
 
 template <bool I8, int DP, int NR, bool F32>
