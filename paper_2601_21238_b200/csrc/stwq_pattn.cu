@@ -57,6 +57,7 @@ int paged_attention(stwq_ctx* ctx, const void* Q, int64_t q_ts, int64_t q_hs, co
         return STWQ_ERR_ALIGN;
     if (q_ts < 0 || q_hs < 0 || !stwq_disjoint(T, Hq, d, o_ts, o_hs)) return STWQ_ERR_DIM;
     if (q_ts % 8 != 0 || q_hs % 8 != 0 || o_ts % e16 != 0 || o_hs % e16 != 0) return STWQ_ERR_ALIGN;
+    if ((int64_t)n_pages * Hkv * (page_size / 16) > 0x7fffffffll) return STWQ_ERR_DIM;    // 16-key blocks of a pool, counted in 32 bits
     const int g = Hq / Hkv;
     if (max_new > T) max_new = (int)T;
     if ((int64_t)max_new * g > 0x3fffff00) return STWQ_ERR_DIM;

@@ -27,6 +27,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "stwq_paged.cuh"
 #include "stwq_pattn.cuh"
 #include "stwq_ptx.cuh"
@@ -108,7 +110,8 @@ struct Ring {
     static constexpr int vbytes = DP * es / 8;            // value bytes per thread and key (8 threads share a key)
     static constexpr int half = 16 * DP * es;             // bytes of 16 key rows, or value rows, at most
     static constexpr int stage = 2 * half;                // per warp and 16 keys
-    static constexpr int stages = DP * es >= 256 ? 2 : (DP * es >= 128 ? 4 : 6);
+    static constexpr int stages = DP * es >= 256 ? 2 : (DP * es >= 128 ? (I8 ? 3 : 4) : 6);
+    static constexpr int ctas(int nr) { return I8 && nr == 1 ? 4 : 3; }   // per SM: codes take more instructions a byte
     static constexpr int ring = kWarps * stages * stage;
     static constexpr int bars = ring;                     // one barrier per warp and stage
     static constexpr int smem = bars + 256;
@@ -122,15 +125,16 @@ __device__ __forceinline__ float2 unpack2(uint32_t w)
 }
 
 template <bool I8, int DP, int NR, bool F32>
-__global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const PaParams p, const int min_blocks)
+__global__ void __launch_bounds__(kThreads, F32 ? 2 : Ring<I8, DP>::ctas(NR)) pattn_few_kernel(const PaParams p, const int min_blocks, const int ex_rows)
 {
     using R = Ring<I8, DP>;
     constexpr int NT = DP / 16;                           // channel tiles of O^T
     constexpr int NK = DP / 16;                           // steps of S^T
     extern __shared__ __align__(16) uint8_t smem[];
-    // after the ring: first block of each request
-    long long* pre = reinterpret_cast<long long*>(smem + R::smem);        // [B + 1]
+    // after the ring: the exchange buffer, then the first block of each request
+    long long* pre = reinterpret_cast<long long*>(smem + R::smem + kWarps * ex_rows * DP * 4);        // [B + 1]
     __shared__ long long wsum[kWarps];
+    __shared__ int wbig[kWarps];
     __shared__ float sm_m[kWarps][8 * NR], sm_l[kWarps][8 * NR];
     __shared__ uint32_t sm_last, sm_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -154,7 +158,15 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
         const int per = (p.B + kThreads - 1) / kThreads;
         const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
         long long sum = 0;
-        for (int b = b0; b < b1; ++b) sum += blocks_of(pa_request(p, b, bad));
+        int big = 0;                                      // blocks of the largest unit
+        for (int b = b0; b < b1; ++b) {
+            const PaReq q = pa_request(p, b, bad);
+            const long long n = blocks_of(q);
+            sum += n;
+            if (n > 0) big = max(big, max(1, (q.kv + kBlk - 1) / kBlk));
+        }
+        big = __reduce_max_sync(0xffffffffu, big);
+        if (lane == 0) wbig[warp] = big;
         long long s = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -175,10 +187,39 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
     if (bad && blockIdx.x == 0) atomicOr(p.status, STWQ_DEV_PAGES);
     const long long N = pre[p.B];
     if (N == 0) return;
-    // ranges of at least min_blocks: a range costs a set-up and, when it splits a unit, a trip through workspace
-    const long long G = max(1ll, min((long long)gridDim.x, (N + min_blocks - 1) / min_blocks));
+    // Ranges of at least min_blocks: a range costs a set-up and, when it splits a unit, a trip through workspace. And so long
+    // that no unit is split over more than kMaxParts of them.
+    long long G = max(1ll, min((long long)gridDim.x, (N + min_blocks - 1) / min_blocks));
+    {
+        int big = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) big = max(big, wbig[w]);
+        G = min(G, max(1ll, (long long)((double)N / (double)big * (kMaxParts - 2))));
+    }
     if (blockIdx.x >= G) return;
-    const long long lo = N * blockIdx.x / G, hi = N * (blockIdx.x + 1) / G;
+    auto share = [&](long long c) -> long long {          // N c / G
+        return N <= (1 << 21) ? (long long)((uint32_t)N * (uint32_t)c / (uint32_t)G) : N * c / G;
+    };
+    auto request_at = [&](long long at) -> int {          // last b with pre[b] <= at
+        int x0 = 0, x1 = p.B;
+        while (x1 - x0 > 1) {
+            const int m = (x0 + x1) >> 1;
+            if (pre[m] <= at) x0 = m;
+            else x1 = m;
+        }
+        return x0;
+    };
+    // A border inside a unit that is small against the ranges moves to the unit's start: no workspace trip for it.
+    auto border = [&](long long at, int& b) -> long long {
+        if (at >= N) return N;
+        b = request_at(at);
+        const int nb = (int)((pre[b + 1] - pre[b]) / p.Hkv);
+        if ((long long)nb * 6 * G > N) return at;
+        const long long in = at - pre[b];
+        return pre[b] + (in < 0x7fffffff ? (long long)((int)in / nb) : in / nb) * nb;
+    };
+    int b = 0, b_end = 0;
+    const long long hi = border(share(blockIdx.x + 1), b_end), lo = border(share(blockIdx.x), b);
     if (lo >= hi) return;
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * R::stages * R::stage;
@@ -186,32 +227,66 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
     const int64_t row_bytes = (int64_t)d * R::es;
 
     uint32_t used = 0;                                    // blocks this warp has taken: stage and parity run on over the units
-    long long at = lo;
-    int b = 0;
-    {
-        int x0 = 0, x1 = p.B;                             // last b with pre[b] <= at
-        while (x1 - x0 > 1) {
-            const int m = (x0 + x1) >> 1;
-            if (pre[m] <= at) x0 = m;
-            else x1 = m;
-        }
-        b = x0;
-    }
-    while (at < hi) {
+    // A segment: the blocks blk0 .. blk1 of the unit (request, key head), and this warp's 16-key blocks first + 4 i of them.
+    struct Seg {
+        PaReq q;
+        int b, hk, nb, blk0, blk1, first, n16;
+        long long unit0;
+    };
+    auto locate = [&](long long at, int b) -> Seg {
+        Seg s;
         while (pre[b + 1] <= at) ++b;
         bool dummy = false;
-        const PaReq q = pa_request(p, b, dummy);
-        const int nb = max(1, (q.kv + kBlk - 1) / kBlk);
-        const int hk = (int)((at - pre[b]) / nb);
-        const long long unit0 = pre[b] + (long long)hk * nb;
-        const int blk0 = (int)(at - unit0);
-        const int blk1 = (int)min((long long)nb, hi - unit0);
-        const int rows = q.n * p.g;
+        s.b = b;
+        s.q = pa_request(p, b, dummy);
+        s.nb = max(1, (s.q.kv + kBlk - 1) / kBlk);
+        const long long in = at - pre[b];
+        s.hk = in < 0x7fffffff ? (int)in / s.nb : (int)(in / s.nb);
+        s.unit0 = pre[b] + (long long)s.hk * s.nb;
+        s.blk0 = (int)(at - s.unit0);
+        s.blk1 = (int)min((long long)s.nb, hi - s.unit0);
+        s.first = s.blk0 * kWarps + warp;
+        const int end16 = min(s.blk1 * kWarps, (s.q.kv + 15) / 16);
+        s.n16 = s.first < end16 ? (end16 - s.first + kWarps - 1) / kWarps : 0;
+        return s;
+    };
+    // where the segment's block it0 + lane lies in the pools, in blocks of 16 keys (at least 256 bytes: fits 32 bits)
+    auto load_ids = [&](const Seg& s, int it0) -> uint32_t {
+        const int it = it0 + lane;
+        if (it >= s.n16) return 0u;
+        const int b16 = s.first + kWarps * it, page = b16 / per_page;
+        int id = __ldg(p.table + (int64_t)s.b * p.W + page);
+        if (id < 0 || id >= p.n_pages) {
+            atomicOr(p.status, STWQ_DEV_PAGES);
+            id = 0;
+        }
+        return ((uint32_t)id * (uint32_t)p.Hkv + (uint32_t)s.hk) * (uint32_t)per_page + (uint32_t)(b16 - page * per_page);
+    };
+    const uint32_t blk_bytes = (uint32_t)(16 * row_bytes);
+    uint32_t ids = 0, ids_next = 0;                       // of the segment being loaded: its blocks 0 .. 31, 32 .. 63, and so on
+    auto issue = [&](const Seg& sg, int it) {             // the whole warp; the stage has been read
+        if (it >= sg.n16) return;
+        if ((it & 31) == 0 && it > 0) {
+            ids = ids_next;
+            ids_next = load_ids(sg, it + 32);
+        }
+        const uint32_t at16 = __shfl_sync(0xffffffffu, ids, it & 31);
+        if (lane == 0) {
+            const int s = (used + it) % R::stages;
+            const uint64_t base = (uint64_t)at16 * blk_bytes;
+            const uint32_t dst = ring + s * R::stage;
+            mbar_expect_tx(bars + 8 * s, 2 * blk_bytes);
+            bulk_load(dst, reinterpret_cast<const uint8_t*>(p.Kp) + base, blk_bytes, bars + 8 * s);
+            bulk_load(dst + R::half, reinterpret_cast<const uint8_t*>(p.Vp) + base, blk_bytes, bars + 8 * s);
+        }
+    };
 
-        // ---- queries: B operand, row r (and r + 8), this thread's channels
-        uint32_t qf[NR][NK][2];
-        float qscale[NR][2];                              // for rows 2t, 2t + 1: softmax scale, log2(e), inverse power of two
-        int limit[NR][2];                                 // visible keys of rows 2t, 2t + 1
+    // ---- queries: B operand, row r (and r + 8), this thread's channels
+    uint32_t qf[NR][NK][2];
+    float qscale[NR][2];                                  // for rows 2t, 2t + 1: softmax scale, log2(e), inverse power of two
+    auto load_q = [&](const Seg& sg) {
+        const PaReq& q = sg.q;
+        const int rows = q.n * p.g, hk = sg.hk;
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             const int row = nr * 8 + r;
@@ -261,12 +336,38 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
                         qf[nr][4 * j + k / 2][k & 1] = pack2<true>(__uint_as_float(raw[j][k] << 16) * up, __uint_as_float(raw[j][k] & 0xffff0000u) * up);
             }
 #pragma unroll
+            for (int e2 = 0; e2 < 2; ++e2) qscale[nr][e2] = p.scale * kPaLog2e * __shfl_sync(0xffffffffu, inv, (2 * t + e2) * 4);
+        }
+    };
+
+    Seg cur = locate(lo, b);
+    ids = load_ids(cur, 0);
+    ids_next = load_ids(cur, 32);
+#pragma unroll
+    for (int s = 0; s < R::stages; ++s) issue(cur, s);
+    load_q(cur);
+    for (;;) {
+        const PaReq q = cur.q;
+        const int hk = cur.hk, nb = cur.nb, blk0 = cur.blk0, blk1 = cur.blk1, first = cur.first, n16 = cur.n16;
+        const long long unit0 = cur.unit0;
+        const int rows = q.n * p.g;
+        // the segment after this one: its page ids are on their way while this one is worked on
+        const bool more = unit0 + blk1 < hi;
+        Seg nxt = cur;
+        uint32_t nxt_ids = 0, nxt_ids2 = 0;
+        if (more) {
+            nxt = locate(unit0 + blk1, cur.b);
+            nxt_ids = load_ids(nxt, 0);
+            nxt_ids2 = load_ids(nxt, 32);
+        }
+        int limit[NR][2];                                 // visible keys of rows 2t, 2t + 1
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
             for (int e2 = 0; e2 < 2; ++e2) {
                 const int rr = nr * 8 + 2 * t + e2;
-                qscale[nr][e2] = p.scale * kPaLog2e * __shfl_sync(0xffffffffu, inv, (2 * t + e2) * 4);
                 limit[nr][e2] = rr >= rows ? 0 : (p.causal ? q.kv - q.n + rr / p.g + 1 : q.kv);
             }
-        }
         const int min_limit = p.causal ? q.kv - q.n + 1 : q.kv;           // the shortest row that exists
 
         float o[NR][NT][4];
@@ -280,46 +381,6 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
             m[nr][0] = m[nr][1] = -INFINITY;
             l[nr][0] = l[nr][1] = 0.0f;
         }
-
-        // ---- the 16-key blocks of this warp: first + 4 i
-        const int first = blk0 * kWarps + warp;
-        const int end16 = min(blk1 * kWarps, (q.kv + 15) / 16);
-        const int n16 = first < end16 ? (end16 - first + kWarps - 1) / kWarps : 0;
-        const int32_t* trow = p.table + (int64_t)b * p.W;
-        int ids = 0, ids_next = 0;                        // page of block it0 + lane, of block it0 + 32 + lane
-        auto load_ids = [&](int it0) -> int {
-            const int it = it0 + lane;
-            int id = 0;
-            if (it < n16) {
-                id = __ldg(trow + (first + kWarps * it) / per_page);
-                if (id < 0 || id >= p.n_pages) {
-                    atomicOr(p.status, STWQ_DEV_PAGES);
-                    id = 0;
-                }
-            }
-            return id;
-        };
-        ids = load_ids(0);
-        ids_next = load_ids(32);
-        const uint32_t blk_bytes = (uint32_t)(16 * row_bytes);
-        auto issue = [&](int it) {                        // the whole warp; the stage has been read
-            if (it >= n16) return;
-            if ((it & 31) == 0 && it > 0) {
-                ids = ids_next;
-                ids_next = load_ids(it + 32);
-            }
-            const int id = __shfl_sync(0xffffffffu, ids, it & 31);
-            if (lane == 0) {
-                const int b16 = first + kWarps * it, s = (used + it) % R::stages;
-                const int64_t base = (((int64_t)id * p.Hkv + hk) * S + (b16 % per_page) * 16) * row_bytes;
-                const uint32_t dst = ring + s * R::stage;
-                mbar_expect_tx(bars + 8 * s, 2 * blk_bytes);
-                bulk_load(dst, reinterpret_cast<const uint8_t*>(p.Kp) + base, blk_bytes, bars + 8 * s);
-                bulk_load(dst + R::half, reinterpret_cast<const uint8_t*>(p.Vp) + base, blk_bytes, bars + 8 * s);
-            }
-        };
-#pragma unroll
-        for (int s = 0; s < R::stages; ++s) issue(s);
 
         bool ok = true;
         const int rb = (int)row_bytes;
@@ -488,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
                 }
             }
             __syncwarp();                                 // the stage's bytes are in registers: refill it
-            issue(it + R::stages);
+            issue(cur, it + R::stages);
         }
         if (!ok && lane == 0) {                           // gave up: let the copies in flight land before their buffer goes
             const unsigned long long w0 = globaltimer_ns();
@@ -497,10 +558,16 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
                     if (globaltimer_ns() - w0 > p.wait_limit_ns) break;
         }
         used += n16;
-        __syncthreads();                                  // every warp is done with its ring: it becomes the exchange buffer
+        if (more) {                                       // the next segment's blocks and queries come in during the exchange
+            ids = nxt_ids;
+            ids_next = nxt_ids2;
+#pragma unroll
+            for (int s = 0; s < R::stages; ++s) issue(nxt, s);
+            load_q(nxt);
+        }
 
         // ---- the four warps' parts
-        float* ex = reinterpret_cast<float*>(smem);       // [kWarps][8 NR][DP]
+        float* ex = reinterpret_cast<float*>(smem + R::smem);             // [kWarps][ex_rows][DP]
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
@@ -515,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
                     sm_l[warp][row] = s;
                 }
                 if (row < rows) {
-                    float* dst = ex + (warp * 8 * NR + row) * DP;
+                    float* dst = ex + (warp * ex_rows + row) * DP;
 #pragma unroll
                     for (int i = 0; i < NT; ++i) {
                         const int ch = I8 ? r * (DP / 8) + 2 * i : (i >> 2) * 64 + r * 8 + (i & 3) * 2;
@@ -550,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float f = M == -INFINITY ? 0.0f : ex2(sm_m[w][row] - M);
-                const float2 v = *reinterpret_cast<const float2*>(ex + (w * 8 * NR + row) * DP + ch);
+                const float2 v = *reinterpret_cast<const float2*>(ex + (w * ex_rows + row) * DP + ch);
                 a = fmaf(f, v.x, a);
                 b2 = fmaf(f, v.y, b2);
                 L = fmaf(f, sm_l[w][row], L);
@@ -564,39 +631,59 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : 3) pattn_few_kernel(const 
         }
         if (!whole) {
             // CTA c owns blocks c N / G .. (c + 1) N / G: the unit's first and last block give its CTAs
-            const long long c0 = ((unit0 + 1) * G - 1) / N, c1 = ((unit0 + nb) * G - 1) / N;
+            auto holder = [&](long long L) -> long long {
+                return N <= (1 << 21) ? (long long)(((uint32_t)(L + 1) * (uint32_t)G - 1u) / (uint32_t)N) : ((L + 1) * G - 1) / N;
+            };
+            const int c0 = (int)holder(unit0), np = (int)holder(unit0 + nb - 1) - c0 + 1;
             __threadfence();
             __syncthreads();
-            uint32_t* cnt = p.counters + ((int64_t)b * p.Hkv + hk);
+            uint32_t* cnt = p.counters + ((int64_t)cur.b * p.Hkv + hk);
             if (tid == 0) {
                 const uint32_t n = atomicAdd(cnt, 1u);
-                sm_last = n == (uint32_t)(c1 - c0) ? 1u : 0u;
+                sm_last = n == (uint32_t)(np - 1) ? 1u : 0u;
                 if (sm_last) *cnt = 0u;                   // zero again for the next call
                 __threadfence();
             }
             __syncthreads();
             if (sm_last) {
-                auto part_of = [&](long long c) { return p.part + (c * 2 + (c == c0 ? 1 : 0)) * slots; };
+                auto part_of = [&](int c) { return p.part + ((int64_t)(c0 + c) * 2 + (c == 0 ? 1 : 0)) * slots; };
+                float2* pm = reinterpret_cast<float2*>(ex);               // [np][rows]: (max, sum), then (factor, sum); np <= kMaxParts
+                static_assert(kMaxParts * 8 <= kWarps * DP * 4, "fits the exchange buffer for any number of rows");
+                for (int x = tid; x < np * rows; x += kThreads) {
+                    const int c = x / rows;
+                    pm[x] = __ldcg(reinterpret_cast<const float2*>(part_of(c) + 8 * NR * DP + 2 * (x - c * rows)));
+                }
+                __syncthreads();
+                if (tid < rows) {
+                    float M = -INFINITY, L = 0.0f;
+                    for (int c = 0; c < np; ++c) M = fmaxf(M, pm[c * rows + tid].x);
+                    for (int c = 0; c < np; ++c) {
+                        const float2 v = pm[c * rows + tid];
+                        const float f = M == -INFINITY ? 0.0f : ex2(v.x - M);
+                        L = fmaf(f, v.y, L);
+                        pm[c * rows + tid].x = f;
+                    }
+                    sm_l[0][tid] = L;
+                }
+                __syncthreads();
                 for (int x = tid; x < rows * (DP / 2); x += kThreads) {
                     const int row = x / (DP / 2), ch = (x - row * (DP / 2)) * 2;
-                    float M = -INFINITY, a = 0.0f, b2 = 0.0f, L = 0.0f;
-                    for (long long c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(part_of(c) + 8 * NR * DP + 2 * row));
-                    for (long long c = c0; c <= c1; ++c) {
-                        const float* src = part_of(c);
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 8 * NR * DP + 2 * row));
-                        const float f = M == -INFINITY ? 0.0f : ex2(ml.x - M);
-                        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + row * DP + ch));
+                    if (ch >= d) continue;
+                    float a = 0.0f, b2 = 0.0f;
+#pragma unroll 8
+                    for (int c = 0; c < np; ++c) {
+                        const float2 v = __ldcg(reinterpret_cast<const float2*>(part_of(c) + row * DP + ch));
+                        const float f = pm[c * rows + row].x;
                         a = fmaf(f, v.x, a);
                         b2 = fmaf(f, v.y, b2);
-                        L = fmaf(f, ml.y, L);
                     }
-                    if (ch < d) write_out(row, ch, a, b2, L);
+                    write_out(row, ch, a, b2, sm_l[0][row]);
                 }
             }
         }
-        fence_async_smem();                               // the exchange buffer is a ring again: these accesses come before its copies
-        __syncthreads();
-        at = unit0 + blk1;
+        if (!more) break;
+        __syncthreads();                                  // the exchange buffer has been read
+        cur = nxt;
     }
     // a wait that ran out leaves wrong values behind, but the units' counters as they have to be
     if (tid == 0 && sm_abort != 0u) atomicOr(p.status, STWQ_DEV_TIMEOUT);
@@ -606,12 +693,13 @@ template <bool I8, int DP, int NR, bool F32>
 int launch_as(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
 {
     auto kern = pattn_few_kernel<I8, DP, NR, F32>;
-    const int smem = Ring<I8, DP>::smem + (p.B + 1) * 8;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem > 48 * 1024 ? 112 * 1024 : 48 * 1024);
+    const int ex_rows = (int)std::min<int64_t>((int64_t)p.max_new * p.g, 8 * NR);
+    const int smem = Ring<I8, DP>::smem + kWarps * ex_rows * DP * 4 + (p.B + 1) * 8;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem > 48 * 1024 ? 140 * 1024 : 48 * 1024);
     if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
-    int64_t grid = (int64_t)ctx->sm_count * 3;
+    int64_t grid = (int64_t)ctx->sm_count * (F32 ? 2 : Ring<I8, DP>::ctas(NR));
     if (grid > (int64_t)p.B * p.Hkv * kMaxParts) grid = (int64_t)p.B * p.Hkv * kMaxParts;
-    kern<<<(unsigned)grid, kThreads, smem, st>>>(p, 2);
+    kern<<<(unsigned)grid, kThreads, smem, st>>>(p, 2, ex_rows);
     ctx->launches += 1;
     e = cudaGetLastError();
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
@@ -629,7 +717,7 @@ size_t stwq_pattn_few_part_bytes(const stwq_ctx* ctx, int B, int Hkv, int d)
 {
     (void)B; (void)Hkv;
     const int DP = d <= 64 ? 64 : 128;
-    return (size_t)ctx->sm_count * 3 * 2 * 16 * (DP + 2) * 4;
+    return (size_t)ctx->sm_count * 4 * 2 * 16 * (DP + 2) * 4;
 }
 
 int stwq_launch_pattn_few(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
