@@ -173,6 +173,14 @@ def check_rows(where, device, name, t, dtypes, shape, inner):
         step *= int(t.shape[-k])
 
 
+def _ok(t, dtype, shape, device):
+    """Whether t is a dense tensor of this type and shape on `device` (the quick form of check_args for one operand)."""
+    try:
+        return t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous()
+    except (AttributeError, TypeError):
+        return False
+
+
 def _kinds(torch):
     return {_F32: torch.float32, _BF16: torch.bfloat16, _I8: torch.int8, _I32: torch.int32}
 
@@ -229,6 +237,7 @@ class Context:
         self._L = load_library()
         self.device = device
         self._kinds = _kinds(torch)
+        self._i32, self._f32 = torch.int32, torch.float32
         self._row_kinds = {d: tuple(self._kinds[x] for x in d) for d in ((_F32,), (_BF16,), (_F32, _BF16))}
         h = C.c_void_p()
         self._check(self._L.stwq_create(C.byref(h), device), "stwq_create")
@@ -364,23 +373,8 @@ class Context:
                                      _p(O), self._stream(stream)), "qattn_pv")
 
     # ---- serving over a paged KV cache
-    def _fast(self, where, *specs):
-        """check_args in a form that costs little when all is well: the step calls of a decode loop are short."""
-        dev, kinds = self.device, self._kinds
-        try:
-            for _, t, dtype, shape, optional in specs:
-                if t is None:
-                    if optional:
-                        continue
-                    break
-                if t.dtype is not kinds[dtype] or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
-                    break
-            else:
-                return
-        except (AttributeError, TypeError):
-            pass
-        check_args(where, dev, *specs)
-
+    # The step calls of a decode loop are short, so their operands are first looked over in a form that costs little
+    # (module function _ok); only when something is off does check_args go through them again and say what.
     def _rows(self, where, name, t, dtypes, shape):
         """check_rows for operands whose last dimension is dense, in the quick form. Returns the strides."""
         try:
@@ -401,27 +395,36 @@ class Context:
 
     def page_plan(self, cached_lens, new_lens, free_pages, page_size, block_table, cu_new, kv_lens, slot_map, pos_ids,
                   pages_used, stream=None):
+        dev, i32 = self.device, self._i32
         B, W = _mk(block_table, "block_table")
-        T, F = int(slot_map.numel()), int(free_pages.numel())
-        self._fast("page_plan", ("cached_lens", cached_lens, _I32, (B,), False), ("new_lens", new_lens, _I32, (B,), False),
-                   ("free_pages", free_pages, _I32, (F,), False), ("block_table", block_table, _I32, (B, W), False),
-                   ("cu_new", cu_new, _I32, (B + 1,), False), ("kv_lens", kv_lens, _I32, (B,), False),
-                   ("slot_map", slot_map, _I32, (T,), False), ("pos_ids", pos_ids, _I32, (T,), False),
-                   ("pages_used", pages_used, _I32, (1,), False))
-        self._check(self._L.page_plan(self._h, cached_lens.data_ptr(), new_lens.data_ptr(), B, free_pages.data_ptr() or None, F,
-                                      page_size, block_table.data_ptr(), W, cu_new.data_ptr(), kv_lens.data_ptr(),
-                                      slot_map.data_ptr(), pos_ids.data_ptr(), T, pages_used.data_ptr(), self._raw_stream(stream)),
-                    "page_plan")
+        T, F = slot_map.numel(), free_pages.numel()
+        if not (_ok(cached_lens, i32, (B,), dev) and _ok(new_lens, i32, (B,), dev) and _ok(free_pages, i32, (F,), dev)
+                and _ok(block_table, i32, (B, W), dev) and _ok(cu_new, i32, (B + 1,), dev) and _ok(kv_lens, i32, (B,), dev)
+                and _ok(slot_map, i32, (T,), dev) and _ok(pos_ids, i32, (T,), dev) and _ok(pages_used, i32, (1,), dev)):
+            self._args("page_plan", ("cached_lens", cached_lens, _I32, (B,), False), ("new_lens", new_lens, _I32, (B,), False),
+                       ("free_pages", free_pages, _I32, (F,), False), ("block_table", block_table, _I32, (B, W), False),
+                       ("cu_new", cu_new, _I32, (B + 1,), False), ("kv_lens", kv_lens, _I32, (B,), False),
+                       ("slot_map", slot_map, _I32, (T,), False), ("pos_ids", pos_ids, _I32, (T,), False),
+                       ("pages_used", pages_used, _I32, (1,), False))
+        rc = self._L.page_plan(self._h, cached_lens.data_ptr(), new_lens.data_ptr(), B, free_pages.data_ptr() or None, F, page_size,
+                               block_table.data_ptr(), W, cu_new.data_ptr(), kv_lens.data_ptr(), slot_map.data_ptr(),
+                               pos_ids.data_ptr(), T, pages_used.data_ptr(), self._raw_stream(stream))
+        if rc:
+            self._check(rc, "page_plan")
 
-    def _head_args(self, where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k, *more):
+    def _head_args(self, where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k):
         """Checks of the operands that qk_norm_rope and kv_append_paged share; returns T, ld, x_dtype, weights' heads, rot, P."""
         ld = self._rows(where, "QKV", QKV, (_F32, _BF16), (None, (Hq + 2 * Hkv) * d))[0]
         T = QKV.shape[0]
         P, rot = (cs.shape if cs is not None and len(cs.shape) == 2 else (s_k.numel() if s_k is not None else 1, 0))
         flat_q, flat_k = w_q is not None and len(w_q.shape) == 1, w_k is not None and len(w_k.shape) == 1
-        self._fast(where, ("pos_ids", pos_ids, _I32, (T,), False), ("w_q", w_q, _F32, (d,) if flat_q else (Hq, d), True),
-                   ("w_k", w_k, _F32, (d,) if flat_k else (Hkv, d), True), ("cs", cs, _F32, (P, rot), True),
-                   ("s_k", s_k, _F32, (P,), True), *more)
+        dev, f32 = self.device, self._f32
+        if not (_ok(pos_ids, self._i32, (T,), dev) and (w_q is None or _ok(w_q, f32, (d,) if flat_q else (Hq, d), dev))
+                and (w_k is None or _ok(w_k, f32, (d,) if flat_k else (Hkv, d), dev)) and (cs is None or _ok(cs, f32, (P, rot), dev))
+                and (s_k is None or _ok(s_k, f32, (P,), dev))):
+            self._args(where, ("pos_ids", pos_ids, _I32, (T,), False), ("w_q", w_q, _F32, (d,) if flat_q else (Hq, d), True),
+                       ("w_k", w_k, _F32, (d,) if flat_k else (Hkv, d), True), ("cs", cs, _F32, (P, rot), True),
+                       ("s_k", s_k, _F32, (P,), True))
         return (T, ld if T > 1 else max(ld, (Hq + 2 * Hkv) * d), OUT_BF16 if QKV.dtype is self._torch.bfloat16 else OUT_F32,
                 0 if w_q is None else 1 if flat_q else Hq, 0 if w_k is None else 1 if flat_k else Hkv, rot, P)
 
@@ -444,7 +447,9 @@ class Context:
             raise StwqError(ERR_DIM, where, "Kp and Vp are [n_pages, Hkv, page_size, d]")
         shape = tuple(Kp.shape)
         i8 = Kp.dtype is self._torch.int8
-        self._fast(where, ("Kp", Kp, _I8 if i8 else _BF16, shape, False), ("Vp", Vp, _I8 if i8 else _BF16, shape, False))
+        kind = self._torch.int8 if i8 else self._torch.bfloat16
+        if not (_ok(Kp, kind, shape, self.device) and _ok(Vp, kind, shape, self.device)):
+            self._args(where, ("Kp", Kp, _I8 if i8 else _BF16, shape, False), ("Vp", Vp, _I8 if i8 else _BF16, shape, False))
         return (*shape, KV_INT8 if i8 else KV_BF16)
 
     def kv_append_paged(self, QKV, pos_ids, slot_map, Hq, Hkv, w_q, w_k, norm, eps, cs, rope, s_k, s_v, bits, Qo, Kp, Vp,
@@ -455,9 +460,9 @@ class Context:
             raise StwqError(ERR_DIM, where, f"the pool has {hk} key heads, the call {Hkv}")
         if kv == KV_INT8 and s_k is None:
             raise StwqError(ERR_NULL, where, "s_k is None")
-        T, ld, x_dtype, nq, nk, rot, P = self._head_args(where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k,
-                                                         ("slot_map", slot_map, _I32, tuple(QKV.shape[:1]), False),
-                                                         ("s_v", s_v, _F32, (Hkv, d), kv == KV_BF16))
+        T, ld, x_dtype, nq, nk, rot, P = self._head_args(where, QKV, pos_ids, Hq, Hkv, d, w_q, w_k, cs, s_k)
+        if not (_ok(slot_map, self._i32, (T,), self.device) and (s_v is None and kv == KV_BF16 or _ok(s_v, self._f32, (Hkv, d), self.device))):
+            self._args(where, ("slot_map", slot_map, _I32, (T,), False), ("s_v", s_v, _F32, (Hkv, d), kv == KV_BF16))
         qs = self._rows(where, "Qo", Qo, (_BF16,), (T, Hq, d))
         self._check(self._L.kv_append_paged(self._h, QKV.data_ptr(), ld, x_dtype, pos_ids.data_ptr(),
                                             slot_map.data_ptr(), T, Hq, Hkv, d, w_q.data_ptr() if nq else None, nq,
@@ -476,9 +481,11 @@ class Context:
         os_ = self._rows(where, "O", O, (_OUT_DTYPES[out_dtype],), (T, Hq, d))
         B, W = _mk(block_table, "block_table")
         P = int(s_k.numel()) if s_k is not None else 1
-        self._fast(where, ("cu_new", cu_new, _I32, (B + 1,), False), ("block_table", block_table, _I32, (B, W), False),
-                   ("kv_lens", kv_lens, _I32, (B,), False), ("s_k", s_k, _F32, (P,), kv == KV_BF16),
-                   ("s_v", s_v, _F32, (Hkv, d), kv == KV_BF16))
+        dev, i32, f32, opt = self.device, self._i32, self._f32, kv == KV_BF16
+        if not (_ok(cu_new, i32, (B + 1,), dev) and _ok(block_table, i32, (B, W), dev) and _ok(kv_lens, i32, (B,), dev)
+                and (s_k is None and opt or _ok(s_k, f32, (P,), dev)) and (s_v is None and opt or _ok(s_v, f32, (Hkv, d), dev))):
+            self._args(where, ("cu_new", cu_new, _I32, (B + 1,), False), ("block_table", block_table, _I32, (B, W), False),
+                       ("kv_lens", kv_lens, _I32, (B,), False), ("s_k", s_k, _F32, (P,), opt), ("s_v", s_v, _F32, (Hkv, d), opt))
         self._check(self._L.paged_attention(self._h, Q.data_ptr(), qs[0], qs[1], cu_new.data_ptr(), T, max_new, B, Hq, Hkv,
                                             d, block_table.data_ptr(), W, kv_lens.data_ptr(), Kp.data_ptr(), Vp.data_ptr(), NP, S, kv,
                                             None if s_k is None else s_k.data_ptr(), P, None if s_v is None else s_v.data_ptr(),
@@ -491,9 +498,13 @@ class Context:
     def sample_tokens(self, logits, temperature, top_k, top_p, min_p, u, tokens, probs=None, kept=None, stream=None):
         ld = self._rows("sample_tokens", "logits", logits, (_F32, _BF16), (None, None))[0]
         B, V = logits.shape
-        self._fast("sample_tokens", ("temperature", temperature, _F32, (B,), True), ("top_k", top_k, _I32, (B,), True),
-                   ("top_p", top_p, _F32, (B,), True), ("min_p", min_p, _F32, (B,), True), ("u", u, _F32, (B,), False),
-                   ("tokens", tokens, _I32, (B,), False), ("probs", probs, _F32, (B,), True), ("kept", kept, _I32, (B,), True))
+        dev, i32, f32, n = self.device, self._i32, self._f32, (B,)
+        if not ((temperature is None or _ok(temperature, f32, n, dev)) and (top_k is None or _ok(top_k, i32, n, dev))
+                and (top_p is None or _ok(top_p, f32, n, dev)) and (min_p is None or _ok(min_p, f32, n, dev)) and _ok(u, f32, n, dev)
+                and _ok(tokens, i32, n, dev) and (probs is None or _ok(probs, f32, n, dev)) and (kept is None or _ok(kept, i32, n, dev))):
+            self._args("sample_tokens", ("temperature", temperature, _F32, n, True), ("top_k", top_k, _I32, n, True),
+                       ("top_p", top_p, _F32, n, True), ("min_p", min_p, _F32, n, True), ("u", u, _F32, n, False),
+                       ("tokens", tokens, _I32, n, False), ("probs", probs, _F32, n, True), ("kept", kept, _I32, n, True))
         q = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         self._check(self._L.sample_tokens(self._h, logits.data_ptr(), OUT_BF16 if logits.dtype is self._torch.bfloat16 else OUT_F32,
                                           max(ld, V) if B == 1 else ld, B, V, q(temperature), q(top_k),
