@@ -787,11 +787,11 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             tc_fence_after();
         }
         auto write16 = [&](int cb, float (&o)[16], float rl_sum) {       // 16 channels of the row
-            const float inv_l = rl_sum > 0.0f ? __fdividef(1.0f, rl_sum) : 0.0f;
+            // no visible key: zeros. The sum of a row that sees any is about 1 or more; masked scores add at most 2^-126 each.
+            const bool none = rl_sum < 5.4e-20f;
+            const float inv_l = __fdividef(1.0f, rl_sum);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                o[k] = rl_sum != 0.0f ? o[k] * inv_l : 0.0f;             // no visible key: zeros
-            }
+            for (int k = 0; k < 16; ++k) o[k] = none ? 0.0f : o[k] * inv_l;
             if (I8) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
