@@ -10,8 +10,9 @@
 //    columns already read and is the A operand of the second product straight from there: no trip through shared memory.
 //  * K and V tiles are gathered page by page by four loader warps with cp.async into the 128-byte-swizzled layouts: K rows as
 //    K-major, V rows as they are (MN-major B operand: no transpose). Codes pass through registers and become fp16.
-//  * The running maximum is a reference that moves only when a row exceeds it by 2^10 (see the few-row kernel): the
-//    rescale of O in tensor memory is rare, and each score is read once.
+//  * The running maximum is a reference that moves only when a row exceeds it by about 2^10 (see the few-row kernel),
+//    which the sum of its exponentials shows: no maximum is taken, the rescale of O in tensor memory is rare, and
+//    each score is read once.
 //  * With fewer units than SMs the keys of a unit are cut into equal ranges; partial (m, l, O) go to workspace and the
 //    last CTA adds them in key order.
 //  * fp32 output: P is kept as a sum of 16-bit terms (bf16: three, fp16: two; 22 to 24 significant bits), all multiplied by V.
@@ -37,7 +38,6 @@ constexpr int kKT = 128;                     // keys per tile
 constexpr int kHalf = 128 * 128;             // bytes of 128 rows of 128 bytes
 constexpr int kMaxStages = 4;
 constexpr int kMaxSplit = 32;
-constexpr float kSlack = 10.0f;
 constexpr int kPolyEvery = 4;                // one pair of exponentials in so many goes through the fma pipe instead of the ex2 unit
 constexpr int kTmemCols = 512, kColS = 0, kColO = 256;
 constexpr int kColMore = 128, kColSum = 384; // fp32 output: further terms of P (64 columns each), the fp32 sum of O
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         free_tmem();
         return;
     }
-    const int unit = blockIdx.x / nS, split = blockIdx.x - unit * nS;
+    const int unit = nS == 1 ? (int)blockIdx.x : (int)blockIdx.x / nS, split = (int)blockIdx.x - unit * nS;
     int b = 0;
     {
         int x0 = 0, x1 = p.B;
@@ -341,7 +341,8 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         free_tmem();
         return;
     }
-    const int t0 = (int)((uint32_t)tiles * (uint32_t)split / (uint32_t)eS), t1 = (int)((uint32_t)tiles * (uint32_t)(split + 1) / (uint32_t)eS);   // tiles < 2^24, eS <= 32
+    const int t0 = eS == 1 ? 0 : (int)((uint32_t)tiles * (uint32_t)split / (uint32_t)eS);               // tiles < 2^24, eS <= 32
+    const int t1 = eS == 1 ? tiles : (int)((uint32_t)tiles * (uint32_t)(split + 1) / (uint32_t)eS);
     const int nt0 = max(0, min(tiles0, t1) - t0), nt1 = max(0, min(tiles1, t1) - t0);
     const int n = max(nt0, nt1);
 
@@ -629,24 +630,28 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 const uint32_t mine = qrow + lane * 128;
                 auto piece = [&](int c) { return mine + (c >> 3) * kHalf + (((c & 7) ^ (lane & 7)) << 4); };
                 float mx = 0.0f;
-                for (int c = 0; c < d / 8; ++c) {
-                    const uint4 v = ld_shared_v4(piece(c));
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                uint4 v[NH * 8];
+#pragma unroll
+                for (int c = 0; c < NH * 8; ++c) v[c] = c < d / 8 ? ld_shared_v4(piece(c)) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int c = 0; c < NH * 8; ++c) {
+                    const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u))));
+                        mx = max3(mx, fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u)));
                 }
                 int e = (int)(__float_as_uint(mx) >> 23) - 127;
                 e = mx > 0.0f && mx < INFINITY ? max(e, -100) : 13;
                 const float up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
                 inv = __uint_as_float((uint32_t)(e - 13 + 127) << 23);
-                for (int c = 0; c < d / 8; ++c) {
-                    const uint4 v = ld_shared_v4(piece(c));
-                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = pack_f16(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xffff0000u) * up);
-                    st_shared_v4(piece(c), w[0], w[1], w[2], w[3]);
-                }
+                for (int c = 0; c < NH * 8; ++c)
+                    if (c < d / 8) {
+                        uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) w[k] = pack_f16(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xffff0000u) * up);
+                        st_shared_v4(piece(c), w[0], w[1], w[2], w[3]);
+                    }
             }
             fence_async_smem();
             __syncwarp();
@@ -657,7 +662,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + kColS + 128 * x + lanes, to = tmem + kColO + 128 * x + lanes;
         const int min_vis = __reduce_min_sync(0xffffffffu, live ? vis : 0x7fffffff);
-        float m = -INFINITY, l = 0.0f;
+        float m = vis > 0 ? -INFINITY : 0.0f, l = 0.0f;   // a row that sees nothing needs no reference: its sum stays next to nothing
         float m_sum = -INFINITY;                          // the reference that the fp32 sum of O stands against
         auto add_up = [&](bool more) {                     // sum = sum 2^(m_sum - m) + O
             const float f = more && m > -INFINITY ? ex2_approx(m_sum - m) : 0.0f;
@@ -730,49 +735,75 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 tmem_ld_wait();
                 scores(qd, 0);
                 scores(qd, 1);
-                const float mx = cc * (F32 ? tile_max : fmaxf(maximum(0), maximum(1)));      // cc > 0
-                if ((!F32 || qd == 0) && __any_sync(0xffffffffu, mx > m + kSlack)) {
-                    // the reference moves: what was summed, written and accumulated so far is scaled down to it
-                    const float mn = fmaxf(m, mx);
-                    const float f = mn == -INFINITY ? 1.0f : ex2_approx(m - mn);
-                    m = mn;
-                    l *= f;
-                    if (!F32) rescale<I8>(to, j > 0 ? d : 0, ts, 2 * qd, f);
-                }
-                const float mm = m == -INFINITY ? 0.0f : m - (I8 ? 4.0f : 0.0f);       // fp16: four octaves up keep small probabilities' bits
-                const uint64_t negm2 = dup_f2(-mm);
+                // The exponentials are taken against the reference as it stands. Only when some row has none yet, or its sum
+                // over these 64 keys shows that a score exceeded it by more than the slack, are the scores read again, the
+                // reference moved to their maximum, and what was summed and written so far scaled down to it.
+                bool move = F32 ? qd == 0 : __any_sync(0xffffffffu, m == -INFINITY);
+                constexpr int kHeld = F32 ? 1 : 2;        // halves kept until the sum is known to be fine
+                uint32_t w[kHeld][kTerms][16];
+                auto store_p = [&](int h) {               // over columns whose scores have been read
+                    tmem_st16(ts + 32 * qd + 16 * h, w[h % kHeld][0]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[kTerms][16];
+                    for (int e = 1; e < kTerms; ++e) tmem_st16(tmem + kColMore + lanes + 64 * (e - 1) + 32 * qd + 16 * h, w[h % kHeld][e]);
+                };
+                float part;
+                for (int pass = 0;; ++pass) {
+                    if (move) {
+                        if (!F32 && pass > 0) {          // the registers hold the next scores already
+                            tmem_ld_wait();
+                            tmem_ld32(ts + 64 * qd, v[0]);
+                            tmem_ld32(ts + 64 * qd + 32, v[1]);
+                            tmem_ld_wait();
+                            scores(qd, 0);
+                            scores(qd, 1);
+                        }
+                        const float mx = cc * (F32 ? tile_max : fmaxf(maximum(0), maximum(1)));            // cc > 0
+                        const float mn = fmaxf(m, mx);
+                        const float f = mn == -INFINITY ? 1.0f : ex2_approx(m - mn);
+                        m = mn;
+                        l *= f;
+                        if (!F32) rescale<I8>(to, j > 0 ? d : 0, ts, 2 * qd, f);
+                    }
+                    const float mm = m == -INFINITY ? 0.0f : m - (I8 ? 4.0f : 0.0f);   // fp16: four octaves up keep small probabilities' bits
+                    const uint64_t negm2 = dup_f2(-mm);
                     uint64_t l2[2] = {0ull, 0ull};        // (0, 0)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const uint64_t e2 = fma_f2(pack_u2(v[h][2 * k], v[h][2 * k + 1]), cc2, negm2);
-                        float a, c;
-                        if (!F32 && k % kPolyEvery == kPolyEvery - 1) unpack_f2(exp2_poly(e2), a, c);
-                        else {
-                            unpack_f2(e2, a, c);
-                            a = ex2_approx(a);
-                            c = ex2_approx(c);
-                        }
-                        l2[k & 1] = add_f2(l2[k & 1], pack_f2(a, c));
+                    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                        for (int e = 0; e < kTerms; ++e) {
-                            w[e][k] = pack_p<I8>(a, c);
-                            if (e + 1 < kTerms) {
-                                const float2 r = unpack_p<I8>(w[e][k]);
-                                a -= r.x;
-                                c -= r.y;
+                        for (int k = 0; k < 16; ++k) {
+                            const uint64_t e2 = fma_f2(pack_u2(v[h][2 * k], v[h][2 * k + 1]), cc2, negm2);
+                            float a, c;
+                            if (!F32 && k % kPolyEvery == kPolyEvery - 1) unpack_f2(exp2_poly(e2), a, c);
+                            else {
+                                unpack_f2(e2, a, c);
+                                a = ex2_approx(a);
+                                c = ex2_approx(c);
+                            }
+                            l2[k & 1] = add_f2(l2[k & 1], pack_f2(a, c));
+#pragma unroll
+                            for (int e = 0; e < kTerms; ++e) {
+                                w[h % kHeld][e][k] = pack_p<I8>(a, c);
+                                if (e + 1 < kTerms) {
+                                    const float2 r = unpack_p<I8>(w[h % kHeld][e][k]);
+                                    a -= r.x;
+                                    c -= r.y;
+                                }
                             }
                         }
+                        if (qd == 0) tmem_ld32(ts + 64 + 32 * h, v[h]);    // the next scores into the registers just used up
+                        if (F32) store_p(h);
                     }
-                    if (qd == 0) tmem_ld32(ts + 64 + 32 * h, v[h]);        // the next scores into the registers just used up
                     float la, lb;
                     unpack_f2(add_f2(l2[0], l2[1]), la, lb);
-                    l += la + lb;
-                    tmem_st16(ts + 32 * qd + 16 * h, w[0]);                // columns whose scores have been read
-#pragma unroll
-                    for (int e = 1; e < kTerms; ++e) tmem_st16(tmem + kColMore + lanes + 64 * (e - 1) + 32 * qd + 16 * h, w[e]);
+                    part = la + lb;
+                    if (F32 || pass > 0) break;
+                    move = __any_sync(0xffffffffu, !(part <= (I8 ? 16.0f : 1.0f) * 1024.0f));
+                    if (!move) break;
+                }
+                l += part;
+                if (!F32) {
+                    store_p(0);
+                    store_p(1);
                 }
             }
             tmem_st_wait();
