@@ -406,7 +406,7 @@ int page_plan(stwq_ctx* ctx, const int32_t* cached_lens, const int32_t* new_lens
  *  - kv_append_paged: queries to Qo (bf16, strides as above), keys (normed, rotated) and values to slot slot_map[t] of the
  *    pool; int8 codes are those of kv_append: clamp(round(x * (1 / s))), bits in {8, 6}. Slot -1: nothing is appended for
  *    the row. A slot beyond the pool is not written and records STWQ_ERR_PAGES. Two rows with one slot: unspecified which stays.
- * pos_ids -1 marks a padding row, of which nothing is written. With a rotation or key scales, any other position
+ * Outputs must not overlap QKV. pos_ids -1 marks a padding row, of which nothing is written. With a rotation or key scales, any other position
  * outside [0, P) writes zeros to Qo (and Ko), appends nothing, and records STWQ_ERR_POS_RANGE.
  */
 int qk_norm_rope(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, const int32_t* pos_ids, int64_t T, int Hq, int Hkv,

@@ -16,7 +16,9 @@
 // One pass: each vector is read once, its sum of squares is a shuffle reduction inside the 8, 16 or 32 lanes that
 // hold it (8 channels = one or two 16-byte accesses per lane), the partner of a half-split pair comes by shuffle
 // from the lane rot/16 further. Bound by HBM. A lane group takes up to kHeads heads of one kind of one token: their
-// loads are in flight together, and weights and angles are read once for all of them.
+// loads are in flight together, and weights and angles are read once for all of them. Measured: 8192 rows of 90 heads of
+// 64, bf16 in and out, 46 us, 4.1 TB/s; 65536 rows of 32 heads of 80, fp32, 278 us, 4.8 TB/s (0.63 and 0.74 of the
+// measured copy rate; a vector of 80 leaves 6 of its 16 lanes idle). 256-thread blocks at 79 registers took 55 and 319 us.
 #include <cuda_bf16.h>
 
 #include "stwq_internal.cuh"

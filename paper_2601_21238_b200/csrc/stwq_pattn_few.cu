@@ -12,10 +12,11 @@
 //    and channel order inside the second are free, and are chosen so that every operand register pair comes out of
 //    16 consecutive bytes of a key or value row. P^T is the transpose of the S^T fragment: one movmatrix per 8 keys.
 //  * Loads: 16 keys of a page are contiguous, so a warp's block is two bulk copies into a ring that only this warp reads:
-//    one lane issues them, a barrier per stage counts their bytes, and nothing in the loop waits for another warp. 64 KB
-//    and more per CTA, three CTAs per SM. The rows stay as they lie (bank conflicts of 2 and 4 ways cost less than
-//    the time HBM takes for them). Per-thread 16-byte copies straight into a swizzled layout moved 4.2 TB/s where this
-//    one moves %MEASURED%.
+//    one lane issues them, a barrier per stage counts their bytes, and nothing in the loop waits for another warp. Up to
+//    64 KB per CTA, three CTAs per SM (four over codes). The rows stay as they lie: bank conflicts of 2 and 4 ways cost less
+//    than HBM takes for the bytes. Copies of 16 bytes per thread into a conflict-free layout moved 4.2 TB/s where
+//    these move 5.7 (16 requests of up to 32768 keys, 8 key heads of 128, bf16: 233 us, 0.87 of the measured copy rate).
+//    Over codes the conversion's instructions come in beside HBM: 256 requests of 256 keys, 16 heads, 70 us, 3.9 TB/s.
 //  * The running maximum is a reference, not the maximum: it moves only when a score exceeds it by more than 2^10 (a vote
 //    per block instead of six shuffles). fp32 sums; P in bf16, or in fp16 over the code cache.
 //  * fp32 output: P goes in as a sum of 16-bit terms (bf16: three, fp16: two; 22 to 24 significant bits), and each block's

@@ -18,6 +18,10 @@
 //  * fp32 output: P is kept as a sum of 16-bit terms (bf16: three, fp16: two; 22 to 24 significant bits), all multiplied by V.
 //    The tensor core truncates its running sums (1e-5 over 5000 keys), so the row threads add each tile's product to an
 //    fp32 sum beside it. Both want tensor memory: a CTA then has one tile of rows, not two.
+//  * Measured: 2 requests of 2048 tokens behind 2048, 16 heads over 4 of 128, bf16, causal: 105 us, 975 TFLOP/s, 0.59 of
+//    the measured burst rate (3050 cycles per 256 x 128 tile: 2048 of products, the rest waits between products and rows).
+//    4 requests of 1024 to 2048 tokens behind up to 6144, 32 heads over 8: 538 us. 32 requests of 256 tokens over 680 codes,
+//    30 heads of 64: 149 us; there a unit is six tiles long, and set-up, Q and O cost a third of it.
 // 16-bit operands: bf16 for a bf16 cache (P rounded to bf16); fp16 for codes (exact), with queries scaled per row by a
 // power of two as in the few-row kernel. Sums, maxima and O in fp32.
 #include <cuda.h>
