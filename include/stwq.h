@@ -428,10 +428,11 @@ int kv_append_paged(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, con
  * multiple of 16, <= 128; page_size a multiple of 16; B <= 4096; scale > 0. Token slots at or beyond L are never read, so
  * stale pages may hold anything; values of visible keys must be finite (a masked key has weight 0, and 0 * Inf is NaN).
  * fp32 scores, softmax and sums; probabilities are rounded to bf16 (bf16 cache) or fp16 (codes) for the second product;
- * codes enter both products exactly. Results do not depend on how the work is split over the GPU's SMs at run time.
+ * codes enter both products exactly. The same call gives the same bits every time (split sums are added in the order of the
+ * keys); how a request's keys are grouped, and with it the last bits, depends on the other requests' lengths.
  * STWQ_ERR_PAGES is recorded for lengths outside the table, the scales' P positions, T or max_new (clamped), and for a
  * needed page id outside [0, n_pages) (page 0 is read instead).
- * Workspace: partial results and arrival counters, at most 20 MB; stwq_reserve_paged_attention sizes it ahead of time.
+ * Workspace: partial results and arrival counters, at most 40 MB; stwq_reserve_paged_attention sizes it ahead of time.
  */
 int paged_attention(stwq_ctx* ctx, const void* Q, int64_t q_ts, int64_t q_hs, const int32_t* cu_new, int64_t T, int max_new, int B,
                     int Hq, int Hkv, int d, const int32_t* block_table, int W, const int32_t* kv_lens, const void* Kp, const void* Vp,

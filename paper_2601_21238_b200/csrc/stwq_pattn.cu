@@ -10,11 +10,10 @@ constexpr int kMaxB = 4096;                  // requests per call (both kernels 
 int ensure(stwq_ctx* ctx, int B, int Hkv, int d, cudaStream_t st)
 {
     const size_t few = stwq_pattn_few_part_bytes(ctx, B, Hkv, d), tiled = stwq_pattn_tiled_part_bytes(ctx, d);
-    int rc = stwq_ensure_ws(ctx, &ctx->ws_pattn, &ctx->ws_pattn_bytes, few > tiled ? few : tiled, st, 0);
+    int rc = stwq_ensure_ws(ctx, &ctx->ws_pattn, &ctx->ws_pattn_bytes, tiled + few, st, 0);        // the two kernels may overlap
     if (rc != STWQ_OK) return rc;
     // arrival counters: zero when allocated, and every call leaves them at zero
-    size_t n = (size_t)B * (size_t)Hkv;
-    if (n < (size_t)ctx->sm_count) n = (size_t)ctx->sm_count;
+    const size_t n = (size_t)ctx->sm_count + (size_t)B * (size_t)Hkv;
     return stwq_ensure_ws(ctx, &ctx->ws_pcnt, &ctx->ws_pcnt_bytes, n * 4, st, n * 4);
 }
 
@@ -78,12 +77,15 @@ int paged_attention(stwq_ctx* ctx, const void* Q, int64_t q_ts, int64_t q_hs, co
     p.wait_limit_ns = (unsigned long long)ctx->wait_limit_ms * 1000000ull;
     p.few_max = kFewRows;
     // requests of up to 16 rows per key head (decoding ones) go to the kernel that streams the cache, the others to the
-    // tiled one; a step that holds both runs both, one after the other
-    if ((int64_t)max_new * g > kFewRows) {
+    // tiled one; a step that may hold both runs both, the second as a programmatic dependent of the first
+    const bool tiled = (int64_t)max_new * g > kFewRows;
+    if (tiled) {
         rc = stwq_launch_pattn_tiled(ctx, p, st);
         if (rc != STWQ_OK || g > kFewRows) return rc;
     }
-    return g > kFewRows ? STWQ_OK : stwq_launch_pattn_few(ctx, p, st);
+    p.part = reinterpret_cast<float*>(static_cast<char*>(ctx->ws_pattn) + stwq_pattn_tiled_part_bytes(ctx, d));
+    p.counters += ctx->sm_count;
+    return stwq_launch_pattn_few(ctx, p, tiled, st);
 }
 
 }  // extern "C"

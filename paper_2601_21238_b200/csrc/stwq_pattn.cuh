@@ -42,7 +42,8 @@ __device__ __forceinline__ PaReq pa_request(const PaParams& p, int b, bool& bad)
 
 constexpr float kPaLog2e = 1.4426950408889634f;
 
-int stwq_launch_pattn_few(stwq_ctx* ctx, const PaParams& p, cudaStream_t st);
+// dependent: launched right behind the tiled kernel of the same call, which it may overlap
+int stwq_launch_pattn_few(stwq_ctx* ctx, const PaParams& p, bool dependent, cudaStream_t st);
 int stwq_launch_pattn_tiled(stwq_ctx* ctx, const PaParams& p, cudaStream_t st);
 // bytes of partial results that the launch of a call of these sizes may need
 size_t stwq_pattn_few_part_bytes(const stwq_ctx* ctx, int B, int Hkv, int d);

@@ -187,7 +187,13 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : Ring<I8, DP>::ctas(NR)) pa
     }
     if (bad && blockIdx.x == 0) atomicOr(p.status, STWQ_DEV_PAGES);
     const long long N = pre[p.B];
-    if (N == 0) return;
+    // Behind the tiled kernel this one is launched as its programmatic dependent and shares nothing with it; it only must
+    // not complete before it, so that what follows in the stream finds both done.
+    auto after_tiled = []() { asm volatile("griddepcontrol.wait;" ::: "memory"); };
+    if (N == 0) {
+        after_tiled();
+        return;
+    }
     // Ranges of at least min_blocks: a range costs a set-up and, when it splits a unit, a trip through workspace. And so long
     // that no unit is split over more than kMaxParts of them.
     long long G = max(1ll, min((long long)gridDim.x, (N + min_blocks - 1) / min_blocks));
@@ -197,7 +203,10 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : Ring<I8, DP>::ctas(NR)) pa
         for (int w = 0; w < kWarps; ++w) big = max(big, wbig[w]);
         G = min(G, max(1ll, (long long)((double)N / (double)big * (kMaxParts - 2))));
     }
-    if (blockIdx.x >= G) return;
+    if (blockIdx.x >= G) {
+        after_tiled();
+        return;
+    }
     auto share = [&](long long c) -> long long {          // N c / G
         return N <= (1 << 21) ? (long long)((uint32_t)N * (uint32_t)c / (uint32_t)G) : N * c / G;
     };
@@ -221,7 +230,10 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : Ring<I8, DP>::ctas(NR)) pa
     };
     int b = 0, b_end = 0;
     const long long hi = border(share(blockIdx.x + 1), b_end), lo = border(share(blockIdx.x), b);
-    if (lo >= hi) return;
+    if (lo >= hi) {
+        after_tiled();
+        return;
+    }
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * R::stages * R::stage;
     const int d = p.d, S = p.S, per_page = S / 16;
@@ -688,10 +700,11 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : Ring<I8, DP>::ctas(NR)) pa
     }
     // a wait that ran out leaves wrong values behind, but the units' counters as they have to be
     if (tid == 0 && sm_abort != 0u) atomicOr(p.status, STWQ_DEV_TIMEOUT);
+    after_tiled();
 }
 
 template <bool I8, int DP, int NR, bool F32>
-int launch_as(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
+int launch_as(stwq_ctx* ctx, const PaParams& p, bool dependent, cudaStream_t st)
 {
     auto kern = pattn_few_kernel<I8, DP, NR, F32>;
     const int ex_rows = (int)std::min<int64_t>((int64_t)p.max_new * p.g, 8 * NR);
@@ -700,16 +713,26 @@ int launch_as(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
     if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
     int64_t grid = (int64_t)ctx->sm_count * (F32 ? 2 : Ring<I8, DP>::ctas(NR));
     if (grid > (int64_t)p.B * p.Hkv * kMaxParts) grid = (int64_t)p.B * p.Hkv * kMaxParts;
-    kern<<<(unsigned)grid, kThreads, smem, st>>>(p, 2, ex_rows);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = dependent ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, kern, p, 2, ex_rows);
     ctx->launches += 1;
-    e = cudaGetLastError();
+    if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
 }
 
 template <bool I8, int DP, int NR>
-int launch(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
+int launch(stwq_ctx* ctx, const PaParams& p, bool dependent, cudaStream_t st)
 {
-    return p.out_bf16 ? launch_as<I8, DP, NR, false>(ctx, p, st) : launch_as<I8, DP, NR, true>(ctx, p, st);
+    return p.out_bf16 ? launch_as<I8, DP, NR, false>(ctx, p, dependent, st) : launch_as<I8, DP, NR, true>(ctx, p, dependent, st);
 }
 
 }  // namespace
@@ -721,14 +744,14 @@ size_t stwq_pattn_few_part_bytes(const stwq_ctx* ctx, int B, int Hkv, int d)
     return (size_t)ctx->sm_count * 4 * 2 * 16 * (DP + 2) * 4;
 }
 
-int stwq_launch_pattn_few(stwq_ctx* ctx, const PaParams& p, cudaStream_t st)
+int stwq_launch_pattn_few(stwq_ctx* ctx, const PaParams& p, bool dependent, cudaStream_t st)
 {
     const bool i8 = p.s_k != nullptr;
     const bool two = (int64_t)p.max_new * p.g > 8;
     if (p.d <= 64) {
-        if (i8) return two ? launch<true, 64, 2>(ctx, p, st) : launch<true, 64, 1>(ctx, p, st);
-        return two ? launch<false, 64, 2>(ctx, p, st) : launch<false, 64, 1>(ctx, p, st);
+        if (i8) return two ? launch<true, 64, 2>(ctx, p, dependent, st) : launch<true, 64, 1>(ctx, p, dependent, st);
+        return two ? launch<false, 64, 2>(ctx, p, dependent, st) : launch<false, 64, 1>(ctx, p, dependent, st);
     }
-    if (i8) return two ? launch<true, 128, 2>(ctx, p, st) : launch<true, 128, 1>(ctx, p, st);
-    return two ? launch<false, 128, 2>(ctx, p, st) : launch<false, 128, 1>(ctx, p, st);
+    if (i8) return two ? launch<true, 128, 2>(ctx, p, dependent, st) : launch<true, 128, 1>(ctx, p, dependent, st);
+    return two ? launch<false, 128, 2>(ctx, p, dependent, st) : launch<false, 128, 1>(ctx, p, dependent, st);
 }

@@ -245,6 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     int* pre = reinterpret_cast<int*>(smem + L::offPre);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;      // warp: uniform
 
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // the few-row kernel of the same call may start where there is room
     // barriers and tensor memory, while the lengths are on their way
     if (tid == 0) {
         for (int x = 0; x < 2; ++x) {
@@ -904,32 +905,47 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                 const float4* p0 = reinterpret_cast<const float4*>(p.part) + (int64_t)unit * nS * part_f4;
                 float M = -INFINITY, Ls = 0.0f;
                 float* fs = reinterpret_cast<float*>(smem + L::offV);    // [eS][256]: the operand tiles are no longer needed
+#pragma unroll 8
                 for (int s = 0; s < eS; ++s) {
                     const float2 v = __ldcg(reinterpret_cast<const float2*>(p0 + s * part_f4 + (DP / 4) * 256) + pr);
                     M = fmaxf(M, v.x);
                 }
+#pragma unroll 8
                 for (int s = 0; s < eS; ++s) {
                     const float2 v = __ldcg(reinterpret_cast<const float2*>(p0 + s * part_f4 + (DP / 4) * 256) + pr);
                     const float f = M == -INFINITY ? 0.0f : ex2_approx(v.x - M);
                     fs[s * 256 + pr] = f;
                     Ls = fmaf(f, v.y, Ls);
                 }
-                for (int cb = 0; cb < d; cb += 16) {
-                    float o[16];
+                // 64 channels at a time: sixteen loads in flight per part (the latency of L2 is what this costs)
+#pragma unroll 1
+                for (int hb = 0; hb < d; hb += 64) {
+                    float o[64];
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) o[k] = 0.0f;
+                    for (int k = 0; k < 64; ++k) o[k] = 0.0f;
+#pragma unroll 1
                     for (int s = 0; s < eS; ++s) {
                         const float f = fs[s * 256 + pr];
+                        const float4* src = p0 + s * part_f4 + (hb / 4) * 256 + pr;
+                        float4 v[16];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float4 v = __ldcg(p0 + s * part_f4 + (cb / 4 + k) * 256 + pr);
-                            o[4 * k] = fmaf(f, v.x, o[4 * k]);
-                            o[4 * k + 1] = fmaf(f, v.y, o[4 * k + 1]);
-                            o[4 * k + 2] = fmaf(f, v.z, o[4 * k + 2]);
-                            o[4 * k + 3] = fmaf(f, v.w, o[4 * k + 3]);
+                        for (int k = 0; k < 16; ++k) v[k] = hb + 4 * k < d ? __ldcg(src + k * 256) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            o[4 * k] = fmaf(f, v[k].x, o[4 * k]);
+                            o[4 * k + 1] = fmaf(f, v[k].y, o[4 * k + 1]);
+                            o[4 * k + 2] = fmaf(f, v[k].z, o[4 * k + 2]);
+                            o[4 * k + 3] = fmaf(f, v[k].w, o[4 * k + 3]);
                         }
                     }
-                    if (live || !F32) write16(cb, o, Ls);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (hb + 16 * c < d && (live || !F32)) {
+                            float o16[16];
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o16[k] = o[16 * c + k];
+                            write16(hb + 16 * c, o16, Ls);
+                        }
                 }
                 store_rows();
             }
