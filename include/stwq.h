@@ -406,8 +406,8 @@ int page_plan(stwq_ctx* ctx, const int32_t* cached_lens, const int32_t* new_lens
  *  - kv_append_paged: queries to Qo (bf16, strides as above), keys (normed, rotated) and values to slot slot_map[t] of the
  *    pool; int8 codes are those of kv_append: clamp(round(x * (1 / s))), bits in {8, 6}. Slot -1: nothing is appended for
  *    the row. A slot beyond the pool is not written and records STWQ_ERR_PAGES. Two rows with one slot: unspecified which stays.
- * Outputs must not overlap QKV. pos_ids -1 marks a padding row, of which nothing is written. With a rotation or key scales, any other position
- * outside [0, P) writes zeros to Qo (and Ko), appends nothing, and records STWQ_ERR_POS_RANGE.
+ * Outputs must not overlap QKV. pos_ids -1 marks a padding row, of which nothing is written. With a rotation or key
+ * scales, any other position outside [0, P) writes zeros to Qo (and Ko), appends nothing, and records STWQ_ERR_POS_RANGE.
  */
 int qk_norm_rope(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, const int32_t* pos_ids, int64_t T, int Hq, int Hkv,
                  int d, const float* w_q, int w_q_heads, const float* w_k, int w_k_heads, int norm, float eps, const float* cs,
@@ -425,8 +425,8 @@ int kv_append_paged(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, con
  * (causal != 0) or all j < L. A row that sees no key gives zeros. Rows of O outside every request are left as they were.
  * Q, O: element (t, h, c) at t * ts + h * hs + c (strides in elements, 16-byte multiples); Q bf16, O out_dtype (fp32 or
  * bf16). max_new: no request of the step has more new tokens (host-side bound, at most T). Hq a multiple of Hkv; d a
- * multiple of 16, <= 128; page_size a multiple of 16; B <= 4096; scale > 0. Token slots at or beyond L are never read, so
- * stale pages may hold anything; values of visible keys must be finite (a masked key has weight 0, and 0 * Inf is NaN).
+ * multiple of 16, <= 128; page_size a multiple of 16; B <= 4096; scale > 0. What slots at or beyond L hold does not
+ * matter (NaN included); the values of a request's keys below L must be finite (a masked key has weight 0, and 0 * Inf is NaN).
  * fp32 scores, softmax and sums; probabilities are rounded to bf16 (bf16 cache) or fp16 (codes) for the second product;
  * codes enter both products exactly. The same call gives the same bits every time (split sums are added in the order of the
  * keys); how a request's keys are grouped, and with it the last bits, depends on the other requests' lengths.

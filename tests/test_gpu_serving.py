@@ -347,3 +347,18 @@ def test_sampling_limits_can_be_left_out_and_repeat_bit_for_bit(gpu):
     for _ in range(5):
         for x, y in zip(a, run_sample(gpu, X, 0.9, 0, 0.93, 0.0, 0.77)):
             np.testing.assert_array_equal(x, y)
+
+
+@pytest.mark.parametrize("V", [16385, 17408, 45000, 128001, 360448])
+def test_sampling_with_limits_that_keep_many(gpu, V):
+    """top-k on both sides of what is compacted, nuclei of nearly everything, few distinct values and one value only."""
+    torch = gpu.torch
+    r = np.random.default_rng(V)
+    rows = (r.standard_normal((4, V)) * 0.5).astype(np.float32)
+    rows[1] = np.round(rows[1] * 4) / 4                        # a handful of values: borders inside long ties
+    rows[2] = -1.5                                             # one value
+    rows[3, : V // 2] = -np.inf
+    X = gpu.T(rows)
+    for k in (2047, 2048, 2049, 9000, V - 1, 0):
+        for p, mp, u in ((1.0, 0.0, 0.999), (0.9995, 0.0, 0.4), (0.5, 0.02, 0.7)):
+            check_sample(gpu, X, [1.0, 0.8, 0.5, 2.0], k, p, mp, u)
