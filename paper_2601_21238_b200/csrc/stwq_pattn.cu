@@ -75,13 +75,18 @@ int paged_attention(stwq_ctx* ctx, const void* Q, int64_t q_ts, int64_t q_hs, co
     p.counters = static_cast<uint32_t*>(ctx->ws_pcnt);
     p.status = ctx->d_status;
     p.wait_limit_ns = (unsigned long long)ctx->wait_limit_ms * 1000000ull;
-    p.few_max = kFewRows;
-    // requests of up to 16 rows per key head (decoding ones) go to the kernel that streams the cache, the others to the
-    // tiled one; a step that may hold both runs both, the second as a programmatic dependent of the first
+    // Requests of up to 16 rows per key head (decoding ones) go to the kernel that streams the cache, the others to the
+    // tiled one; a step that may hold both runs both, the second as a programmatic dependent of the first. Where all units of
+    // the step together cannot outnumber the SMs, the tiled kernel cuts every unit's keys over the idle ones and takes the
+    // decoding requests too (2 requests of up to 20 tokens: 15 against 23 us with both kernels; 4 of up to 8 tokens
+    // behind up to 4000, 4 heads per key head: 29 against 56). With more units than SMs it does not cut keys, and a
+    // long decoding request would wait for one CTA.
     const bool tiled = (int64_t)max_new * g > kFewRows;
+    const bool alone = tiled && (g > kFewRows || (int64_t)Hkv * ((T * g + 127) / 128 + B) <= ctx->sm_count);
+    p.few_max = alone ? 0 : kFewRows;
     if (tiled) {
         rc = stwq_launch_pattn_tiled(ctx, p, st);
-        if (rc != STWQ_OK || g > kFewRows) return rc;
+        if (rc != STWQ_OK || alone) return rc;
     }
     p.part = reinterpret_cast<float*>(static_cast<char*>(ctx->ws_pattn) + stwq_pattn_tiled_part_bytes(ctx, d));
     p.counters += ctx->sm_count;
