@@ -341,7 +341,8 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
     };
     const int tiles0 = (last_limit(0) + kKT - 1) / kKT, tiles1 = kX == 1 ? 0 : (last_limit(1) + kKT - 1) / kKT;
     const int tiles = max(tiles0, tiles1);
-    const int eS = min(nS, max(1, (tiles + 1) / 2));      // ranges of at least two tiles
+    // Ranges of the keys: a tile takes about 3000 cycles, adding up a part about 2000, so their number goes with the root
+    const int eS = min(nS, max(1, (int)sqrtf(1.5f * (float)tiles)));
     if (split >= eS) {
         free_tmem();
         return;
