@@ -150,3 +150,14 @@ def test_many_rows(gpu, case, int8):
         assert gpu.ctx.stwq_device_status() == 0
         check(gpu, s, causal, bf16, O)
         assert gpu.torch.equal(O, call(gpu, s, causal, bf16))
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_ranges_end_anywhere_in_a_unit(gpu, seed):
+    """Lengths of every remainder, so that the ranges of blocks that the CTAs take end at, near and far from the units' ends;
+    called twice, since the units' counters have to be back at zero."""
+    r = np.random.default_rng(900 + seed)
+    B = (3, 8, 8, 20, 40, 70)[seed]
+    s = make(gpu, r.integers(1, 3, B), r.integers(0, (3000, 1024, 300, 700, 400, 200)[seed], B), 4, 4 if seed % 2 else 2, 64, 16, seed == 4, 70 + seed, pad=1)
+    for _ in range(2):
+        check(gpu, s, True, True, call(gpu, s, True, True))
