@@ -37,7 +37,11 @@ int stwq_ensure_ws(stwq_ctx* ctx, void** buf, size_t* have, size_t bytes, cudaSt
     }
     void* p = nullptr;
     cudaError_t e = cudaMalloc(&p, bytes);
-    if (e == cudaSuccess && zero_prefix > 0) e = cudaMemset(p, 0, zero_prefix);
+    if (e == cudaSuccess && zero_prefix > 0) {
+        // waited for: a later call may come on a stream that is not ordered behind this one
+        e = cudaMemsetAsync(p, 0, zero_prefix, st);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
     if (e != cudaSuccess) {
         ctx->last_cuda_error = (int)e;
         (void)cudaGetLastError();
@@ -143,6 +147,7 @@ int stwq_create(stwq_ctx** out, int device)
     DeviceGuard g(device);
     cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&ctx->d_status), 256);
     if (e == cudaSuccess) e = cudaMemset(ctx->d_status, 0, 256);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);             // before any stream's kernels report into it
     if (e != cudaSuccess) {
         delete ctx;
         return STWQ_ERR_CUDA;

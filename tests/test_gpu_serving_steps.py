@@ -328,3 +328,32 @@ def test_the_c_boundary_refuses_bad_sizes_and_writes_nothing(gpu):
     assert L.stwq_reserve_paged_attention(h, 0, 2, 1, 64) == DIM and L.stwq_reserve_paged_attention(h, 2, 2, 1, 40) == ALIGN
     torch.cuda.synchronize()
     assert (out == 3.0).all() and gpu.ctx.stwq_device_status() == 0
+
+
+def test_first_call_of_a_context_beside_a_busy_default_stream(gpu):
+    """The workspace of a fresh context, reserved from the host and used on a stream that is not ordered behind the default
+    one: its counters have to be zero by then, whatever the memory held and however busy the default stream is."""
+    torch, pk = gpu.torch, gpu.pk
+    s = make(gpu, [1] * 9, list(range(0, 1800, 200)), 8, 2, 128, 16, False, 3)
+    want = call(gpu, s, True, True)
+    args = [s["Q"], gpu.T(s["cu"]), 1, gpu.T(s["table"]), gpu.T(s["kv"]), s["Kp"], s["Vp"], None, None, float(s["scale"]), True, pk.OUT_BF16]
+    side = torch.cuda.Stream()
+    for reserve in (True, False):
+        ctx = pk.Context(0)
+        try:
+            O = torch.zeros_like(want)
+            dirty = [torch.full((1 << 18,), 3, dtype=torch.int32, device=gpu.dev) for _ in range(32)]
+            torch.cuda.synchronize()
+            del dirty
+            torch.cuda.empty_cache()
+            torch.cuda._sleep(50_000_000)                           # the default stream is busy for some 30 ms
+            if reserve:
+                ctx.stwq_reserve_paged_attention(9, 8, 2, 128)
+            for _ in range(2):
+                ctx.paged_attention(*args, O, stream=side)
+                side.synchronize()
+                assert torch.equal(O, want)
+            torch.cuda.synchronize()
+            assert ctx.stwq_device_status() == 0
+        finally:
+            ctx.close()
