@@ -384,7 +384,8 @@ enum { STWQ_ROPE_HALF = 0, STWQ_ROPE_PAIRS = 1 };
  *  - cu_new [B+1], kv_lens [B] (cached + new), slot_map [T], pos_ids [T] out: where token t of the packed step goes, and
  *    its position in its request. T is the capacity of the two lists: entries behind the last token become -1.
  *  - pages_used [1] out: how many entries of free_pages were taken.
- * B <= 4096, W * page_size < 2^31. STWQ_ERR_PAGES is recorded, and the outputs stay consistent, when a length is
+ * B <= 4096, W * page_size < 2^31. An output that overlaps an input is refused (STWQ_ERR_ALIGN): kv_lens cannot replace
+ * cached_lens in place. STWQ_ERR_PAGES is recorded, and the outputs stay consistent, when a length is
  * negative (taken as 0) or longer than a row of the table, when T or free_pages is too small (tokens beyond T are
  * dropped, cu_new ends at T; tokens without a page get slot -1, kv_lens counts those that have one), or when a needed
  * entry is a negative page id. Slots do not check ids against a pool size (kv_append_paged does).
@@ -424,7 +425,7 @@ int kv_append_paged(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, con
  * For request b with n = cu_new[b+1] - cu_new[b] new tokens and L = kv_lens[b] keys, its token i sees keys j < L - n + i + 1
  * (causal != 0) or all j < L. A row that sees no key gives zeros. Rows of O outside every request are left as they were.
  * Q, O: element (t, h, c) at t * ts + h * hs + c (strides in elements, 16-byte multiples); Q bf16, O out_dtype (fp32 or
- * bf16). max_new: no request of the step has more new tokens (host-side bound, at most T). Hq a multiple of Hkv; d a
+ * bf16); O must not overlap Q or the pools. max_new: no request of the step has more new tokens (host-side bound, at most T). Hq a multiple of Hkv; d a
  * multiple of 16, <= 128; page_size a multiple of 16; B <= 4096; scale > 0. What slots at or beyond L hold does not
  * matter (NaN included); the values of a request's keys below L must be finite (a masked key has weight 0, and 0 * Inf is NaN).
  * fp32 scores, softmax and sums; probabilities are rounded to bf16 (bf16 cache) or fp16 (codes) for the second product;

@@ -477,6 +477,12 @@ int page_plan(stwq_ctx* ctx, const int32_t* cached_lens, const int32_t* new_lens
     if (!free_pages && n_free > 0) return STWQ_ERR_NULL;
     if (B <= 0 || B > kPlanMaxB || n_free < 0 || W <= 0 || page_size <= 0 || T <= 0 || T > 0x7fffffff) return STWQ_ERR_DIM;
     if ((int64_t)W * page_size > 0x7fffffff) return STWQ_ERR_DIM;
+    // every block reads the inputs for itself, while the first already writes the lists: not in place
+    const struct { const int32_t* at; int64_t n; } in[] = {{cached_lens, B}, {new_lens, B}, {free_pages, n_free}},
+        out[] = {{block_table, (int64_t)B * W}, {cu_new, B + 1}, {kv_lens, B}, {slot_map, T}, {pos_ids, T}, {pages_used, 1}};
+    for (const auto& a : in)
+        for (const auto& b : out)
+            if (a.n > 0 && a.at < b.at + b.n && b.at < a.at + a.n) return STWQ_ERR_ALIGN;
     StwqDevGuard g(ctx->device);
     PlanParams p;
     p.cached = cached_lens; p.fresh = new_lens; p.free_pages = free_pages;

@@ -357,3 +357,20 @@ def test_first_call_of_a_context_beside_a_busy_default_stream(gpu):
             assert ctx.stwq_device_status() == 0
         finally:
             ctx.close()
+
+
+def test_a_plan_in_place_is_refused(gpu):
+    torch, pk = gpu.torch, gpu.pk
+    z = lambda *n: torch.zeros(n, dtype=torch.int32, device=gpu.dev)  # noqa: E731
+    cached, new, pages = z(4), z(4) + 2, torch.arange(12, dtype=torch.int32, device=gpu.dev)
+    outs = dict(block_table=z(4, 3), cu_new=z(5), kv_lens=z(4), slot_map=z(8), pos_ids=z(8), pages_used=z(1))
+    for name, alias in (("kv_lens", cached), ("kv_lens", new), ("slot_map", pages[4:]), ("pages_used", new[3:]), ("block_table", pages.view(4, 3))):
+        with pytest.raises(pk.StwqError) as e:
+            gpu.ctx.page_plan(cached, new, pages, 16, **{**outs, name: alias})
+        assert e.value.code == pk.binding.ERR_ALIGN, name
+    # neighbours, and an empty list that begins inside an output, do not overlap
+    both = z(8)
+    gpu.ctx.page_plan(both[:4], new, pages, 16, **{**outs, "kv_lens": both[4:]})
+    assert both.tolist() == [0] * 4 + [2] * 4 and outs["slot_map"].tolist() == [0, 1, 16, 17, 32, 33, 48, 49]
+    gpu.ctx.page_plan(cached, z(4), outs["slot_map"][3:3], 16, **outs)
+    assert outs["pages_used"].item() == 0 and outs["slot_map"].tolist() == [-1] * 8 and gpu.ctx.stwq_device_status() == 0
