@@ -192,6 +192,7 @@ template <bool I8>
 __device__ __noinline__ void rescale(uint32_t to, int d, uint32_t tp, int blocks, float f)
 {
     uint32_t w[16];
+    tmem_st_wait();                                       // the blocks of P were stored without a wait, and are read back here
 #pragma unroll 1
     for (int cb = 0; cb < d; cb += 16) {
         tmem_ld16(to + cb, w);

@@ -1,0 +1,103 @@
+"""paged_attention on scores that are far from flat: keys that exceed everything before them, by little and by much, so that
+the running reference of the softmax has to move in every place where it can; against softmax attention in 64 bits."""
+import numpy as np
+import pytest
+
+from test_gpu_paged_attention import call, d_units, make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+
+    import paper_2601_21238_b200 as pk
+    from paper_2601_21238_b200 import build as pkbuild
+    pkbuild.build()
+    ctx = pk.Context(0)
+
+    class G:
+        pass
+    g = G()
+    g.torch, g.ctx, g.pk, g.dev = torch, ctx, pk, torch.device("cuda:0")
+    g.T = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(g.dev)
+    yield g
+    ctx.close()
+
+
+def peaked(gpu, new, cached, Hq, Hkv, d, S, int8, seed, jumps, factors=(1.0, 1.0, 1.0, 0.5, 0.0, -1.0), pad=0):
+    """The step of make() with channel 0 taken for the peaks: key j of every request scores jumps[j] (in nats, on top of the
+    other channels' noise for a bf16 cache, alone for codes) times the row's factor, and every other key has a zero there."""
+    torch = gpu.torch
+    r = np.random.default_rng(seed + 1)
+    s = make(gpu, new, cached, Hq, Hkv, d, S, int8, seed, pad=pad)
+    s["Q"][:, :, 0] = gpu.T((8 * r.choice(factors, (s["T"], Hq))).astype(np.float32)).to(torch.bfloat16)
+    for b in range(len(s["new"])):
+        at = np.arange(s["kv"][b])
+        page, off = gpu.T(s["table"][b, at // S].astype(np.int64)), gpu.T(at % S)
+        s["Kp"][page, :, off, 0] = 0
+        for j, nats in jumps.items():
+            if j >= len(at):
+                continue
+            if int8:
+                s["Kp"][page[j], :, off[j]] = 0
+                s["Kp"][page[j], :, off[j], 0] = 127
+                s["s_k"][j] = nats / (127 * 8 * s["scale"])
+            else:
+                s["Kp"][page[j], :, off[j], 0] = nats / (8 * s["scale"])
+    s["K"] = s["Kp"].float().cpu().numpy().astype(np.float64)
+    return s
+
+
+def compare(gpu, s, causal, bf16, O):
+    """Within the roundings of the kernels: P goes to 16 bits (bf16 2^-8; fp16 2^-11, and 2^-25 absolute beside a sum of 16 or
+    more) and once more when a reference moves behind it; fp32 output keeps 22 bits of it. A score is off by d + 8 roundings of
+    its terms' magnitude, which enters numerator and sum; an exponential by 2^-20, or 7.5e-5 where the cubic takes it (16-bit
+    output). Sums over L keys and a rescale per move in fp32. The store."""
+    q64 = s["Q"].float().cpu().numpy().astype(np.float64)
+    got = O.float().cpu().numpy().astype(np.float64)
+    S, g, int8 = s["S"], s["Hq"] // s["Hkv"], s["s_k"] is not None
+    p_err = (2 * 2.0 ** -11 if int8 else 2 * 2.0 ** -8) + 2 * 7.5e-5 if bf16 else 2.0 ** -21
+    for b in range(len(s["new"])):
+        n, L, t0 = int(s["new"][b]), int(s["kv"][b]), int(s["cu"][b])
+        j = np.arange(L)
+        for h in range(s["Hkv"] if n else 0):
+            k, v = s["K"][s["table"][b, j // S], h, j % S], s["V"][s["table"][b, j // S], h, j % S]
+            if int8:
+                k, v = k * s["s_k"][:L, None].astype(np.float64), v * s["s_v"][h].astype(np.float64)
+            q = q64[t0:t0 + n, h * g:(h + 1) * g]
+            x = np.einsum("ngd,ld->ngl", q, k) * s["scale"]
+            a = np.einsum("ngd,ld->ngl", np.abs(q), np.abs(k)).max() * s["scale"]
+            seen = j[None] < (L - n + np.arange(n)[:, None] + 1 if causal else np.full((n, 1), L))
+            assert seen.any(-1).all()
+            x = np.where(seen[:, None], x, -np.inf)
+            p = np.exp(x - x.max(-1, keepdims=True))
+            p /= p.sum(-1, keepdims=True)
+            want, mag = np.einsum("ngl,ld->ngd", p, v), np.einsum("ngl,ld->ngd", p, np.abs(v))
+            tol = mag * (p_err + np.expm1(2 * (d_units(s["d"]) * a + 2.0 ** -20)) + (L + 32) * 2.0 ** -23)
+            if int8:
+                tol += 2 * L * 2.0 ** -25 * np.abs(v).max()
+            tol += (2.0 ** -8 if bf16 else 2.0 ** -24) * (np.abs(want) + tol)
+            err = np.abs(got[t0:t0 + n, h * g:(h + 1) * g] - want)
+            assert (err <= tol + 1e-30).all(), (b, h, float(np.nanmax(err / (tol + 1e-30))), np.argwhere(~(err <= tol + 1e-30))[:4].tolist())
+    assert (got[int(s["cu"][-1]):] == 7.0).all()
+
+
+# new, cached, Hq, Hkv, d, S: one unit whose keys are cut over many CTAs, units that fill the SMs (their keys are not cut), odd sizes
+TILED = [([40], [390], 1, 1, 64, 16), ([24], [400], 80, 80, 64, 16), ([20, 33], [420, 387], 80, 40, 128, 64), ([150, 2], [300, 431], 6, 3, 80, 16),
+         ([300], [140], 4, 4, 48, 32), ([3], [430], 20, 1, 128, 16), ([1] * 30 + [120], [400] * 30 + [330], 8, 2, 128, 16), ([2, 12], [420, 430], 4, 2, 64, 16)]
+# the reference moves in the first keys' second half, in either half of later tiles, and twice within one; each by less than 80 nats
+STEPS = {3: 5.0, 70: 18.0, 100: 36.0, 135: 70.0, 195: 130.0, 200: 150.0, 330: 215.0, 400: 223.0}
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("case", range(len(TILED)))
+def test_reference_moves_in_the_tiles(gpu, case, int8):
+    new, cached, Hq, Hkv, d, S = TILED[case]
+    s = peaked(gpu, new, cached, Hq, Hkv, d, S, int8, 300 + case, STEPS, pad=case % 3)
+    for causal, bf16 in ((True, True), (False, True), (True, False)):
+        O = call(gpu, s, causal, bf16)
+        assert gpu.ctx.stwq_device_status() == 0
+        compare(gpu, s, causal, bf16, O)
+        assert gpu.torch.equal(O, call(gpu, s, causal, bf16))
