@@ -11,8 +11,8 @@
 //  * K and V tiles are gathered page by page by four loader warps with cp.async into the 128-byte-swizzled layouts: K rows as
 //    K-major, V rows as they are (MN-major B operand: no transpose). Codes pass through registers and become fp16.
 //  * The running maximum is a reference that moves only when a row exceeds it by about 2^10 (see the few-row kernel),
-//    which the sum of its exponentials shows: no maximum is taken, the rescale of O in tensor memory is rare, and
-//    each score is read once.
+//    which the sum of its exponentials shows (and a maximum over the quarter that the cubic takes): the rescale of O in tensor
+//    memory is rare, and each score is read once.
 //  * With fewer units than SMs the keys of a unit are cut into equal ranges; partial (m, l, O) go to workspace and the
 //    last CTA adds them in key order.
 //  * fp32 output: P is kept as a sum of 16-bit terms (bf16: three, fp16: two; 22 to 24 significant bits), all multiplied by V.
@@ -142,7 +142,8 @@ __device__ __forceinline__ void unpack_u2(uint64_t v, uint32_t& lo, uint32_t& hi
     hi = __float_as_uint(b);
 }
 // 2^x on a pair without the ex2 unit: x = n + r with |r| <= 1/2 (adding 1.5 2^23 rounds to the integer), a cubic for 2^r
-// (least maximum relative error, 7.5e-5: a quarter of fp16's half step), n added to the exponent. x is cut at -126.
+// (least maximum relative error, 7.5e-5: a quarter of fp16's half step), n added to the exponent. x is cut at -126; from 128 on
+// the exponent runs over into the sign, so the caller has to look at x as well as at the result.
 __device__ __forceinline__ uint64_t exp2_poly(uint64_t x2)
 {
     float x0, x1;
@@ -774,15 +775,18 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     const float mm = m == -INFINITY ? 0.0f : m - (I8 ? 4.0f : 0.0f);   // fp16: four octaves up keep small probabilities' bits
                     const uint64_t negm2 = dup_f2(-mm);
                     uint64_t l2[2] = {0ull, 0ull};        // (0, 0)
+                    float hi = -INFINITY;                 // the largest argument of the cubic, whose result means nothing from 2^128 on
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
                             const uint64_t e2 = fma_f2(pack_u2(v[h][2 * k], v[h][2 * k + 1]), cc2, negm2);
                             float a, c;
-                            if (!F32 && k % kPolyEvery == kPolyEvery - 1) unpack_f2(exp2_poly(e2), a, c);
-                            else {
-                                unpack_f2(e2, a, c);
+                            unpack_f2(e2, a, c);
+                            if (!F32 && k % kPolyEvery == kPolyEvery - 1) {
+                                hi = max3(hi, a, c);
+                                unpack_f2(exp2_poly(e2), a, c);
+                            } else {
                                 a = ex2_approx(a);
                                 c = ex2_approx(c);
                             }
@@ -804,7 +808,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     unpack_f2(add_f2(l2[0], l2[1]), la, lb);
                     part = la + lb;
                     if (F32 || pass > 0) break;
-                    move = __any_sync(0xffffffffu, !(part <= (I8 ? 16.0f : 1.0f) * 1024.0f));
+                    move = __any_sync(0xffffffffu, !(part <= (I8 ? 16.0f : 1.0f) * 1024.0f) || hi > (I8 ? 14.0f : 10.0f));
                     if (!move) break;
                 }
                 l += part;

@@ -101,3 +101,16 @@ def test_reference_moves_in_the_tiles(gpu, case, int8):
         assert gpu.ctx.stwq_device_status() == 0
         compare(gpu, s, causal, bf16, O)
         assert gpu.torch.equal(O, call(gpu, s, causal, bf16))
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("nats", [92.0, 140.0, 200.0, 280.0])
+@pytest.mark.parametrize("shape", [([40], [390], 2, 2, 64, 16), ([20], [410], 80, 80, 64, 16), ([130], [300], 1, 1, 128, 32)])
+def test_a_key_far_above_all_before_it(gpu, shape, nats, int8):
+    """One key 133 to 404 octaves above the reference that the row's first keys set, in every column of eight."""
+    new, cached, Hq, Hkv, d, S = shape
+    for c in range(8):
+        s = peaked(gpu, new, cached, Hq, Hkv, d, S, int8, 400 + c, {(72, 136, 200, 328)[(c + c // 4) % 4] + c: nats}, pad=1)
+        O = call(gpu, s, True, True)
+        assert gpu.ctx.stwq_device_status() == 0
+        compare(gpu, s, True, True, O)
