@@ -428,6 +428,7 @@ int kv_append_paged(stwq_ctx* ctx, const void* QKV, int64_t ld, int x_dtype, con
  * bf16); O must not overlap Q or the pools. max_new: no request of the step has more new tokens (host-side bound, at most T). Hq a multiple of Hkv; d a
  * multiple of 16, <= 128; page_size a multiple of 16; B <= 4096; scale > 0. What slots at or beyond L hold does not
  * matter (NaN included); the values of a request's keys below L must be finite (a masked key has weight 0, and 0 * Inf is NaN).
+ * A visible score that is NaN or +Inf makes the row NaN, and so do visible scores that are all -Inf; masked ones do not matter.
  * fp32 scores, softmax and sums; probabilities are rounded to bf16 (bf16 cache) or fp16 (codes) for the second product;
  * codes enter both products exactly. The same call gives the same bits every time (split sums are added in the order of the
  * keys); how a request's keys are grouped, and with it the last bits, depends on the other requests' lengths.

@@ -142,8 +142,8 @@ __device__ __forceinline__ void unpack_u2(uint64_t v, uint32_t& lo, uint32_t& hi
     hi = __float_as_uint(b);
 }
 // 2^x on a pair without the ex2 unit: x = n + r with |r| <= 1/2 (adding 1.5 2^23 rounds to the integer), a cubic for 2^r
-// (least maximum relative error, 7.5e-5: a quarter of fp16's half step), n added to the exponent. x is cut at -126; from 128 on
-// the exponent runs over into the sign, so the caller has to look at x as well as at the result.
+// (least maximum relative error, 7.5e-5: a quarter of fp16's half step), n added to the exponent. x is cut at -126 (NaN too); from
+// 128 on the exponent runs over into the sign, so the caller has to look at x as well as at the result.
 __device__ __forceinline__ uint64_t exp2_poly(uint64_t x2)
 {
     float x0, x1;
@@ -169,6 +169,12 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c)           // NaN if any of them is
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 // The bounded wait of the GEMM kernels behind a few polls that do not read the timer.
@@ -754,7 +760,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
 #pragma unroll
                     for (int e = 1; e < kTerms; ++e) tmem_st16(tmem + kColMore + lanes + 64 * (e - 1) + 32 * qd + 16 * h, w[h % kHeld][e]);
                 };
-                float part;
+                float part, hi;                           // sum; largest argument of the cubic, whose result means nothing from 2^128 on
                 for (int pass = 0;; ++pass) {
                     if (move) {
                         if (!F32 && pass > 0) {          // the registers hold the next scores already
@@ -775,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     const float mm = m == -INFINITY ? 0.0f : m - (I8 ? 4.0f : 0.0f);   // fp16: four octaves up keep small probabilities' bits
                     const uint64_t negm2 = dup_f2(-mm);
                     uint64_t l2[2] = {0ull, 0ull};        // (0, 0)
-                    float hi = -INFINITY;                 // the largest argument of the cubic, whose result means nothing from 2^128 on
+                    hi = -INFINITY;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -784,7 +790,7 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                             float a, c;
                             unpack_f2(e2, a, c);
                             if (!F32 && k % kPolyEvery == kPolyEvery - 1) {
-                                hi = max3(hi, a, c);
+                                hi = max3_nan(hi, a, c);
                                 unpack_f2(exp2_poly(e2), a, c);
                             } else {
                                 a = ex2_approx(a);
@@ -808,9 +814,10 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
                     unpack_f2(add_f2(l2[0], l2[1]), la, lb);
                     part = la + lb;
                     if (F32 || pass > 0) break;
-                    move = __any_sync(0xffffffffu, !(part <= (I8 ? 16.0f : 1.0f) * 1024.0f) || hi > (I8 ? 14.0f : 10.0f));
+                    move = __any_sync(0xffffffffu, !(part <= (I8 ? 16.0f : 1.0f) * 1024.0f) || !(hi <= (I8 ? 14.0f : 10.0f)));
                     if (!move) break;
                 }
+                if (!F32 && move && hi != hi) part = hi;  // a NaN that only the cubic saw
                 l += part;
                 if (!F32) {
                     store_p(0);
@@ -829,11 +836,11 @@ __global__ void __launch_bounds__(kThreads, 1) pattn_tiled_kernel(const PaParams
             tc_fence_after();
         }
         auto write16 = [&](int cb, float (&o)[16], float rl_sum) {       // 16 channels of the row
-            // no visible key: zeros. The sum of a row that sees any is about 1 or more; masked scores add at most 2^-126 each.
-            const bool none = rl_sum < 5.4e-20f;
-            const float inv_l = __fdividef(1.0f, rl_sum);
+            // no visible key: zeros. The sum of a row with a score above -Inf is about 1 or more, and scores at -Inf add at most
+            // 2^-126 each: a row that sees nothing else is 0 / 0
+            const float inv_l = rl_sum < 5.4e-20f ? __uint_as_float(0x7fffffffu) : __fdividef(1.0f, rl_sum);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] = none ? 0.0f : o[k] * inv_l;
+            for (int k = 0; k < 16; ++k) o[k] = vis > 0 ? o[k] * inv_l : 0.0f;
             if (I8) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {

@@ -65,21 +65,29 @@ def compare(gpu, s, causal, bf16, O):
         for h in range(s["Hkv"] if n else 0):
             k, v = s["K"][s["table"][b, j // S], h, j % S], s["V"][s["table"][b, j // S], h, j % S]
             if int8:
-                k, v = k * s["s_k"][:L, None].astype(np.float64), v * s["s_v"][h].astype(np.float64)
+                v = v * s["s_v"][h].astype(np.float64)
+            s_k = s["s_k"][:L].astype(np.float64) if int8 else 1.0
             q = q64[t0:t0 + n, h * g:(h + 1) * g]
-            x = np.einsum("ngd,ld->ngl", q, k) * s["scale"]
-            a = np.einsum("ngd,ld->ngl", np.abs(q), np.abs(k)).max() * s["scale"]
+            with np.errstate(invalid="ignore"):
+                x = np.einsum("ngd,ld->ngl", q, k) * s_k * s["scale"]
+            a = np.einsum("ngd,ld->ngl", np.abs(q), np.abs(k)) * np.abs(s_k)
+            a = a[np.isfinite(a)].max(initial=0.0) * s["scale"]
             seen = j[None] < (L - n + np.arange(n)[:, None] + 1 if causal else np.full((n, 1), L))
             assert seen.any(-1).all()
             x = np.where(seen[:, None], x, -np.inf)
-            p = np.exp(x - x.max(-1, keepdims=True))
+            with np.errstate(invalid="ignore"):
+                p = np.exp(x - x.max(-1, keepdims=True))
             p /= p.sum(-1, keepdims=True)
+            nan = np.isnan(p).any(-1)                            # a visible score is NaN or +Inf, or all of them are -Inf
+            assert np.isnan(got[t0:t0 + n, h * g:(h + 1) * g][nan]).all(), (b, h)
+            p[nan] = 0
             want, mag = np.einsum("ngl,ld->ngd", p, v), np.einsum("ngl,ld->ngd", p, np.abs(v))
             tol = mag * (p_err + np.expm1(2 * (d_units(s["d"]) * a + 2.0 ** -20)) + (L + 32) * 2.0 ** -23)
             if int8:
                 tol += 2 * L * 2.0 ** -25 * np.abs(v).max()
             tol += (2.0 ** -8 if bf16 else 2.0 ** -24) * (np.abs(want) + tol)
             err = np.abs(got[t0:t0 + n, h * g:(h + 1) * g] - want)
+            err[nan] = 0
             assert (err <= tol + 1e-30).all(), (b, h, float(np.nanmax(err / (tol + 1e-30))), np.argwhere(~(err <= tol + 1e-30))[:4].tolist())
     assert (got[int(s["cu"][-1]):] == 7.0).all()
 
@@ -114,3 +122,42 @@ def test_a_key_far_above_all_before_it(gpu, shape, nats, int8):
         O = call(gpu, s, True, True)
         assert gpu.ctx.stwq_device_status() == 0
         compare(gpu, s, True, True, O)
+
+
+def nonfinite(gpu, shape, int8, kind, c, seed):
+    """A step with NaN or Inf among its scores: in one key (column c of eight, so that rows before it do not see it), in one query,
+    in all keys before a finite one, in all keys."""
+    new, cached, Hq, Hkv, d, S = shape
+    s = peaked(gpu, new, cached, Hq, Hkv, d, S, int8, seed, {3: 5.0, 300: 30.0}, factors=(1.0,), pad=1)
+    nan, inf = float("nan"), float("inf")
+    L = int(s["kv"].max())
+    at = {"nan key": [L - 24 + c], "nan key early": [72 + c], "inf key": [L - 24 + c], "-inf keys": range(L - 10), "-inf everywhere": range(L)}.get(kind, [])
+    value = nan if "nan" in kind else -inf if kind[0] == "-" else inf
+    if kind == "nan query":
+        s["Q"][s["T"] // 2, :, 1 + c] = nan
+    for b in range(len(s["new"])):
+        j = np.array([i for i in at if i < s["kv"][b]], np.int64)
+        page, off = gpu.T(s["table"][b, j // S].astype(np.int64)), gpu.T(j % S)
+        if int8:                                                 # Inf by way of the key's scale: every score of the key is that, or NaN
+            s["s_k"][j] = abs(value)
+            s["Kp"][page, :, off] = 0
+            s["Kp"][page, :, off, 0] = -127 if value < 0 else 127
+        else:
+            s["Kp"][page, :, off, 0] = value
+    s["K"] = s["Kp"].float().cpu().numpy().astype(np.float64)
+    return s
+
+
+KINDS = ["nan key", "nan key early", "nan query", "inf key", "-inf keys", "-inf everywhere"]
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("shape", [([40], [390], 2, 2, 64, 16), ([20], [410], 80, 80, 64, 16), ([90, 33], [300, 350], 4, 2, 128, 32)])
+def test_nan_and_infinite_scores_in_the_tiles(gpu, shape, kind, int8):
+    for c in range(8):
+        s = nonfinite(gpu, shape, int8, kind, c, 500 + c)
+        for bf16 in (True, False):
+            O = call(gpu, s, True, bf16)
+            assert gpu.ctx.stwq_device_status() == 0
+            compare(gpu, s, True, bf16, O)
