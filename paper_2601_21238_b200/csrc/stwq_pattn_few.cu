@@ -420,6 +420,7 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : Ring<I8, DP>::ctas(NR)) pa
                 // the last keys' block: value rows beyond them may hold anything, and 0 * Inf is not 0
                 for (int x = lane; x < 16 * rb / 16; x += 32)
                     if ((first + kWarps * it) * 16 + x * 16 / rb >= q.kv) st_shared_v4(st + R::half + x * 16, 0u, 0u, 0u, 0u);
+                fence_async_smem();                       // ordinary stores, before the bulk copy that refills the stage
                 __syncwarp();
             }
             const int j0 = (first + kWarps * it) * 16;

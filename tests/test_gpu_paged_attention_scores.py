@@ -161,3 +161,18 @@ def test_nan_and_infinite_scores_in_the_tiles(gpu, shape, kind, int8):
             O = call(gpu, s, True, bf16)
             assert gpu.ctx.stwq_device_status() == 0
             compare(gpu, s, True, bf16, O)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_units_behind_one_that_ends_inside_a_block(gpu, d, int8):
+    """Short requests of every remainder modulo 16, many to a CTA: the stage whose last value rows were cleared is refilled with
+    the next unit's keys at once, and none of those may be lost. Large values make a lost row show."""
+    r = np.random.default_rng(d)
+    s = peaked(gpu, [1] * 600, r.integers(1, 150, 600), 16, 8, d, 16, int8, 700, {})
+    s["Vp"] = s["Vp"] * 0 + 100 if int8 else s["Vp"] * 0 + 64        # (dead slots stay NaN)
+    s["V"] = s["Vp"].float().cpu().numpy().astype(np.float64)
+    for _ in range(4):
+        O = call(gpu, s, True, True)
+        assert gpu.ctx.stwq_device_status() == 0
+        compare(gpu, s, True, True, O)
