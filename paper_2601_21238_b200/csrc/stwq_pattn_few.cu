@@ -615,15 +615,16 @@ __global__ void __launch_bounds__(kThreads, F32 ? 2 : Ring<I8, DP>::ctas(NR)) pa
         const int slots = 8 * NR * (DP + 2);              // floats of a partial result: O, then (max, sum) per row
         float* part = p.part + ((int64_t)blockIdx.x * 2 + (blk0 == 0 ? 1 : 0)) * slots;
         auto write_out = [&](int row, int ch, float a, float b2, float lsum) {       // two channels of a row
-            const float inv = lsum > 0.0f ? __fdividef(1.0f, lsum) : 0.0f;           // no visible key: zeros
-            a = lsum > 0.0f ? a * inv : 0.0f;
-            b2 = lsum > 0.0f ? b2 * inv : 0.0f;
+            const int ti = row / p.g;
+            const bool sees = (p.causal ? q.kv - q.n + ti + 1 : q.kv) > 0;           // no visible key: zeros
+            const float inv = __fdividef(1.0f, lsum);                                // all scores at -Inf: 0 / 0
+            a = sees ? a * inv : 0.0f;
+            b2 = sees ? b2 * inv : 0.0f;
             if (I8) {
                 const float2 sv = *reinterpret_cast<const float2*>(p.s_v + (int64_t)hk * d + ch);
                 a *= sv.x;
                 b2 *= sv.y;
             }
-            const int ti = row / p.g;
             const int64_t at_o = (int64_t)(q.t0 + ti) * p.o_ts + (int64_t)(hk * p.g + row - ti * p.g) * p.o_hs + ch;
             if (!F32) *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.O) + at_o) = pack2<false>(a, b2);
             else *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.O) + at_o) = make_float2(a, b2);

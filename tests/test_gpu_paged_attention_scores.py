@@ -176,3 +176,15 @@ def test_units_behind_one_that_ends_inside_a_block(gpu, d, int8):
         O = call(gpu, s, True, True)
         assert gpu.ctx.stwq_device_status() == 0
         compare(gpu, s, True, True, O)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("shape", [([1], [430], 1, 1, 64, 16), ([4, 1], [430, 409], 4, 1, 128, 16), ([1] * 40, [390 + i for i in range(40)], 16, 4, 64, 32)])
+def test_nan_and_infinite_scores_of_few_rows(gpu, shape, kind, int8):
+    for c in range(8):
+        s = nonfinite(gpu, shape, int8, kind, c, 600 + c)
+        for bf16 in (True, False):
+            O = call(gpu, s, True, bf16)
+            assert gpu.ctx.stwq_device_status() == 0
+            compare(gpu, s, True, bf16, O)
