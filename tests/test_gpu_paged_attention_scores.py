@@ -188,3 +188,18 @@ def test_nan_and_infinite_scores_of_few_rows(gpu, shape, kind, int8):
             O = call(gpu, s, True, bf16)
             assert gpu.ctx.stwq_device_status() == 0
             compare(gpu, s, True, bf16, O)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("shape", [([1], [430], 1, 1, 64, 16), ([4, 1], [430, 99], 4, 1, 128, 16), ([1] * 40, [390 + i for i in range(40)], 16, 4, 64, 32),
+                                   ([16], [420], 1, 1, 80, 16), ([3], [5000], 12, 4, 112, 64)])
+def test_reference_moves_with_few_rows(gpu, shape, int8):
+    """By little and by much: over keys of one warp, over warps, over the CTAs that share a unit."""
+    new, cached, Hq, Hkv, d, S = shape
+    for jumps in (STEPS, {72: 92.0}, {203: 280.0}, {5: 140.0, 333: 200.0}):
+        s = peaked(gpu, new, cached, Hq, Hkv, d, S, int8, 800, jumps, pad=1)
+        for causal, bf16 in ((True, True), (False, True), (True, False)):
+            O = call(gpu, s, causal, bf16)
+            assert gpu.ctx.stwq_device_status() == 0
+            compare(gpu, s, causal, bf16, O)
+            assert gpu.torch.equal(O, call(gpu, s, causal, bf16))
