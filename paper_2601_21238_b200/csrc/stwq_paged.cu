@@ -136,31 +136,33 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanParam
     }
     __syncthreads();
 
+    // A row holds below 2^31 tokens, and so does a step: lengths, positions and the roundings to pages fit unsigned 32 bits.
+    const uint32_t S = (uint32_t)p.S;
     const int stride = gridDim.x * kPlanThreads, me = blockIdx.x * kPlanThreads + threadIdx.x;
     for (long long x = me; x < n_pages; x += stride) {
         const int b = owner(s_pg, p.B, (int)x);
-        const int col = (s_c[b] + p.S - 1) / p.S + (int)(x - s_pg[b]);
+        const int col = (int)(((uint32_t)s_c[b] + S - 1u) / S) + (int)(x - s_pg[b]);
         if (col < p.W) p.table[(int64_t)b * p.W + col] = x < p.F ? p.free_pages[x] : -1;
     }
     for (long long t = me; t < p.T; t += stride) {
         int slot = -1, pos = -1;
         if (t < tokens) {
             const int b = owner(s_cu, p.B, (int)t);
-            const int c = s_c[b];
-            pos = c + (int)(t - s_cu[b]);
-            const int pi = pos / p.S, before = (c + p.S - 1) / p.S;
+            const uint32_t c = (uint32_t)s_c[b], at = c + (uint32_t)(t - s_cu[b]);
+            const uint32_t pi = at / S, before = (c + S - 1u) / S, off = at - pi * S;
+            pos = (int)min(at, 0x7fffffffu);                        // a token that far lies behind its row
             int id = -1;
-            if (pi < p.W) {
+            if (pi < (uint32_t)p.W) {
                 if (pi < before) {
                     id = p.table[(int64_t)b * p.W + pi];            // the page that the cached tokens end in
                     bad |= id < 0;
                 } else {
-                    const int64_t f = (int64_t)s_pg[b] + (pi - before);
+                    const int64_t f = (int64_t)s_pg[b] + (int)(pi - before);
                     if (f < p.F) id = p.free_pages[f];
                     bad |= f < p.F && id < 0;
                 }
             }
-            if (id >= 0 && (int64_t)id * p.S + pos % p.S <= 0x7fffffff) slot = id * p.S + pos % p.S;
+            if (id >= 0 && (int64_t)id * p.S + off <= 0x7fffffff) slot = id * p.S + (int)off;
             else bad = true;
         }
         p.slots[t] = slot;

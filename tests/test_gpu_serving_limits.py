@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from conftest import ROOT
-from test_gpu_serving import rope_cs, run_plan
+from test_gpu_serving import run_plan
 
 pytestmark = pytest.mark.gpu
 
@@ -62,71 +62,3 @@ def test_page_plan_next_to_2_31(gpu, S, W, cached, new, table):
     if table is not None:
         table = [1 if first_new <= i < -(-min(cached + new, W * S) // S) else p for i, p in enumerate(table)]
         assert row.tolist() == [table]
-
-
-@pytest.mark.parametrize("B", [4084, 4085, 4090, 4095])
-def test_page_plan_of_large_batches_in_a_fresh_process(B):
-    """The first plan of a process (a larger one before it could have raised the kernel's shared memory limit)."""
-    code = f"""
-import torch, paper_2601_21238_b200 as pk
-z = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")
-ctx = pk.Context(0)
-slots = z({B})
-ctx.page_plan(z({B}), z({B}) + 1, torch.arange({B}, dtype=torch.int32, device="cuda"), 16, z({B}, 1), z({B} + 1), z({B}), slots, z({B}), z(1))
-assert ctx.stwq_device_status() == 0
-assert torch.equal(slots, 16 * torch.arange({B}, dtype=torch.int32, device="cuda"))
-ctx.close()
-"""
-    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=120)
-    assert r.returncode == 0, r.stderr[-2000:]
-
-
-@pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("d,rot", [(64, 32), (128, 64), (80, 48), (256, 16), (48, 0), (64, 64)])
-@pytest.mark.parametrize("pairs", [0, 1])
-def test_infinities_beside_the_rotated_channels(gpu, d, rot, pairs, bf16):
-    """Channels from rot on are not turned: an Inf or NaN there stays what it is, and changes no other channel."""
-    torch, pk = gpu.torch, gpu.pk
-    r = np.random.default_rng(d + rot)
-    T, Hq, Hkv, P = 9, 5, 2, 20
-    pos, cs = gpu.T(r.integers(0, P, T).astype(np.int32)), gpu.T(rope_cs(r, P, rot)) if rot else None
-    x = r.standard_normal((T, Hq + 2 * Hkv, d)).astype(np.float32)
-    odd = np.zeros(x.shape, bool)
-    odd[:, :, rot:] = r.uniform(size=x[:, :, rot:].shape) < 0.2
-    y = np.where(odd, r.choice(np.array([np.inf, -np.inf, np.nan], np.float32), x.shape), x)
-    outs = []
-    for a in (x, y):
-        X = gpu.T(a.reshape(T, -1))
-        X = X.to(torch.bfloat16) if bf16 else X
-        Q, K = torch.full((T, Hq, d), 7.0, device=gpu.dev), torch.full((T, Hkv, d), 7.0, device=gpu.dev)
-        gpu.ctx.qk_norm_rope(X, pos, Hq, Hkv, None, None, pk.NORM_NONE, 1e-6, cs, pairs, Q, K)
-        outs.append(torch.cat([Q, K], 1).cpu().numpy())
-    assert gpu.ctx.stwq_device_status() == 0
-    o = odd[:, :Hq + Hkv]
-    np.testing.assert_array_equal(outs[1][~o], outs[0][~o])
-    np.testing.assert_array_equal(outs[1][o], y[:, :Hq + Hkv][o])
-
-
-@pytest.mark.parametrize("norm,eps", [(1, 1e-6), (2, 1e-6), (2, 0.0), (2, 100.0)])
-@pytest.mark.parametrize("d", [16, 80, 128, 256])
-def test_norm_of_a_vector_with_a_nan_or_an_infinity(gpu, d, norm, eps):
-    """As the formulas have it: a NaN makes every channel of its vector NaN; an Inf becomes NaN (Inf / Inf) beside zeros; the
-    other vectors are what they are without it. A zero vector is 0, or 0 / 0 with eps = 0."""
-    torch = gpu.torch
-    r = np.random.default_rng(d)
-    T, Hq, Hkv = 6, 3, 2
-    x = r.standard_normal((T, Hq + 2 * Hkv, d)).astype(np.float32)
-    y = x.copy()
-    y[1, 0, d // 3], y[2, Hq, d - 1], y[3, 1, 5], y[4, Hq + 1, 0], y[5, 2] = np.nan, np.nan, np.inf, -np.inf, 0
-    outs = []
-    for a in (x, y):
-        Q, K = torch.full((T, Hq, d), 7.0, device=gpu.dev), torch.full((T, Hkv, d), 7.0, device=gpu.dev)
-        gpu.ctx.qk_norm_rope(gpu.T(a.reshape(T, -1)), gpu.T(np.arange(T, dtype=np.int32)), Hq, Hkv, None, None, norm, eps, None, 0, Q, K)
-        outs.append(torch.cat([Q, K], 1).cpu().numpy())
-    assert gpu.ctx.stwq_device_status() == 0
-    want = outs[0].copy()
-    want[1, 0], want[2, Hq] = np.nan, np.nan
-    want[3, 1], want[4, Hq + 1] = 0, 0
-    want[3, 1, 5], want[4, Hq + 1, 0] = np.nan, np.nan
-    want[5, 2] = np.nan if eps == 0 else 0
-    np.testing.assert_array_equal(outs[1], want)
