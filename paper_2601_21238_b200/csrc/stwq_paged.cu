@@ -492,7 +492,7 @@ int page_plan(stwq_ctx* ctx, const int32_t* cached_lens, const int32_t* new_lens
     p.table = block_table; p.cu = cu_new; p.kv = kv_lens; p.slots = slot_map; p.pos = pos_ids; p.used = pages_used;
     p.status = ctx->d_status;
     const size_t smem = (size_t)(3 * B + 2) * 4;
-    if (smem > 48 * 1024) {
+    if (smem > 48 * 1024 - 256) {                        // beside the kernel's static shared memory (the warps' sums)
         const cudaError_t e = cudaFuncSetAttribute(page_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (3 * kPlanMaxB + 2) * 4);
         if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
     }

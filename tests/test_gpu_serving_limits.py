@@ -62,3 +62,20 @@ def test_page_plan_next_to_2_31(gpu, S, W, cached, new, table):
     if table is not None:
         table = [1 if first_new <= i < -(-min(cached + new, W * S) // S) else p for i, p in enumerate(table)]
         assert row.tolist() == [table]
+
+
+@pytest.mark.parametrize("B", [4084, 4085, 4090, 4095])
+def test_page_plan_of_large_batches_in_a_fresh_process(B):
+    """The first plan of a process (a larger one before it could have raised the kernel's shared memory limit)."""
+    code = f"""
+import torch, paper_2601_21238_b200 as pk
+z = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")
+ctx = pk.Context(0)
+slots = z({B})
+ctx.page_plan(z({B}), z({B}) + 1, torch.arange({B}, dtype=torch.int32, device="cuda"), 16, z({B}, 1), z({B} + 1), z({B}), slots, z({B}), z(1))
+assert ctx.stwq_device_status() == 0
+assert torch.equal(slots, 16 * torch.arange({B}, dtype=torch.int32, device="cuda"))
+ctx.close()
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr[-2000:]
