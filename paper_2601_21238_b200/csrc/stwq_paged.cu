@@ -365,7 +365,8 @@ __global__ void __launch_bounds__(kNrThreads, 8) norm_rope_kernel(const NrParams
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
                         const uint64_t o = pack_f2(__shfl_sync(lanes, x[k][i], from, LPV), __shfl_sync(lanes, x[k][i + 1], from, LPV));
-                        unpack_f2(fma_f2(o, pack_f2(s[i], s[i + 1]), mul_f2(pack_f2(x[k][i], x[k][i + 1]), pack_f2(c[i], c[i + 1]))), x[k][i], x[k][i + 1]);
+                        if (turns)                        // (an Inf in a channel that is not turned stays one: 0 * Inf is not 0)
+                            unpack_f2(fma_f2(o, pack_f2(s[i], s[i + 1]), mul_f2(pack_f2(x[k][i], x[k][i + 1]), pack_f2(c[i], c[i + 1]))), x[k][i], x[k][i + 1]);
                     }
             }
         }

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from conftest import ROOT
-from test_gpu_serving import run_plan
+from test_gpu_serving import rope_cs, run_plan
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +79,29 @@ ctx.close()
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("d,rot", [(64, 32), (128, 64), (80, 48), (256, 16), (48, 0), (64, 64)])
+@pytest.mark.parametrize("pairs", [0, 1])
+def test_infinities_beside_the_rotated_channels(gpu, d, rot, pairs, bf16):
+    """Channels from rot on are not turned: an Inf or NaN there stays what it is, and changes no other channel."""
+    torch, pk = gpu.torch, gpu.pk
+    r = np.random.default_rng(d + rot)
+    T, Hq, Hkv, P = 9, 5, 2, 20
+    pos, cs = gpu.T(r.integers(0, P, T).astype(np.int32)), gpu.T(rope_cs(r, P, rot)) if rot else None
+    x = r.standard_normal((T, Hq + 2 * Hkv, d)).astype(np.float32)
+    odd = np.zeros(x.shape, bool)
+    odd[:, :, rot:] = r.uniform(size=x[:, :, rot:].shape) < 0.2
+    y = np.where(odd, r.choice(np.array([np.inf, -np.inf, np.nan], np.float32), x.shape), x)
+    outs = []
+    for a in (x, y):
+        X = gpu.T(a.reshape(T, -1))
+        X = X.to(torch.bfloat16) if bf16 else X
+        Q, K = torch.full((T, Hq, d), 7.0, device=gpu.dev), torch.full((T, Hkv, d), 7.0, device=gpu.dev)
+        gpu.ctx.qk_norm_rope(X, pos, Hq, Hkv, None, None, pk.NORM_NONE, 1e-6, cs, pairs, Q, K)
+        outs.append(torch.cat([Q, K], 1).cpu().numpy())
+    assert gpu.ctx.stwq_device_status() == 0
+    o = odd[:, :Hq + Hkv]
+    np.testing.assert_array_equal(outs[1][~o], outs[0][~o])
+    np.testing.assert_array_equal(outs[1][o], y[:, :Hq + Hkv][o])
