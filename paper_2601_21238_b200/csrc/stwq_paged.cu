@@ -195,6 +195,12 @@ struct NrParams {
     uint32_t* status;
 };
 
+__device__ __forceinline__ float min_nan(float a, float b)          // NaN if either is
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 __device__ __forceinline__ void load8(const float* p, float (&v)[8])
 {
     const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
@@ -316,8 +322,9 @@ __global__ void __launch_bounds__(kNrThreads, 8) norm_rope_kernel(const NrParams
             const float inv_d = 1.0f / (float)p.d, inv_eps = 1.0f / p.eps;
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
-                // 1 / max(|x|, eps) = min(rsqrt(x.x), 1 / eps); rsqrtf is good to 2 ulp, and takes 0 and Inf as the formula does
-                const float r = p.norm == STWQ_NORM_RMS ? rsqrtf(fmaf(ss[k], inv_d, p.eps)) : fminf(rsqrtf(ss[k]), inv_eps);
+                // 1 / max(|x|, eps) = min(rsqrt(x.x), 1 / eps); rsqrtf is good to 2 ulp, and takes 0 and Inf as the formula does.
+                // The minimum keeps NaN, as the formula does: a vector with one is NaN in all its channels.
+                const float r = p.norm == STWQ_NORM_RMS ? rsqrtf(fmaf(ss[k], inv_d, p.eps)) : min_nan(rsqrtf(ss[k]), inv_eps);
                 if (k > 0 && whs != 0 && wp != nullptr && k < heads && e0 < p.d) load8(wp + (int64_t)(h0 + k) * whs + e0, w);
 #pragma unroll
                 for (int i = 0; i < 8; i += 2)

@@ -105,3 +105,28 @@ def test_infinities_beside_the_rotated_channels(gpu, d, rot, pairs, bf16):
     o = odd[:, :Hq + Hkv]
     np.testing.assert_array_equal(outs[1][~o], outs[0][~o])
     np.testing.assert_array_equal(outs[1][o], y[:, :Hq + Hkv][o])
+
+
+@pytest.mark.parametrize("norm,eps", [(1, 1e-6), (2, 1e-6), (2, 0.0), (2, 100.0)])
+@pytest.mark.parametrize("d", [16, 80, 128, 256])
+def test_norm_of_a_vector_with_a_nan_or_an_infinity(gpu, d, norm, eps):
+    """As the formulas have it: a NaN makes every channel of its vector NaN; an Inf becomes NaN (Inf / Inf) beside zeros; the
+    other vectors are what they are without it. A zero vector is 0, or 0 / 0 with eps = 0."""
+    torch = gpu.torch
+    r = np.random.default_rng(d)
+    T, Hq, Hkv = 6, 3, 2
+    x = r.standard_normal((T, Hq + 2 * Hkv, d)).astype(np.float32)
+    y = x.copy()
+    y[1, 0, d // 3], y[2, Hq, d - 1], y[3, 1, 5], y[4, Hq + 1, 0], y[5, 2] = np.nan, np.nan, np.inf, -np.inf, 0
+    outs = []
+    for a in (x, y):
+        Q, K = torch.full((T, Hq, d), 7.0, device=gpu.dev), torch.full((T, Hkv, d), 7.0, device=gpu.dev)
+        gpu.ctx.qk_norm_rope(gpu.T(a.reshape(T, -1)), gpu.T(np.arange(T, dtype=np.int32)), Hq, Hkv, None, None, norm, eps, None, 0, Q, K)
+        outs.append(torch.cat([Q, K], 1).cpu().numpy())
+    assert gpu.ctx.stwq_device_status() == 0
+    want = outs[0].copy()
+    want[1, 0], want[2, Hq] = np.nan, np.nan
+    want[3, 1], want[4, Hq + 1] = 0, 0
+    want[3, 1, 5], want[4, Hq + 1, 0] = np.nan, np.nan
+    want[5, 2] = np.nan if eps == 0 else 0
+    np.testing.assert_array_equal(outs[1], want)
