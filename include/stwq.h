@@ -446,7 +446,7 @@ int stwq_reserve_paged_attention(stwq_ctx* ctx, int B, int Hq, int Hkv, int d);
  * Token sampling with temperature, top-k, top-p and min-p from given uniform numbers.
  * logits: B rows of V (fp32 or bf16, x_dtype), rows ld elements apart; NaN counts as -Inf and a token at -Inf is never
  * drawn. Per row (a NULL vector switches its limit off): w_i = exp((x_i - max) / temperature); temperature <= 0 is
- * greedy (the largest, lowest index first). Order: larger x first, equal x by lower index.
+ * greedy (the largest, lowest index first); logits at +Inf share everything between them. Order: larger x first, equal x by lower index.
  *   top_k > 0 keeps the first top_k; top_p < 1 then keeps the shortest prefix of those whose mass reaches top_p of theirs
  *   (at least one); min_p keeps w_i >= min_p. u in [0, 1): the token is the first kept index whose running sum of kept weights,
  *   in index order, exceeds u times their total.

@@ -239,7 +239,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
     const double min_p = min_pf > 0.0f ? fmin((double)min_pf, 1.0) : 0.0;
     Weigher wg;
     wg.m = (double)value_of(maxkey);
-    wg.c = greedy ? 256.0 : 369.3299304675746 / (double)temp;      // 256 log2(e)
+    // 256 log2(e) / t; an infinite temperature counts as the largest finite one, so that nothing is divided Inf by Inf
+    wg.c = greedy ? 256.0 : 369.3299304675746 / (double)fminf(temp, 3.4028234663852886e38f);
     wg.low = (float)fmax(wg.m - 46.0 * 256.0 / wg.c, -3.4028234663852886e38);      // 46 octaves below (an infinite maximum leaves the others at 0)
     wg.maxkey = maxkey;
     wg.table = sh.table;
@@ -467,7 +468,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const SmpParams p
         const int e = (int)(__float_as_uint(__fsub_rn(fmax_, value_of(key))) >> 21) - (121 << 2);
         return min(max(e, 0), kCoarse - 1);
     };
-    const float half_octaves = greedy ? 1.0f : 2.885390082f / temp;
+    const float half_octaves = greedy ? 1.0f : 2.885390082f / fminf(temp, 3.4028234663852886e38f);
     auto weight_bin = [&](uint32_t key) -> int {
         if (key == maxkey) return 0;
         return (int)fminf(__fmul_rn(__fsub_rn(fmax_, value_of(key)), half_octaves), (float)(kCoarse - 1));

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from conftest import ROOT
-from test_gpu_serving import rope_cs, run_plan
+from test_gpu_serving import rope_cs, run_plan, run_sample
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +130,40 @@ def test_norm_of_a_vector_with_a_nan_or_an_infinity(gpu, d, norm, eps):
     want[3, 1, 5], want[4, Hq + 1, 0] = np.nan, np.nan
     want[5, 2] = np.nan if eps == 0 else 0
     np.testing.assert_array_equal(outs[1], want)
+
+
+@pytest.mark.parametrize("V", [37, 3000, 40000])
+def test_sampling_at_the_ends_of_the_temperature(gpu, V):
+    """From the smallest number to Inf, with finite rows and rows that hold +Inf: the limits of the weights."""
+    r = np.random.default_rng(V)
+    x = r.standard_normal((6, V)).astype(np.float32)
+    x[1, [5, V - 2]] = np.inf
+    x[2, V // 2:] = -np.inf
+    x[3, 9] = np.inf
+    x[3, 10:20] = -3.4e38
+    x[4] = np.float32(-3.4028235e38)                             # every logit at the type's lowest value
+    x[5, ::2] = np.nan
+    X = gpu.T(x)
+    live = x > -np.inf                                           # (NaN is not)
+    m = np.where(live, x, -np.inf).max(1)
+    top = live & (x == m[:, None])
+    for temp, flat in ((1e-45, False), (1e-30, False), (1e35, True), (3.4e38, True), (np.inf, True)):
+        for k, p, mp in ((0, 1.0, 0.0), (20, 1.0, 0.0), (0, 0.5, 0.0), (0, 1.0, 0.5)):
+            for u in (0.0, 0.51, 1 - 2.0 ** -24):
+                tok, prob, kept = run_sample(gpu, X, temp, k, p, mp, u)
+                for i in range(6):
+                    infinite = m[i] == np.inf
+                    if flat and not infinite and i not in (4,):  # all weights 1 (1e35: 2^-42 off at most): the first live tokens, evenly
+                        n = int(live[i].sum())
+                        order = np.flatnonzero(live[i])[np.argsort(-x[i][live[i]], kind="stable")]
+                        want = min(n, k) if k else n
+                        want = -(-want // 2) if p < 1 else want
+                        assert kept[i] == want and tok[i] in order[:want]
+                        assert abs(prob[i] - 1 / want) <= 2.0 ** -22 / want
+                    else:                                        # the largest share the mass
+                        share = np.flatnonzero(top[i])
+                        assert tok[i] in share
+                        c = len(share)
+                        c = min(c, k) if k else c
+                        c = max(1, -(-c // 2)) if p < 1 else c
+                        assert abs(prob[i] - 1 / c) <= 2.0 ** -22 / c
