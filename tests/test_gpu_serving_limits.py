@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 
 from conftest import ROOT
+from test_gpu_paged_attention import call, check, make
 from test_gpu_serving import rope_cs, run_plan, run_sample
 
 pytestmark = pytest.mark.gpu
@@ -167,3 +168,122 @@ def test_sampling_at_the_ends_of_the_temperature(gpu, V):
                         c = min(c, k) if k else c
                         c = max(1, -(-c // 2)) if p < 1 else c
                         assert abs(prob[i] - 1 / c) <= 2.0 ** -22 / c
+
+
+MIXED = ([1] * 30 + [120, 40, 1, 7], [20 * i for i in range(30)] + [60, 500, 2000, 3])
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_a_captured_mixed_step_of_both_kernels(gpu, int8):
+    """Decoding requests beside chunks, more units than SMs: the few-row kernel is launched behind the tiled one as its dependent.
+    Captured, replayed on another stream with other inputs, a kernel that reads the output right behind it."""
+    torch, pk = gpu.torch, gpu.pk
+    s = make(gpu, *MIXED, 32, 8, 64, 16, int8, 31)
+    ctx = pk.Context(0)
+    try:
+        ctx.stwq_reserve_paged_attention(len(s["new"]), 32, 8, 64)
+        t = lambda a: None if a is None else gpu.T(a)  # noqa: E731
+        O = torch.zeros((s["T"], 32, 64), dtype=torch.bfloat16, device=gpu.dev)
+        copy = torch.zeros_like(O)
+        args = [s["Q"], gpu.T(s["cu"]), 120, gpu.T(s["table"]), gpu.T(s["kv"]), s["Kp"], s["Vp"], t(s["s_k"]), t(s["s_v"]), float(s["scale"]), True, pk.OUT_BF16, O]
+        side, other = torch.cuda.Stream(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        before = ctx.stwq_launch_count()
+        with torch.cuda.stream(side):
+            ctx.paged_attention(*args)
+        torch.cuda.synchronize()
+        assert ctx.stwq_launch_count() - before == 2             # both kernels
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            ctx.paged_attention(*args)
+            copy.copy_(O)
+            ctx.paged_attention(*args)
+        for seed in range(3):
+            s["Q"].copy_(torch.randn(s["Q"].shape, device=gpu.dev, generator=torch.Generator(device=gpu.dev).manual_seed(seed)).to(torch.bfloat16))
+            O.fill_(9.0)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(other):
+                g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(O, copy) and ctx.stwq_device_status() == 0
+            check(gpu, s, True, True, O)
+            assert torch.equal(O, call(gpu, s, True, True))
+    finally:
+        ctx.close()
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("new,cached", [([1, 1, 2], [70, 500, 33]), ([90, 5], [40, 300]), MIXED])
+def test_strided_queries_and_outputs(gpu, new, cached, int8):
+    """Queries as a view of the rows of the qkv linear or head-major, outputs into a wider row or head-major: the same bits as
+    dense ones, and nothing else written."""
+    torch = gpu.torch
+    s = make(gpu, new, cached, 8, 2, 64, 16, int8, 41, pad=2)
+    for bf16 in (True, False):
+        want = call(gpu, s, True, bf16)
+        dt = want.dtype
+        row = torch.randn((s["T"], 12 * 64 + 8), device=gpu.dev).to(torch.bfloat16)
+        row[:, 8:8 + 8 * 64] = s["Q"].view(s["T"], -1)
+        views = [row[:, 8:8 + 8 * 64].view(s["T"], 8, 64), s["Q"].transpose(0, 1).contiguous().transpose(0, 1)]
+        wide, heads = torch.full((s["T"], 1000), 7.0, dtype=dt, device=gpu.dev), torch.full((8, s["T"], 64), 7.0, dtype=dt, device=gpu.dev)
+        outs = [wide[:, 16:16 + 8 * 64].view(s["T"], 8, 64), heads.transpose(0, 1)]
+        for q, o in zip(views, outs):
+            call(gpu, dict(s, Q=q), True, bf16, O=o)
+            assert gpu.ctx.stwq_device_status() == 0 and torch.equal(o, want)
+        assert (wide[:, :16] == 7.0).all() and (wide[:, 16 + 8 * 64:] == 7.0).all()
+
+
+def test_requests_that_share_pages(gpu):
+    """Two requests with one prefix in common read the same pages."""
+    for new in ([1, 1, 1], [60, 1, 30]):
+        s = make(gpu, new, [320 - n for n in new], 4, 2, 128, 16, False, 51)
+        s["table"][1, :16] = s["table"][0, :16]
+        s["table"][2] = s["table"][0]
+        O = call(gpu, s, True, True)
+        assert gpu.ctx.stwq_device_status() == 0
+        check(gpu, s, True, True, O)
+
+
+@pytest.mark.parametrize("n,Hq", [(1, 16), (3, 2), (20, 1)])
+def test_attention_of_the_largest_batch(gpu, n, Hq):
+    r = np.random.default_rng(n)
+    new = r.integers(0, n + 1, 4096)
+    s = make(gpu, new, r.integers(0, 60, 4096), Hq, 1, 128, 16, False, 61)
+    O = call(gpu, s, True, True)
+    assert gpu.ctx.stwq_device_status() == 0
+    check(gpu, s, True, True, O)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("B,n,Hq", [(64, 1, 8), (2, 24, 4)])
+def test_a_million_keys_per_request(gpu, B, n, Hq, int8):
+    """2^20 - 5 keys of one page over and over: 64-bit positions in the list of all blocks. Attention over repeated keys is attention
+    over the page's keys, weighed by how often each is seen."""
+    torch, S, d, Hkv, L = gpu.torch, 16, 64, 4, 2 ** 20 - 5
+    r = np.random.default_rng(71)
+    W = 2 ** 16
+    table = np.ones((B, W), np.int32)
+    Q = gpu.T(r.standard_normal((B * n, Hq, d)).astype(np.float32)).to(torch.bfloat16)
+    if int8:
+        Kp, Vp = (gpu.T(r.integers(-100, 101, (2, Hkv, S, d)).astype(np.int8)) for _ in range(2))
+        s_k, s_v = np.full(L, 1 / 64, np.float32), np.full((Hkv, d), 1 / 64, np.float32)
+    else:
+        Kp, Vp = (gpu.T(r.standard_normal((2, Hkv, S, d)).astype(np.float32)).to(torch.bfloat16) for _ in range(2))
+        s_k = s_v = None
+    s = dict(Q=Q, cu=np.arange(B + 1, dtype=np.int32) * n, kv=np.full(B, L, np.int32), table=table, S=S, T=B * n, new=np.full(B, n), d=d, Hq=Hq, Hkv=Hkv,
+             scale=0.125, Kp=Kp, Vp=Vp, s_k=s_k, s_v=s_v)
+    O = call(gpu, s, True, True).float().cpu().numpy().reshape(B, n, Hkv, Hq // Hkv, d).astype(np.float64)
+    assert gpu.ctx.stwq_device_status() == 0
+    k, v = (a[1].float().cpu().numpy().astype(np.float64) * (1 / 64 if int8 else 1) for a in (Kp, Vp))
+    q = Q.float().cpu().numpy().astype(np.float64).reshape(B, n, Hkv, Hq // Hkv, d)
+    seen = L - n + np.arange(n) + 1
+    times = (seen[:, None] - np.arange(S)[None] + S - 1) // S    # how often key j of the page is seen
+    p = np.exp(np.einsum("bnhgd,hjd->bnhgj", q, k) * 0.125) * times[None, :, None, None]
+    p /= p.sum(-1, keepdims=True)
+    want, mag = np.einsum("bnhgj,hjd->bnhgd", p, v), np.einsum("bnhgj,hjd->bnhgd", p, np.abs(v))
+    a = np.einsum("bnhgd,hjd->bnhgj", np.abs(q), np.abs(k)).max() * 0.125
+    # P to 16 bits, scores and exponentials as in the other tests; a running sum of at most 2^20 / 16 terms of a thread or of the
+    # tensor core (each at most 2^-23 of the sum so far, truncated), in numerator and denominator; the store
+    tol = mag * (2.0 ** -8 + 2 * ((d + 8) * 2.0 ** -23 * a + 2.0 ** -20 + 7.5e-5) + 2 * 2.0 ** 16 * 2.0 ** -23)
+    tol += 2.0 ** -8 * (np.abs(want) + tol)
+    assert (np.abs(O - want) <= tol).all(), float((np.abs(O - want) / tol).max())
