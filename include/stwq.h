@@ -400,12 +400,13 @@ int page_plan(stwq_ctx* ctx, const int32_t* cached_lens, const int32_t* new_lens
  * apart (16-byte multiples). w_q / w_k: NULL with *_heads 0, or [d] (heads = 1: shared), or [Hq, d] / [Hkv, d]; used by the
  * norm only. cs [P, rot] fp32: rot/2 cosines, then rot/2 sines, for each position (any angles: 1-D or 2-D grids);
  * NULL with rot = 0 for no rotation. rot <= d; channels from rot on are not turned. d a multiple of 16, <= 256; rot a
- * multiple of 16. fp32 arithmetic, one rounding at the store.
+ * multiple of 16. fp32 arithmetic, one rounding at the store; NaN and Inf come out as the formulas have them.
  *  - qk_norm_rope: Qo [T, Hq, d] and Ko [T, Hkv, d] of out_dtype (fp32 or bf16), element (t, h, c) at
  *    t * ts + h * hs + c (strides in elements, 16-byte multiples: a head-major [H, T, d] output feeds kv_append and
  *    qattention). Values are not touched.
  *  - kv_append_paged: queries to Qo (bf16, strides as above), keys (normed, rotated) and values to slot slot_map[t] of the
- *    pool; int8 codes are those of kv_append: clamp(round(x * (1 / s))), bits in {8, 6}. Slot -1: nothing is appended for
+ *    pool; int8 codes are those of kv_append: clamp(round(x * (1 / s))), bits in {8, 6}. Any page size and d up to 256 are taken;
+ *    paged_attention reads pages of a multiple of 16 with d <= 128. Slot -1: nothing is appended for
  *    the row. A slot beyond the pool is not written and records STWQ_ERR_PAGES. Two rows with one slot: unspecified which stays.
  * Outputs must not overlap QKV. pos_ids -1 marks a padding row, of which nothing is written. With a rotation or key
  * scales, any other position outside [0, P) writes zeros to Qo (and Ko), appends nothing, and records STWQ_ERR_POS_RANGE.

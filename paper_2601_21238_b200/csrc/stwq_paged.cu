@@ -17,8 +17,9 @@
 // hold it (8 channels = one or two 16-byte accesses per lane), the partner of a half-split pair comes by shuffle
 // from the lane rot/16 further. Bound by HBM. A lane group takes up to kHeads heads of one kind of one token: their
 // loads are in flight together, and weights and angles are read once for all of them. Measured: 8192 rows of 90 heads of
-// 64, bf16 in and out, 46 us, 4.1 TB/s; 65536 rows of 32 heads of 80, fp32, 278 us, 4.8 TB/s (0.63 and 0.74 of the
-// measured copy rate; a vector of 80 leaves 6 of its 16 lanes idle). 256-thread blocks at 79 registers took 55 and 319 us.
+// 64, bf16 in and out, 45 us, 4.2 TB/s; 65536 rows of 32 heads of 80, fp32, 275 us, 4.9 TB/s (0.64 and 0.74 of the
+// measured copy rate; a vector of 80 leaves 6 of its 16 lanes idle). 256-thread blocks at 79 registers took 55 and 319 us; held to
+// 64 registers, the forms for up to 128 channels spill 12 to 56 bytes a thread. The same 8192 rows into code pages take 53 us.
 #include <cuda_bf16.h>
 
 #include "stwq_internal.cuh"

@@ -18,10 +18,13 @@
 //  * fp32 output: P is kept as a sum of 16-bit terms (bf16: three, fp16: two; 22 to 24 significant bits), all multiplied by V.
 //    The tensor core truncates its running sums (1e-5 over 5000 keys), so the row threads add each tile's product to an
 //    fp32 sum beside it. Both want tensor memory: a CTA then has one tile of rows, not two.
-//  * Measured: 2 requests of 2048 tokens behind 2048, 16 heads over 4 of 128, bf16, causal: 105 us, 975 TFLOP/s, 0.59 of
-//    the measured burst rate (3050 cycles per 256 x 128 tile: 2048 of products, the rest waits between products and rows).
-//    4 requests of 1024 to 2048 tokens behind up to 6144, 32 heads over 8: 538 us. 32 requests of 256 tokens over 680 codes,
-//    30 heads of 64: 149 us; there a unit is six tiles long, and set-up, Q and O cost a third of it.
+//  * Measured: 2 requests of 2048 tokens behind 2048, 16 heads over 4 of 128, bf16, causal: 108 us, 950 TFLOP/s, 0.57 of
+//    the measured burst rate (2048 cycles of products per 256 x 128 tile, the rest waits between products and rows).
+//    4 requests of 1024 to 2048 tokens behind up to 6144, 32 heads over 8: 550 us in a burst, 630 to 645 in long runs; 1777 us with
+//    fp32 output. 32 requests of 256 tokens over 680 codes, 30 heads of 64: 153 us; there a unit is six tiles long, and set-up, Q
+//    and O cost a third of it. Looking at what the cubic gets (its result alone hides an overflow) is 2 to 3 % of these.
+//  * Where scores are far from flat the reference moves more often: the long chunks take 756 us with queries 4 times as large
+//    (scores of a standard deviation of 5), 918 us with 16 times; the codes 196 us with 4 times.
 // 16-bit operands: bf16 for a bf16 cache (P rounded to bf16); fp16 for codes (exact), with queries scaled per row by a
 // power of two as in the few-row kernel. Sums, maxima and O in fp32.
 #include <cuda.h>
@@ -142,7 +145,7 @@ __device__ __forceinline__ void unpack_u2(uint64_t v, uint32_t& lo, uint32_t& hi
     hi = __float_as_uint(b);
 }
 // 2^x on a pair without the ex2 unit: x = n + r with |r| <= 1/2 (adding 1.5 2^23 rounds to the integer), a cubic for 2^r
-// (least maximum relative error, 7.5e-5: a quarter of fp16's half step), n added to the exponent. x is cut at -126 (NaN too); from
+// (least maximum relative error, 7.5e-5: below a quarter of fp16's half step), n added to the exponent. x is cut at -126 (NaN too); from
 // 128 on the exponent runs over into the sign, so the caller has to look at x as well as at the result.
 __device__ __forceinline__ uint64_t exp2_poly(uint64_t x2)
 {

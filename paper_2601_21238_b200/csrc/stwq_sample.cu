@@ -24,7 +24,8 @@
 // added up over distributed shared memory); every later pass runs on shared memory. What bounds it: instruction issue
 // of the passes (a row of 16384 logits with top-k 2000 and top-p takes about 70 thousand cycles of a 512-thread CTA, two
 // of which share an SM: 256 rows in 46 us), and the latency of a pass for few rows. HBM needs 1.3 us for the same rows.
-// Top-p without top-k computes an fp64 weight for every token: 64 rows of 128000 in 101 us.
+// Top-p without top-k computes an fp64 weight for every token: 64 rows of 128000 in 102 to 133 us (how many clusters of eight
+// are resident at once differs from GPU to GPU). Without limits the same rows take 56 us, greedy ones 34.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
