@@ -80,7 +80,9 @@ int paged_attention(stwq_ctx* ctx, const void* Q, int64_t q_ts, int64_t q_hs, co
     // the step together cannot outnumber the SMs, the tiled kernel cuts every unit's keys over the idle ones and takes the
     // decoding requests too (2 requests of up to 20 tokens: 15 against 23 us with both kernels; 4 of up to 8 tokens
     // behind up to 4000, 4 heads per key head: 29 against 56). With more units than SMs it does not cut keys, and a
-    // long decoding request would wait for one CTA.
+    // long decoding request would wait for one CTA. Steps with more than 16 query heads per key head have no other kernel and do
+    // wait: 200 requests of up to 512 keys, 32 heads over one of 128, take 29 us, and 407 us when one of them has 32768 keys (16
+    // heads, in the few-row kernel: 41 and 68 us).
     const bool tiled = (int64_t)max_new * g > kFewRows;
     const bool alone = tiled && (g > kFewRows || (int64_t)Hkv * ((T * g + 127) / 128 + B) <= ctx->sm_count);
     p.few_max = alone ? 0 : kFewRows;
