@@ -10,6 +10,7 @@
  *   online    qlinear          quantize -> int8 GEMM -> dequantize (+bias, +GELU)
  *   online    qlinear_q        the same from precomputed codes
  *   serving   page_plan, kv_append_paged, paged_attention, sample_tokens   (a decoder's step over a paged cache)
+ *   and       block_norm, linear_w4g, token_logprobs                       (what stands around it in the same step)
  * and, beside the path: chained layers, bf16 activations, the asymmetric quantizer, the dynamic
  * token-wise baseline, packed 4-bit weights, quantized attention with a quantized KV cache, and the
  * selection of calibration samples (each documented at its declaration below).
@@ -63,8 +64,9 @@ enum {
     STWQ_ERR_NOMEM = -10,         /* workspace allocation failed                             */
     STWQ_ERR_CAPTURE = -11,       /* the call would have to (re)allocate workspace while its stream is being
                                      captured into a CUDA graph; reserve the workspace before capturing */
-    STWQ_ERR_PAGES = -12          /* page bookkeeping saw a length, page id, slot or table entry out of range
+    STWQ_ERR_PAGES = -12,         /* page bookkeeping saw a length, page id, slot or table entry out of range
                                      (the call's description says what it did instead)      */
+    STWQ_ERR_TOKEN = -13          /* a given token was outside [-1, V); its log probability is NaN */
 };
 
 /*
@@ -79,8 +81,9 @@ enum {
  *                       from those of the exact activation.
  */
 enum { STWQ_ACT_NONE = 0, STWQ_ACT_GELU_ERF = 1, STWQ_ACT_GELU_TANH = 2, STWQ_ACT_GELU_FAST = 3 };
-/* element type of Y. INT32 returns the raw accumulators (no scale, bias or activation). */
-enum { STWQ_OUT_F32 = 0, STWQ_OUT_BF16 = 1, STWQ_OUT_INT32 = 2 };
+/* element type of Y. INT32 returns the raw accumulators (no scale, bias or activation); INT8 is an output of block_norm
+   only: the codes that the next linear's static quantizer gives. */
+enum { STWQ_OUT_F32 = 0, STWQ_OUT_BF16 = 1, STWQ_OUT_INT32 = 2, STWQ_OUT_INT8 = 3 };
 
 /*
  * Create a context on `device` (a CUDA ordinal). Synchronous. Allocates a small status
@@ -371,8 +374,9 @@ int qattn_pv(stwq_ctx* ctx, const uint8_t* Pq, int G, int Tq, int Tk_pad, int d,
  * request b. Tokens of a step are packed: request b owns rows cu_new[b] .. cu_new[b+1] - 1.
  */
 enum { STWQ_KV_BF16 = 0, STWQ_KV_INT8 = 1 };
-/* norm of a head vector x: none; x / sqrt(mean x^2 + eps) * w; x / max(|x|, eps) * w (no weights: w = 1) */
-enum { STWQ_NORM_NONE = 0, STWQ_NORM_RMS = 1, STWQ_NORM_L2 = 2 };
+/* norm of a head vector x: none; x / sqrt(mean x^2 + eps) * w; x / max(|x|, eps) * w (no weights: w = 1).
+   LAYER is a norm of block_norm's rows only (and L2 one of head vectors only): (x - mean) / sqrt(mean (x - mean)^2 + eps) */
+enum { STWQ_NORM_NONE = 0, STWQ_NORM_RMS = 1, STWQ_NORM_L2 = 2, STWQ_NORM_LAYER = 3 };
 /* which channels a rotation pairs: (i, i + rot/2) or (2i, 2i + 1), i < rot/2 */
 enum { STWQ_ROPE_HALF = 0, STWQ_ROPE_PAIRS = 1 };
 
@@ -460,6 +464,72 @@ int sample_tokens(stwq_ctx* ctx, const void* logits, int x_dtype, int64_t ld, in
                   int32_t* kept, void* stream);
 
 /*
+ * What a transformer block does between its linears, in one pass over the rows: the residual sum with the norm behind the
+ * branch, its gate and a residual scale, then the norm before the next branch with its modulation, stored in floating point
+ * or as the codes of the next linear's static quantizer (qlinear_q takes them as they are). (The paper's decoders, VAR, RAR
+ * and MAR, have such blocks; Appendix B folds the channel scale of qkv / fc1 into them.) Row m, g = cond_ids[m]:
+ *     h'[m] = H[m] + res_scale * gate[g] * (Npost(O[m]) * w_post + b_post)          (h' = H[m] without O)
+ *     y[m]  = (Npre(h'[m]) * w_pre + b_pre) * (1 + scale[g]) + shift[g]
+ *     Hout[m] = h'[m],   Y[m] = y[m], y[m] / s_ch, or clamp(round((y * (1 / s_ch)) * (1 / s_tok[pos_ids[m]])))
+ * N is STWQ_NORM_NONE, _RMS or _LAYER over the C channels; a NULL vector is 1 (weights, gate, s_ch) or 0 (biases, scale, shift).
+ *  - H, Hout: M rows of h_dtype (fp32 or bf16), O of o_dtype, rows ldh / ldho / ldo elements apart. O NULL: no residual sum, and
+ *    Hout must be NULL. Hout NULL with O: the sum is not stored. Y NULL: only the sum. At least one of Hout and Y.
+ *  - gate, scale, shift: [G, C] of c_dtype (fp32 or bf16), rows ldc elements apart (slices of one conditioning tensor);
+ *    cond_ids [M], or NULL for row 0 everywhere (a per-channel gate). w, b, s_ch [C] fp32.
+ *  - Y: y_dtype STWQ_OUT_F32, _BF16 or _INT8 (needs pos_ids, s_tok [P], bits in {8, 6}), rows ldy elements apart. The division
+ *    by s_ch multiplies by its reciprocal, as stwq_quantize does; s_tok, P and bits belong to the codes only.
+ *  - pos_ids [M], optional for floating outputs: -1 marks a padding row, which is neither read nor written.
+ * C a multiple of 8, <= 16384; rows and pointers 16-byte aligned (rows of codes: 8). Hout may be H, and Y may be H or O, in
+ * place (same rows, same type); outputs must not overlap an operand in any other way (STWQ_ERR_ALIGN).
+ * fp32 arithmetic, one rounding at each store; y is computed from h' before its rounding. NaN and Inf come out as the formulas
+ * have them (codes: NaN gives 0). A cond_id outside [0, G), and for codes a position outside [0, P) other than -1, records
+ * STWQ_ERR_POS_RANGE: Hout is then H (cond_id) and Y zeros.
+ */
+int block_norm(stwq_ctx* ctx, const void* H, int64_t ldh, int h_dtype, const void* O, int64_t ldo, int o_dtype, int64_t M, int C,
+               const int32_t* cond_ids, int G, const void* gate, const void* scale, const void* shift, int64_t ldc, int c_dtype,
+               int post_norm, const float* w_post, const float* b_post, float res_scale, int pre_norm, const float* w_pre,
+               const float* b_pre, float eps, void* Hout, int64_t ldho, const int32_t* pos_ids, const float* s_ch,
+               const float* s_tok, int P, int bits, void* Y, int64_t ldy, int y_dtype, void* stream);
+
+/*
+ * Few-row products with 4-bit weights that have a scale per group of input channels (weight-only: the activations stay in
+ * floating point, as the head and the linears of a decode step run where the per-channel scales of qlinear_w4 cost too much).
+ *     Y[m,n] = act(sum_g s_g[n,g] sum_{k in group g} X[m,k] code[n,k] + bias[n])
+ *  - gps_fold_group4: W [N,K] fp32 -> Wp [N, K/2] bytes (the nibbles of gps_fold_packed4: even channel low, two's complement,
+ *    codes in [-8, 7]) and s_g [N, K/group] of s_dtype (fp32 or bf16): per group a = max |W s_ch|, s = 2a / 15 (1 if a = 0, floored
+ *    at 2^-64), rounded to s_dtype first; code = clamp(round(W s_ch / s)). group = K gives gps_fold_packed4's codes and scales.
+ *  - linear_w4g: X M rows of x_dtype (fp32 or bf16), ldx elements apart (16-byte multiples); bias [N] fp32 or NULL; Y [M,N] dense,
+ *    fp32 or bf16. A channel scale s_ch of the fold is divided out of X by its producer (block_norm's s_ch).
+ * group a multiple of 32 that divides K; M <= 64: every row beyond 8 adds work that the weights' stream does not hide,
+ * and beyond 64 rows the tiled GEMM of qlinear_w4 is the right call. X, Wp 16-byte aligned.
+ * Products of codes and activations are exact (fp32 activations enter as three bf16 parts), sums fp32 in a fixed order: the
+ * same call gives the same bits. Results below 2^-100 lose bits. A row of X with NaN or Inf gives NaN or Inf in that row of Y as the formula has it.
+ */
+int gps_fold_group4(stwq_ctx* ctx, const float* W, int N, int K, const float* s_ch, int group, uint8_t* Wp, void* s_g, int s_dtype,
+                    void* stream);
+int linear_w4g(stwq_ctx* ctx, const void* X, int64_t ldx, int x_dtype, int64_t M, int K, int N, const uint8_t* Wp, const void* s_g,
+               int s_dtype, int group, const float* bias, int act, int out_dtype, void* Y, void* stream);
+
+/*
+ * Log probabilities of given tokens, with their ranks, the entropy of the distribution and its likeliest tokens: what scoring
+ * of prompts and the answers of a served step need beside sample_tokens. Rows, temperature and order as there (NaN counts as
+ * -Inf, a token at -Inf is never drawn; larger x first, equal x by lower index; temperature <= 0 or NaN is greedy; logits at +Inf
+ * share everything between them), without limits:
+ *     p_i = exp((x_i - max) / t) / S,   S = sum_j exp((x_j - max) / t)
+ *  - logprobs [B] = ln p of tokens[b]; ranks [B] = how many tokens stand before it (0 = likeliest); entropy [B] = -sum p ln p;
+ *    top_ids, top_logprobs [B, k]: the first k tokens of the order, k <= 32. Every output but logprobs may be NULL (both top
+ *    vectors, with k = 0). tokens NULL: logprobs and ranks NULL too.
+ *  - A token that is never drawn: -Inf, rank -1. Token -1 (no token: a padding row, a row sample_tokens could not draw for): 0, rank -1.
+ *    Any other token outside [0, V): NaN, rank -1, and STWQ_ERR_TOKEN is recorded.
+ *  - Fewer than k tokens that can be drawn: the rest of top_ids is -1, of top_logprobs -Inf. A row without any: entropy 0.
+ * fp32; S and the entropy sum are good to a few units of 2^-24, so a log probability near 0 is good to about 1e-7 absolute.
+ * Sums have a fixed order: the same call gives the same bits. V <= 360448, ld >= V.
+ */
+int token_logprobs(stwq_ctx* ctx, const void* logits, int x_dtype, int64_t ld, int B, int V, const float* temperature,
+                   const int32_t* tokens, float* logprobs, int32_t* ranks, float* entropy, int k, int32_t* top_ids,
+                   float* top_logprobs, void* stream);
+
+/*
  * qlinear without any allocation. (The paper has no counterpart to this call; it exists for the
  * way the library gets embedded.) qlinear needs a context, whose creation allocates, and keeps
  * the int8 copy of X in workspace that may be (re)allocated during a call. Hosts that cannot
@@ -488,7 +558,7 @@ int qlinear_static(const float* X, const int32_t* pos_ids, int64_t M, int K, int
 
 /*
  * Synchronise `stream`, then return and clear the status recorded by device code since the
- * last call: STWQ_OK, STWQ_ERR_POS_RANGE, STWQ_ERR_NONFINITE, STWQ_ERR_PAGES or
+ * last call: STWQ_OK, STWQ_ERR_POS_RANGE, STWQ_ERR_NONFINITE, STWQ_ERR_PAGES, STWQ_ERR_TOKEN or
  * STWQ_ERR_DEVICE_TIMEOUT.
  */
 int stwq_device_status(stwq_ctx* ctx, void* stream);

@@ -14,11 +14,11 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libstwq.so")
 
 ACT_NONE, ACT_GELU_ERF, ACT_GELU_TANH, ACT_GELU_FAST = 0, 1, 2, 3
-OUT_F32, OUT_BF16, OUT_INT32 = 0, 1, 2
+OUT_F32, OUT_BF16, OUT_INT32, OUT_INT8 = 0, 1, 2, 3
 OPT_GEMM_PATH, OPT_WAIT_LIMIT_MS = 1, 2
 OPT_TILE_N, OPT_VARIANT, OPT_KSPLIT = 100, 101, 102
 KV_BF16, KV_INT8 = 0, 1
-NORM_NONE, NORM_RMS, NORM_L2 = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_L2, NORM_LAYER = 0, 1, 2, 3
 ROPE_HALF, ROPE_PAIRS = 0, 1
 STATIC_MAX_CODES = 4 * 1024 * 1024
 
@@ -29,7 +29,7 @@ _SYMBOLS = ["stwq_create", "stwq_destroy", "stwq_reserve", "stwq_calibrate", "gp
             "stwq_workspace_generation", "stwq_selftest_wait_expiry", "stwq_probe_int8_peak", "gps_fold_packed4", "stwq_unpack4",
             "qlinear_w4", "kv_append", "qattention", "stwq_reserve_attention", "qattn_softmax_quantize", "qattn_pv",
             "dgc_select", "page_plan", "qk_norm_rope", "kv_append_paged", "sample_tokens",
-            "paged_attention", "stwq_reserve_paged_attention"]
+            "paged_attention", "stwq_reserve_paged_attention", "block_norm", "gps_fold_group4", "linear_w4g", "token_logprobs"]
 
 _lib = None
 
@@ -105,6 +105,11 @@ def load_library():
                                   f32, i32, i32, vp, i64, i64, vp]
     L.stwq_reserve_paged_attention.argtypes = [vp, i32, i32, i32, i32]
     L.sample_tokens.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.block_norm.argtypes = [vp, vp, i64, i32, vp, i64, i32, i64, i32, vp, i32, vp, vp, vp, i64, i32, i32, vp, vp, f32, i32, vp, vp, f32,
+                             vp, i64, vp, vp, vp, i32, i32, vp, i64, i32, vp]
+    L.gps_fold_group4.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, i32, vp]
+    L.linear_w4g.argtypes = [vp, vp, i64, i32, i64, i32, i32, vp, vp, i32, i32, vp, i32, i32, vp, vp]
+    L.token_logprobs.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     L.stwq_device_status.argtypes = [vp, vp]
     L.stwq_set_option.argtypes = [vp, i32, i32]
     L.stwq_launch_count.argtypes = [vp]
@@ -510,6 +515,107 @@ class Context:
                                           max(ld, V) if B == 1 else ld, B, V, q(temperature), q(top_k),
                                           q(top_p), q(min_p), u.data_ptr(), tokens.data_ptr(), q(probs), q(kept),
                                           self._raw_stream(stream)), "sample_tokens")
+
+    # ---- around the attention of a step: norms with gate and residual, few-row 4-bit linears, log probabilities
+    def block_norm(self, H, O, cond_ids, gate, scale, shift, post_norm, w_post, b_post, res_scale, pre_norm, w_pre, b_pre, eps, Hout,
+                   pos_ids, s_ch, s_tok, bits, Y, stream=None):
+        where, dev, f32, i32, bf = "block_norm", self.device, self._f32, self._i32, self._torch.bfloat16
+        both = (_F32, _BF16)
+        ldh = self._rows(where, "H", H, both, (None, None))[0]
+        M, C = H.shape
+        h_dtype = OUT_BF16 if H.dtype is bf else OUT_F32
+        ldo = ldho = ldy = C
+        o_dtype = y_dtype = OUT_F32
+        if O is not None:
+            ldo = self._rows(where, "O", O, both, (M, C))[0]
+            o_dtype = OUT_BF16 if O.dtype is bf else OUT_F32
+        if Hout is not None:
+            ldho = self._rows(where, "Hout", Hout, (_BF16,) if h_dtype else (_F32,), (M, C))[0]
+        if Y is not None:
+            if Y.dtype is self._torch.int8:
+                check_rows(where, dev, "Y", Y, (_I8,), (M, C), 1)
+                ldy, y_dtype = Y.stride(0), OUT_INT8
+            else:
+                ldy = self._rows(where, "Y", Y, both, (M, C))[0]
+                y_dtype = OUT_BF16 if Y.dtype is bf else OUT_F32
+        if M == 1:                                       # the stride of a single row means nothing
+            ldh = ldo = ldho = ldy = C
+        G = ldc = c_dtype = 0
+        for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+            if t is None:
+                continue
+            ld = self._rows(where, name, t, both, (G or None, C))[0]
+            if G and ((ld != ldc and G > 1) or t.dtype is not kind):
+                raise StwqError(ERR_DIM, where, "gate, scale and shift have one type and one row stride")
+            G, ldc, kind = t.shape[0], ld, t.dtype
+            c_dtype = OUT_BF16 if kind is bf else OUT_F32
+        if cond_ids is None and G > 1:
+            raise StwqError(ERR_NULL, where, "cond_ids is None, and the conditioning has more than one row")
+        if G == 1:
+            ldc = C
+        P = s_tok.numel() if s_tok is not None else 0
+        for name, t, n, kind in (("cond_ids", cond_ids, M, i32), ("pos_ids", pos_ids, M, i32), ("w_post", w_post, C, f32), ("b_post", b_post, C, f32),
+                                 ("w_pre", w_pre, C, f32), ("b_pre", b_pre, C, f32), ("s_ch", s_ch, C, f32), ("s_tok", s_tok, P, f32)):
+            if t is not None and not _ok(t, kind, (n,), dev):
+                self._args(where, (name, t, _I32 if kind is i32 else _F32, (n,), True))
+        q = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        rc = self._L.block_norm(self._h, H.data_ptr(), ldh, h_dtype, q(O), ldo, o_dtype, M, C, q(cond_ids), G, q(gate), q(scale), q(shift), ldc,
+                                c_dtype, post_norm, q(w_post), q(b_post), res_scale, pre_norm, q(w_pre), q(b_pre), eps, q(Hout), ldho, q(pos_ids),
+                                q(s_ch), q(s_tok), P, bits, q(Y), ldy, y_dtype, self._raw_stream(stream))
+        if rc:
+            self._check(rc, where)
+
+    def gps_fold_group4(self, W, s_ch, Wp, s_g, stream=None):
+        N, K = _mk(W, "W")
+        n, groups = _mk(s_g, "s_g")
+        bf = s_g.dtype is self._torch.bfloat16
+        if groups <= 0 or K % groups:
+            raise StwqError(ERR_DIM, "gps_fold_group4", f"s_g has {groups} groups, which do not divide {K} channels")
+        self._args("gps_fold_group4", ("W", W, _F32, (N, K), False), ("s_ch", s_ch, _F32, (K,), True), ("Wp", Wp, _U8, (N, K // 2), False),
+                   ("s_g", s_g, _BF16 if bf else _F32, (N, groups), False))
+        self._check(self._L.gps_fold_group4(self._h, _p(W), N, K, _p(s_ch), K // groups, _p(Wp), _p(s_g), OUT_BF16 if bf else OUT_F32,
+                                            self._stream(stream)), "gps_fold_group4")
+
+    def linear_w4g(self, X, Wp, s_g, bias, act, out_dtype, Y, stream=None):
+        where, dev, f32, bf = "linear_w4g", self.device, self._f32, self._torch.bfloat16
+        ldx = self._rows(where, "X", X, (_F32, _BF16), (None, None))[0]
+        M, K = X.shape
+        N, groups = _mk(s_g, "s_g")
+        if groups <= 0 or K % groups:
+            raise StwqError(ERR_DIM, where, f"s_g has {groups} groups, which do not divide {K} channels")
+        if out_dtype not in (OUT_F32, OUT_BF16):
+            raise StwqError(ERR_BITS, where, f"out_dtype {out_dtype} is not OUT_F32 / OUT_BF16")
+        s_bf = s_g.dtype is bf
+        if not (_ok(Wp, self._torch.uint8, (N, K // 2), dev) and _ok(s_g, bf if s_bf else f32, (N, groups), dev)
+                and (bias is None or _ok(bias, f32, (N,), dev)) and _ok(Y, bf if out_dtype else f32, (M, N), dev)):
+            self._args(where, ("Wp", Wp, _U8, (N, K // 2), False), ("s_g", s_g, _BF16 if s_bf else _F32, (N, groups), False),
+                       ("bias", bias, _F32, (N,), True), ("Y", Y, _OUT_DTYPES[out_dtype], (M, N), False))
+        rc = self._L.linear_w4g(self._h, X.data_ptr(), ldx if M > 1 else K, OUT_BF16 if X.dtype is bf else OUT_F32, M, K, N, Wp.data_ptr(),
+                                s_g.data_ptr(), OUT_BF16 if s_bf else OUT_F32, K // groups, None if bias is None else bias.data_ptr(), act,
+                                out_dtype, Y.data_ptr(), self._raw_stream(stream))
+        if rc:
+            self._check(rc, where)
+
+    def token_logprobs(self, logits, temperature, tokens, logprobs, ranks=None, entropy=None, top_ids=None, top_logprobs=None, stream=None):
+        where, dev, i32, f32 = "token_logprobs", self.device, self._i32, self._f32
+        ld = self._rows(where, "logits", logits, (_F32, _BF16), (None, None))[0]
+        B, V = logits.shape
+        n, k = (B,), 0
+        if top_ids is not None:
+            k = _mk(top_ids, "top_ids")[1]
+        if not ((temperature is None or _ok(temperature, f32, n, dev)) and (tokens is None or _ok(tokens, i32, n, dev))
+                and (logprobs is None or _ok(logprobs, f32, n, dev)) and (ranks is None or _ok(ranks, i32, n, dev))
+                and (entropy is None or _ok(entropy, f32, n, dev)) and (top_ids is None or _ok(top_ids, i32, (B, k), dev))
+                and (top_logprobs is None or _ok(top_logprobs, f32, (B, k), dev))):
+            self._args(where, ("temperature", temperature, _F32, n, True), ("tokens", tokens, _I32, n, True), ("logprobs", logprobs, _F32, n, True),
+                       ("ranks", ranks, _I32, n, True), ("entropy", entropy, _F32, n, True), ("top_ids", top_ids, _I32, (B, k), True),
+                       ("top_logprobs", top_logprobs, _F32, (B, k), True))
+        q = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        rc = self._L.token_logprobs(self._h, logits.data_ptr(), OUT_BF16 if logits.dtype is self._torch.bfloat16 else OUT_F32,
+                                    max(ld, V) if B == 1 else ld, B, V, q(temperature), q(tokens), q(logprobs), q(ranks), q(entropy), k, q(top_ids),
+                                    q(top_logprobs), self._raw_stream(stream))
+        if rc:
+            self._check(rc, where)
 
     def _quantize_specs(self, X, x_dtype, pos_ids, s_ch, s_tok, Xq):
         M, K = _mk(X)

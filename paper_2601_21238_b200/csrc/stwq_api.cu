@@ -581,6 +581,7 @@ int stwq_device_status(stwq_ctx* ctx, void* stream)
     if (h & STWQ_DEV_POS_RANGE) return STWQ_ERR_POS_RANGE;
     if (h & STWQ_DEV_NONFINITE) return STWQ_ERR_NONFINITE;
     if (h & STWQ_DEV_PAGES) return STWQ_ERR_PAGES;
+    if (h & STWQ_DEV_TOKEN) return STWQ_ERR_TOKEN;
     return STWQ_OK;
 }
 
@@ -606,6 +607,7 @@ const char* stwq_strerror(int status)
         case STWQ_ERR_NOMEM: return "workspace allocation failed";
         case STWQ_ERR_CAPTURE: return "workspace would have to grow during stream capture (reserve it first)";
         case STWQ_ERR_PAGES: return "a length, page id, slot or block-table entry was out of range";
+        case STWQ_ERR_TOKEN: return "a given token was outside [-1, V)";
         default: return "unknown status";
     }
 }

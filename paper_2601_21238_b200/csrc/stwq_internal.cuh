@@ -11,6 +11,7 @@
 #define STWQ_DEV_NONFINITE 2u
 #define STWQ_DEV_TIMEOUT 4u
 #define STWQ_DEV_PAGES 8u
+#define STWQ_DEV_TOKEN 16u
 
 struct stwq_ctx {
     int device;
