@@ -4,240 +4,381 @@
 //     h' = h + r g (Npost(o) wp + bp),   y = (Npre(h') w + b) (1 + scale) + shift,
 //     N: x / sqrt(mean(x^2) + eps), or (x - m) / sqrt(mean((x - m)^2) + eps) with m = mean(x), or x
 //     out: y, y (1/s_ch), or the codes clamp(round((y rc) rt)), rc = 1/s_ch, rt = 1/s_tok[pos]
-// Each row is read once and stays in registers: a mean and a sum of squares are one reduction each over the threads of the
-// row, the squares are those of the centred values. Bound by HBM: |h| + |o| in, |h'| + |y| out; the vectors of C channels
-// (weights, gate, scale, shift) come from L1 and L2, which is why a group of threads takes consecutive rows.
+// Each row is read once: its 16-byte pieces are copied asynchronously into shared memory while the rows before it are worked on, and
+// its channels stay in registers from there on. A mean and a sum of squares are one reduction each over the threads of the row; the
+// squares are those of the centred values. Vectors of C channels (weights, gate, scale, shift) come from L1 and L2.
+// Bound: HBM asks for |h| + |o| in, |h'| + |y| out. 65536 rows of 1280 (fp32 stream, bf16 branch and output) take 169 us, 6.0 TB/s, 0.91 of
+// the measured copy rate; with everything in bf16 the instructions count (some 25 per channel and lane, issue slots half busy, 16 warps of up
+// to 128 registers on an SM): 8192 rows of 1920 30 us, 4.2 TB/s; 20000 of 1024 with two weighted norms 38 us, 4.4 TB/s.
 #include <cuda_bf16.h>
 
 #include "stwq_internal.cuh"
 #include "stwq_paged.cuh"
+#include "stwq_ptx.cuh"
+
+using namespace stwq_ptx;       // packed fp32 arithmetic
 
 namespace {
 
 constexpr int kMaxC = 16384;
 constexpr int kMaxThreads = 512;           // of one row
-constexpr int kWarpRows = 4;               // rows a block works on where a warp holds a row
+constexpr int kTeams = 4;                  // rows a block works on at a time, where a warp holds a row
+constexpr int kMaxRows = 32;               // rows of a team in turn: a lane keeps the ids of one
 
 struct BnParams {
     const void *H, *O, *gate, *scale, *shift;
     void *Ho, *Y;
     int64_t ldh, ldo, ldc, ldho, ldy, M;
-    int C, G, P, h_bf, o_bf, c_bf, y_dtype, post, pre, qmin, qmax, rows;
+    int C, G, P, y_dtype, post, pre, qmin, qmax, rows, depth;
     const int32_t *cond, *pos;
     const float *wp, *bp, *w, *b, *s_ch, *s_tok;
     float res_scale, eps, inv_C;
     uint32_t* status;
 };
 
-// Eight elements from `at` on. Rows are read with plain loads: the outputs may replace them.
-__device__ __forceinline__ void load8(const void* base, int64_t at, int bf, float (&v)[8])
-{
-    if (bf) {
-        const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(base) + at);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// Eight channels. Two fp32 values per instruction where there is one for it; each half rounds as the scalar instruction does.
+struct F8 {
+    uint64_t p[4];
+    __device__ __forceinline__ void fill(float v)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    } else {
-        const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + at);
-        const float4 a = q[0], b = q[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        for (int i = 0; i < 4; ++i) p[i] = dup_f2(v);
     }
-}
-__device__ __forceinline__ void store8(void* base, int64_t at, int bf, const float (&v)[8])
-{
-    if (bf) {
-        uint32_t w[4];
+    template <bool BF>
+    __device__ __forceinline__ void widen(const uint4& a, const uint4& b)
+    {
+        if (BF) {
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&b);
+            for (int i = 0; i < 4; ++i) p[i] = pack_f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+        } else {
+            p[0] = pack_f2(__uint_as_float(a.x), __uint_as_float(a.y));
+            p[1] = pack_f2(__uint_as_float(a.z), __uint_as_float(a.w));
+            p[2] = pack_f2(__uint_as_float(b.x), __uint_as_float(b.y));
+            p[3] = pack_f2(__uint_as_float(b.z), __uint_as_float(b.w));
         }
-        *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(base) + at) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-        float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(base) + at);
-        q[0] = make_float4(v[0], v[1], v[2], v[3]);
-        q[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
+    template <bool BF>
+    __device__ __forceinline__ void store(char* at) const
+    {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack_f2(p[i], v[2 * i], v[2 * i + 1]);
+        if (BF) *reinterpret_cast<uint4*>(at) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        else {
+            reinterpret_cast<float4*>(at)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4*>(at)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+    }
+};
+__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
+#define STWQ_EACH(v) _Pragma("unroll") for (int v = 0; v < VPT; ++v)
+#define STWQ_PAIRS(i) _Pragma("unroll") for (int i = 0; i < 4; ++i)
 
-// Sum over the threads of a row, the same value in all of them, added in a fixed order. `red` holds two sets of one value per
-// warp, used in turn: no warp writes a set again before all have passed the barrier of the other one.
-template <bool WARP>
-__device__ __forceinline__ float row_sum(float v, float (*red)[kMaxThreads / 32], int& turn)
+// A warp holds VPT vectors of 256 consecutive channels of a row, a lane eight channels of each: vector v of a lane starts
+// 256 v channels behind its first. on[v]: whether it lies in the row.
+template <int VPT, bool BF>
+struct Side {                              // of a vector of C channels that no call writes, as it lies in memory
+    uint4 q[VPT][BF ? 1 : 2];
+    // KEEP false: an ordinary load, which the compiler does not carry from row to row in registers (that costs more by the warps it displaces)
+    template <bool KEEP>
+    __device__ __forceinline__ void load(const void* lane0, const bool (&on)[VPT])
+    {
+        STWQ_EACH(v)
+#pragma unroll
+            for (int i = 0; i < (BF ? 1 : 2); ++i) {
+                const uint4* src = reinterpret_cast<const uint4*>(lane0) + v * (BF ? 32 : 64) + i;
+                q[v][i] = make_uint4(0u, 0u, 0u, 0u);         // left undefined it would live from row to row
+                if (on[v]) {
+                    if (KEEP) q[v][i] = __ldg(src);
+                    else asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q[v][i].x), "=r"(q[v][i].y), "=r"(q[v][i].z), "=r"(q[v][i].w) : "l"(src) : "memory");
+                }
+            }
+    }
+    __device__ __forceinline__ F8 get(int v) const
+    {
+        F8 x;
+        x.widen<BF>(q[v][0], q[v][BF ? 0 : 1]);
+        return x;
+    }
+};
+
+// A warp's part of a row in shared memory, copied 16 bytes at a time: lane l copies piece 32 i + l. bf16: a piece is a lane's
+// vector; fp32: pieces 2l and 2l + 1 are, and every other four lanes' pieces change places, so that reads of eight lanes do not meet.
+template <int VPT, bool BF>
+struct Slot {
+    static constexpr int kBytes = VPT * (BF ? 512 : 1024);       // of a warp
+    // `row`: the warp's first channel; `left`: bytes from there to the end of the row
+    __device__ __forceinline__ static void fetch(uint32_t slot, const char* row, int left, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < kBytes / 512; ++i) {
+            const int at = i * 512 + 16 * lane;
+            const uint32_t to = slot + i * 512 + 16 * (BF ? lane : lane ^ ((lane >> 3) & 1));
+            if (at < left) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + at) : "memory");
+        }
+    }
+    __device__ __forceinline__ static F8 read(const char* slot, int v, int lane)
+    {
+        F8 x;
+        const uint4* q = reinterpret_cast<const uint4*>(slot) + v * (BF ? 32 : 64);
+        if (BF) {
+            const uint4 a = q[lane];
+            x.widen<BF>(a, a);
+        } else {
+            const int turned = (lane >> 2) & 1;
+            x.widen<BF>(q[2 * lane + turned], q[2 * lane + 1 - turned]);
+        }
+        return x;
+    }
+};
+
+// The sum over a row, in all its threads, added in a fixed order. The two sets of `red` are used in turn: no warp writes a set
+// again before all have passed the barrier of the other.
+template <bool MULTI>
+__device__ __forceinline__ float row_sum(uint64_t v2, float (*red)[kMaxThreads / 32], int& turn)
 {
+    float a, b;
+    unpack_f2(v2, a, b);
+    float v = a + b;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (WARP) return v;
-    float* r = red[turn];
+    if (!MULTI) return v;
+    float* set = red[turn];
     turn ^= 1;
-    if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = v;
+    if ((threadIdx.x & 31) == 0) set[threadIdx.x >> 5] = v;
     __syncthreads();
     float s = 0.0f;
-    for (int i = 0; i < (int)(blockDim.x >> 5); i += 4) {           // sets are padded with zeros
-        const float4 q = *reinterpret_cast<const float4*>(r + i);
+    for (int i = 0; i < (int)(blockDim.x >> 5); i += 4) {          // sets are padded with zeros
+        const float4 q = *reinterpret_cast<const float4*>(set + i);
         s += (q.x + q.y) + (q.z + q.w);
     }
     return s;
 }
 
-// x <- N(x) w + b
-template <int VPT, bool WARP>
-__device__ __forceinline__ void normalise(float (&x)[VPT][8], int kind, const float* w, const float* b, const BnParams& p, int tid, int nt,
+// x <- N(x) w + b. Channels beyond the row hold zeros before, and anything after.
+template <int VPT, bool MULTI>
+__device__ __forceinline__ void normalise(F8 (&x)[VPT], const bool (&on)[VPT], int kind, const float* w, const float* b, int lane0, const BnParams& p,
                                           float (*red)[kMaxThreads / 32], int& turn)
 {
-    float mean = 0.0f, r = 1.0f;
     if (kind == STWQ_NORM_LAYER) {
-        float s = 0.0f;
-#pragma unroll
-        for (int v = 0; v < VPT; ++v)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += x[v][i];               // vectors beyond the row hold zeros
-        mean = row_sum<WARP>(s, red, turn) * p.inv_C;
+        uint64_t s = dup_f2(0.0f);
+        STWQ_EACH(v) STWQ_PAIRS(i) s = add_f2(s, x[v].p[i]);
+        const uint64_t m = dup_f2(-row_sum<MULTI>(s, red, turn) * p.inv_C);
+        STWQ_EACH(v) if (on[v]) STWQ_PAIRS(i) x[v].p[i] = add_f2(x[v].p[i], m);
     }
     if (kind != STWQ_NORM_NONE) {
-        float s = 0.0f;
-#pragma unroll
-        for (int v = 0; v < VPT; ++v)
-            if ((v * nt + tid) * 8 < p.C)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float d = x[v][i] - mean;
-                    s = fmaf(d, d, s);
-                }
-        r = rsqrtf(fmaf(row_sum<WARP>(s, red, turn), p.inv_C, p.eps));
+        uint64_t q = dup_f2(0.0f);
+        STWQ_EACH(v) STWQ_PAIRS(i) q = fma_f2(x[v].p[i], x[v].p[i], q);
+        const uint64_t r = dup_f2(rsqrtf(fmaf(row_sum<MULTI>(q, red, turn), p.inv_C, p.eps)));
+        STWQ_EACH(v) STWQ_PAIRS(i) x[v].p[i] = mul_f2(x[v].p[i], r);
     }
-#pragma unroll
-    for (int v = 0; v < VPT; ++v) {
-        const int e0 = (v * nt + tid) * 8;
-        if (e0 >= p.C) break;
-        float a[8];
-        if (kind != STWQ_NORM_NONE)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[v][i] = (x[v][i] - mean) * r;
-        if (w != nullptr) {
-            load8(w, e0, 0, a);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[v][i] *= a[i];
+    if (w != nullptr) {
+        Side<VPT, false> f;
+        f.template load<false>(w + lane0, on);
+        STWQ_EACH(v) {
+            const F8 a = f.get(v);
+            STWQ_PAIRS(i) x[v].p[i] = mul_f2(x[v].p[i], a.p[i]);
         }
-        if (b != nullptr) {
-            load8(b, e0, 0, a);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[v][i] += a[i];
+    }
+    if (b != nullptr) {
+        Side<VPT, false> f;
+        f.template load<false>(b + lane0, on);
+        STWQ_EACH(v) {
+            const F8 a = f.get(v);
+            STWQ_PAIRS(i) x[v].p[i] = add_f2(x[v].p[i], a.p[i]);
         }
     }
 }
 
-// VPT vectors of eight channels per thread; WARP: a warp holds a row, else the block does.
-template <int VPT, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) block_norm_kernel(const BnParams p)
+// A team (a warp, or with MULTI the warps of a block) goes through its rows with the next `depth` on their way into its slots
+// (two, or one where two do not fit).
+template <int VPT, bool MULTI, bool HB, bool OB, bool CB>
+__global__ void __launch_bounds__(MULTI ? kMaxThreads : 32 * kTeams, MULTI ? (VPT == 1 ? 2 : 1) : VPT == 1 ? 8 : 4) block_norm_kernel(const BnParams p)
 {
     __shared__ __align__(16) float red[2][kMaxThreads / 32];
-    const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, nt = WARP ? 32 : blockDim.x;
-    const int64_t group = WARP ? (int64_t)blockIdx.x * kWarpRows + (threadIdx.x >> 5) : blockIdx.x;
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int teams = MULTI ? 1 : kTeams, me = MULTI ? 0 : warp;
+    const int first = MULTI ? warp * (256 * VPT) : 0, lane0 = first + 8 * lane;   // first channel of the warp, of the lane
+    const int slot_bytes = Slot<VPT, HB>::kBytes + (p.O != nullptr ? Slot<VPT, OB>::kBytes : 0);
+    char* slots = smem + warp * p.depth * slot_bytes;
+    float* rc = reinterpret_cast<float*>(smem + warps * p.depth * slot_bytes);    // [C] 1 / s_ch
+    if (MULTI && threadIdx.x < 2 * (kMaxThreads / 32)) (&red[0][0])[threadIdx.x] = 0.0f;
+    if (p.s_ch != nullptr)
+#pragma unroll 4
+        for (int i = threadIdx.x; i < p.C / 4; i += blockDim.x) {
+            const float4 f = __ldg(reinterpret_cast<const float4*>(p.s_ch) + i);
+            reinterpret_cast<float4*>(rc)[i] = make_float4(__frcp_rn(f.x), __frcp_rn(f.y), __frcp_rn(f.z), __frcp_rn(f.w));
+        }
+    bool on[VPT];
+    STWQ_EACH(v) on[v] = lane0 + 256 * v < p.C;
     int turn = 0;
-    if (!WARP) {
-        if (threadIdx.x < 2 * (kMaxThreads / 32)) (&red[0][0])[threadIdx.x] = 0.0f;
-        __syncthreads();
-    }
-    const int64_t r1 = min(p.M, (group + 1) * p.rows);
-    for (int64_t row = group * p.rows; row < r1; ++row) {
-        const int pos = p.pos != nullptr ? p.pos[row] : 0;
-        if (pos == -1) continue;                                    // a padding row
-        int g = p.cond != nullptr ? p.cond[row] : 0;
-        const bool bad_g = g < 0 || g >= p.G, bad_pos = p.y_dtype == STWQ_OUT_INT8 && (pos < 0 || pos >= p.P);
-        if ((bad_g || bad_pos) && tid == 0) atomicOr(p.status, STWQ_DEV_POS_RANGE);
-        if (bad_g) g = 0;
-        const int64_t gc = g * p.ldc;
 
-        float h[VPT][8];
-#pragma unroll
-        for (int v = 0; v < VPT; ++v) {
-            const int e0 = (v * nt + tid) * 8;
-            if (e0 < p.C) load8(p.H, row * p.ldh + e0, p.h_bf, h[v]);
-            else
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] = 0.0f;
+    // a block's rows are consecutive, its teams take them in turn; a lane keeps what goes with one row of its team: bit or lane j, row j
+    const int64_t row0 = (int64_t)blockIdx.x * p.rows * teams + me, my_row = row0 + (int64_t)lane * teams;
+    const bool mine = lane < p.rows && my_row < p.M, codes = p.y_dtype == STWQ_OUT_INT8;
+    const int my_pos = mine && p.pos != nullptr ? p.pos[my_row] : 0;
+    int my_cond = mine && p.cond != nullptr ? p.cond[my_row] : 0;
+    const uint32_t live = __ballot_sync(0xffffffffu, mine && my_pos != -1);       // not behind the last row, not padding
+    const uint32_t bad_g = __ballot_sync(0xffffffffu, mine && my_pos != -1 && (my_cond < 0 || my_cond >= p.G));
+    const uint32_t bad_y = bad_g | __ballot_sync(0xffffffffu, mine && codes && my_pos != -1 && (my_pos < 0 || my_pos >= p.P));
+    if (bad_y != 0u && lane0 == 0) atomicOr(p.status, STWQ_DEV_POS_RANGE);
+    if ((bad_g >> lane) & 1u) my_cond = 0;
+    const float my_rt = codes && mine && my_pos >= 0 && my_pos < p.P ? __frcp_rn(p.s_tok[my_pos]) : 1.0f;
+
+    // running addresses: of the next row to fetch, of the row at hand
+    constexpr int kH = HB ? 2 : 4, kO = OB ? 2 : 4;
+    const char* h_next = reinterpret_cast<const char*>(p.H) + (row0 * p.ldh + first) * kH;
+    const char* o_next = reinterpret_cast<const char*>(p.O) + (row0 * p.ldo + first) * kO;
+    char* ho = reinterpret_cast<char*>(p.Ho) + (row0 * p.ldho + lane0) * kH;
+    const int y_bytes = codes ? 1 : p.y_dtype == STWQ_OUT_BF16 ? 2 : 4;
+    char* y = reinterpret_cast<char*>(p.Y) + (row0 * p.ldy + lane0) * y_bytes;
+    const int64_t h_step = p.ldh * teams * kH, o_step = p.ldo * teams * kO, ho_step = p.ldho * teams * kH, y_step = p.ldy * teams * y_bytes;
+    uint32_t to = smem_u32(slots), coming = live;                 // where the next row goes; bit 0: whether it is a live one
+    const uint32_t flip = p.depth > 1 ? to ^ (to + slot_bytes) : 0u;
+    auto fetch = [&]() {
+        if (coming & 1u) {
+            Slot<VPT, HB>::fetch(to, h_next, (p.C - first) * kH, lane);
+            if (p.O != nullptr) Slot<VPT, OB>::fetch(to + Slot<VPT, HB>::kBytes, o_next, (p.C - first) * kO, lane);
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        coming >>= 1;
+        h_next += h_step;
+        o_next += o_step;
+        to ^= flip;
+    };
+    // what no row fills stays zero
+    for (int i = lane; i < p.depth * slot_bytes / 16; i += 32) reinterpret_cast<uint4*>(slots)[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncwarp();
+    fetch();
+    if (p.depth > 1) fetch();
+    if (MULTI || p.s_ch != nullptr) __syncthreads();
+
+    const char* slot = slots;
+    const int slot_step = p.depth > 1 ? slot_bytes : 0;
+#pragma unroll 1
+    for (int j = 0; j < 32 && (live >> j) != 0u; ++j, ho += ho_step, y += y_step) {
+        const char* here = slot + (j & 1) * slot_step;
+        if (!((live >> j) & 1u)) {                                // the same in all threads of the team
+            fetch();
+            continue;
+        }
+        const int64_t side = (__shfl_sync(0xffffffffu, my_cond, j) * p.ldc + lane0) * (CB ? 2 : 4);
+        Side<VPT, CB> gate;
+        if (p.gate != nullptr) gate.template load<true>(reinterpret_cast<const char*>(p.gate) + side, on);
+        if (p.depth > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();                                             // the pieces that other lanes copied
+        F8 h[VPT];
+        STWQ_EACH(v) h[v] = Slot<VPT, HB>::read(here, v, lane);
         if (p.O != nullptr) {
-            float o[VPT][8];
-#pragma unroll
-            for (int v = 0; v < VPT; ++v) {
-                const int e0 = (v * nt + tid) * 8;
-                if (e0 < p.C) load8(p.O, row * p.ldo + e0, p.o_bf, o[v]);
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[v][i] = 0.0f;
-            }
-            normalise<VPT, WARP>(o, p.post, p.wp, p.bp, p, tid, nt, red, turn);
-#pragma unroll
-            for (int v = 0; v < VPT; ++v) {
-                const int e0 = (v * nt + tid) * 8;
-                if (e0 >= p.C) break;
-                float a[8];
-                if (p.gate != nullptr) load8(p.gate, gc + e0, p.c_bf, a);
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) a[i] = 1.0f;
-                if (!bad_g)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) h[v][i] = fmaf(p.res_scale * a[i], o[v][i], h[v][i]);
-                if (p.Ho != nullptr) store8(p.Ho, row * p.ldho + e0, p.h_bf, h[v]);
-            }
+            F8 o[VPT];
+            STWQ_EACH(v) o[v] = Slot<VPT, OB>::read(here + Slot<VPT, HB>::kBytes, v, lane);
+            normalise<VPT, MULTI>(o, on, p.post, p.wp, p.bp, lane0, p, red, turn);
+            const uint64_t f = dup_f2(p.res_scale);
+            if (p.gate != nullptr)
+                STWQ_EACH(v)
+                {
+                    const F8 g = gate.get(v);
+                    STWQ_PAIRS(i) o[v].p[i] = mul_f2(o[v].p[i], g.p[i]);
+                }
+            if (!((bad_g >> j) & 1u)) STWQ_EACH(v) if (on[v]) STWQ_PAIRS(i) h[v].p[i] = fma_f2(f, o[v].p[i], h[v].p[i]);
+            if (p.Ho != nullptr) STWQ_EACH(v) if (on[v]) h[v].template store<HB>(ho + v * 256 * kH);
         }
+        __syncwarp();                                             // all lanes have read the slot
+        fetch();
         if (p.Y == nullptr) continue;
-        normalise<VPT, WARP>(h, p.pre, p.w, p.b, p, tid, nt, red, turn);
-        const float rt = p.y_dtype == STWQ_OUT_INT8 && !bad_pos ? __frcp_rn(p.s_tok[pos]) : 1.0f;
-#pragma unroll
-        for (int v = 0; v < VPT; ++v) {
-            const int e0 = (v * nt + tid) * 8;
-            if (e0 >= p.C) break;
-            float a[8];
-            if (p.scale != nullptr) {
-                load8(p.scale, gc + e0, p.c_bf, a);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] *= 1.0f + a[i];
+        Side<VPT, CB> scale, shift;
+        if (p.scale != nullptr) scale.template load<true>(reinterpret_cast<const char*>(p.scale) + side, on);
+        if (p.shift != nullptr) shift.template load<true>(reinterpret_cast<const char*>(p.shift) + side, on);
+        normalise<VPT, MULTI>(h, on, p.pre, p.w, p.b, lane0, p, red, turn);
+        if (p.scale != nullptr) {
+            const uint64_t one = dup_f2(1.0f);
+            STWQ_EACH(v)
+            {
+                const F8 a = scale.get(v);
+                STWQ_PAIRS(i) h[v].p[i] = mul_f2(h[v].p[i], add_f2(a.p[i], one));
             }
-            if (p.shift != nullptr) {
-                load8(p.shift, gc + e0, p.c_bf, a);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] += a[i];
-            }
-            if (p.s_ch != nullptr) {
-                load8(p.s_ch, e0, 0, a);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] = __fmul_rn(h[v][i], __frcp_rn(a[i]));
-            }
-            if (bad_g || bad_pos)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] = 0.0f;
-            if (p.y_dtype == STWQ_OUT_INT8) {
-                uint32_t w[2] = {0u, 0u};
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    w[i >> 2] |= (uint32_t)(stwq_code(__fmul_rn(h[v][i], rt), p.qmin, p.qmax) & 0xFF) << (8 * (i & 3));
-                *reinterpret_cast<uint2*>(reinterpret_cast<int8_t*>(p.Y) + row * p.ldy + e0) = make_uint2(w[0], w[1]);
-            } else store8(p.Y, row * p.ldy + e0, p.y_dtype == STWQ_OUT_BF16, h[v]);
         }
+        if (p.shift != nullptr)
+            STWQ_EACH(v)
+            {
+                const F8 a = shift.get(v);
+                STWQ_PAIRS(i) h[v].p[i] = add_f2(h[v].p[i], a.p[i]);
+            }
+        if (p.s_ch != nullptr)
+            STWQ_EACH(v) if (on[v])
+            {
+                const uint4* q = reinterpret_cast<const uint4*>(rc + lane0 + 256 * v);
+                F8 a;
+                a.widen<false>(q[0], q[1]);
+                STWQ_PAIRS(i) h[v].p[i] = mul_f2(h[v].p[i], a.p[i]);
+            }
+        if ((bad_y >> j) & 1u) STWQ_EACH(v) h[v].fill(0.0f);
+        if (codes) {
+            const uint64_t rt = dup_f2(__shfl_sync(0xffffffffu, my_rt, j));
+            STWQ_EACH(v) if (on[v])
+            {
+                uint32_t w[2] = {0u, 0u};
+                STWQ_PAIRS(i)
+                {
+                    float u0, u1;
+                    unpack_f2(mul_f2(h[v].p[i], rt), u0, u1);
+                    w[i >> 1] |= ((uint32_t)(stwq_code(u0, p.qmin, p.qmax) & 0xFF) | (uint32_t)(stwq_code(u1, p.qmin, p.qmax) & 0xFF) << 8) << (16 * (i & 1));
+                }
+                *reinterpret_cast<uint2*>(y + 256 * v) = make_uint2(w[0], w[1]);
+            }
+        } else if (y_bytes == 2) STWQ_EACH(v) { if (on[v]) h[v].template store<true>(y + 512 * v); }
+        else STWQ_EACH(v) { if (on[v]) h[v].template store<false>(y + 1024 * v); }
     }
 }
 
-template <int VPT, bool WARP>
+template <int VPT, bool MULTI, bool HB, bool OB, bool CB>
 int launch_bn(stwq_ctx* ctx, BnParams& p, int threads, cudaStream_t st)
 {
-    // consecutive rows per group while the groups still fill the GPU once
-    const int64_t per_sm = WARP ? 2048 / 32 : 2048 / threads, slots = per_sm * ctx->sm_count;
-    int64_t rows = (p.M + slots - 1) / slots;
-    if (rows > 8) rows = 8;
-    p.rows = (int)rows;
-    const int64_t groups = (p.M + rows - 1) / rows, blocks = WARP ? (groups + kWarpRows - 1) / kWarpRows : groups;
-    block_norm_kernel<VPT, WARP><<<(unsigned)blocks, WARP ? 32 * kWarpRows : threads, 0, st>>>(p);
+    const int teams = MULTI ? 1 : kTeams, block = MULTI ? threads : 32 * kTeams;
+    const int slot = (block / 32) * (Slot<VPT, HB>::kBytes + (p.O != nullptr ? Slot<VPT, OB>::kBytes : 0));
+    const size_t side = p.s_ch != nullptr ? (size_t)p.C * 4 : 0;
+    p.depth = (size_t)2 * slot + side <= 220 * 1024 ? 2 : 1;
+    const size_t smem = (size_t)p.depth * slot + side;
+    auto kern = block_norm_kernel<VPT, MULTI, HB, OB, CB>;
+    cudaError_t e = cudaSuccess;
+    if (smem > 40 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+    if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
+    // Rows per team: whole waves of the blocks that fit an SM, by shared memory and registers (64 or up to 128 a thread)
+    int64_t fit = (int64_t)(200 * 1024 / (smem + 1024));
+    const int threads_fit = VPT == 1 ? 1024 : 512;
+    if (fit > threads_fit / block) fit = threads_fit / block;
+    if (fit < 1) fit = 1;
+    const int64_t slots = fit * ctx->sm_count * teams, waves = (p.M + slots * kMaxRows - 1) / (slots * kMaxRows);
+    p.rows = (int)((p.M + slots * waves - 1) / (slots * waves));
+    const int64_t blocks = (p.M + (int64_t)p.rows * teams - 1) / ((int64_t)p.rows * teams);
+    kern<<<(unsigned)blocks, block, smem, st>>>(p);
     ctx->launches += 1;
-    const cudaError_t e = cudaGetLastError();
+    e = cudaGetLastError();
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
+}
+
+// Vectors per thread: with few rows one (a row is done soonest); else two or three, whichever leaves fewer lanes without channels, three
+// where they are equal (8192 rows of 1920: 29 us with 2, 31 with 3, 37 with 4; 65536 of 1280: 189, 169, 169); four where 16 warps need them.
+template <bool HB, bool OB, bool CB>
+int launch_bn_any(stwq_ctx* ctx, BnParams& p, cudaStream_t st)
+{
+    const int warps = (p.C / 8 + 31) / 32;                // with one vector per thread
+    if (warps == 1) return launch_bn<1, false, HB, OB, CB>(ctx, p, 32, st);
+    if (p.M <= 2 * ctx->sm_count && warps <= kMaxThreads / 32) return launch_bn<1, true, HB, OB, CB>(ctx, p, 32 * warps, st);
+    if (warps == 2) return launch_bn<2, false, HB, OB, CB>(ctx, p, 32, st);
+    if (warps == 3) return launch_bn<3, false, HB, OB, CB>(ctx, p, 32, st);
+    const int t2 = (warps + 1) / 2, t3 = (warps + 2) / 3;
+    if (t2 <= kMaxThreads / 32 && 2 * t2 < 3 * t3) return launch_bn<2, true, HB, OB, CB>(ctx, p, 32 * t2, st);
+    if (t3 <= kMaxThreads / 32) return launch_bn<3, true, HB, OB, CB>(ctx, p, 32 * t3, st);
+    return launch_bn<4, true, HB, OB, CB>(ctx, p, 32 * ((warps + 3) / 4), st);
 }
 
 // A matrix of rows: M rows of `width` bytes, `pitch` bytes apart.
@@ -303,7 +444,7 @@ extern "C" int block_norm(stwq_ctx* ctx, const void* H, int64_t ldh, int h_dtype
     p.H = H; p.O = O; p.gate = gate; p.scale = scale; p.shift = shift; p.Ho = Hout; p.Y = Y;
     p.ldh = ldh; p.ldo = ldo; p.ldc = cond ? ldc : 0; p.ldho = ldho; p.ldy = ldy; p.M = M;
     p.C = C; p.G = cond ? G : 1; p.P = P;
-    p.h_bf = h_dtype == STWQ_OUT_BF16; p.o_bf = o_dtype == STWQ_OUT_BF16; p.c_bf = c_dtype == STWQ_OUT_BF16; p.y_dtype = Y ? y_dtype : STWQ_OUT_F32;
+    p.y_dtype = Y ? y_dtype : STWQ_OUT_F32;
     p.post = post_norm; p.pre = pre_norm;
     p.qmax = (1 << (bits == 6 ? 5 : 7)) - 1;
     p.qmin = -p.qmax - 1;
@@ -313,12 +454,15 @@ extern "C" int block_norm(stwq_ctx* ctx, const void* H, int64_t ldh, int h_dtype
     p.status = ctx->d_status;
     StwqDevGuard dev(ctx->device);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int vecs = C / 8;
-    if (vecs <= 32) return launch_bn<1, true>(ctx, p, 32, st);
-    if (vecs <= 64) return launch_bn<2, true>(ctx, p, 32, st);
-    const int vpt = vecs <= kMaxThreads ? 1 : vecs <= 2 * kMaxThreads ? 2 : 4;
-    const int threads = 32 * ((vecs + 32 * vpt - 1) / (32 * vpt));
-    if (vpt == 1) return launch_bn<1, false>(ctx, p, threads, st);
-    if (vpt == 2) return launch_bn<2, false>(ctx, p, threads, st);
-    return launch_bn<4, false>(ctx, p, threads, st);
+    const bool hb = h_dtype == STWQ_OUT_BF16, ob = !O || o_dtype == STWQ_OUT_BF16, cb = !cond || c_dtype == STWQ_OUT_BF16;
+    switch (4 * hb + 2 * ob + cb) {
+        case 0: return launch_bn_any<false, false, false>(ctx, p, st);
+        case 1: return launch_bn_any<false, false, true>(ctx, p, st);
+        case 2: return launch_bn_any<false, true, false>(ctx, p, st);
+        case 3: return launch_bn_any<false, true, true>(ctx, p, st);
+        case 4: return launch_bn_any<true, false, false>(ctx, p, st);
+        case 5: return launch_bn_any<true, false, true>(ctx, p, st);
+        case 6: return launch_bn_any<true, true, false>(ctx, p, st);
+        default: return launch_bn_any<true, true, true>(ctx, p, st);
+    }
 }
