@@ -8,13 +8,13 @@
 // codes widened into shared memory first; here a word of eight codes becomes four bf16 pairs in registers by masks and
 // one subtraction each (0x3e00 | (nibble ^ 8) is 2^-3 + (code + 8) 2^-10 as bf16; less 2^-3 + 2^-7 it is code 2^-10, exactly).
 // The 2^-10 keeps 128 codes times the largest activation inside fp32; it leaves the result at the end (bits below 2^-126 are lost).
-// A lane loads 32 consecutive channels of a row (16 bytes), four lanes 128; the order in which channels meet in a product
-// does not matter as long as both operands keep it, so word i of the four lanes gives the 32 channels of two products.
-// Scales: where a group is a multiple of 128 channels, the products of one 128-channel chunk share it, and the chunk's fp32 sum
-// is scaled once. Finer groups (a multiple of 32) differ between the four lanes; there the eight columns of B are 4 lanes x 2
-// tokens, each column zero outside its lane's channels, so that every lane finds its own group's sums in its own accumulators.
+// A chunk is 128 input channels: 64 bytes of codes of each row, copied asynchronously into a ring of stages that every warp has for
+// itself, with the chunk's activations beside them. The order in which channels meet in a product does not matter as long as both
+// operands keep it. Where a group is a multiple of 128 channels, a lane takes 16 bytes of a row (32 channels), the chunk's products
+// share a scale, and the chunk's fp32 sum is scaled once. Finer groups (a multiple of 32): the four lanes of a row take the four words
+// of one group's 16 bytes together, two products per group, and the sum of each group is scaled.
 // fp32 activations enter as three bf16 parts, cut off bit by bit (8 + 8 + 8 bits: exact), the smallest first.
-// The warps of a block take different chunks of the same rows; their sums meet in shared memory and are added in warp order.
+// The warps of a block take different chunks of the same output channels; their sums meet in shared memory and are added in warp order.
 #include <cuda_bf16.h>
 
 #include "stwq_internal.cuh"
@@ -62,7 +62,8 @@ __global__ void __launch_bounds__(256) fold_group4_kernel(const float* __restric
 struct W4Params {
     const void* X;
     int64_t ldx;
-    int M, K, N, group, per_row, chunks;
+    int M, K, N, per_row, chunks, tiles, stages;
+    uint32_t group32, magic;                // 32-channel units per group, and ceil(2^32 / that): i / group32 = umulhi(i, magic) for i < 2^12
     const uint8_t* Wp;
     const void* s_g;
     int s_bf;
@@ -91,174 +92,323 @@ __device__ __forceinline__ float activate(float z, int act)
     if (act == STWQ_ACT_GELU_ERF) return fabsf(z) == INFINITY ? z * (z > 0.0f ? 1.0f : 0.0f) : apply_act<STWQ_ACT_GELU_ERF>(z);
     return act == STWQ_ACT_GELU_TANH ? apply_act<STWQ_ACT_GELU_TANH>(z) : apply_act<STWQ_ACT_GELU_FAST>(z);
 }
-__device__ __forceinline__ uint4 ld_weights(const uint8_t* p)
+// 16 bytes into shared memory; zeros where `in` is false
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool in)
 {
-    uint4 v;
-    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ uint4 lds128(const char* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// RT: tiles of 16 output channels per warp; MT: tiles of tokens (8, or 2 with FINE groups); XF: X is fp32.
-template <int RT, int MT, bool XF, bool FINE>
-__global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4Params p)
+// A warp's stage: 16 RT rows of 64 bytes of codes, 8 MT rows of 128 activations. 16-byte pieces change places within a row so that
+// the lanes of a read do not meet in a bank (`row`: of the codes or of the activations; `p`: piece).
+template <bool FINE>
+__device__ __forceinline__ int code_piece(int row, int p) { return FINE ? p ^ ((row >> 1) & 3) : p; }
+template <bool XF, bool FINE>
+__device__ __forceinline__ int x_piece(int row, int p)
 {
-    constexpr int kTok = FINE ? 2 : 8;                    // tokens per tile
-    constexpr int kCols = MT * kTok, kRows = RT * 16;
-    extern __shared__ __align__(16) float part[];         // [warps][kRows][kCols]
+    if (FINE) return XF ? p ^ (row & 1) : p ^ ((row & 1) << 2);
+    return XF ? p ^ (((p >> 3) & 3) | ((row & 1) << 2)) : p ^ (((p >> 3) & 1) | ((row & 1) << 1));
+}
+template <int RT, int MT, bool XF>
+struct Stage {
+    static constexpr int kCodes = RT * 1024, kRow = XF ? 512 : 256, kBytes = kCodes + MT * 8 * kRow;
+};
+
+// Where a lane's copies of codes come from: 16-byte piece t of rows g, g + 8, ... of a tile of 16 RT output channels. Rows behind the
+// last output channel repeat it.
+template <int RT>
+struct CodeFeed {
+    const uint8_t* row[RT * 2];
+    int tile, chunk, slot;
+    __device__ __forceinline__ CodeFeed() : slot(0) {}
+    __device__ __forceinline__ void enter(const W4Params& p, int to_tile, int warp, int g, int t)
+    {
+        tile = to_tile;
+        chunk = warp;
+#pragma unroll
+        for (int i = 0; i < RT * 2; ++i) {
+            const int n = min(to_tile * (RT * 16) + i * 8 + g, p.N - 1);
+            row[i] = p.Wp + (int64_t)n * (p.K >> 1) + t * 16;
+        }
+    }
+    template <bool FINE>
+    __device__ __forceinline__ void copy(const W4Params& p, uint32_t to, int g, int t) const
+    {
+        const bool in = chunk * 128 + t * 32 < p.K;      // else zeros; the address stays inside the row
+        const int at = in ? chunk * 64 : -16 * t;
+#pragma unroll
+        for (int i = 0; i < RT * 2; ++i) copy16(to + (uint32_t)((i * 8 + g) * 64 + code_piece<FINE>(i * 8 + g, t) * 16), row[i] + at, in);
+    }
+};
+// The same for the activations: piece q of rows r, r + kStep, ... of the tokens at hand.
+template <int MT, bool XF, bool FINE>
+struct XFeed {
+    static constexpr int kRow = XF ? 512 : 256, kPieces = kRow / 16, kPer = XF ? 4 : 8, kStep = 32 / kPieces, kSize = XF ? 4 : 2;
+    const char* base;                                     // of row r
+    int64_t step;
+    int r, q;
+    __device__ __forceinline__ void enter(const W4Params& p, int m0, int lane)
+    {
+        r = lane / kPieces;
+        q = lane % kPieces;
+        step = p.ldx * (kStep * kSize);
+        base = reinterpret_cast<const char*>(p.X) + (m0 + r) * p.ldx * kSize;
+    }
+    __device__ __forceinline__ void copy(const W4Params& p, uint32_t to, int chunk, int rows) const
+    {
+        const int k = chunk * 128 + q * kPer;
+        const bool in = k < p.K;
+        const char* src = base + (in ? k * kSize : 0);
+#pragma unroll
+        for (int i = 0; i < MT * 8 / kStep; ++i) {
+            const int row = i * kStep + r;
+            if (row < rows) copy16(to + (uint32_t)(row * kRow + x_piece<XF, FINE>(row, q) * 16), src + i * step, in);
+        }
+    }
+};
+template <int RT>
+struct Scales {
+    int64_t row[RT][2];                                   // element offsets of the rows
+    __device__ __forceinline__ void enter(const W4Params& p, int tile, int g)
+    {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) row[r][h] = (int64_t)min(tile * (RT * 16) + r * 16 + h * 8 + g, p.N - 1) * p.per_row;
+    }
+    __device__ __forceinline__ void load(const W4Params& p, int chunk, int t, float (&s)[RT][2]) const
+    {
+        const int unit = min(chunk * 4 + t, p.K / 32 - 1), gi = p.group32 == 1u ? unit : (int)__umulhi((uint32_t)unit, p.magic);
+        if (p.s_bf) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[r][h] = __bfloat162float(__ldg(reinterpret_cast<const __nv_bfloat16*>(p.s_g) + (row[r][h] + gi)));
+        } else {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[r][h] = __ldg(reinterpret_cast<const float*>(p.s_g) + (row[r][h] + gi));
+        }
+    }
+};
+
+// RT: tiles of 16 output channels, MT: tiles of 8 tokens; XF: X is fp32; FINE: groups that are no multiple of 128.
+// A block goes through tiles of 16 RT output channels; its warps take the chunks of 128 input channels in turn, each with its own
+// ring of stages that runs on over the end of a tile.
+template <int RT, int MT, bool XF, bool FINE>
+__global__ void __launch_bounds__(32 * kMaxWarps / RT) linear_w4g_kernel(const W4Params p)
+{
+    using S = Stage<RT, MT, XF>;
+    constexpr int kCols = MT * 8, kRows = RT * 16;
+    extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int g = lane >> 2, t = lane & 3;
-    const int n0 = blockIdx.x * kRows, m0 = blockIdx.y * kCols;
-    const int col = FINE ? (g & 1) : g;                   // the token of this lane's B fragments
-    const bool holds = !FINE || (g >> 1) == t;
+    const int m0 = blockIdx.y * kCols, m_here = min(p.M - m0, kCols);
+    char* ring = smem + warp * p.stages * S::kBytes;
+    float* part = reinterpret_cast<float*>(smem + warps * p.stages * S::kBytes);  // two sets of [warps][kCols][kRows], used in turn
+    // rows of activations that no copy fills stay zero
+    for (int i = lane; i < p.stages * S::kBytes / 16; i += 32) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncwarp();
 
-    float acc[RT][MT][4];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int j = 0; j < MT; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[r][j][i] = 0.0f;
+    CodeFeed<RT> feed;
+    feed.enter(p, (int)blockIdx.x, warp, g, t);
+    XFeed<MT, XF, FINE> xfeed;
+    xfeed.enter(p, m0, lane);
+    const uint32_t ring_u = smem_u32(ring);
+    // copies of the next chunk of this warp, `stages` - 1 ahead of the products; a group even where there is none
+    auto copy = [&]() {
+        if (feed.tile < p.tiles && feed.chunk < p.chunks) {
+            const uint32_t to = ring_u + (uint32_t)(feed.slot * S::kBytes);
+            feed.template copy<FINE>(p, to, g, t);
+            xfeed.copy(p, to + S::kCodes, feed.chunk, m_here);
+            feed.slot = feed.slot + 1 < p.stages ? feed.slot + 1 : 0;
+            feed.chunk += warps;
+            if (feed.chunk >= p.chunks) feed.enter(p, feed.tile + (int)gridDim.x, warp, g, t);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll 1
+    for (int i = 1; i < p.stages; ++i) copy();
+    // scales of this lane's rows and 32 channels, loaded one chunk ahead
+    Scales<RT> scales;
+    scales.enter(p, (int)blockIdx.x, g);
+    float s[RT][2];
+    scales.load(p, min(warp, p.chunks - 1), t, s);
 
-    for (int c = warp; c < p.chunks; c += warps) {
-        const int k = c * 128 + t * 32;
-        const bool in = k < p.K;
-        uint4 w[RT][2];
-        float s[RT][2];
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int64_t n = min(n0 + r * 16 + h * 8 + g, p.N - 1);
-                w[r][h] = in ? ld_weights(p.Wp + (n * p.K + k) / 2) : make_uint4(0u, 0u, 0u, 0u);
-                const int64_t at = n * p.per_row + min(k, p.K - 1) / p.group;
-                s[r][h] = p.s_bf ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p.s_g)[at]) : reinterpret_cast<const float*>(p.s_g)[at];
-            }
-        float sum[RT][MT][4];
+    int slot = 0, turn = 0;
+    for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, turn ^= 1) {
+        float acc[RT][MT][4];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int j = 0; j < MT; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[r][j][i] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {                     // word i: channels 8i .. 8i + 7 of the lane's 32
-            uint32_t a[RT][2][4];
+                for (int i = 0; i < 4; ++i) acc[r][j][i] = 0.0f;
+#pragma unroll 1
+        for (int c = warp; c < p.chunks; c += warps) {
+            copy();
+            if (p.stages == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+            else asm volatile("cp.async.wait_group 2;" ::: "memory");
+            __syncwarp();
+            float now[RT][2];
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const uint32_t lo = i == 0 ? w[r][0].x : i == 1 ? w[r][0].y : i == 2 ? w[r][0].z : w[r][0].w;
-                const uint32_t hi = i == 0 ? w[r][1].x : i == 1 ? w[r][1].y : i == 2 ? w[r][1].z : w[r][1].w;
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    a[r][q][0] = codes2(lo, 2 * q);
-                    a[r][q][1] = codes2(hi, 2 * q);
-                    a[r][q][2] = codes2(lo, 2 * q + 1);
-                    a[r][q][3] = codes2(hi, 2 * q + 1);
-                }
+                now[r][0] = s[r][0];
+                now[r][1] = s[r][1];
             }
+            if (c + warps < p.chunks) scales.load(p, c + warps, t, s);
+            else {
+                scales.enter(p, min(tile + (int)gridDim.x, p.tiles - 1), g);
+                scales.load(p, warp, t, s);
+            }
+            const char* codes = ring + slot * S::kBytes;
+            const char* xs = codes + S::kCodes;
+            uint4 w[RT][2];
+            if (!FINE)
 #pragma unroll
-            for (int j = 0; j < MT; ++j) {
-                const int m = m0 + j * kTok + col;
-                const bool on = in && holds && m < p.M;
-                if constexpr (!XF) {
-                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                    if (on) x = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.X) + m * p.ldx + k + 8 * i));
-                    const uint32_t b[4] = {__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
-                                           __byte_perm(x.y, x.w, 0x7632)};       // channels (0,4), (1,5), (2,6), (3,7)
+                for (int r = 0; r < RT; ++r)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        mma_bf16(sum[r][j], a[r][0], b[0], b[1]);
-                        mma_bf16(sum[r][j], a[r][1], b[2], b[3]);
+                    for (int h = 0; h < 2; ++h) w[r][h] = lds128(codes + (r * 16 + h * 8 + g) * 64 + t * 16);
+            float sum[RT][MT][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                 // 32 channels: word i of the four lanes, or (FINE) the four words of group i
+                if (FINE || i == 0)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+#pragma unroll
+                        for (int j = 0; j < MT; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sum[r][j][e] = 0.0f;
+                uint32_t a[RT][2][4];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    uint32_t v[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int row = r * 16 + h * 8 + g;
+                        v[h] = FINE ? *reinterpret_cast<const uint32_t*>(codes + row * 64 + code_piece<FINE>(row, i) * 16 + t * 4) : word_of(w[r][h], i);
                     }
-                } else {
-                    float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-                    if (on) {
-                        const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.X) + m * p.ldx + k + 8 * i);
-                        const float4 u = __ldg(src), v = __ldg(src + 1);
-                        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
-                        x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+                    for (int q = 0; q < 2; ++q) {
+                        a[r][q][0] = codes2(v[0], 2 * q);
+                        a[r][q][1] = codes2(v[1], 2 * q);
+                        a[r][q][2] = codes2(v[0], 2 * q + 1);
+                        a[r][q][3] = codes2(v[1], 2 * q + 1);
                     }
-                    uint32_t b[3][4];                     // the top, middle and bottom 8 bits of the significands
-                    float rest[8];
+                }
+                const int eight = FINE ? 4 * i + t : 4 * t + i;                   // this lane's eight channels of the chunk
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        rest[e] = x[e] - __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
-                        if (!(fabsf(x[e]) < INFINITY)) rest[e] = 0.0f;           // Inf and NaN stand in the first part alone
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) b[0][e] = __byte_perm(__float_as_uint(x[e]), __float_as_uint(x[e + 4]), 0x7632);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) b[1][e] = __byte_perm(__float_as_uint(rest[e]), __float_as_uint(rest[e + 4]), 0x7632);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) rest[e] -= __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) b[2][e] = __byte_perm(__float_as_uint(rest[e]), __float_as_uint(rest[e + 4]), 0x7632);
-#pragma unroll
-                    for (int q = 2; q >= 0; --q)
+                for (int j = 0; j < MT; ++j) {
+                    const char* xr = xs + (j * 8 + g) * S::kRow;
+                    if constexpr (!XF) {
+                        const uint4 x = lds128(xr + x_piece<XF, FINE>(g, eight) * 16);
+                        const uint32_t b[4] = {__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
+                                               __byte_perm(x.y, x.w, 0x7632)};    // channels (0,4), (1,5), (2,6), (3,7)
 #pragma unroll
                         for (int r = 0; r < RT; ++r) {
-                            mma_bf16(sum[r][j], a[r][0], b[q][0], b[q][1]);
-                            mma_bf16(sum[r][j], a[r][1], b[q][2], b[q][3]);
+                            mma_bf16(sum[r][j], a[r][0], b[0], b[1]);
+                            mma_bf16(sum[r][j], a[r][1], b[2], b[3]);
                         }
+                    } else {
+                        const uint4 u = lds128(xr + x_piece<XF, FINE>(g, 2 * eight) * 16), v = lds128(xr + x_piece<XF, FINE>(g, 2 * eight + 1) * 16);
+                        const uint32_t x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+                        uint32_t b[3][4];                 // the top, middle and bottom 8 bits of the significands
+                        float rest[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            rest[e] = __uint_as_float(x[e]) - __uint_as_float(x[e] & 0xffff0000u);
+                            if (!(fabsf(__uint_as_float(x[e])) < INFINITY)) rest[e] = 0.0f;       // Inf and NaN stand in the first part alone
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            b[0][e] = __byte_perm(x[e], x[e + 4], 0x7632);
+                            b[1][e] = __byte_perm(__float_as_uint(rest[e]), __float_as_uint(rest[e + 4]), 0x7632);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) rest[e] -= __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) b[2][e] = __byte_perm(__float_as_uint(rest[e]), __float_as_uint(rest[e + 4]), 0x7632);
+#pragma unroll
+                        for (int q = 2; q >= 0; --q)
+#pragma unroll
+                            for (int r = 0; r < RT; ++r) {
+                                mma_bf16(sum[r][j], a[r][0], b[q][0], b[q][1]);
+                                mma_bf16(sum[r][j], a[r][1], b[q][2], b[q][3]);
+                            }
+                    }
                 }
+                if (FINE || i == 3)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        // FINE: lane i of the four holds the scales of these 32 channels
+                        const float s0 = FINE ? __shfl_sync(0xffffffffu, now[r][0], (lane & ~3) | i) : now[r][0];
+                        const float s1 = FINE ? __shfl_sync(0xffffffffu, now[r][1], (lane & ~3) | i) : now[r][1];
+#pragma unroll
+                        for (int j = 0; j < MT; ++j) {
+                            acc[r][j][0] = fmaf(s0, sum[r][j][0], acc[r][j][0]);
+                            acc[r][j][1] = fmaf(s0, sum[r][j][1], acc[r][j][1]);
+                            acc[r][j][2] = fmaf(s1, sum[r][j][2], acc[r][j][2]);
+                            acc[r][j][3] = fmaf(s1, sum[r][j][3], acc[r][j][3]);
+                        }
+                    }
             }
+            slot = slot + 1 < p.stages ? slot + 1 : 0;
+            __syncwarp();                                 // all lanes have read the stage that is filled next
         }
+        // ---- sums of the warps, added in their order
+        float* set = part + turn * warps * kRows * kCols;
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int j = 0; j < MT; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[r][j][i] = fmaf(s[r][i >> 1], sum[r][j][i], acc[r][j][i]);
-    }
-    // ---- sums of the warps. A lane holds columns 2t, 2t + 1: two tokens, or (FINE) its own groups' part of tokens 0 and 1
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int j = 0; j < MT; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v = acc[r][j][i];
-                if (FINE) {
-                    v += __shfl_xor_sync(0xffffffffu, v, 1);
-                    v += __shfl_xor_sync(0xffffffffu, v, 2);
-                    if (t != 0) continue;
-                }
-                part[((warp * kCols) + j * kTok + (FINE ? 0 : 2 * t) + (i & 1)) * kRows + r * 16 + (i >> 1) * 8 + g] = v;
-            }
-    __syncthreads();
-    for (int e = threadIdx.x; e < kRows * kCols; e += blockDim.x) {
-        const int m = m0 + e / kRows, n = n0 + e % kRows;
-        if (m >= p.M || n >= p.N) continue;
-        float v = 0.0f;
-        for (int u = 0; u < warps; ++u) v += part[u * kRows * kCols + e];
-        v *= 1024.0f;
-        if (p.bias != nullptr) v += p.bias[n];
-        v = activate(v, p.act);
-        const int64_t at = (int64_t)m * p.N + n;
-        if (p.y_bf) reinterpret_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(v);
-        else reinterpret_cast<float*>(p.Y)[at] = v;
+                for (int i = 0; i < 4; ++i) set[(warp * kCols + j * 8 + 2 * t + (i & 1)) * kRows + r * 16 + (i >> 1) * 8 + g] = acc[r][j][i];
+        __syncthreads();
+        for (int e = threadIdx.x; e < kRows * m_here; e += blockDim.x) {
+            const int m = m0 + e / kRows, n = tile * kRows + e % kRows;
+            if (n >= p.N) continue;
+            float v = 0.0f;
+            for (int u = 0; u < warps; ++u) v += set[u * kRows * kCols + e];
+            v *= 1024.0f;
+            if (p.bias != nullptr) v += p.bias[n];
+            v = activate(v, p.act);
+            const int64_t at = (int64_t)m * p.N + n;
+            if (p.y_bf) reinterpret_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(v);
+            else reinterpret_cast<float*>(p.Y)[at] = v;
+        }
     }
 }
 
 template <int RT, int MT, bool XF, bool FINE>
-int launch_w4(stwq_ctx* ctx, const W4Params& p, cudaStream_t st)
+int launch_w4(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
 {
-    constexpr int kCols = MT * (FINE ? 2 : 8), kRows = RT * 16;
+    constexpr int kCols = MT * 8, kRows = RT * 16, kStage = Stage<RT, MT, XF>::kBytes;
     int warps = 1;
-    while (warps < kMaxWarps && warps < p.chunks) warps *= 2;
-    const size_t smem = (size_t)warps * kRows * kCols * 4;
-    const dim3 grid((unsigned)((p.N + kRows - 1) / kRows), (unsigned)((p.M + kCols - 1) / kCols));
-    linear_w4g_kernel<RT, MT, XF, FINE><<<grid, 32 * warps, smem, st>>>(p);
+    while (warps < kMaxWarps / RT && warps < p.chunks && 2 * warps * (3 * kStage + 2 * kRows * kCols * 4) <= 200 * 1024) warps *= 2;
+    p.tiles = (p.N + kRows - 1) / kRows;
+    const int sets = 2 * warps * kRows * kCols * 4;
+    p.stages = warps * 4 * kStage + sets <= 112 * 1024 ? 4 : 3;
+    const size_t smem = (size_t)warps * p.stages * kStage + sets;
+    auto kern = linear_w4g_kernel<RT, MT, XF, FINE>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
+    const int per_sm = smem <= 112 * 1024 && warps * 2 <= kMaxWarps ? 2 : 1, slots = per_sm * ctx->sm_count;
+    const dim3 grid((unsigned)(p.tiles < slots ? p.tiles : slots), (unsigned)((p.M + kCols - 1) / kCols));
+    kern<<<grid, 32 * warps, smem, st>>>(p);
     ctx->launches += 1;
-    const cudaError_t e = cudaGetLastError();
+    e = cudaGetLastError();
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
 }
 
-template <int RT, int MT, bool FINE>
-int launch_w4_any(stwq_ctx* ctx, const W4Params& p, bool xf, cudaStream_t st)
+template <bool FINE>
+int launch_w4_any(stwq_ctx* ctx, W4Params& p, bool xf, cudaStream_t st)
 {
-    return xf ? launch_w4<RT, MT, true, FINE>(ctx, p, st) : launch_w4<RT, MT, false, FINE>(ctx, p, st);
+    const bool wide = p.N >= 32 * ctx->sm_count;          // tiles of 32 output channels for every SM
+    if (xf) return wide ? launch_w4<2, 1, true, FINE>(ctx, p, st) : launch_w4<1, 1, true, FINE>(ctx, p, st);
+    if (p.M <= 8) return wide ? launch_w4<2, 1, false, FINE>(ctx, p, st) : launch_w4<1, 1, false, FINE>(ctx, p, st);
+    return wide ? launch_w4<2, 2, false, FINE>(ctx, p, st) : launch_w4<1, 2, false, FINE>(ctx, p, st);
 }
 
 int check_group(int N, int K, int group)
@@ -303,14 +453,13 @@ int linear_w4g(stwq_ctx* ctx, const void* X, int64_t ldx, int x_dtype, int64_t M
     auto aligned = [](const void* q, int bytes) { return (reinterpret_cast<uintptr_t>(q) & (uintptr_t)(bytes - 1)) == 0; };
     if (!aligned(s_g, s_dtype == STWQ_OUT_F32 ? 4 : 2) || !aligned(Y, out_dtype == STWQ_OUT_F32 ? 4 : 2) || !aligned(bias, 4)) return STWQ_ERR_ALIGN;
     W4Params p;
-    p.X = X; p.ldx = ldx; p.M = (int)M; p.K = K; p.N = N; p.group = group; p.per_row = K / group; p.chunks = (K + 127) / 128;
+    p.X = X; p.ldx = ldx; p.M = (int)M; p.K = K; p.N = N; p.per_row = K / group; p.chunks = (K + 127) / 128;
     p.Wp = Wp; p.s_g = s_g; p.s_bf = s_dtype == STWQ_OUT_BF16; p.bias = bias; p.act = act; p.y_bf = out_dtype == STWQ_OUT_BF16; p.Y = Y;
+    p.group32 = (uint32_t)group / 32;
+    p.magic = (uint32_t)(((1ull << 32) + p.group32 - 1) / p.group32);
     StwqDevGuard dev(ctx->device);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // tokens per pass over the weights: 8 or 16; 2, 4 or 8 with groups that differ between the lanes
-    if (group % 128 == 0) return M <= 8 ? launch_w4_any<1, 1, false>(ctx, p, xf, st) : launch_w4_any<1, 2, false>(ctx, p, xf, st);
-    if (M <= 2) return launch_w4_any<1, 1, true>(ctx, p, xf, st);
-    return M <= 4 ? launch_w4_any<1, 2, true>(ctx, p, xf, st) : launch_w4_any<1, 4, true>(ctx, p, xf, st);
+    return group % 128 == 0 ? launch_w4_any<false>(ctx, p, xf, st) : launch_w4_any<true>(ctx, p, xf, st);
 }
 
 }  // extern "C"
