@@ -81,7 +81,8 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
 // Nibbles q and q + 4 of a word as a pair of bf16: the codes times 2^-10.
 __device__ __forceinline__ uint32_t codes2(uint32_t w, int q)
 {
-    const uint32_t t = ((w >> (4 * q)) & 0x000f000fu) ^ 0x3e083e08u;
+    uint32_t t;                                           // (w & mask) ^ bias in one operation
+    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(t) : "r"(w >> (4 * q)), "r"(0x000f000fu), "r"(0x3e083e08u));
     const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&t), __float2bfloat162_rn(0.1328125f));
     return *reinterpret_cast<const uint32_t*>(&v);
 }
@@ -110,9 +111,9 @@ __device__ __forceinline__ int x_piece(int row, int p)
     if (FINE) return XF ? p ^ (row & 1) : p ^ ((row & 1) << 2);
     return XF ? p ^ (((p >> 3) & 3) | ((row & 1) << 2)) : p ^ (((p >> 3) & 1) | ((row & 1) << 1));
 }
-template <int RT, int MT, bool XF>
+template <int RT, int MT, bool XF, bool RES>
 struct Stage {
-    static constexpr int kCodes = RT * 1024, kRow = XF ? 512 : 256, kBytes = kCodes + MT * 8 * kRow;
+    static constexpr int kCodes = RT * 1024, kRow = XF ? 512 : 256, kBytes = kCodes + (RES ? 0 : MT * 8 * kRow);
 };
 
 // Where a lane's copies of codes come from: 16-byte piece t of rows g, g + 8, ... of a tile of 16 RT output channels. Rows behind the
@@ -167,62 +168,98 @@ struct XFeed {
         }
     }
 };
-template <int RT>
+// Scales of a chunk. FINE: a lane loads those of its 32 channels for its 2 RT rows. Else the four lanes of a row have the same ones, and
+// lane t loads those of row t of the 2 RT.
+template <int RT, bool FINE>
 struct Scales {
-    int64_t row[RT][2];                                   // element offsets of the rows
-    __device__ __forceinline__ void enter(const W4Params& p, int tile, int g)
+    static constexpr int kN = FINE ? 2 * RT : 1;
+    const char* row[kN];
+    __device__ __forceinline__ void enter(const W4Params& p, int tile, int g, int t)
     {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) row[r][h] = (int64_t)min(tile * (RT * 16) + r * 16 + h * 8 + g, p.N - 1) * p.per_row;
+        for (int i = 0; i < kN; ++i) {
+            const int n = min(tile * (RT * 16) + (FINE ? i : t % (2 * RT)) * 8 + g, p.N - 1);
+            row[i] = reinterpret_cast<const char*>(p.s_g) + (((int64_t)n * p.per_row) << (p.s_bf ? 1 : 2));
+        }
     }
-    __device__ __forceinline__ void load(const W4Params& p, int chunk, int t, float (&s)[RT][2]) const
+    __device__ __forceinline__ void load(const W4Params& p, int chunk, int t, float (&s)[kN]) const
     {
-        const int unit = min(chunk * 4 + t, p.K / 32 - 1), gi = p.group32 == 1u ? unit : (int)__umulhi((uint32_t)unit, p.magic);
+        const int unit = min(chunk * 4 + (FINE ? t : 0), p.K / 32 - 1), gi = p.group32 == 1u ? unit : (int)__umulhi((uint32_t)unit, p.magic);
         if (p.s_bf) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) s[r][h] = __bfloat162float(__ldg(reinterpret_cast<const __nv_bfloat16*>(p.s_g) + (row[r][h] + gi)));
+            for (int i = 0; i < kN; ++i) s[i] = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const unsigned short*>(row[i]) + gi) << 16);
         } else {
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) s[r][h] = __ldg(reinterpret_cast<const float*>(p.s_g) + (row[r][h] + gi));
+            for (int i = 0; i < kN; ++i) s[i] = __ldg(reinterpret_cast<const float*>(row[i]) + gi);
         }
+    }
+    // of row half h of tile r and (FINE) group i of the chunk
+    __device__ __forceinline__ static float get(const float (&s)[kN], int r, int h, int i, int lane)
+    {
+        return __shfl_sync(0xffffffffu, s[FINE ? 2 * r + h : 0], (lane & ~3) | (FINE ? i : 2 * r + h));
     }
 };
 
-// RT: tiles of 16 output channels, MT: tiles of 8 tokens; XF: X is fp32; FINE: groups that are no multiple of 128.
+// Eight activations as B operands of two products: pairs of channels (0,4), (1,5), (2,6), (3,7); fp32 ones as three such sets, the top,
+// middle and bottom 8 bits of the significands. Inf and NaN stand in the first part alone.
+__device__ __forceinline__ uint4 pairs_bf16(const uint4& x)
+{
+    return make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+}
+__device__ __forceinline__ void pairs_f32(const uint4& u, const uint4& v, uint4 (&b)[3])
+{
+    const uint32_t x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        r[e] = __uint_as_float(x[e]) - __uint_as_float(x[e] & 0xffff0000u);
+        if (!(fabsf(__uint_as_float(x[e])) < INFINITY)) r[e] = 0.0f;
+    }
+    b[0] = make_uint4(__byte_perm(x[0], x[4], 0x7632), __byte_perm(x[1], x[5], 0x7632), __byte_perm(x[2], x[6], 0x7632), __byte_perm(x[3], x[7], 0x7632));
+#pragma unroll
+    for (int k = 1; k < 3; ++k) {
+        uint32_t y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            y[e] = __float_as_uint(r[e]);
+            if (k == 1) r[e] -= __uint_as_float(y[e] & 0xffff0000u);
+        }
+        b[k] = make_uint4(__byte_perm(y[0], y[4], 0x7632), __byte_perm(y[1], y[5], 0x7632), __byte_perm(y[2], y[6], 0x7632), __byte_perm(y[3], y[7], 0x7632));
+    }
+}
+
+// RT: tiles of 16 output channels, MT: tiles of 8 tokens; XF: X is fp32; FINE: groups that are no multiple of 128; RES: all activations
+// lie in shared memory as operands from the start (one tile of tokens), else those of a chunk come with its codes.
 // A block goes through tiles of 16 RT output channels; its warps take the chunks of 128 input channels in turn, each with its own
 // ring of stages that runs on over the end of a tile.
-template <int RT, int MT, bool XF, bool FINE>
-__global__ void __launch_bounds__(32 * kMaxWarps / RT) linear_w4g_kernel(const W4Params p)
+template <int RT, int MT, bool XF, bool FINE, bool RES>
+__global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4Params p)
 {
-    using S = Stage<RT, MT, XF>;
-    constexpr int kCols = MT * 8, kRows = RT * 16;
+    using S = Stage<RT, MT, XF, RES>;
+    constexpr int kCols = MT * 8, kRows = RT * 16, kParts = XF ? 3 : 1;
+    static_assert(!RES || MT == 1, "one tile of tokens");
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int g = lane >> 2, t = lane & 3;
     const int m0 = blockIdx.y * kCols, m_here = min(p.M - m0, kCols);
     char* ring = smem + warp * p.stages * S::kBytes;
     float* part = reinterpret_cast<float*>(smem + warps * p.stages * S::kBytes);  // two sets of [warps][kCols][kRows], used in turn
-    // rows of activations that no copy fills stay zero
-    for (int i = lane; i < p.stages * S::kBytes / 16; i += 32) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);
-    __syncwarp();
-
+    uint4* resident = reinterpret_cast<uint4*>(part + 2 * warps * kRows * kCols);  // [chunk][word][part][token][t]
+    if (!RES) {                                           // rows of activations that no copy fills stay zero
+        for (int i = lane; i < p.stages * S::kBytes / 16; i += 32) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncwarp();
+    }
     CodeFeed<RT> feed;
     feed.enter(p, (int)blockIdx.x, warp, g, t);
     XFeed<MT, XF, FINE> xfeed;
-    xfeed.enter(p, m0, lane);
+    if (!RES) xfeed.enter(p, m0, lane);
     const uint32_t ring_u = smem_u32(ring);
     // copies of the next chunk of this warp, `stages` - 1 ahead of the products; a group even where there is none
     auto copy = [&]() {
         if (feed.tile < p.tiles && feed.chunk < p.chunks) {
             const uint32_t to = ring_u + (uint32_t)(feed.slot * S::kBytes);
             feed.template copy<FINE>(p, to, g, t);
-            xfeed.copy(p, to + S::kCodes, feed.chunk, m_here);
+            if (!RES) xfeed.copy(p, to + S::kCodes, feed.chunk, m_here);
             feed.slot = feed.slot + 1 < p.stages ? feed.slot + 1 : 0;
             feed.chunk += warps;
             if (feed.chunk >= p.chunks) feed.enter(p, feed.tile + (int)gridDim.x, warp, g, t);
@@ -231,11 +268,43 @@ __global__ void __launch_bounds__(32 * kMaxWarps / RT) linear_w4g_kernel(const W
     };
 #pragma unroll 1
     for (int i = 1; i < p.stages; ++i) copy();
-    // scales of this lane's rows and 32 channels, loaded one chunk ahead
-    Scales<RT> scales;
-    scales.enter(p, (int)blockIdx.x, g);
-    float s[RT][2];
+    // scales of this lane's rows and channels, loaded one chunk ahead
+    Scales<RT, FINE> scales;
+    scales.enter(p, (int)blockIdx.x, g, t);
+    float s[Scales<RT, FINE>::kN];
     scales.load(p, min(warp, p.chunks - 1), t, s);
+    // columns of absent tokens repeat the last one's operands: nothing reads them
+    const int b_lane = RES ? min(g, m_here - 1) * 4 + t : 0;
+    if (RES) {
+        // words ci = 4 chunk + i of the tokens; eight rows of four lanes take as many words at once as there are tokens less
+        const int shift = m_here > 4 ? 3 : m_here > 2 ? 2 : m_here > 1 ? 1 : 0, token = g & ((1 << shift) - 1), per = 8 >> shift;
+        constexpr int kAtOnce = XF ? 4 : 8;               // words in flight per lane
+        for (int c0 = warp * per + (g >> shift); c0 < p.chunks * 4; c0 += kAtOnce * warps * per) {
+            uint4 u[kAtOnce], v[XF ? kAtOnce : 1];
+#pragma unroll
+            for (int n = 0; n < kAtOnce; ++n) {
+                const int ci = c0 + n * warps * per, k = (ci >> 2) * 128 + 8 * (FINE ? 4 * (ci & 3) + t : 4 * t + (ci & 3));
+                u[n] = make_uint4(0u, 0u, 0u, 0u);
+                if (XF) v[XF ? n : 0] = make_uint4(0u, 0u, 0u, 0u);
+                if (token < m_here && k < p.K) {
+                    const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p.X) + ((m0 + token) * p.ldx + k) * (XF ? 4 : 2));
+                    u[n] = __ldg(src);
+                    if (XF) v[XF ? n : 0] = __ldg(src + 1);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < kAtOnce; ++n) {
+                const int ci = c0 + n * warps * per;
+                if (ci >= p.chunks * 4 || token >= m_here) continue;
+                uint4 b[3], *to = resident + (ci * kParts * m_here + token) * 4 + t;
+                if (XF) pairs_f32(u[n], v[XF ? n : 0], b);
+                else b[0] = pairs_bf16(u[n]);
+#pragma unroll
+                for (int q = 0; q < kParts; ++q) to[q * 4 * m_here] = b[q];
+            }
+        }
+        __syncthreads();
+    }
 
     int slot = 0, turn = 0;
     for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, turn ^= 1) {
@@ -252,19 +321,17 @@ __global__ void __launch_bounds__(32 * kMaxWarps / RT) linear_w4g_kernel(const W
             if (p.stages == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
             else asm volatile("cp.async.wait_group 2;" ::: "memory");
             __syncwarp();
-            float now[RT][2];
+            float now[Scales<RT, FINE>::kN];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                now[r][0] = s[r][0];
-                now[r][1] = s[r][1];
-            }
+            for (int i = 0; i < Scales<RT, FINE>::kN; ++i) now[i] = s[i];
             if (c + warps < p.chunks) scales.load(p, c + warps, t, s);
             else {
-                scales.enter(p, min(tile + (int)gridDim.x, p.tiles - 1), g);
+                scales.enter(p, min(tile + (int)gridDim.x, p.tiles - 1), g, t);
                 scales.load(p, warp, t, s);
             }
             const char* codes = ring + slot * S::kBytes;
             const char* xs = codes + S::kCodes;
+            const uint4* bs = resident + c * (16 * kParts) * m_here + b_lane;
             uint4 w[RT][2];
             if (!FINE)
 #pragma unroll
@@ -302,49 +369,24 @@ __global__ void __launch_bounds__(32 * kMaxWarps / RT) linear_w4g_kernel(const W
 #pragma unroll
                 for (int j = 0; j < MT; ++j) {
                     const char* xr = xs + (j * 8 + g) * S::kRow;
-                    if constexpr (!XF) {
-                        const uint4 x = lds128(xr + x_piece<XF, FINE>(g, eight) * 16);
-                        const uint32_t b[4] = {__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
-                                               __byte_perm(x.y, x.w, 0x7632)};    // channels (0,4), (1,5), (2,6), (3,7)
+                    uint4 b[3];
+                    if (RES) {
+#pragma unroll
+                        for (int q = 0; q < kParts; ++q) b[q] = bs[(i * kParts + q) * 4 * m_here];
+                    } else if (XF) pairs_f32(lds128(xr + x_piece<XF, FINE>(g, 2 * eight) * 16), lds128(xr + x_piece<XF, FINE>(g, 2 * eight + 1) * 16), b);
+                    else b[0] = pairs_bf16(lds128(xr + x_piece<XF, FINE>(g, eight) * 16));
+#pragma unroll
+                    for (int q = kParts - 1; q >= 0; --q)                         // the smallest part first
 #pragma unroll
                         for (int r = 0; r < RT; ++r) {
-                            mma_bf16(sum[r][j], a[r][0], b[0], b[1]);
-                            mma_bf16(sum[r][j], a[r][1], b[2], b[3]);
+                            mma_bf16(sum[r][j], a[r][0], b[q].x, b[q].y);
+                            mma_bf16(sum[r][j], a[r][1], b[q].z, b[q].w);
                         }
-                    } else {
-                        const uint4 u = lds128(xr + x_piece<XF, FINE>(g, 2 * eight) * 16), v = lds128(xr + x_piece<XF, FINE>(g, 2 * eight + 1) * 16);
-                        const uint32_t x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-                        uint32_t b[3][4];                 // the top, middle and bottom 8 bits of the significands
-                        float rest[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            rest[e] = __uint_as_float(x[e]) - __uint_as_float(x[e] & 0xffff0000u);
-                            if (!(fabsf(__uint_as_float(x[e])) < INFINITY)) rest[e] = 0.0f;       // Inf and NaN stand in the first part alone
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            b[0][e] = __byte_perm(x[e], x[e + 4], 0x7632);
-                            b[1][e] = __byte_perm(__float_as_uint(rest[e]), __float_as_uint(rest[e + 4]), 0x7632);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) rest[e] -= __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) b[2][e] = __byte_perm(__float_as_uint(rest[e]), __float_as_uint(rest[e + 4]), 0x7632);
-#pragma unroll
-                        for (int q = 2; q >= 0; --q)
-#pragma unroll
-                            for (int r = 0; r < RT; ++r) {
-                                mma_bf16(sum[r][j], a[r][0], b[q][0], b[q][1]);
-                                mma_bf16(sum[r][j], a[r][1], b[q][2], b[q][3]);
-                            }
-                    }
                 }
                 if (FINE || i == 3)
 #pragma unroll
                     for (int r = 0; r < RT; ++r) {
-                        // FINE: lane i of the four holds the scales of these 32 channels
-                        const float s0 = FINE ? __shfl_sync(0xffffffffu, now[r][0], (lane & ~3) | i) : now[r][0];
-                        const float s1 = FINE ? __shfl_sync(0xffffffffu, now[r][1], (lane & ~3) | i) : now[r][1];
+                        const float s0 = Scales<RT, FINE>::get(now, r, 0, i, lane), s1 = Scales<RT, FINE>::get(now, r, 1, i, lane);
 #pragma unroll
                         for (int j = 0; j < MT; ++j) {
                             acc[r][j][0] = fmaf(s0, sum[r][j][0], acc[r][j][0]);
@@ -381,20 +423,23 @@ __global__ void __launch_bounds__(32 * kMaxWarps / RT) linear_w4g_kernel(const W
     }
 }
 
-template <int RT, int MT, bool XF, bool FINE>
-int launch_w4(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
+template <int RT, int MT, bool XF, bool FINE, bool RES>
+int launch_w4(stwq_ctx* ctx, W4Params& p, size_t resident, cudaStream_t st)
 {
-    constexpr int kCols = MT * 8, kRows = RT * 16, kStage = Stage<RT, MT, XF>::kBytes;
+    constexpr int kCols = MT * 8, kRows = RT * 16, kStage = Stage<RT, MT, XF, RES>::kBytes, kSets = 2 * kRows * kCols * 4;
+    // Two blocks of eight warps on an SM where rings of three stages and the activations fit twice, else one of up to sixteen; four stages
+    // where there is room.
+    constexpr size_t kHalf = 112 * 1024, kAll = 220 * 1024;
+    const bool two = 8 * (3 * kStage + kSets) + resident <= kHalf;
     int warps = 1;
-    while (warps < kMaxWarps / RT && warps < p.chunks && 2 * warps * (3 * kStage + 2 * kRows * kCols * 4) <= 200 * 1024) warps *= 2;
+    while (2 * warps <= (two ? 8 : kMaxWarps) && warps < p.chunks && (size_t)2 * warps * (3 * kStage + kSets) + resident <= (two ? kHalf : kAll)) warps *= 2;
+    p.stages = (size_t)warps * (4 * kStage + kSets) + resident <= (two ? kHalf : kAll) ? 4 : 3;
+    const size_t smem = (size_t)warps * (p.stages * kStage + kSets) + resident;
     p.tiles = (p.N + kRows - 1) / kRows;
-    const int sets = 2 * warps * kRows * kCols * 4;
-    p.stages = warps * 4 * kStage + sets <= 112 * 1024 ? 4 : 3;
-    const size_t smem = (size_t)warps * p.stages * kStage + sets;
-    auto kern = linear_w4g_kernel<RT, MT, XF, FINE>;
+    auto kern = linear_w4g_kernel<RT, MT, XF, FINE, RES>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
-    const int per_sm = smem <= 112 * 1024 && warps * 2 <= kMaxWarps ? 2 : 1, slots = per_sm * ctx->sm_count;
+    const int slots = (two ? 2 : 1) * ctx->sm_count;
     const dim3 grid((unsigned)(p.tiles < slots ? p.tiles : slots), (unsigned)((p.M + kCols - 1) / kCols));
     kern<<<grid, 32 * warps, smem, st>>>(p);
     ctx->launches += 1;
@@ -402,13 +447,17 @@ int launch_w4(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
 }
 
-template <bool FINE>
-int launch_w4_any(stwq_ctx* ctx, W4Params& p, bool xf, cudaStream_t st)
+template <bool FINE, bool XF>
+int launch_w4_any(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
 {
     const bool wide = p.N >= 32 * ctx->sm_count;          // tiles of 32 output channels for every SM
-    if (xf) return wide ? launch_w4<2, 1, true, FINE>(ctx, p, st) : launch_w4<1, 1, true, FINE>(ctx, p, st);
-    if (p.M <= 8) return wide ? launch_w4<2, 1, false, FINE>(ctx, p, st) : launch_w4<1, 1, false, FINE>(ctx, p, st);
-    return wide ? launch_w4<2, 2, false, FINE>(ctx, p, st) : launch_w4<1, 2, false, FINE>(ctx, p, st);
+    const int tok = p.M < 8 ? p.M : 8;
+    // activations as operands in shared memory, if that leaves room for the rings of eight warps
+    const size_t resident = (size_t)tok * p.chunks * 128 * (XF ? 6 : 2);
+    if (resident <= 96 * 1024 && (XF || p.M <= 8))
+        return wide ? launch_w4<2, 1, XF, FINE, true>(ctx, p, resident, st) : launch_w4<1, 1, XF, FINE, true>(ctx, p, resident, st);
+    if (XF || p.M <= 8) return wide ? launch_w4<2, 1, XF, FINE, false>(ctx, p, 0, st) : launch_w4<1, 1, XF, FINE, false>(ctx, p, 0, st);
+    return wide ? launch_w4<2, 2, false, FINE, false>(ctx, p, 0, st) : launch_w4<1, 2, false, FINE, false>(ctx, p, 0, st);
 }
 
 int check_group(int N, int K, int group)
@@ -459,7 +508,8 @@ int linear_w4g(stwq_ctx* ctx, const void* X, int64_t ldx, int x_dtype, int64_t M
     p.magic = (uint32_t)(((1ull << 32) + p.group32 - 1) / p.group32);
     StwqDevGuard dev(ctx->device);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return group % 128 == 0 ? launch_w4_any<false>(ctx, p, xf, st) : launch_w4_any<true>(ctx, p, xf, st);
+    if (group % 128 == 0) return xf ? launch_w4_any<false, true>(ctx, p, st) : launch_w4_any<false, false>(ctx, p, st);
+    return xf ? launch_w4_any<true, true>(ctx, p, st) : launch_w4_any<true, false>(ctx, p, st);
 }
 
 }  // extern "C"
