@@ -174,15 +174,19 @@ template <int RT, bool FINE>
 struct Scales {
     static constexpr int kN = FINE ? 2 * RT : 1;
     const char* row[kN];
-    __device__ __forceinline__ void enter(const W4Params& p, int tile, int g, int t)
+    int tile, chunk;
+    __device__ __forceinline__ void enter(const W4Params& p, int to_tile, int warp, int g, int t)
     {
+        tile = min(to_tile, p.tiles - 1);                 // beyond the last one nothing uses what is loaded
+        chunk = min(warp, p.chunks - 1);
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             const int n = min(tile * (RT * 16) + (FINE ? i : t % (2 * RT)) * 8 + g, p.N - 1);
             row[i] = reinterpret_cast<const char*>(p.s_g) + (((int64_t)n * p.per_row) << (p.s_bf ? 1 : 2));
         }
     }
-    __device__ __forceinline__ void load(const W4Params& p, int chunk, int t, float (&s)[kN]) const
+    // the scales of the chunk at hand, and on to this warp's next
+    __device__ __forceinline__ void load(const W4Params& p, int warp, int warps, int g, int t, float (&s)[kN])
     {
         const int unit = min(chunk * 4 + (FINE ? t : 0), p.K / 32 - 1), gi = p.group32 == 1u ? unit : (int)__umulhi((uint32_t)unit, p.magic);
         if (p.s_bf) {
@@ -192,6 +196,8 @@ struct Scales {
 #pragma unroll
             for (int i = 0; i < kN; ++i) s[i] = __ldg(reinterpret_cast<const float*>(row[i]) + gi);
         }
+        chunk += warps;
+        if (chunk >= p.chunks) enter(p, tile + (int)gridDim.x, warp, g, t);
     }
     // of row half h of tile r and (FINE) group i of the chunk
     __device__ __forceinline__ static float get(const float (&s)[kN], int r, int h, int i, int lane)
@@ -229,7 +235,7 @@ __device__ __forceinline__ void pairs_f32(const uint4& u, const uint4& v, uint4 
 }
 
 // RT: tiles of 16 output channels, MT: tiles of 8 tokens; XF: X is fp32; FINE: groups that are no multiple of 128; RES: all activations
-// lie in shared memory as operands from the start (one tile of tokens), else those of a chunk come with its codes.
+// lie in shared memory as operands from the start, else those of a chunk come with its codes.
 // A block goes through tiles of 16 RT output channels; its warps take the chunks of 128 input channels in turn, each with its own
 // ring of stages that runs on over the end of a tile.
 template <int RT, int MT, bool XF, bool FINE, bool RES>
@@ -237,7 +243,6 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
 {
     using S = Stage<RT, MT, XF, RES>;
     constexpr int kCols = MT * 8, kRows = RT * 16, kParts = XF ? 3 : 1;
-    static_assert(!RES || MT == 1, "one tile of tokens");
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int g = lane >> 2, t = lane & 3;
@@ -268,17 +273,22 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
     };
 #pragma unroll 1
     for (int i = 1; i < p.stages; ++i) copy();
-    // scales of this lane's rows and channels, loaded one chunk ahead
+    // scales of this lane's rows and channels, loaded two chunks ahead
     Scales<RT, FINE> scales;
-    scales.enter(p, (int)blockIdx.x, g, t);
-    float s[Scales<RT, FINE>::kN];
-    scales.load(p, min(warp, p.chunks - 1), t, s);
+    constexpr int kS = Scales<RT, FINE>::kN;
+    scales.enter(p, (int)blockIdx.x, warp, g, t);
+    float s0[kS], s1[kS];
+    scales.load(p, warp, warps, g, t, s0);
+    scales.load(p, warp, warps, g, t, s1);
     // columns of absent tokens repeat the last one's operands: nothing reads them
-    const int b_lane = RES ? min(g, m_here - 1) * 4 + t : 0;
+    int b_lane[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) b_lane[j] = min(j * 8 + g, m_here - 1) * 4 + t;
     if (RES) {
         // words ci = 4 chunk + i of the tokens; eight rows of four lanes take as many words at once as there are tokens less
-        const int shift = m_here > 4 ? 3 : m_here > 2 ? 2 : m_here > 1 ? 1 : 0, token = g & ((1 << shift) - 1), per = 8 >> shift;
+        const int shift = m_here > 4 ? 3 : m_here > 2 ? 2 : m_here > 1 ? 1 : 0, per = 8 >> shift;
         constexpr int kAtOnce = XF ? 4 : 8;               // words in flight per lane
+        for (int token = g & ((1 << shift) - 1); token < m_here; token += 8)
         for (int c0 = warp * per + (g >> shift); c0 < p.chunks * 4; c0 += kAtOnce * warps * per) {
             uint4 u[kAtOnce], v[XF ? kAtOnce : 1];
 #pragma unroll
@@ -286,7 +296,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
                 const int ci = c0 + n * warps * per, k = (ci >> 2) * 128 + 8 * (FINE ? 4 * (ci & 3) + t : 4 * t + (ci & 3));
                 u[n] = make_uint4(0u, 0u, 0u, 0u);
                 if (XF) v[XF ? n : 0] = make_uint4(0u, 0u, 0u, 0u);
-                if (token < m_here && k < p.K) {
+                if (k < p.K) {
                     const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p.X) + ((m0 + token) * p.ldx + k) * (XF ? 4 : 2));
                     u[n] = __ldg(src);
                     if (XF) v[XF ? n : 0] = __ldg(src + 1);
@@ -295,7 +305,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
 #pragma unroll
             for (int n = 0; n < kAtOnce; ++n) {
                 const int ci = c0 + n * warps * per;
-                if (ci >= p.chunks * 4 || token >= m_here) continue;
+                if (ci >= p.chunks * 4) continue;
                 uint4 b[3], *to = resident + (ci * kParts * m_here + token) * 4 + t;
                 if (XF) pairs_f32(u[n], v[XF ? n : 0], b);
                 else b[0] = pairs_bf16(u[n]);
@@ -321,17 +331,16 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
             if (p.stages == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
             else asm volatile("cp.async.wait_group 2;" ::: "memory");
             __syncwarp();
-            float now[Scales<RT, FINE>::kN];
+            float now[kS];
 #pragma unroll
-            for (int i = 0; i < Scales<RT, FINE>::kN; ++i) now[i] = s[i];
-            if (c + warps < p.chunks) scales.load(p, c + warps, t, s);
-            else {
-                scales.enter(p, min(tile + (int)gridDim.x, p.tiles - 1), g, t);
-                scales.load(p, warp, t, s);
+            for (int i = 0; i < kS; ++i) {
+                now[i] = s0[i];
+                s0[i] = s1[i];
             }
+            scales.load(p, warp, warps, g, t, s1);
             const char* codes = ring + slot * S::kBytes;
             const char* xs = codes + S::kCodes;
-            const uint4* bs = resident + c * (16 * kParts) * m_here + b_lane;
+            const uint4* bs = resident + c * (16 * kParts) * m_here;
             uint4 w[RT][2];
             if (!FINE)
 #pragma unroll
@@ -372,7 +381,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
                     uint4 b[3];
                     if (RES) {
 #pragma unroll
-                        for (int q = 0; q < kParts; ++q) b[q] = bs[(i * kParts + q) * 4 * m_here];
+                        for (int q = 0; q < kParts; ++q) b[q] = bs[(i * kParts + q) * 4 * m_here + b_lane[j]];
                     } else if (XF) pairs_f32(lds128(xr + x_piece<XF, FINE>(g, 2 * eight) * 16), lds128(xr + x_piece<XF, FINE>(g, 2 * eight + 1) * 16), b);
                     else b[0] = pairs_bf16(lds128(xr + x_piece<XF, FINE>(g, eight) * 16));
 #pragma unroll
@@ -386,13 +395,13 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
                 if (FINE || i == 3)
 #pragma unroll
                     for (int r = 0; r < RT; ++r) {
-                        const float s0 = Scales<RT, FINE>::get(now, r, 0, i, lane), s1 = Scales<RT, FINE>::get(now, r, 1, i, lane);
+                        const float lo = Scales<RT, FINE>::get(now, r, 0, i, lane), hi = Scales<RT, FINE>::get(now, r, 1, i, lane);
 #pragma unroll
                         for (int j = 0; j < MT; ++j) {
-                            acc[r][j][0] = fmaf(s0, sum[r][j][0], acc[r][j][0]);
-                            acc[r][j][1] = fmaf(s0, sum[r][j][1], acc[r][j][1]);
-                            acc[r][j][2] = fmaf(s1, sum[r][j][2], acc[r][j][2]);
-                            acc[r][j][3] = fmaf(s1, sum[r][j][3], acc[r][j][3]);
+                            acc[r][j][0] = fmaf(lo, sum[r][j][0], acc[r][j][0]);
+                            acc[r][j][1] = fmaf(lo, sum[r][j][1], acc[r][j][1]);
+                            acc[r][j][2] = fmaf(hi, sum[r][j][2], acc[r][j][2]);
+                            acc[r][j][3] = fmaf(hi, sum[r][j][3], acc[r][j][3]);
                         }
                     }
             }
@@ -427,20 +436,21 @@ template <int RT, int MT, bool XF, bool FINE, bool RES>
 int launch_w4(stwq_ctx* ctx, W4Params& p, size_t resident, cudaStream_t st)
 {
     constexpr int kCols = MT * 8, kRows = RT * 16, kStage = Stage<RT, MT, XF, RES>::kBytes, kSets = 2 * kRows * kCols * 4;
-    // Two blocks of eight warps on an SM where rings of three stages and the activations fit twice, else one of up to sixteen; four stages
-    // where there is room.
+    // Two blocks of eight warps on an SM where there are tiles for them and rings of three stages and the activations fit twice, else one
+    // of up to sixteen; four stages where there is room.
     constexpr size_t kHalf = 112 * 1024, kAll = 220 * 1024;
-    const bool two = 8 * (3 * kStage + kSets) + resident <= kHalf;
+    p.tiles = (p.N + kRows - 1) / kRows;
+    const bool two = p.tiles > ctx->sm_count && 8 * (3 * kStage + kSets) + resident <= kHalf;
     int warps = 1;
     while (2 * warps <= (two ? 8 : kMaxWarps) && warps < p.chunks && (size_t)2 * warps * (3 * kStage + kSets) + resident <= (two ? kHalf : kAll)) warps *= 2;
     p.stages = (size_t)warps * (4 * kStage + kSets) + resident <= (two ? kHalf : kAll) ? 4 : 3;
     const size_t smem = (size_t)warps * (p.stages * kStage + kSets) + resident;
-    p.tiles = (p.N + kRows - 1) / kRows;
     auto kern = linear_w4g_kernel<RT, MT, XF, FINE, RES>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
     const int slots = (two ? 2 : 1) * ctx->sm_count;
-    const dim3 grid((unsigned)(p.tiles < slots ? p.tiles : slots), (unsigned)((p.M + kCols - 1) / kCols));
+    const int passes = (p.M + kCols - 1) / kCols, share = slots / passes > 0 ? slots / passes : 1;        // over the weights, side by side
+    const dim3 grid((unsigned)(p.tiles < share ? p.tiles : share), (unsigned)passes);
     kern<<<grid, 32 * warps, smem, st>>>(p);
     ctx->launches += 1;
     e = cudaGetLastError();
@@ -451,11 +461,13 @@ template <bool FINE, bool XF>
 int launch_w4_any(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
 {
     const bool wide = p.N >= 32 * ctx->sm_count;          // tiles of 32 output channels for every SM
-    const int tok = p.M < 8 ? p.M : 8;
-    // activations as operands in shared memory, if that leaves room for the rings of eight warps
-    const size_t resident = (size_t)tok * p.chunks * 128 * (XF ? 6 : 2);
-    if (resident <= 96 * 1024 && (XF || p.M <= 8))
-        return wide ? launch_w4<2, 1, XF, FINE, true>(ctx, p, resident, st) : launch_w4<1, 1, XF, FINE, true>(ctx, p, resident, st);
+    // activations as operands in shared memory, where that leaves room for the rings: of up to 8 tokens, and of up to 16 fp32 ones, which
+    // are cut into their parts once instead of once per tile
+    const size_t token = (size_t)p.chunks * 128 * (XF ? 6 : 2), one = token * (p.M < 8 ? p.M : 8), both = token * (p.M < 16 ? p.M : 16);
+    if (XF && p.M > 8 && both <= 144 * 1024)
+        return wide ? launch_w4<2, 2, true, FINE, true>(ctx, p, both, st) : launch_w4<1, 2, true, FINE, true>(ctx, p, both, st);
+    if (one <= 96 * 1024 && (XF || p.M <= 8))
+        return wide ? launch_w4<2, 1, XF, FINE, true>(ctx, p, one, st) : launch_w4<1, 1, XF, FINE, true>(ctx, p, one, st);
     if (XF || p.M <= 8) return wide ? launch_w4<2, 1, XF, FINE, false>(ctx, p, 0, st) : launch_w4<1, 1, XF, FINE, false>(ctx, p, 0, st);
     return wide ? launch_w4<2, 2, false, FINE, false>(ctx, p, 0, st) : launch_w4<1, 2, false, FINE, false>(ctx, p, 0, st);
 }
