@@ -10,6 +10,7 @@
 // least k logits reach; the few runs that reach it (about k) are read again, their logits that reach it (about k) are
 // ranked by counting over 64-bit keys (value, then lower index), which are all different. Where too many reach the bound
 // (a constant row), the k tokens are found one after the other.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include "stwq_internal.cuh"
@@ -17,21 +18,21 @@
 #include "stwq_ptx.cuh"
 
 using namespace stwq_ptx;       // packed fp32 arithmetic
+namespace cg = cooperative_groups;
 
 namespace {
 
 constexpr int kMaxV = 360448;
 constexpr int kTop = 32;
-constexpr int kNt = 512;
-constexpr int kGroups = kNt / 4;             // of four threads
-constexpr int kCand = 2048;                  // logits that reach the bound
+constexpr int kMaxCluster = 8;
+constexpr int kCand = 2048;                  // logits of a block that reach its bound
 constexpr int kRuns = 1024;                  // runs that do
 constexpr float kLow = -200.0f;              // octaves below which a weight is 0
 
 struct LpParams {
     const void* X;
     int64_t ld;
-    int V, k;
+    int V, k, slice;                         // slice: logits of a block of the cluster
     const float* temperature;
     const int32_t* tokens;
     float *logprobs, *entropy, *top_lp;
@@ -39,15 +40,19 @@ struct LpParams {
     uint32_t* status;
 };
 
+template <int NT>
 struct LpShared {
-    float m[kNt / 32], s[kNt / 32], a[kNt / 32];
-    uint32_t n[kNt / 32];
-    float gmax[kGroups];
+    float m[NT / 32], s[NT / 32], a[NT / 32];
+    uint32_t n[NT / 32];
+    __align__(16) float gmax[NT / 4];        // of the runs of four threads
     float bound;
     uint32_t n_cand, n_runs;
-    unsigned long long best[kNt / 32];
+    unsigned long long best[NT / 32];
     unsigned long long cand[kCand];
     int32_t runs[kRuns];
+    float row_m[kMaxCluster], row_s[kMaxCluster], row_a[kMaxCluster];          // of the blocks of a row, in the first one
+    uint32_t row_n[kMaxCluster];
+    unsigned long long row_top[kMaxCluster * kTop];
 };
 
 template <typename XT>
@@ -60,22 +65,37 @@ __device__ __forceinline__ float value<__nv_bfloat16>(const __nv_bfloat16* p, in
 // 32 bytes of logits
 template <typename XT>
 struct Vec {
+    static constexpr int kPer = 32 / sizeof(XT);
     uint32_t w[8];
     __device__ __forceinline__ void load(const XT* p)
     {
-        asm("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-            : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
     }
-    __device__ __forceinline__ void get(float (&x)[32 / sizeof(XT)]) const
+    __device__ __forceinline__ void get(float (&x)[kPer]) const
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (sizeof(XT) == 4) x[i] = __uint_as_float(w[i]);
             else {
                 x[2 * i] = __uint_as_float(w[i] << 16);
-                x[(2 * i + 1) % (32 / sizeof(XT))] = __uint_as_float(w[i] & 0xffff0000u);
+                x[(2 * i + 1) % kPer] = __uint_as_float(w[i] & 0xffff0000u);
             }
         }
+    }
+    // the largest, NaN left out (NaN where there is nothing else)
+    __device__ __forceinline__ float largest(const float (&x)[kPer]) const
+    {
+        if (sizeof(XT) == 4) {
+            float m = x[0];
+#pragma unroll
+            for (int i = 1; i < kPer; ++i) m = fmaxf(m, x[i]);
+            return m;
+        }
+        __nv_bfloat162 m = *reinterpret_cast<const __nv_bfloat162*>(&w[0]);
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = __hmax2(m, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+        return fmaxf(__low2float(m), __high2float(m));
     }
 };
 
@@ -90,17 +110,22 @@ __device__ __forceinline__ float value_of(unsigned long long key)
     const uint32_t k = (uint32_t)(key >> 32);
     return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
 }
+__device__ __forceinline__ int index_of(unsigned long long key) { return (int)(0xffffffffu - (uint32_t)key); }
 // octaves between a logit and the maximum; the maximum itself at 0 (also at +Inf), masked ones (NaN too) at kLow
 __device__ __forceinline__ float octaves(float x, float m, float c) { return x == m ? 0.0f : fmaxf((x - m) * c, kLow); }
 
-// What a thread (then a warp, a block) has seen of a row.
+// What a thread has seen of a row: the maximum, and relative to it S and A, each as two partial sums.
+template <int PER>
 struct Sums {
-    float m, s, a;
+    float m;
+    uint64_t s, a;
+    bool odd;                                // a logit that has no weight came by
     __device__ __forceinline__ void raise(float to, float c)                 // `to` > m
     {
-        const float d = octaves(m, to, c), f = ex2_approx(d);
-        a = f * fmaf(d, s, a);
-        s *= f;
+        const float d = octaves(m, to, c);
+        const uint64_t f = dup_f2(ex2_approx(d));
+        a = mul_f2(f, fma_f2(dup_f2(d), s, a));
+        s = mul_f2(f, s);
         m = to;
     }
     __device__ __forceinline__ void add(float x, float c)                    // one logit
@@ -108,233 +133,369 @@ struct Sums {
         if (x > m) raise(x, c);
         if (!(x > -INFINITY)) return;
         const float z = octaves(x, m, c), w = ex2_approx(z);
-        s += w;
-        a = fmaf(w, z, a);
+        s = fma_f2(pack_f2(w, 0.0f), pack_f2(1.0f, 1.0f), s);
+        a = fma_f2(pack_f2(w, 0.0f), pack_f2(z, 0.0f), a);
     }
-    __device__ __forceinline__ void join(float om, float os, float oa, float c)
+    // a vector whose largest is vm. Weights of -Inf and NaN are not told apart from the others until the sums show NaN (0 * -Inf); from then on
+    // the thread clamps every exponent.
+    __device__ __forceinline__ void add(const float (&x)[PER], float vm, float c)
     {
-        Sums o = {om, os, oa};
-        if (o.m > m) raise(o.m, c);
-        else if (m > o.m) o.raise(m, c);
-        s += o.s;
-        a += o.a;
+        if (vm > m) raise(vm, c);
+        if (vm == INFINITY) {
+            float n = 0.0f;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) n += x[j] == INFINITY ? 1.0f : 0.0f;
+            s = fma_f2(pack_f2(n, 0.0f), pack_f2(1.0f, 1.0f), s);
+            return;
+        }
+        const uint64_t off = dup_f2(-m), scale = dup_f2(c);
+        if (!odd) {
+            uint64_t vs = 0ull, va = 0ull;
+#pragma unroll
+            for (int j = 0; j < PER; j += 2) {
+                const uint64_t z = mul_f2(add_f2(pack_f2(x[j], x[j + 1]), off), scale);
+                float z0, z1;
+                unpack_f2(z, z0, z1);
+                const uint64_t w = pack_f2(ex2_approx(z0), ex2_approx(z1));
+                vs = add_f2(vs, w);
+                va = fma_f2(w, z, va);
+            }
+            float a0, a1;
+            unpack_f2(va, a0, a1);
+            if (a0 + a1 == a0 + a1) {
+                s = add_f2(s, vs);
+                a = add_f2(a, va);
+                return;
+            }
+            odd = true;
+        }
+#pragma unroll
+        for (int j = 0; j < PER; j += 2) {
+            float z0, z1;
+            unpack_f2(mul_f2(add_f2(pack_f2(x[j], x[j + 1]), off), scale), z0, z1);
+            z0 = fmaxf(z0, kLow);
+            z1 = fmaxf(z1, kLow);
+            const uint64_t w = pack_f2(ex2_approx(z0), ex2_approx(z1));
+            s = add_f2(s, w);
+            a = fma_f2(w, pack_f2(z0, z1), a);
+        }
+    }
+    static __device__ __forceinline__ uint64_t add_f2(uint64_t u, uint64_t v)
+    {
+        uint64_t r;
+        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(u), "l"(v));
+        return r;
     }
 };
 
-template <typename XT>
-__global__ void __launch_bounds__(kNt, 2) logprob_kernel(const LpParams p)
+__device__ __forceinline__ float warp_max(float v)                           // NaN left out
 {
-    constexpr int kPer = 32 / sizeof(XT);                 // logits per vector
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// A block of NT threads takes a row, or (CL) a slice of one; the first block of the cluster joins the slices.
+template <typename XT, int NT, bool CL>
+__global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const LpParams p)
+{
+    constexpr int kPer = Vec<XT>::kPer, kGroups = NT / 4, kWarps = NT / 32, kAhead = 2;
     extern __shared__ __align__(16) float run_max[];      // [runs of 4 vectors]
-    __shared__ LpShared sh;
+    __shared__ LpShared<NT> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t row = blockIdx.x;
-    const XT* src = reinterpret_cast<const XT*>(p.X) + row * p.ld;
-    const int head = min(p.V, (int)(((32u - (uint32_t)(reinterpret_cast<uintptr_t>(src) & 31u)) & 31u) / sizeof(XT)));
-    const int nvec = (p.V - head) / kPer, tail0 = head + nvec * kPer;
+    cg::cluster_group::arrival_token begun;
+    if (CL) begun = cg::this_cluster().barrier_arrive();  // waited for before shared memory of another block is written
+    const int blocks = CL ? (int)cg::this_cluster().num_blocks() : 1, rank = CL ? (int)cg::this_cluster().block_rank() : 0;
+    const int64_t row = CL ? blockIdx.x / blocks : blockIdx.x;
+    const int i0 = rank * p.slice, V = max(0, min(p.V - i0, p.slice));           // this block's logits: i0 .. i0 + V - 1 of the row
+    const XT* src = reinterpret_cast<const XT*>(p.X) + row * p.ld + i0;
+    const int head = min(V, (int)(((32u - (uint32_t)(reinterpret_cast<uintptr_t>(src) & 31u)) & 31u) / sizeof(XT)));
+    const int nvec = (V - head) / kPer, tail0 = head + nvec * kPer, ends = head + (V - tail0);
     const int n_runs = (nvec + 3) / 4;
     const XT* body = src + head;
 
+    Vec<XT> ahead[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (tid + u * NT < nvec) ahead[u].load(body + (int64_t)(tid + u * NT) * kPer);
     // an infinite temperature counts as the largest finite one; the sums of a greedy row are not used
     const float temp = p.temperature != nullptr ? p.temperature[row] : 1.0f;
     const bool greedy = !(temp > 0.0f);
     const float t = greedy ? 1.0f : fminf(temp, 3.402823466e38f), c = fminf(1.4426950408889634f / t, 3.402823466e38f);
-    const int token = p.tokens != nullptr ? p.tokens[row] : -1;
-    const bool valid = token >= 0 && token < p.V;
-    const float xt = valid ? value(src, token) : -INFINITY;
+    const int given = p.tokens != nullptr ? p.tokens[row] : -1;
+    const bool valid = given >= 0 && given < p.V;
+    const float xt = valid ? value(reinterpret_cast<const XT*>(p.X) + row * p.ld, given) : -INFINITY;
     const bool ranked = xt > -INFINITY;
+    const int token = given - i0;                         // in this block's count
     // what a logit before the token has to exceed to stand before it in the order: the next value below (an equal one does);
     // behind the token it has to exceed the token's
     const float below = __fadd_rn(xt, 0.0f) == 0.0f ? -1.401298464e-45f
                         : __uint_as_float(xt > 0.0f ? __float_as_uint(xt) - 1u : __float_as_uint(xt) + 1u);
 
-    Sums me = {-INFINITY, 0.0f, 0.0f};
+    Sums<kPer> me = {-INFINITY, 0ull, 0ull, false};
     uint32_t before = 0u;
     float gmax = -INFINITY;
-    for (int i = tid; i < head + (p.V - tail0); i += kNt) {          // the ragged ends, logit by logit
-        const int at = i < head ? i : tail0 + (i - head);
+    if (tid < ends) {                                     // the ragged ends, logit by logit (fewer than 32)
+        const int at = tid < head ? tid : tail0 + (tid - head);
         const float x = value(src, at);
         me.add(x, c);
         gmax = fmaxf(gmax, x);
         if (ranked && x > (at < token ? below : xt)) ++before;
     }
-    for (int i0 = 0; i0 < nvec; i0 += kNt) {
-        const int i = i0 + tid;
-        float vm = -INFINITY;
-        if (i < nvec) {
-            Vec<XT> v;
-            v.load(body + (int64_t)i * kPer);
-            float x[kPer];
-            v.get(x);
+    for (int b0 = 0; b0 < nvec; b0 += kAhead * NT) {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) vm = fmaxf(vm, x[j]);      // leaves NaN out
-            if (vm > me.m) me.raise(vm, c);
-            if (vm == INFINITY) {
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = b0 + u * NT + tid;
+            float vm = -INFINITY;
+            if (i < nvec) {
+                float x[kPer];
+                ahead[u].get(x);
+                vm = fmaxf(vm, ahead[u].largest(x));
+                if (i + kAhead * NT < nvec) ahead[u].load(body + (int64_t)(i + kAhead * NT) * kPer);
+                me.add(x, vm, c);
+                if (ranked) {
+                    const int at = head + i * kPer;
+                    const float thr = at + kPer <= token ? below : xt;
+                    if (vm > thr)
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) me.s += x[j] == INFINITY ? 1.0f : 0.0f;
-            } else {
+                        for (int j = 0; j < kPer; ++j) before += x[j] > thr ? 1u : 0u;
+                    if (token >= at && token < at + kPer)             // equal logits before the token, in its own vector
 #pragma unroll
-                for (int j = 0; j < kPer; j += 2) {
-                    float z0, z1;
-                    unpack_f2(mul_f2(fma_f2(pack_f2(1.0f, 1.0f), pack_f2(x[j], x[j + 1]), dup_f2(-me.m)), dup_f2(c)), z0, z1);
-                    z0 = fmaxf(z0, kLow);                             // -Inf and NaN: weight 0
-                    z1 = fmaxf(z1, kLow);
-                    const float w0 = ex2_approx(z0), w1 = ex2_approx(z1);
-                    me.s += w0 + w1;
-                    me.a = fmaf(w0, z0, fmaf(w1, z1, me.a));
+                        for (int j = 0; j < kPer; ++j) before += x[j] == xt && at + j < token ? 1u : 0u;
                 }
             }
-            if (ranked) {
-                const int at = head + i * kPer;
-                const float thr = at + kPer <= token ? below : xt;
-                if (vm > thr)
-#pragma unroll
-                    for (int j = 0; j < kPer; ++j) before += x[j] > thr ? 1u : 0u;
-                if (token >= at && token < at + kPer)                 // equal logits before the token, in its own vector
-#pragma unroll
-                    for (int j = 0; j < kPer; ++j) before += x[j] == xt && at + j < token ? 1u : 0u;
+            if (p.k > 0) {
+                float rm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, 1));
+                rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, 2));
+                gmax = fmaxf(gmax, rm);
+                if ((tid & 3) == 0 && i < nvec) run_max[i >> 2] = rm;
             }
         }
-        if (p.k > 0) {
-            float rm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, 1));
-            rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, 2));
-            gmax = fmaxf(gmax, rm);
-            if ((tid & 3) == 0 && i < nvec) run_max[i >> 2] = rm;
-        }
     }
-    // ---- the block's sums, added in the order of warps and lanes
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float om = __shfl_down_sync(0xffffffffu, me.m, o), os = __shfl_down_sync(0xffffffffu, me.s, o), oa = __shfl_down_sync(0xffffffffu, me.a, o);
-        me.join(om, os, oa, c);
-    }
-    before = __reduce_add_sync(0xffffffffu, before);
-    if (lane == 0) {
-        sh.m[warp] = me.m; sh.s[warp] = me.s; sh.a[warp] = me.a; sh.n[warp] = before;
-    }
+    // ---- the block's maximum, then its sums relative to it, added in the order of lanes and warps
+    const float wm = warp_max(me.m);
+    if (lane == 0) sh.m[warp] = wm;
     gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, 1));
     gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, 2));
     if ((tid & 3) == 0) sh.gmax[tid >> 2] = gmax;
     if (tid == 0) {
         sh.n_cand = 0u;
         sh.n_runs = 0u;
-        sh.bound = -INFINITY;
     }
     __syncthreads();
-    Sums all = {sh.m[0], sh.s[0], sh.a[0]};
-    uint32_t rank = sh.n[0];
-    for (int w = 1; w < kNt / 32; ++w) {
-        all.join(sh.m[w], sh.s[w], sh.a[w], c);
-        rank += sh.n[w];
+    float bm = sh.m[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) bm = fmaxf(bm, sh.m[w]);
+    {
+        float s0, s1, a0, a1;
+        unpack_f2(me.s, s0, s1);
+        unpack_f2(me.a, a0, a1);
+        const float d = octaves(me.m, bm, c), f = ex2_approx(d), s = s0 + s1;
+        const float ws = warp_sum(f * s), wa = warp_sum(f * fmaf(d, s, a0 + a1));
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) {
+            sh.s[warp] = ws;
+            sh.a[warp] = wa;
+            sh.n[warp] = before;
+        }
     }
-    const bool any = all.m > -INFINITY;
-    const float ln_s = any ? logf(all.s) : 0.0f;
+    // ---- the k-th largest of the groups' maxima, ties broken by the group: four threads count for a group
+    if (p.k > 0) {
+        const int q = tid >> 2, from = (tid & 3) * (kGroups / 4);
+        const float v = sh.gmax[q];
+        int ahead_of = 0;
+#pragma unroll 4
+        for (int j = from; j < from + kGroups / 4; j += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(&sh.gmax[j]);
+            ahead_of += (u.x > v || (u.x == v && j < q)) + (u.y > v || (u.y == v && j + 1 < q)) + (u.z > v || (u.z == v && j + 2 < q)) +
+                        (u.w > v || (u.w == v && j + 3 < q));
+        }
+        ahead_of += __shfl_xor_sync(0xffffffffu, ahead_of, 1);
+        ahead_of += __shfl_xor_sync(0xffffffffu, ahead_of, 2);
+        if ((tid & 3) == 0 && ahead_of == p.k - 1) sh.bound = v;
+    }
+    __syncthreads();
+    float bs = 0.0f, ba = 0.0f;
+    uint32_t bn = 0u;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        bs += sh.s[w];
+        ba += sh.a[w];
+        bn += sh.n[w];
+    }
+    if (CL) cg::this_cluster().barrier_wait(static_cast<cg::cluster_group::arrival_token&&>(begun));
+    if (CL && tid == 0) {
+        LpShared<NT>* first = cg::this_cluster().map_shared_rank(&sh, 0);
+        first->row_m[rank] = bm;
+        first->row_s[rank] = bs;
+        first->row_a[rank] = ba;
+        first->row_n[rank] = bn;
+    }
+
+    // ---- the block's likeliest k, as keys in `top`, largest first
+    unsigned long long* top = CL ? cg::this_cluster().map_shared_rank(&sh, 0)->row_top + rank * kTop : sh.row_top;
+    if (p.k > 0) {
+        const float bound = sh.bound;
+        auto take = [&](float x, int i) {
+            if (x >= bound && x > -INFINITY) {
+                const uint32_t at = atomicAdd(&sh.n_cand, 1u);
+                if (at < kCand) sh.cand[at] = key_of(x, i0 + i);
+            }
+        };
+        if (tid < ends) {
+            const int at = tid < head ? tid : tail0 + (tid - head);
+            take(value(src, at), at);
+        }
+        for (int r = tid; r < n_runs; r += NT)
+            if (run_max[r] >= bound && run_max[r] > -INFINITY) {
+                const uint32_t at = atomicAdd(&sh.n_runs, 1u);
+                if (at < kRuns) sh.runs[at] = r;
+            }
+        __syncthreads();
+        if (sh.n_runs <= kRuns)
+            for (uint32_t r = warp; r < sh.n_runs; r += kWarps) {
+                const int at0 = sh.runs[r] * 4 * kPer;
+                for (int j = lane; j < 4 * kPer && at0 + j < nvec * kPer; j += 32) take(value(body, at0 + j), head + at0 + j);
+            }
+        __syncthreads();
+        if (sh.n_runs <= kRuns && sh.n_cand <= kCand) {
+            const int n = (int)sh.n_cand;
+            for (int i = tid; i < n; i += NT) {
+                const unsigned long long key = sh.cand[i];
+                int ahead_of = 0;
+                for (int j = 0; j < n; ++j) ahead_of += sh.cand[j] > key ? 1 : 0;
+                if (ahead_of < p.k) top[ahead_of] = key;
+            }
+            for (int i = n + tid; i < p.k; i += NT) top[i] = 0ull;
+        } else {                                          // too many at the bound: the next largest key, k times
+            unsigned long long last = ~0ull;
+            for (int q = 0; q < p.k; ++q) {
+                unsigned long long best = 0ull;
+                for (int i = tid; i < V; i += NT) {
+                    const unsigned long long key = key_of(value(src, i), i0 + i);
+                    if (key < last && key > best) best = key;
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    const unsigned long long u = __shfl_xor_sync(0xffffffffu, best, o);
+                    best = u > best ? u : best;
+                }
+                if (lane == 0) sh.best[warp] = best;
+                __syncthreads();
+                for (int w = 0; w < kWarps; ++w) best = sh.best[w] > best ? sh.best[w] : best;
+                if (tid == 0) top[q] = best;
+                last = best;
+                __syncthreads();
+            }
+        }
+    }
+    if (CL) {
+        cg::this_cluster().sync();
+        if (rank != 0) return;
+        bm = sh.row_m[0];
+        for (int r = 1; r < blocks; ++r) bm = fmaxf(bm, sh.row_m[r]);
+        bs = ba = 0.0f;
+        bn = 0u;
+        for (int r = 0; r < blocks; ++r) {
+            const float d = octaves(sh.row_m[r], bm, c), f = ex2_approx(d);
+            bs += f * sh.row_s[r];
+            ba += f * fmaf(d, sh.row_s[r], sh.row_a[r]);
+            bn += sh.row_n[r];
+        }
+    } else if (p.k > 0) __syncthreads();
+
+    // ---- the row
+    const bool any = bm > -INFINITY;
+    const float ln_s = any ? logf(bs) : 0.0f;
     auto ln_p = [&](float x, bool first) {
         if (greedy) return first ? 0.0f : -INFINITY;
-        return (x == all.m ? 0.0f : (x - all.m) / t) - ln_s;
+        return (x == bm ? 0.0f : (x - bm) / t) - ln_s;
     };
     if (tid == 0) {
         if (p.tokens != nullptr) {
             float lp;
-            if (token == -1) lp = 0.0f;
+            if (given == -1) lp = 0.0f;
             else if (!valid) {
                 lp = __uint_as_float(0x7fffffffu);
                 atomicOr(p.status, STWQ_DEV_TOKEN);
-            } else lp = ranked ? ln_p(xt, rank == 0u) : -INFINITY;
+            } else lp = ranked ? ln_p(xt, bn == 0u) : -INFINITY;
             p.logprobs[row] = lp;
-            if (p.ranks != nullptr) p.ranks[row] = ranked ? (int32_t)rank : -1;
+            if (p.ranks != nullptr) p.ranks[row] = ranked ? (int32_t)bn : -1;
         }
-        if (p.entropy != nullptr) p.entropy[row] = greedy || !any ? 0.0f : fmaxf(ln_s - 0.6931471805599453f * (all.a / all.s), 0.0f);
+        if (p.entropy != nullptr) p.entropy[row] = greedy || !any ? 0.0f : fmaxf(ln_s - 0.6931471805599453f * (ba / bs), 0.0f);
     }
     if (p.k == 0) return;
-
-    // ---- the likeliest k: the k-th largest of the groups' maxima, ties broken by the group
-    if (tid < kGroups) {
-        const float v = sh.gmax[tid];
-        int ahead = 0;
-        for (int j = 0; j < kGroups; ++j) {
-            const float u = sh.gmax[j];
-            ahead += u > v || (u == v && j < tid) ? 1 : 0;
-        }
-        if (ahead == p.k - 1) sh.bound = v;
-    }
-    __syncthreads();
-    const float bound = sh.bound;
-    auto take = [&](float x, int i) {
-        if (x >= bound && x > -INFINITY) {
-            const uint32_t at = atomicAdd(&sh.n_cand, 1u);
-            if (at < kCand) sh.cand[at] = key_of(x, i);
-        }
-    };
-    for (int i = tid; i < head + (p.V - tail0); i += kNt) {
-        const int at = i < head ? i : tail0 + (i - head);
-        take(value(src, at), at);
-    }
-    for (int r = tid; r < n_runs; r += kNt)
-        if (run_max[r] >= bound && run_max[r] > -INFINITY) {
-            const uint32_t at = atomicAdd(&sh.n_runs, 1u);
-            if (at < kRuns) sh.runs[at] = r;
-        }
-    __syncthreads();
-    if (sh.n_runs <= kRuns)
-        for (uint32_t r = warp; r < sh.n_runs; r += kNt / 32) {
-            const int at0 = sh.runs[r] * 4 * kPer;
-            for (int j = lane; j < 4 * kPer && at0 + j < nvec * kPer; j += 32) take(value(body, at0 + j), head + at0 + j);
-        }
-    __syncthreads();
     int32_t* ids = p.top_ids + row * p.k;
     float* lps = p.top_lp + row * p.k;
-    if (sh.n_runs <= kRuns && sh.n_cand <= kCand) {
-        const int n = (int)sh.n_cand;
-        for (int i = tid; i < n; i += kNt) {
-            const unsigned long long key = sh.cand[i];
-            int ahead = 0;
-            for (int j = 0; j < n; ++j) ahead += sh.cand[j] > key ? 1 : 0;
-            if (ahead < p.k) {
-                ids[ahead] = (int32_t)(0xffffffffu - (uint32_t)key);
-                lps[ahead] = ln_p(value_of(key), ahead == 0);
-            }
-        }
-        for (int i = n + tid; i < p.k; i += kNt) {
-            ids[i] = -1;
-            lps[i] = -INFINITY;
-        }
+    auto put = [&](unsigned long long key, int at) {
+        ids[at] = key ? index_of(key) : -1;
+        lps[at] = key ? ln_p(value_of(key), at == 0) : -INFINITY;
+    };
+    if (!CL) {
+        if (tid < p.k) put(sh.row_top[tid], tid);
         return;
     }
-    unsigned long long last = ~0ull;                      // too many at the bound: the next largest key, k times
-    for (int q = 0; q < p.k; ++q) {
-        unsigned long long best = 0ull;
-        for (int i = tid; i < p.V; i += kNt) {
-            const unsigned long long key = key_of(value(src, i), i);
-            if (key < last && key > best) best = key;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const unsigned long long u = __shfl_xor_sync(0xffffffffu, best, o);
-            best = u > best ? u : best;
-        }
-        if (lane == 0) sh.best[warp] = best;
-        __syncthreads();
-        for (int w = 0; w < kNt / 32; ++w) best = sh.best[w] > best ? sh.best[w] : best;
-        if (tid == 0) {
-            ids[q] = best ? (int32_t)(0xffffffffu - (uint32_t)best) : -1;
-            lps[q] = best ? ln_p(value_of(best), q == 0) : -INFINITY;
-        }
-        last = best;
-        __syncthreads();
+    // the blocks' lists together: keys that are not 0 are all different; those that are come last
+    if (tid < blocks * p.k) {
+        const int list = tid / p.k, j = tid - list * p.k;
+        const unsigned long long key = sh.row_top[list * kTop + j];
+        int ahead_of = 0;
+        for (int r = 0; r < blocks; ++r)
+            for (int i = 0; i < p.k; ++i) {
+                const unsigned long long u = sh.row_top[r * kTop + i];
+                ahead_of += u > key || (u == key && (r < list || (r == list && i < j))) ? 1 : 0;
+            }
+        if (ahead_of < p.k) put(key, ahead_of);
     }
 }
 
-template <typename XT>
-int launch_lp(stwq_ctx* ctx, const LpParams& p, int B, cudaStream_t st)
+template <typename XT, int NT, bool CL>
+int launch_lp(stwq_ctx* ctx, LpParams& p, int B, int blocks, cudaStream_t st)
 {
-    const size_t smem = p.k > 0 ? (size_t)(p.V / (4 * (32 / (int)sizeof(XT))) + 2) * 4 : 0;
-    cudaError_t e = cudaFuncSetAttribute(logprob_kernel<XT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxV / 32 + 2) * 4);
+    constexpr int kRun = 4 * Vec<XT>::kPer;
+    p.slice = CL ? ((p.V + blocks - 1) / blocks + kRun - 1) / kRun * kRun : p.V;
+    const size_t smem = p.k > 0 ? (size_t)(p.slice / kRun + 2) * 4 : 0;
+    auto kern = logprob_kernel<XT, NT, CL>;
+    cudaError_t e = cudaSuccess;
+    if (smem > 16 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxV / 32 + 2) * 4);
     if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
-    logprob_kernel<XT><<<(unsigned)B, kNt, smem, st>>>(p);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(B * blocks));
+    cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    if (CL) {
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)blocks;
+        at[0].val.clusterDim.y = 1;
+        at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+    }
+    e = cudaLaunchKernelEx(&cfg, kern, p);
     ctx->launches += 1;
-    e = cudaGetLastError();
+    if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
+}
+
+template <typename XT>
+int launch_lp_any(stwq_ctx* ctx, LpParams& p, int B, cudaStream_t st)
+{
+    // few rows: several blocks a row while SMs would idle and a block keeps two vectors a thread
+    int blocks = 1;
+    while (blocks < kMaxCluster && B * blocks * 2 <= ctx->sm_count && p.V / (2 * blocks) >= 512 * Vec<XT>::kPer) blocks *= 2;
+    if (blocks > 1) return launch_lp<XT, 512, true>(ctx, p, B, blocks, st);
+    const int vecs = p.V / Vec<XT>::kPer;
+    if (vecs <= 512) return launch_lp<XT, 128, false>(ctx, p, B, 1, st);
+    if (vecs <= 2048) return launch_lp<XT, 256, false>(ctx, p, B, 1, st);
+    return launch_lp<XT, 512, false>(ctx, p, B, 1, st);
 }
 
 }  // namespace
@@ -345,7 +506,7 @@ extern "C" int token_logprobs(stwq_ctx* ctx, const void* logits, int x_dtype, in
 {
     if (!ctx || !logits) return STWQ_ERR_NULL;
     if ((tokens == nullptr) != (logprobs == nullptr) || (tokens == nullptr && ranks != nullptr)) return STWQ_ERR_NULL;
-    if (B <= 0 || V <= 0 || V > kMaxV || ld < V || k < 0 || k > kTop) return STWQ_ERR_DIM;
+    if (B <= 0 || B > (1 << 27) || V <= 0 || V > kMaxV || ld < V || k < 0 || k > kTop) return STWQ_ERR_DIM;
     if ((k > 0) != (top_ids != nullptr) || (k > 0) != (top_logprobs != nullptr)) return STWQ_ERR_NULL;
     if (!logprobs && !entropy && k == 0) return STWQ_ERR_NULL;
     if (x_dtype != STWQ_OUT_F32 && x_dtype != STWQ_OUT_BF16) return STWQ_ERR_BITS;
@@ -357,5 +518,5 @@ extern "C" int token_logprobs(stwq_ctx* ctx, const void* logits, int x_dtype, in
     p.logprobs = logprobs; p.entropy = entropy; p.top_lp = top_logprobs; p.ranks = ranks; p.top_ids = top_ids;
     p.status = ctx->d_status;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return x_dtype == STWQ_OUT_BF16 ? launch_lp<__nv_bfloat16>(ctx, p, B, st) : launch_lp<float>(ctx, p, B, st);
+    return x_dtype == STWQ_OUT_BF16 ? launch_lp_any<__nv_bfloat16>(ctx, p, B, st) : launch_lp_any<float>(ctx, p, B, st);
 }

@@ -235,8 +235,12 @@ def test_rows_beyond_2_31_elements(gpu):
     X[-1], _ = logits(gpu, 1, V, "bfloat16", 10)[0][0], None
     t = torch.full((B,), 5, device=gpu.dev, dtype=torch.int32)
     lp, rank, ent, ids, tlp = run(gpu, X, t, None, 0)
+    # the row alone may be split among more blocks, whose sums are grouped differently: each result is held to its own bound
+    rlp, rrank, rent, _, e_s, e_ent = reference(X[-1].double().cpu().numpy(), 5, 1.0, 0)
     one = run(gpu, X[-1:].clone(), t[-1:], None, 0)
-    assert lp[-1] == one[0][0] and rank[-1] == one[1][0] and ent[-1] == one[2][0]
+    for got in ((lp[-1], rank[-1], ent[-1]), (one[0][0], one[1][0], one[2][0])):
+        close(float(got[0]), rlp[5], e_s)
+        assert got[1] == rrank and abs(float(got[2]) - rent) <= e_ent
     assert (rank[:-1] == 5).all() and ((lp[:-1] + np.log(V)).abs() < 2e-5).all()
 
 
