@@ -201,11 +201,29 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
+// How many of the n keys are larger than key `i`, counted by eight threads together (all 32 of a warp call it); keys that are equal (those
+// that are 0) count by position.
+__device__ __forceinline__ int place_of(const unsigned long long* keys, int n, int i, int lane)
+{
+    int ahead_of = 0;
+    if (i < n) {
+        const unsigned long long key = keys[i];
+#pragma unroll 4
+        for (int j = lane & 7; j < n; j += 8) {
+            const unsigned long long u = keys[j];
+            ahead_of += u > key || (u == key && j < i) ? 1 : 0;
+        }
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) ahead_of += __shfl_xor_sync(0xffffffffu, ahead_of, o);
+    return ahead_of;
+}
+
 // A block of NT threads takes a row, or (CL) a slice of one; the first block of the cluster joins the slices.
 template <typename XT, int NT, bool CL>
-__global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const LpParams p)
+__global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const LpParams p)
 {
-    constexpr int kPer = Vec<XT>::kPer, kGroups = NT / 4, kWarps = NT / 32, kAhead = 2;
+    constexpr int kPer = Vec<XT>::kPer, kGroups = NT / 4, kWarps = NT / 32, kAhead = CL ? 4 : 2;       // vectors in flight per thread
     extern __shared__ __align__(16) float run_max[];      // [runs of 4 vectors]
     __shared__ LpShared<NT> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -219,6 +237,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const LpParams p
     const int nvec = (V - head) / kPer, tail0 = head + nvec * kPer, ends = head + (V - tail0);
     const int n_runs = (nvec + 3) / 4;
     const XT* body = src + head;
+    const bool held = nvec <= kAhead * NT;                // all vectors stay in registers
 
     Vec<XT> ahead[kAhead];
 #pragma unroll
@@ -240,7 +259,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const LpParams p
 
     Sums<kPer> me = {-INFINITY, 0ull, 0ull, false};
     uint32_t before = 0u;
-    float gmax = -INFINITY;
+    float gmax = -INFINITY, vmax[kAhead];
     if (tid < ends) {                                     // the ragged ends, logit by logit (fewer than 32)
         const int at = tid < head ? tid : tail0 + (tid - head);
         const float x = value(src, at);
@@ -270,7 +289,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const LpParams p
                         for (int j = 0; j < kPer; ++j) before += x[j] == xt && at + j < token ? 1u : 0u;
                 }
             }
-            if (p.k > 0) {
+            vmax[u] = vm;
+            if (p.k > 0 && held) gmax = fmaxf(gmax, vm);
+            if (p.k > 0 && !held) {
                 float rm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, 1));
                 rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, 2));
                 gmax = fmaxf(gmax, rm);
@@ -339,7 +360,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const LpParams p
     }
 
     // ---- the block's likeliest k, as keys in `top`, largest first
-    unsigned long long* top = CL ? cg::this_cluster().map_shared_rank(&sh, 0)->row_top + rank * kTop : sh.row_top;
+    unsigned long long* top = CL ? cg::this_cluster().map_shared_rank(&sh, 0)->row_top + rank * p.k : sh.row_top;
     if (p.k > 0) {
         const float bound = sh.bound;
         auto take = [&](float x, int i) {
@@ -352,25 +373,38 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const LpParams p
             const int at = tid < head ? tid : tail0 + (tid - head);
             take(value(src, at), at);
         }
-        for (int r = tid; r < n_runs; r += NT)
-            if (run_max[r] >= bound && run_max[r] > -INFINITY) {
-                const uint32_t at = atomicAdd(&sh.n_runs, 1u);
-                if (at < kRuns) sh.runs[at] = r;
+        if (held) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = u * NT + tid;
+                if (i < nvec && vmax[u] >= bound) {
+                    float x[kPer];
+                    ahead[u].get(x);
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) take(x[j], head + i * kPer + j);
+                }
             }
-        __syncthreads();
-        if (sh.n_runs <= kRuns)
-            for (uint32_t r = warp; r < sh.n_runs; r += kWarps) {
-                const int at0 = sh.runs[r] * 4 * kPer;
-                for (int j = lane; j < 4 * kPer && at0 + j < nvec * kPer; j += 32) take(value(body, at0 + j), head + at0 + j);
-            }
+        } else {
+            for (int r = tid; r < n_runs; r += NT)
+                if (run_max[r] >= bound && run_max[r] > -INFINITY) {
+                    const uint32_t at = atomicAdd(&sh.n_runs, 1u);
+                    if (at < kRuns) sh.runs[at] = r;
+                }
+            __syncthreads();
+            if (sh.n_runs <= kRuns)
+                for (uint32_t r = warp; r < sh.n_runs; r += kWarps) {
+                    const int at0 = sh.runs[r] * 4 * kPer;
+#pragma unroll
+                    for (int j = 0; j < 4 * kPer; j += 32)
+                        if (at0 + j + lane < nvec * kPer) take(value(body, at0 + j + lane), head + at0 + j + lane);
+                }
+        }
         __syncthreads();
         if (sh.n_runs <= kRuns && sh.n_cand <= kCand) {
             const int n = (int)sh.n_cand;
-            for (int i = tid; i < n; i += NT) {
-                const unsigned long long key = sh.cand[i];
-                int ahead_of = 0;
-                for (int j = 0; j < n; ++j) ahead_of += sh.cand[j] > key ? 1 : 0;
-                if (ahead_of < p.k) top[ahead_of] = key;
+            for (int first = 0; first < n; first += NT / 8) {
+                const int i = first + (tid >> 3), at = place_of(sh.cand, n, i, lane);
+                if (i < n && at < p.k && (lane & 7) == 0) top[at] = sh.cand[i];
             }
             for (int i = n + tid; i < p.k; i += NT) top[i] = 0ull;
         } else {                                          // too many at the bound: the next largest key, k times
@@ -441,17 +475,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const LpParams p
         if (tid < p.k) put(sh.row_top[tid], tid);
         return;
     }
-    // the blocks' lists together: keys that are not 0 are all different; those that are come last
-    if (tid < blocks * p.k) {
-        const int list = tid / p.k, j = tid - list * p.k;
-        const unsigned long long key = sh.row_top[list * kTop + j];
-        int ahead_of = 0;
-        for (int r = 0; r < blocks; ++r)
-            for (int i = 0; i < p.k; ++i) {
-                const unsigned long long u = sh.row_top[r * kTop + i];
-                ahead_of += u > key || (u == key && (r < list || (r == list && i < j))) ? 1 : 0;
-            }
-        if (ahead_of < p.k) put(key, ahead_of);
+    // the blocks' lists together (p.k apart); places without a token hold 0 and come last
+    const int n = blocks * p.k;
+    for (int first = 0; first < n; first += NT / 8) {
+        const int i = first + (tid >> 3), at = place_of(sh.row_top, n, i, lane);
+        if (i < n && at < p.k && (lane & 7) == 0) put(sh.row_top[i], at);
     }
 }
 
