@@ -111,49 +111,53 @@ __device__ __forceinline__ float value_of(unsigned long long key)
     return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
 }
 __device__ __forceinline__ int index_of(unsigned long long key) { return (int)(0xffffffffu - (uint32_t)key); }
-// octaves between a logit and the maximum; the maximum itself at 0 (also at +Inf), masked ones (NaN too) at kLow
+// octaves between a logit and a reference; the reference itself at 0 (also at +Inf), masked ones (NaN too) at kLow
 __device__ __forceinline__ float octaves(float x, float m, float c) { return x == m ? 0.0f : fmaxf((x - m) * c, kLow); }
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) < INFINITY; }
+// m c, while its rounding is a small part of an octave; else Inf
+__device__ __forceinline__ float times_c(float m, float c) { return fabsf(m * c) < 1e6f ? m * c : INFINITY; }
 
-// What a thread has seen of a row: the maximum, and relative to it S and A, each as two partial sums.
+// What a thread has seen of a row: a reference m, not far below the largest logit, and S and A relative to it, each as two partial
+// sums. With mc = m c rounded to fp32, a logit's octaves are x c - mc in one fma: off from (x - m) c by the rounding of mc, the same for
+// every logit (the end takes it out of S, and A / S - log2 S does not see it). Where m c is large, octaves() serves instead.
 template <int PER>
 struct Sums {
-    float m;
+    float m, mc, c;
     uint64_t s, a;
-    bool odd;                                // a logit that has no weight came by
-    __device__ __forceinline__ void raise(float to, float c)                 // `to` > m
+    bool odd;                                // a logit without a weight came by
+    __device__ __forceinline__ float z_of(float x) const { return finite(mc) ? fmaxf(fmaf(x, c, -mc), kLow) : octaves(x, m, c); }
+    // what sums relative to (m, mc) are multiplied by, in octaves, to stand relative to (to, toc)
+    __device__ __forceinline__ float shift(float to, float toc) const
     {
-        const float d = octaves(m, to, c);
+        return m == to ? 0.0f : finite(mc) && finite(toc) ? fmaxf(mc - toc, kLow) : octaves(m, to, c);
+    }
+    __device__ __forceinline__ void raise(float to)       // `to` > m
+    {
+        const float toc = times_c(to, c), d = shift(to, toc);
         const uint64_t f = dup_f2(ex2_approx(d));
         a = mul_f2(f, fma_f2(dup_f2(d), s, a));
         s = mul_f2(f, s);
         m = to;
+        mc = toc;
     }
-    __device__ __forceinline__ void add(float x, float c)                    // one logit
+    __device__ __forceinline__ void add(float x)                             // one logit
     {
-        if (x > m) raise(x, c);
+        if (x > m) raise(x);
         if (!(x > -INFINITY)) return;
-        const float z = octaves(x, m, c), w = ex2_approx(z);
-        s = fma_f2(pack_f2(w, 0.0f), pack_f2(1.0f, 1.0f), s);
+        const float z = z_of(x), w = ex2_approx(z);
+        s = add_f2(s, pack_f2(w, 0.0f));
         a = fma_f2(pack_f2(w, 0.0f), pack_f2(z, 0.0f), a);
     }
-    // a vector whose largest is vm. Weights of -Inf and NaN are not told apart from the others until the sums show NaN (0 * -Inf); from then on
-    // the thread clamps every exponent.
-    __device__ __forceinline__ void add(const float (&x)[PER], float vm, float c)
+    // A vector. Neither its maximum nor logits without a weight are looked for: logits above the reference make sum w z grow, -Inf and NaN
+    // make it NaN (0 * -Inf). Then, and for vectors of a thread that has met a logit without a weight, more is done.
+    __device__ __forceinline__ void add(const float (&x)[PER])
     {
-        if (vm > m) raise(vm, c);
-        if (vm == INFINITY) {
-            float n = 0.0f;
-#pragma unroll
-            for (int j = 0; j < PER; ++j) n += x[j] == INFINITY ? 1.0f : 0.0f;
-            s = fma_f2(pack_f2(n, 0.0f), pack_f2(1.0f, 1.0f), s);
-            return;
-        }
-        const uint64_t off = dup_f2(-m), scale = dup_f2(c);
         if (!odd) {
+            const uint64_t off = dup_f2(-mc), scale = dup_f2(c);
             uint64_t vs = 0ull, va = 0ull;
 #pragma unroll
             for (int j = 0; j < PER; j += 2) {
-                const uint64_t z = mul_f2(add_f2(pack_f2(x[j], x[j + 1]), off), scale);
+                const uint64_t z = fma_f2(pack_f2(x[j], x[j + 1]), scale, off);
                 float z0, z1;
                 unpack_f2(z, z0, z1);
                 const uint64_t w = pack_f2(ex2_approx(z0), ex2_approx(z1));
@@ -162,23 +166,26 @@ struct Sums {
             }
             float a0, a1;
             unpack_f2(va, a0, a1);
-            if (a0 + a1 == a0 + a1) {
+            if (a0 + a1 < 64.0f) {                        // no logit 4 octaves above the reference: ln p near 0 keeps its digits
                 s = add_f2(s, vs);
                 a = add_f2(a, va);
                 return;
             }
-            odd = true;
         }
+        float vm = x[0];
 #pragma unroll
-        for (int j = 0; j < PER; j += 2) {
-            float z0, z1;
-            unpack_f2(mul_f2(add_f2(pack_f2(x[j], x[j + 1]), off), scale), z0, z1);
-            z0 = fmaxf(z0, kLow);
-            z1 = fmaxf(z1, kLow);
-            const uint64_t w = pack_f2(ex2_approx(z0), ex2_approx(z1));
-            s = add_f2(s, w);
-            a = fma_f2(w, pack_f2(z0, z1), a);
+        for (int j = 1; j < PER; ++j) vm = fmaxf(vm, x[j]);                   // NaN left out
+        if (vm > m) raise(vm);
+        float vs = 0.0f, va = 0.0f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            odd |= !(x[j] > -INFINITY);
+            const float z = z_of(x[j]), w = ex2_approx(z);
+            vs += w;
+            va = fmaf(w, z, va);
         }
+        s = add_f2(s, pack_f2(vs, 0.0f));
+        a = add_f2(a, pack_f2(va, 0.0f));
     }
     static __device__ __forceinline__ uint64_t add_f2(uint64_t u, uint64_t v)
     {
@@ -187,6 +194,22 @@ struct Sums {
         return r;
     }
 };
+// How many logits of a vector exceed thr.
+template <typename XT>
+__device__ __forceinline__ uint32_t above(const Vec<XT>& v, const float (&x)[Vec<XT>::kPer], float thr)
+{
+    if (sizeof(XT) == 4) {
+        uint32_t n = 0u;
+#pragma unroll
+        for (int j = 0; j < Vec<XT>::kPer; ++j) n += x[j] > thr ? 1u : 0u;
+        return n;
+    }
+    const __nv_bfloat162 t = __float2bfloat162_rn(thr);   // thr is a bf16 value; the counts are small integers
+    __nv_bfloat162 n = __hgt2(*reinterpret_cast<const __nv_bfloat162*>(&v.w[0]), t);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) n = __hadd2(n, __hgt2(*reinterpret_cast<const __nv_bfloat162*>(&v.w[i]), t));
+    return (uint32_t)(__low2float(n) + __high2float(n));
+}
 
 __device__ __forceinline__ float warp_max(float v)                           // NaN left out
 {
@@ -254,18 +277,29 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
     const int token = given - i0;                         // in this block's count
     // what a logit before the token has to exceed to stand before it in the order: the next value below (an equal one does);
     // behind the token it has to exceed the token's
-    const float below = __fadd_rn(xt, 0.0f) == 0.0f ? -1.401298464e-45f
-                        : __uint_as_float(xt > 0.0f ? __float_as_uint(xt) - 1u : __float_as_uint(xt) + 1u);
+    constexpr uint32_t kUlp = sizeof(XT) == 4 ? 1u : 0x10000u;
+    const float below = __fadd_rn(xt, 0.0f) == 0.0f ? -__uint_as_float(kUlp)
+                        : __uint_as_float(xt > 0.0f ? __float_as_uint(xt) - kUlp : __float_as_uint(xt) + kUlp);
 
-    Sums<kPer> me = {-INFINITY, 0ull, 0ull, false};
+    Sums<kPer> me = {-INFINITY, INFINITY, c, 0ull, 0ull, false};
     uint32_t before = 0u;
     float gmax = -INFINITY, vmax[kAhead];
     if (tid < ends) {                                     // the ragged ends, logit by logit (fewer than 32)
         const int at = tid < head ? tid : tail0 + (tid - head);
         const float x = value(src, at);
-        me.add(x, c);
+        me.add(x);
         gmax = fmaxf(gmax, x);
         if (ranked && x > (at < token ? below : xt)) ++before;
+    }
+    {   // the largest of the warp's first vectors for a start: logits far above it are rare then, and with them divergence
+        float vm = -INFINITY;
+        if (tid < nvec) {
+            float x[kPer];
+            ahead[0].get(x);
+            vm = fmaxf(vm, ahead[0].largest(x));
+        }
+        vm = warp_max(vm);
+        if (vm > me.m) me.raise(vm);
     }
     for (int b0 = 0; b0 < nvec; b0 += kAhead * NT) {
 #pragma unroll
@@ -275,19 +309,16 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
             if (i < nvec) {
                 float x[kPer];
                 ahead[u].get(x);
-                vm = fmaxf(vm, ahead[u].largest(x));
-                if (i + kAhead * NT < nvec) ahead[u].load(body + (int64_t)(i + kAhead * NT) * kPer);
-                me.add(x, vm, c);
+                if (p.k > 0) vm = fmaxf(vm, ahead[u].largest(x));
                 if (ranked) {
                     const int at = head + i * kPer;
-                    const float thr = at + kPer <= token ? below : xt;
-                    if (vm > thr)
-#pragma unroll
-                        for (int j = 0; j < kPer; ++j) before += x[j] > thr ? 1u : 0u;
+                    before += above<XT>(ahead[u], x, at + kPer <= token ? below : xt);
                     if (token >= at && token < at + kPer)             // equal logits before the token, in its own vector
 #pragma unroll
                         for (int j = 0; j < kPer; ++j) before += x[j] == xt && at + j < token ? 1u : 0u;
                 }
+                if (i + kAhead * NT < nvec) ahead[u].load(body + (int64_t)(i + kAhead * NT) * kPer);
+                me.add(x);
             }
             vmax[u] = vm;
             if (p.k > 0 && held) gmax = fmaxf(gmax, vm);
@@ -310,14 +341,14 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
         sh.n_runs = 0u;
     }
     __syncthreads();
-    float bm = sh.m[0];
+    float bm = sh.m[0];                                    // the blocks' common reference
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) bm = fmaxf(bm, sh.m[w]);
     {
         float s0, s1, a0, a1;
         unpack_f2(me.s, s0, s1);
         unpack_f2(me.a, a0, a1);
-        const float d = octaves(me.m, bm, c), f = ex2_approx(d), s = s0 + s1;
+        const float d = me.shift(bm, times_c(bm, c)), f = ex2_approx(d), s = s0 + s1;
         const float ws = warp_sum(f * s), wa = warp_sum(f * fmaf(d, s, a0 + a1));
         before = __reduce_add_sync(0xffffffffu, before);
         if (lane == 0) {
@@ -437,7 +468,8 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
         bs = ba = 0.0f;
         bn = 0u;
         for (int r = 0; r < blocks; ++r) {
-            const float d = octaves(sh.row_m[r], bm, c), f = ex2_approx(d);
+            const Sums<kPer> part = {sh.row_m[r], times_c(sh.row_m[r], c), c, 0ull, 0ull, false};
+            const float d = part.shift(bm, times_c(bm, c)), f = ex2_approx(d);
             bs += f * sh.row_s[r];
             ba += f * fmaf(d, sh.row_s[r], sh.row_a[r]);
             bn += sh.row_n[r];
@@ -446,7 +478,9 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
 
     // ---- the row
     const bool any = bm > -INFINITY;
-    const float ln_s = any ? logf(bs) : 0.0f;
+    const float ln2 = 0.6931471805599453f, bmc = times_c(bm, c), ln_sums = any ? logf(bs) : 0.0f;
+    // S relative to bm itself: less the rounding of bm c
+    const float ln_s = finite(bmc) ? fmaf(-ln2, fmaf(bm, c, -bmc), ln_sums) : ln_sums;
     auto ln_p = [&](float x, bool first) {
         if (greedy) return first ? 0.0f : -INFINITY;
         return (x == bm ? 0.0f : (x - bm) / t) - ln_s;
@@ -462,7 +496,7 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
             p.logprobs[row] = lp;
             if (p.ranks != nullptr) p.ranks[row] = ranked ? (int32_t)bn : -1;
         }
-        if (p.entropy != nullptr) p.entropy[row] = greedy || !any ? 0.0f : fmaxf(ln_s - 0.6931471805599453f * (ba / bs), 0.0f);
+        if (p.entropy != nullptr) p.entropy[row] = greedy || !any ? 0.0f : fmaxf(fmaf(-ln2, ba / bs, ln_sums), 0.0f);
     }
     if (p.k == 0) return;
     int32_t* ids = p.top_ids + row * p.k;
