@@ -517,53 +517,85 @@ class Context:
                                           self._raw_stream(stream)), "sample_tokens")
 
     # ---- around the attention of a step: norms with gate and residual, few-row 4-bit linears, log probabilities
-    def block_norm(self, H, O, cond_ids, gate, scale, shift, post_norm, w_post, b_post, res_scale, pre_norm, w_pre, b_pre, eps, Hout,
-                   pos_ids, s_ch, s_tok, bits, Y, stream=None):
-        where, dev, f32, i32, bf = "block_norm", self.device, self._f32, self._i32, self._torch.bfloat16
+    # As above the operands of a call are looked over in a quick form (written out, since a call of these is about as long as its kernel);
+    # what that does not pass goes through the checks that say what is wrong.
+    def _check_block_norm(self, H, O, cond_ids, gate, scale, shift, w_post, b_post, w_pre, b_pre, Hout, pos_ids, s_ch, s_tok, Y):
+        where, dev = "block_norm", self.device
         both = (_F32, _BF16)
-        ldh = self._rows(where, "H", H, both, (None, None))[0]
+        check_rows(where, dev, "H", H, both, (None, None), 1)
         M, C = H.shape
-        h_dtype = OUT_BF16 if H.dtype is bf else OUT_F32
-        ldo = ldho = ldy = C
-        o_dtype = y_dtype = OUT_F32
-        if O is not None:
-            ldo = self._rows(where, "O", O, both, (M, C))[0]
-            o_dtype = OUT_BF16 if O.dtype is bf else OUT_F32
-        if Hout is not None:
-            ldho = self._rows(where, "Hout", Hout, (_BF16,) if h_dtype else (_F32,), (M, C))[0]
-        if Y is not None:
-            if Y.dtype is self._torch.int8:
-                check_rows(where, dev, "Y", Y, (_I8,), (M, C), 1)
-                ldy, y_dtype = Y.stride(0), OUT_INT8
-            else:
-                ldy = self._rows(where, "Y", Y, both, (M, C))[0]
-                y_dtype = OUT_BF16 if Y.dtype is bf else OUT_F32
-        if M == 1:                                       # the stride of a single row means nothing
-            ldh = ldo = ldho = ldy = C
-        G = ldc = c_dtype = 0
+        for name, t, kinds in (("O", O, both), ("Hout", Hout, (str(H.dtype),)), ("Y", Y, both + (_I8,))):
+            if t is not None:
+                check_rows(where, dev, name, t, kinds, (M, C), 1)
+        first = None
         for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
             if t is None:
                 continue
-            ld = self._rows(where, name, t, both, (G or None, C))[0]
-            if G and ((ld != ldc and G > 1) or t.dtype is not kind):
+            check_rows(where, dev, name, t, both, (None if first is None else first.shape[0], C), 1)
+            if first is not None and (t.dtype is not first.dtype or (t.stride(0) != first.stride(0) and t.shape[0] > 1)):
                 raise StwqError(ERR_DIM, where, "gate, scale and shift have one type and one row stride")
-            G, ldc, kind = t.shape[0], ld, t.dtype
-            c_dtype = OUT_BF16 if kind is bf else OUT_F32
-        if cond_ids is None and G > 1:
+            first = t if first is None else first
+        if cond_ids is None and first is not None and first.shape[0] > 1:
             raise StwqError(ERR_NULL, where, "cond_ids is None, and the conditioning has more than one row")
+        P = s_tok.numel() if s_tok is not None else 0
+        self._args(where, *[(name, t, kind, (n,), True) for name, t, n, kind in (
+            ("cond_ids", cond_ids, M, _I32), ("pos_ids", pos_ids, M, _I32), ("w_post", w_post, C, _F32), ("b_post", b_post, C, _F32),
+            ("w_pre", w_pre, C, _F32), ("b_pre", b_pre, C, _F32), ("s_ch", s_ch, C, _F32), ("s_tok", s_tok, P, _F32))])
+
+    def block_norm(self, H, O, cond_ids, gate, scale, shift, post_norm, w_post, b_post, res_scale, pre_norm, w_pre, b_pre, eps, Hout,
+                   pos_ids, s_ch, s_tok, bits, Y, stream=None):
+        dev, f32, i32, bf, i8 = self.device, self._f32, self._i32, self._torch.bfloat16, self._torch.int8
+        try:
+            sh, kh, st = H.shape, H.dtype, H.stride()
+            M, C = sh
+            ldh, good = st[0], st[1] == 1 and (kh is bf or kh is f32) and H.get_device() == dev
+            ko, ky, ldo, ldho, ldy, G, ldc, kc = kh, kh, C, C, C, 0, 0, f32
+            if O is not None:
+                ko, st = O.dtype, O.stride()
+                ldo, good = st[0], good and st[1] == 1 and O.shape == sh and (ko is bf or ko is f32) and O.get_device() == dev
+            if Hout is not None:
+                st = Hout.stride()
+                ldho, good = st[0], good and st[1] == 1 and Hout.shape == sh and Hout.dtype is kh and Hout.get_device() == dev
+            if Y is not None:
+                ky, st = Y.dtype, Y.stride()
+                ldy, good = st[0], good and st[1] == 1 and Y.shape == sh and (ky is bf or ky is f32 or ky is i8) and Y.get_device() == dev
+            for t in (gate, scale, shift):
+                if t is not None:
+                    st = t.stride()
+                    if G:
+                        good = good and t.dtype is kc and t.shape == sc and (st[0] == ldc or G == 1)
+                    else:
+                        kc, sc = t.dtype, t.shape
+                        ldc, G, good = st[0], sc[0], good and len(sc) == 2 and sc[1] == C and (kc is bf or kc is f32)
+                    good = good and st[1] == 1 and t.get_device() == dev
+            n, P = (C,), 0
+            good = good and (cond_ids is not None or G < 2) and (cond_ids is None or _ok(cond_ids, i32, (M,), dev))
+            if pos_ids is not None:
+                good = good and _ok(pos_ids, i32, (M,), dev)
+            for t in (w_post, b_post, w_pre, b_pre, s_ch):
+                if t is not None:
+                    good = good and _ok(t, f32, n, dev)
+            if s_tok is not None:
+                P = s_tok.numel()
+                good = good and _ok(s_tok, f32, (P,), dev)
+        except (AttributeError, TypeError, ValueError, IndexError):
+            good = False
+        if not good:
+            self._check_block_norm(H, O, cond_ids, gate, scale, shift, w_post, b_post, w_pre, b_pre, Hout, pos_ids, s_ch, s_tok, Y)
+        if M == 1:                                       # the stride of a single row means nothing
+            ldh = ldo = ldho = ldy = C
         if G == 1:
             ldc = C
-        P = s_tok.numel() if s_tok is not None else 0
-        for name, t, n, kind in (("cond_ids", cond_ids, M, i32), ("pos_ids", pos_ids, M, i32), ("w_post", w_post, C, f32), ("b_post", b_post, C, f32),
-                                 ("w_pre", w_pre, C, f32), ("b_pre", b_pre, C, f32), ("s_ch", s_ch, C, f32), ("s_tok", s_tok, P, f32)):
-            if t is not None and not _ok(t, kind, (n,), dev):
-                self._args(where, (name, t, _I32 if kind is i32 else _F32, (n,), True))
-        q = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        rc = self._L.block_norm(self._h, H.data_ptr(), ldh, h_dtype, q(O), ldo, o_dtype, M, C, q(cond_ids), G, q(gate), q(scale), q(shift), ldc,
-                                c_dtype, post_norm, q(w_post), q(b_post), res_scale, pre_norm, q(w_pre), q(b_pre), eps, q(Hout), ldho, q(pos_ids),
-                                q(s_ch), q(s_tok), P, bits, q(Y), ldy, y_dtype, self._raw_stream(stream))
+        rc = self._L.block_norm(self._h, H.data_ptr(), ldh, 1 if kh is bf else 0, None if O is None else O.data_ptr(), ldo, 1 if ko is bf else 0, M, C,
+                                None if cond_ids is None else cond_ids.data_ptr(), G, None if gate is None else gate.data_ptr(),
+                                None if scale is None else scale.data_ptr(), None if shift is None else shift.data_ptr(), ldc, 1 if kc is bf else 0,
+                                post_norm, None if w_post is None else w_post.data_ptr(), None if b_post is None else b_post.data_ptr(), res_scale,
+                                pre_norm, None if w_pre is None else w_pre.data_ptr(), None if b_pre is None else b_pre.data_ptr(), eps,
+                                None if Hout is None else Hout.data_ptr(), ldho, None if pos_ids is None else pos_ids.data_ptr(),
+                                None if s_ch is None else s_ch.data_ptr(), None if s_tok is None else s_tok.data_ptr(), P, bits,
+                                None if Y is None else Y.data_ptr(), ldy, 3 if ky is i8 else 1 if ky is bf else 0, self._raw_stream(stream))
         if rc:
-            self._check(rc, where)
+            self._check(rc, "block_norm")
 
     def gps_fold_group4(self, W, s_ch, Wp, s_g, stream=None):
         N, K = _mk(W, "W")
@@ -578,42 +610,55 @@ class Context:
 
     def linear_w4g(self, X, Wp, s_g, bias, act, out_dtype, Y, stream=None):
         where, dev, f32, bf = "linear_w4g", self.device, self._f32, self._torch.bfloat16
-        ldx = self._rows(where, "X", X, (_F32, _BF16), (None, None))[0]
-        M, K = X.shape
-        N, groups = _mk(s_g, "s_g")
-        if groups <= 0 or K % groups:
-            raise StwqError(ERR_DIM, where, f"s_g has {groups} groups, which do not divide {K} channels")
-        if out_dtype not in (OUT_F32, OUT_BF16):
-            raise StwqError(ERR_BITS, where, f"out_dtype {out_dtype} is not OUT_F32 / OUT_BF16")
-        s_bf = s_g.dtype is bf
-        if not (_ok(Wp, self._torch.uint8, (N, K // 2), dev) and _ok(s_g, bf if s_bf else f32, (N, groups), dev)
-                and (bias is None or _ok(bias, f32, (N,), dev)) and _ok(Y, bf if out_dtype else f32, (M, N), dev)):
-            self._args(where, ("Wp", Wp, _U8, (N, K // 2), False), ("s_g", s_g, _BF16 if s_bf else _F32, (N, groups), False),
+        try:
+            (M, K), kx, st, (N, groups), ks = X.shape, X.dtype, X.stride(), s_g.shape, s_g.dtype
+            good = (st[1] == 1 and (kx is bf or kx is f32) and X.get_device() == dev and K % groups == 0 and (ks is bf or ks is f32)
+                    and s_g.is_contiguous() and s_g.get_device() == dev and Wp.dtype is self._torch.uint8 and Wp.shape == (N, K // 2)
+                    and Wp.is_contiguous() and Wp.get_device() == dev and (bias is None or _ok(bias, f32, (N,), dev))
+                    and (out_dtype == OUT_F32 or out_dtype == OUT_BF16) and _ok(Y, bf if out_dtype else f32, (M, N), dev))
+        except (AttributeError, TypeError, ValueError, IndexError, ZeroDivisionError):
+            good = False
+        if not good:
+            check_rows(where, dev, "X", X, (_F32, _BF16), (None, None), 1)
+            (M, K), (N, groups) = X.shape, _mk(s_g, "s_g")
+            if groups <= 0 or K % groups:
+                raise StwqError(ERR_DIM, where, f"s_g has {groups} groups, which do not divide {K} channels")
+            if out_dtype not in (OUT_F32, OUT_BF16):
+                raise StwqError(ERR_BITS, where, f"out_dtype {out_dtype} is not OUT_F32 / OUT_BF16")
+            self._args(where, ("Wp", Wp, _U8, (N, K // 2), False), ("s_g", s_g, _BF16 if s_g.dtype is bf else _F32, (N, groups), False),
                        ("bias", bias, _F32, (N,), True), ("Y", Y, _OUT_DTYPES[out_dtype], (M, N), False))
-        rc = self._L.linear_w4g(self._h, X.data_ptr(), ldx if M > 1 else K, OUT_BF16 if X.dtype is bf else OUT_F32, M, K, N, Wp.data_ptr(),
-                                s_g.data_ptr(), OUT_BF16 if s_bf else OUT_F32, K // groups, None if bias is None else bias.data_ptr(), act,
-                                out_dtype, Y.data_ptr(), self._raw_stream(stream))
+        rc = self._L.linear_w4g(self._h, X.data_ptr(), st[0] if M > 1 else K, 1 if kx is bf else 0, M, K, N, Wp.data_ptr(), s_g.data_ptr(),
+                                1 if ks is bf else 0, K // groups, None if bias is None else bias.data_ptr(), act, out_dtype, Y.data_ptr(),
+                                self._raw_stream(stream))
         if rc:
             self._check(rc, where)
 
     def token_logprobs(self, logits, temperature, tokens, logprobs, ranks=None, entropy=None, top_ids=None, top_logprobs=None, stream=None):
-        where, dev, i32, f32 = "token_logprobs", self.device, self._i32, self._f32
-        ld = self._rows(where, "logits", logits, (_F32, _BF16), (None, None))[0]
-        B, V = logits.shape
-        n, k = (B,), 0
-        if top_ids is not None:
-            k = _mk(top_ids, "top_ids")[1]
-        if not ((temperature is None or _ok(temperature, f32, n, dev)) and (tokens is None or _ok(tokens, i32, n, dev))
-                and (logprobs is None or _ok(logprobs, f32, n, dev)) and (ranks is None or _ok(ranks, i32, n, dev))
-                and (entropy is None or _ok(entropy, f32, n, dev)) and (top_ids is None or _ok(top_ids, i32, (B, k), dev))
-                and (top_logprobs is None or _ok(top_logprobs, f32, (B, k), dev))):
+        where, dev, i32, f32, bf = "token_logprobs", self.device, self._i32, self._f32, self._torch.bfloat16
+        k = 0
+        try:
+            (B, V), kx, st = logits.shape, logits.dtype, logits.stride()
+            n = (B,)
+            if top_ids is not None:
+                k = top_ids.shape[1]
+            good = (st[1] == 1 and (kx is bf or kx is f32) and logits.get_device() == dev and (temperature is None or _ok(temperature, f32, n, dev))
+                    and (tokens is None or _ok(tokens, i32, n, dev)) and (logprobs is None or _ok(logprobs, f32, n, dev))
+                    and (ranks is None or _ok(ranks, i32, n, dev)) and (entropy is None or _ok(entropy, f32, n, dev))
+                    and (top_ids is None or _ok(top_ids, i32, (B, k), dev)) and (top_logprobs is None or _ok(top_logprobs, f32, (B, k), dev)))
+        except (AttributeError, TypeError, ValueError, IndexError):
+            good = False
+        if not good:
+            check_rows(where, dev, "logits", logits, (_F32, _BF16), (None, None), 1)
+            B, n = logits.shape[0], (logits.shape[0],)
+            k = 0 if top_ids is None else _mk(top_ids, "top_ids")[1]
             self._args(where, ("temperature", temperature, _F32, n, True), ("tokens", tokens, _I32, n, True), ("logprobs", logprobs, _F32, n, True),
                        ("ranks", ranks, _I32, n, True), ("entropy", entropy, _F32, n, True), ("top_ids", top_ids, _I32, (B, k), True),
                        ("top_logprobs", top_logprobs, _F32, (B, k), True))
-        q = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        rc = self._L.token_logprobs(self._h, logits.data_ptr(), OUT_BF16 if logits.dtype is self._torch.bfloat16 else OUT_F32,
-                                    max(ld, V) if B == 1 else ld, B, V, q(temperature), q(tokens), q(logprobs), q(ranks), q(entropy), k, q(top_ids),
-                                    q(top_logprobs), self._raw_stream(stream))
+        rc = self._L.token_logprobs(self._h, logits.data_ptr(), 1 if kx is bf else 0, st[0] if B > 1 else max(st[0], V), B, V,
+                                    None if temperature is None else temperature.data_ptr(), None if tokens is None else tokens.data_ptr(),
+                                    None if logprobs is None else logprobs.data_ptr(), None if ranks is None else ranks.data_ptr(),
+                                    None if entropy is None else entropy.data_ptr(), k, None if top_ids is None else top_ids.data_ptr(),
+                                    None if top_logprobs is None else top_logprobs.data_ptr(), self._raw_stream(stream))
         if rc:
             self._check(rc, where)
 

@@ -52,6 +52,7 @@ struct stwq_ctx {
     int probe_configured;      // the peak-probe kernel has its shared-memory attribute set
     int attn_configured;       // so has the one-kernel attention head
     int attn_few_configured;   // and the few-query attention kernel
+    uint32_t w4g_configured;   // variants of the few-row 4-bit kernel that have theirs
     void* encode_tiled;        // cuTensorMapEncodeTiled, resolved at create
 };
 

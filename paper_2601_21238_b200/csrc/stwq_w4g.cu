@@ -446,8 +446,13 @@ int launch_w4(stwq_ctx* ctx, W4Params& p, size_t resident, cudaStream_t st)
     p.stages = (size_t)warps * (4 * kStage + kSets) + resident <= (two ? kHalf : kAll) ? 4 : 3;
     const size_t smem = (size_t)warps * (p.stages * kStage + kSets) + resident;
     auto kern = linear_w4g_kernel<RT, MT, XF, FINE, RES>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
+    cudaError_t e = cudaSuccess;
+    constexpr uint32_t kVariant = 1u << ((RT - 1) | (MT - 1) << 1 | (XF ? 4 : 0) | (FINE ? 8 : 0) | (RES ? 16 : 0));
+    if (!(ctx->w4g_configured & kVariant)) {
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAll);
+        if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
+        ctx->w4g_configured |= kVariant;
+    }
     const int slots = (two ? 2 : 1) * ctx->sm_count;
     const int passes = (p.M + kCols - 1) / kCols, share = slots / passes > 0 ? slots / passes : 1;        // over the weights, side by side
     const dim3 grid((unsigned)(p.tiles < share ? p.tiles : share), (unsigned)passes);
