@@ -63,6 +63,7 @@ struct W4Params {
     const void* X;
     int64_t ldx;
     int M, K, N, per_row, chunks, tiles, stages;
+    int side_log;                           // warps that hold different output channels of a tile, as a power of two; the others split K
     uint32_t group32, magic;                // 32-channel units per group, and ceil(2^32 / that): i / group32 = umulhi(i, magic) for i < 2^12
     const uint8_t* Wp;
     const void* s_g;
@@ -123,13 +124,13 @@ struct CodeFeed {
     const uint8_t* row[RT * 2];
     int tile, chunk, slot;
     __device__ __forceinline__ CodeFeed() : slot(0) {}
-    __device__ __forceinline__ void enter(const W4Params& p, int to_tile, int warp, int g, int t)
+    __device__ __forceinline__ void enter(const W4Params& p, int to_tile, int side, int first, int g, int t)
     {
         tile = to_tile;
-        chunk = warp;
+        chunk = first;
 #pragma unroll
         for (int i = 0; i < RT * 2; ++i) {
-            const int n = min(to_tile * (RT * 16) + i * 8 + g, p.N - 1);
+            const int n = min(((to_tile << p.side_log) + side) * (RT * 16) + i * 8 + g, p.N - 1);
             row[i] = p.Wp + (int64_t)n * (p.K >> 1) + t * 16;
         }
     }
@@ -175,18 +176,18 @@ struct Scales {
     static constexpr int kN = FINE ? 2 * RT : 1;
     const char* row[kN];
     int tile, chunk;
-    __device__ __forceinline__ void enter(const W4Params& p, int to_tile, int warp, int g, int t)
+    __device__ __forceinline__ void enter(const W4Params& p, int to_tile, int side, int first, int g, int t)
     {
         tile = min(to_tile, p.tiles - 1);                 // beyond the last one nothing uses what is loaded
-        chunk = min(warp, p.chunks - 1);
+        chunk = min(first, p.chunks - 1);
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
-            const int n = min(tile * (RT * 16) + (FINE ? i : t % (2 * RT)) * 8 + g, p.N - 1);
+            const int n = min(((tile << p.side_log) + side) * (RT * 16) + (FINE ? i : t % (2 * RT)) * 8 + g, p.N - 1);
             row[i] = reinterpret_cast<const char*>(p.s_g) + (((int64_t)n * p.per_row) << (p.s_bf ? 1 : 2));
         }
     }
     // the scales of the chunk at hand, and on to this warp's next
-    __device__ __forceinline__ void load(const W4Params& p, int warp, int warps, int g, int t, float (&s)[kN])
+    __device__ __forceinline__ void load(const W4Params& p, int side, int first, int step, int g, int t, float (&s)[kN])
     {
         const int unit = min(chunk * 4 + (FINE ? t : 0), p.K / 32 - 1), gi = p.group32 == 1u ? unit : (int)__umulhi((uint32_t)unit, p.magic);
         if (p.s_bf) {
@@ -196,8 +197,8 @@ struct Scales {
 #pragma unroll
             for (int i = 0; i < kN; ++i) s[i] = __ldg(reinterpret_cast<const float*>(row[i]) + gi);
         }
-        chunk += warps;
-        if (chunk >= p.chunks) enter(p, tile + (int)gridDim.x, warp, g, t);
+        chunk += step;
+        if (chunk >= p.chunks) enter(p, tile + (int)gridDim.x, side, first, g, t);
     }
     // of row half h of tile r and (FINE) group i of the chunk
     __device__ __forceinline__ static float get(const float (&s)[kN], int r, int h, int i, int lane)
@@ -246,16 +247,19 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int g = lane >> 2, t = lane & 3;
+    // this warp's output channels within a tile, its first chunk, and the step to the next
+    const int side = warp & ((1 << p.side_log) - 1), first = warp >> p.side_log, step = warps >> p.side_log;
     const int m0 = blockIdx.y * kCols, m_here = min(p.M - m0, kCols);
     char* ring = smem + warp * p.stages * S::kBytes;
-    float* part = reinterpret_cast<float*>(smem + warps * p.stages * S::kBytes);  // two sets of [warps][kCols][kRows], used in turn
+    // two sets of [step][kCols][channels of a tile], used in turn
+    float* part = reinterpret_cast<float*>(smem + warps * p.stages * S::kBytes);
     uint4* resident = reinterpret_cast<uint4*>(part + 2 * warps * kRows * kCols);  // [chunk][word][part][token][t]
     if (!RES) {                                           // rows of activations that no copy fills stay zero
         for (int i = lane; i < p.stages * S::kBytes / 16; i += 32) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);
         __syncwarp();
     }
     CodeFeed<RT> feed;
-    feed.enter(p, (int)blockIdx.x, warp, g, t);
+    feed.enter(p, (int)blockIdx.x, side, first, g, t);
     XFeed<MT, XF, FINE> xfeed;
     if (!RES) xfeed.enter(p, m0, lane);
     const uint32_t ring_u = smem_u32(ring);
@@ -266,8 +270,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
             feed.template copy<FINE>(p, to, g, t);
             if (!RES) xfeed.copy(p, to + S::kCodes, feed.chunk, m_here);
             feed.slot = feed.slot + 1 < p.stages ? feed.slot + 1 : 0;
-            feed.chunk += warps;
-            if (feed.chunk >= p.chunks) feed.enter(p, feed.tile + (int)gridDim.x, warp, g, t);
+            feed.chunk += step;
+            if (feed.chunk >= p.chunks) feed.enter(p, feed.tile + (int)gridDim.x, side, first, g, t);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -276,10 +280,10 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
     // scales of this lane's rows and channels, loaded two chunks ahead
     Scales<RT, FINE> scales;
     constexpr int kS = Scales<RT, FINE>::kN;
-    scales.enter(p, (int)blockIdx.x, warp, g, t);
+    scales.enter(p, (int)blockIdx.x, side, first, g, t);
     float s0[kS], s1[kS];
-    scales.load(p, warp, warps, g, t, s0);
-    scales.load(p, warp, warps, g, t, s1);
+    scales.load(p, side, first, step, g, t, s0);
+    scales.load(p, side, first, step, g, t, s1);
     // columns of absent tokens repeat the last one's operands: nothing reads them
     int b_lane[MT];
 #pragma unroll
@@ -318,6 +322,9 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
 
     int slot = 0, turn = 0;
     for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, turn ^= 1) {
+        // this thread's outputs of the tile, threadIdx.x, + blockDim.x, ..., share a channel: blockDim.x is a multiple of the tile's
+        const int channels = kRows << p.side_log, n_out = tile * channels + (threadIdx.x & (channels - 1));
+        const float bias = p.bias != nullptr && n_out < p.N ? __ldg(p.bias + n_out) : 0.0f;
         float acc[RT][MT][4];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
@@ -326,7 +333,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[r][j][i] = 0.0f;
 #pragma unroll 1
-        for (int c = warp; c < p.chunks; c += warps) {
+        for (int c = first; c < p.chunks; c += step) {
             copy();
             if (p.stages == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
             else asm volatile("cp.async.wait_group 2;" ::: "memory");
@@ -337,7 +344,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
                 now[i] = s0[i];
                 s0[i] = s1[i];
             }
-            scales.load(p, warp, warps, g, t, s1);
+            scales.load(p, side, first, step, g, t, s1);
             const char* codes = ring + slot * S::kBytes;
             const char* xs = codes + S::kCodes;
             const uint4* bs = resident + c * (16 * kParts) * m_here;
@@ -408,24 +415,22 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
             slot = slot + 1 < p.stages ? slot + 1 : 0;
             __syncwarp();                                 // all lanes have read the stage that is filled next
         }
-        // ---- sums of the warps, added in their order
+        // ---- sums of the warps that split K, added in their order
         float* set = part + turn * warps * kRows * kCols;
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int j = 0; j < MT; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) set[(warp * kCols + j * 8 + 2 * t + (i & 1)) * kRows + r * 16 + (i >> 1) * 8 + g] = acc[r][j][i];
+                for (int i = 0; i < 4; ++i)
+                    set[(first * kCols + j * 8 + 2 * t + (i & 1)) * channels + side * kRows + r * 16 + (i >> 1) * 8 + g] = acc[r][j][i];
         __syncthreads();
-        for (int e = threadIdx.x; e < kRows * m_here; e += blockDim.x) {
-            const int m = m0 + e / kRows, n = tile * kRows + e % kRows;
-            if (n >= p.N) continue;
+        for (int e = threadIdx.x; e < channels * m_here; e += blockDim.x) {
+            if (n_out >= p.N) break;
             float v = 0.0f;
-            for (int u = 0; u < warps; ++u) v += set[u * kRows * kCols + e];
-            v *= 1024.0f;
-            if (p.bias != nullptr) v += p.bias[n];
-            v = activate(v, p.act);
-            const int64_t at = (int64_t)m * p.N + n;
+            for (int u = 0; u < step; ++u) v += set[u * channels * kCols + e];
+            v = activate(fmaf(v, 1024.0f, bias), p.act);
+            const int64_t at = (int64_t)(m0 + (e >> (p.side_log + (RT == 1 ? 4 : 5)))) * p.N + n_out;
             if (p.y_bf) reinterpret_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(v);
             else reinterpret_cast<float*>(p.Y)[at] = v;
         }
@@ -439,8 +444,8 @@ int launch_w4(stwq_ctx* ctx, W4Params& p, size_t resident, cudaStream_t st)
     // Two blocks of eight warps on an SM where there are tiles for them and rings of three stages and the activations fit twice, else one
     // of up to sixteen; four stages where there is room.
     constexpr size_t kHalf = 112 * 1024, kAll = 220 * 1024;
-    p.tiles = (p.N + kRows - 1) / kRows;
-    const bool two = p.tiles > ctx->sm_count && 8 * (3 * kStage + kSets) + resident <= kHalf;
+    const int strips = (p.N + kRows - 1) / kRows;         // of 16 RT output channels
+    const bool two = strips > ctx->sm_count && 8 * (3 * kStage + kSets) + resident <= kHalf;
     int warps = 1;
     while (2 * warps <= (two ? 8 : kMaxWarps) && warps < p.chunks && (size_t)2 * warps * (3 * kStage + kSets) + resident <= (two ? kHalf : kAll)) warps *= 2;
     p.stages = (size_t)warps * (4 * kStage + kSets) + resident <= (two ? kHalf : kAll) ? 4 : 3;
@@ -455,6 +460,17 @@ int launch_w4(stwq_ctx* ctx, W4Params& p, size_t resident, cudaStream_t st)
     }
     const int slots = (two ? 2 : 1) * ctx->sm_count;
     const int passes = (p.M + kCols - 1) / kCols, share = slots / passes > 0 ? slots / passes : 1;        // over the weights, side by side
+    // A tile costs its chunks per warp and about one more for its end (sums, barrier, addresses): strips side by side have fewer ends,
+    // strips one by one leave fewer blocks idle in the last round.
+    int best = 0x7fffffff;
+    for (int log = 0; (1 << log) <= warps; ++log) {
+        const int tiles = (strips + (1 << log) - 1) >> log, step = warps >> log, cost = (tiles + share - 1) / share * ((p.chunks + step - 1) / step + 1);
+        if (cost < best) {
+            best = cost;
+            p.side_log = log;
+            p.tiles = tiles;
+        }
+    }
     const dim3 grid((unsigned)(p.tiles < share ? p.tiles : share), (unsigned)passes);
     kern<<<grid, 32 * warps, smem, st>>>(p);
     ctx->launches += 1;
