@@ -209,6 +209,32 @@ def test_one_group_per_row_is_the_per_channel_fold(gpu):
     check(gpu, X, Wp2, s_w.view(96, 1), None, 0, Y, True)
 
 
+@pytest.mark.parametrize("N,K,group,M,x", [(40000, 4096, 128, 4, "bf16"), (33001, 2048, 64, 1, "f32"), (40000, 4096, 128, 13, "bf16"), (24000, 8192, 32, 8, "bf16"),
+                                           (128000, 1024, 1024, 2, "bf16")])
+def test_blocks_with_several_tiles(gpu, N, K, group, M, x):
+    """Many tiles for each block, twice in a row and on two streams at once."""
+    torch = gpu.torch
+    Wp, s, g = weights(gpu, N, K, group, seed=M)
+    X = torch.randn((M, K), device=gpu.dev, generator=g).to(torch.bfloat16 if x == "bf16" else torch.float32)
+    p = Wp.long()
+    c = torch.stack([p & 15, p >> 4], -1).flatten(1).double()
+    del p
+    c = torch.where(c > 7, c - 16, c) * s.double().repeat_interleave(group, 1)
+    want, mag = X.double() @ c.T, X.double().abs() @ c.abs().T
+    e = mag * ((25 if x == "f32" else 8) * 2.0 ** -22 + (math.ceil(K / 128) + 16 + 3) * U)
+    other, ctx2 = torch.cuda.Stream(), gpu.pk.Context(0)
+    Y = [torch.full((M, N), 7.0, device=gpu.dev) for _ in range(3)]
+    torch.cuda.synchronize()
+    gpu.ctx.linear_w4g(X, Wp, s, None, 0, gpu.pk.OUT_F32, Y[0])
+    ctx2.linear_w4g(X, Wp, s, None, 0, gpu.pk.OUT_F32, Y[1], stream=other)
+    gpu.ctx.linear_w4g(X, Wp, s, None, 0, gpu.pk.OUT_F32, Y[2])
+    torch.cuda.synchronize()
+    assert gpu.ctx.stwq_device_status() == 0 and ctx2.stwq_device_status() == 0
+    assert ((Y[0].double() - want).abs() <= e).all()
+    assert torch.equal(Y[0], Y[1]) and torch.equal(Y[0], Y[2])
+    ctx2.close()
+
+
 def test_weights_beyond_2_31_elements(gpu):
     """Row offsets in the packed weights pass 32 bits: the last rows agree with a call on them alone."""
     torch = gpu.torch
