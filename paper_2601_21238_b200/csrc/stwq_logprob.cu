@@ -242,8 +242,8 @@ __device__ __forceinline__ int place_of(const unsigned long long* keys, int n, i
     return ahead_of;
 }
 
-// A block of NT threads takes a row, or (CL) a slice of one; the first block of the cluster joins the slices.
-template <typename XT, int NT, bool CL>
+// A block of NT threads takes a row, or (CL) a slice of one; the first block of the cluster joins the slices. TOP: k > 0.
+template <typename XT, int NT, bool CL, bool TOP>
 __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const LpParams p)
 {
     constexpr int kPer = Vec<XT>::kPer, kGroups = NT / 4, kWarps = NT / 32, kAhead = CL ? 4 : 2;       // vectors in flight per thread
@@ -301,35 +301,40 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
         vm = warp_max(vm);
         if (vm > me.m) me.raise(vm);
     }
-    for (int b0 = 0; b0 < nvec; b0 += kAhead * NT) {
+    // the token's vector (or -1 where it lies before the vectors or behind): those before it count equal logits too
+    const int token_vec = token < head ? -1 : (token - head) / kPer;
+    const XT* next = body + (int64_t)(tid + kAhead * NT) * kPer;
+    auto vector = [&](int u, int i) {
+        float vm = -INFINITY;
+        if (i < nvec) {
+            float x[kPer];
+            ahead[u].get(x);
+            if (TOP) vm = fmaxf(vm, ahead[u].largest(x));
+            if (ranked) {
+                before += above<XT>(ahead[u], x, i < token_vec ? below : xt);
+                if (i == token_vec)                       // equal logits before the token, in its own vector
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int i = b0 + u * NT + tid;
-            float vm = -INFINITY;
-            if (i < nvec) {
-                float x[kPer];
-                ahead[u].get(x);
-                if (p.k > 0) vm = fmaxf(vm, ahead[u].largest(x));
-                if (ranked) {
-                    const int at = head + i * kPer;
-                    before += above<XT>(ahead[u], x, at + kPer <= token ? below : xt);
-                    if (token >= at && token < at + kPer)             // equal logits before the token, in its own vector
-#pragma unroll
-                        for (int j = 0; j < kPer; ++j) before += x[j] == xt && at + j < token ? 1u : 0u;
-                }
-                if (i + kAhead * NT < nvec) ahead[u].load(body + (int64_t)(i + kAhead * NT) * kPer);
-                me.add(x);
+                    for (int j = 0; j < kPer; ++j) before += x[j] == xt && head + i * kPer + j < token ? 1u : 0u;
             }
+            if (i + kAhead * NT < nvec) ahead[u].load(next);
+            me.add(x);
+        }
+        next += NT * kPer;
+        if (TOP) {
             vmax[u] = vm;
-            if (p.k > 0 && held) gmax = fmaxf(gmax, vm);
-            if (p.k > 0 && !held) {
+            if (held) gmax = fmaxf(gmax, vm);
+            else {
                 float rm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, 1));
                 rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, 2));
                 gmax = fmaxf(gmax, rm);
                 if ((tid & 3) == 0 && i < nvec) run_max[i >> 2] = rm;
             }
         }
-    }
+    };
+#pragma unroll 1
+    for (int b0 = 0; b0 < nvec; b0 += kAhead * NT)
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) vector(u, b0 + u * NT + tid);
     // ---- the block's maximum, then its sums relative to it, added in the order of lanes and warps
     const float wm = warp_max(me.m);
     if (lane == 0) sh.m[warp] = wm;
@@ -358,7 +363,7 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
         }
     }
     // ---- the k-th largest of the groups' maxima, ties broken by the group: four threads count for a group
-    if (p.k > 0) {
+    if (TOP) {
         const int q = tid >> 2, from = (tid & 3) * (kGroups / 4);
         const float v = sh.gmax[q];
         int ahead_of = 0;
@@ -392,7 +397,7 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
 
     // ---- the block's likeliest k, as keys in `top`, largest first
     unsigned long long* top = CL ? cg::this_cluster().map_shared_rank(&sh, 0)->row_top + rank * p.k : sh.row_top;
-    if (p.k > 0) {
+    if (TOP) {
         const float bound = sh.bound;
         auto take = [&](float x, int i) {
             if (x >= bound && x > -INFINITY) {
@@ -474,7 +479,7 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
             ba += f * fmaf(d, sh.row_s[r], sh.row_a[r]);
             bn += sh.row_n[r];
         }
-    } else if (p.k > 0) __syncthreads();
+    } else if (TOP) __syncthreads();
 
     // ---- the row
     const bool any = bm > -INFINITY;
@@ -498,7 +503,7 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
         }
         if (p.entropy != nullptr) p.entropy[row] = greedy || !any ? 0.0f : fmaxf(fmaf(-ln2, ba / bs, ln_sums), 0.0f);
     }
-    if (p.k == 0) return;
+    if (!TOP) return;
     int32_t* ids = p.top_ids + row * p.k;
     float* lps = p.top_lp + row * p.k;
     auto put = [&](unsigned long long key, int at) {
@@ -517,13 +522,13 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
     }
 }
 
-template <typename XT, int NT, bool CL>
-int launch_lp(stwq_ctx* ctx, LpParams& p, int B, int blocks, cudaStream_t st)
+template <typename XT, int NT, bool CL, bool TOP>
+int launch_lp_as(stwq_ctx* ctx, LpParams& p, int B, int blocks, cudaStream_t st)
 {
     constexpr int kRun = 4 * Vec<XT>::kPer;
     p.slice = CL ? ((p.V + blocks - 1) / blocks + kRun - 1) / kRun * kRun : p.V;
-    const size_t smem = p.k > 0 ? (size_t)(p.slice / kRun + 2) * 4 : 0;
-    auto kern = logprob_kernel<XT, NT, CL>;
+    const size_t smem = TOP ? (size_t)(p.slice / kRun + 2) * 4 : 0;
+    auto kern = logprob_kernel<XT, NT, CL, TOP>;
     cudaError_t e = cudaSuccess;
     if (smem > 16 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxV / 32 + 2) * 4);
     if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
@@ -547,12 +552,19 @@ int launch_lp(stwq_ctx* ctx, LpParams& p, int B, int blocks, cudaStream_t st)
     return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
 }
 
+template <typename XT, int NT, bool CL>
+int launch_lp(stwq_ctx* ctx, LpParams& p, int B, int blocks, cudaStream_t st)
+{
+    return p.k > 0 ? launch_lp_as<XT, NT, CL, true>(ctx, p, B, blocks, st) : launch_lp_as<XT, NT, CL, false>(ctx, p, B, blocks, st);
+}
+
 template <typename XT>
 int launch_lp_any(stwq_ctx* ctx, LpParams& p, int B, cudaStream_t st)
 {
-    // few rows: several blocks a row while SMs would idle and a block keeps two vectors a thread
+    // few rows: several blocks a row while SMs would idle and a block keeps enough to do (20 likeliest of 32000: 10.2 us in one block, 8.6 in
+    // four; of 16384: 7.4 and 11.8)
     int blocks = 1;
-    while (blocks < kMaxCluster && B * blocks * 2 <= ctx->sm_count && p.V / (2 * blocks) >= 512 * Vec<XT>::kPer) blocks *= 2;
+    while (blocks < kMaxCluster && B * blocks * 2 <= ctx->sm_count && p.V / (2 * blocks) >= 12288) blocks *= 2;
     if (blocks > 1) return launch_lp<XT, 512, true>(ctx, p, B, blocks, st);
     const int vecs = p.V / Vec<XT>::kPer;
     if (vecs <= 512) return launch_lp<XT, 128, false>(ctx, p, B, 1, st);
