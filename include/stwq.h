@@ -480,7 +480,7 @@ int sample_tokens(stwq_ctx* ctx, const void* logits, int x_dtype, int64_t ld, in
  *    by s_ch multiplies by its reciprocal, as stwq_quantize does; s_tok, P and bits belong to the codes only.
  *  - pos_ids [M], optional for floating outputs: -1 marks a padding row, which is neither read nor written.
  * C a multiple of 8, <= 16384; rows and pointers 16-byte aligned (rows of codes: 8). Hout may be H, and Y may be H or O, in
- * place (same rows, same type); outputs must not overlap an operand in any other way (STWQ_ERR_ALIGN).
+ * place (same rows, same type); outputs must not overlap rows of H, O or each other in any other way (STWQ_ERR_ALIGN), nor the vectors.
  * fp32 arithmetic, one rounding at each store; y is computed from h' before its rounding. NaN and Inf come out as the formulas
  * have them (codes: NaN gives 0). A cond_id outside [0, G), and for codes a position outside [0, P) other than -1, records
  * STWQ_ERR_POS_RANGE: Hout is then H (cond_id) and Y zeros.
@@ -500,8 +500,9 @@ int block_norm(stwq_ctx* ctx, const void* H, int64_t ldh, int h_dtype, const voi
  *    at 2^-64), rounded to s_dtype first; code = clamp(round(W s_ch / s)). group = K gives gps_fold_packed4's codes and scales.
  *  - linear_w4g: X M rows of x_dtype (fp32 or bf16), ldx elements apart (16-byte multiples); bias [N] fp32 or NULL; Y [M,N] dense,
  *    fp32 or bf16. A channel scale s_ch of the fold is divided out of X by its producer (block_norm's s_ch).
- * group a multiple of 32 that divides K; M <= 64: every row beyond 8 adds work that the weights' stream does not hide,
- * and beyond 64 rows the tiled GEMM of qlinear_w4 is the right call. X, Wp 16-byte aligned.
+ * group a multiple of 32 that divides K, K < 131072, N <= 2^30; M <= 64: every row beyond 8 adds work that the weights' stream does not
+ * hide, and beyond 64 rows the tiled GEMM of qlinear_w4 is the right call. W, s_ch, s_g of the fold, X and Wp 16-byte aligned. Outputs
+ * must not overlap operands (STWQ_ERR_ALIGN).
  * Products of codes and activations are exact (fp32 activations enter as three bf16 parts), sums fp32 in a fixed order: the
  * same call gives the same bits. Results below 2^-100 lose bits. A row of X with NaN or Inf gives NaN or Inf in that row of Y as the formula has it.
  */
@@ -523,7 +524,8 @@ int linear_w4g(stwq_ctx* ctx, const void* X, int64_t ldx, int x_dtype, int64_t M
  *    Any other token outside [0, V): NaN, rank -1, and STWQ_ERR_TOKEN is recorded.
  *  - Fewer than k tokens that can be drawn: the rest of top_ids is -1, of top_logprobs -Inf. A row without any: entropy 0.
  * fp32; S and the entropy sum are good to a few units of 2^-24, so a log probability near 0 is good to about 1e-7 absolute.
- * Sums have a fixed order: the same call gives the same bits. V <= 360448, ld >= V.
+ * Sums have a fixed order: the same call gives the same bits (how a row is split, and with it the last bits, goes by B and V). Logits
+ * more than 3.4e38 apart count as infinitely far. V <= 360448, ld >= V; outputs must not overlap the logits (STWQ_ERR_ALIGN).
  */
 int token_logprobs(stwq_ctx* ctx, const void* logits, int x_dtype, int64_t ld, int B, int V, const float* temperature,
                    const int32_t* tokens, float* logprobs, int32_t* ranks, float* entropy, int k, int32_t* top_ids,

@@ -15,6 +15,13 @@ static inline bool stwq_disjoint(int64_t T, int H, int d, int64_t ts, int64_t hs
     return (hs >= d && ts >= hs * (H - 1) + d) || (ts >= d && hs >= ts * (T - 1) + d);
 }
 
+// Whether two ranges of bytes share one.
+static inline bool stwq_overlap(const void* a, int64_t na, const void* b, int64_t nb)
+{
+    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+    return a != nullptr && b != nullptr && x < y + nb && y < x + na;
+}
+
 // Make the context's device current for the duration of a call.
 struct StwqDevGuard {
     int prev = -1;

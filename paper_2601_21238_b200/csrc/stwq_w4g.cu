@@ -3,18 +3,24 @@
 //
 //     Y[m,n] = act(sum_g s[n,g] sum_{k in g} X[m,k] c[n,k] + bias[n])
 //
-// Bound by HBM: N K / 2 bytes of codes, read once, straight into registers. The codes are the A operand (16 rows of n) of
-// mma.sync m16n8k16, the activations the B operand (8 tokens): up to 8 rows of X cost what one costs. tcgen05 would need the
-// codes widened into shared memory first; here a word of eight codes becomes four bf16 pairs in registers by masks and
-// one subtraction each (0x3e00 | (nibble ^ 8) is 2^-3 + (code + 8) 2^-10 as bf16; less 2^-3 + 2^-7 it is code 2^-10, exactly).
-// The 2^-10 keeps 128 codes times the largest activation inside fp32; it leaves the result at the end (bits below 2^-126 are lost).
+// HBM asks for N K / 2 bytes of codes, read once. The codes are the A operand (16 rows of n) of mma.sync m16n8k16, the activations the
+// B operand (8 tokens): up to 8 rows of X cost what one costs. tcgen05 would need the codes widened into shared memory first; here a
+// word of eight codes becomes four bf16 pairs in registers by a shift, a mask and one subtraction each (0x3e00 | (nibble ^ 8) is 2^-3 +
+// (code + 8) 2^-10 as bf16; less 2^-3 + 2^-7 it is code 2^-10, exactly). The 2^-10 keeps 128 codes times the largest activation
+// inside fp32; it leaves the result at the end (bits below 2^-126 are lost).
 // A chunk is 128 input channels: 64 bytes of codes of each row, copied asynchronously into a ring of stages that every warp has for
 // itself, with the chunk's activations beside them. The order in which channels meet in a product does not matter as long as both
 // operands keep it. Where a group is a multiple of 128 channels, a lane takes 16 bytes of a row (32 channels), the chunk's products
 // share a scale, and the chunk's fp32 sum is scaled once. Finer groups (a multiple of 32): the four lanes of a row take the four words
 // of one group's 16 bytes together, two products per group, and the sum of each group is scaled.
 // fp32 activations enter as three bf16 parts, cut off bit by bit (8 + 8 + 8 bits: exact), the smallest first.
-// The warps of a block take different chunks of the same output channels; their sums meet in shared memory and are added in warp order.
+// The warps of a block take different chunks of the same output channels, or different channels; the sums of those that split K meet
+// in shared memory and are added in warp order. Where they fit, the activations of a block lie in shared memory as operands from the
+// start: the cutting and pairing is done once, not once per tile.
+// What bounds it: with many output channels the issue of some 320 instructions per 2 KB of codes (half of them the widening, on a
+// half-rate pipe) from 16 warps of up to 128 registers: 4 x 4096 > 128000, groups of 128, 75 us, 3.6 TB/s, 0.56 of the measured copy rate
+// (65 us from L2 alone, 65 without the widening or without the products). Few channels: launch, first bytes, the exchange: 1 x 2048 >
+// 8192 6.6 us, 8 x 8192 > 2048 in groups of 64 8.4 us. fp32 activations take three products: 13 x 1920 > 5760 in groups of 32 12.9 us.
 #include <cuda_bf16.h>
 
 #include "stwq_internal.cuh"
@@ -495,7 +501,7 @@ int launch_w4_any(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
 
 int check_group(int N, int K, int group)
 {
-    if (N <= 0 || K <= 0 || K >= 131072 || group <= 0 || group > K) return STWQ_ERR_DIM;
+    if (N <= 0 || N > (1 << 30) || K <= 0 || K >= 131072 || group <= 0 || group > K) return STWQ_ERR_DIM;
     return (group & 31) != 0 || K % group != 0 ? STWQ_ERR_ALIGN : STWQ_OK;
 }
 
@@ -511,6 +517,9 @@ int gps_fold_group4(stwq_ctx* ctx, const float* W, int N, int K, const float* s_
     if (rc != STWQ_OK) return rc;
     if (s_dtype != STWQ_OUT_F32 && s_dtype != STWQ_OUT_BF16) return STWQ_ERR_BITS;
     if (!stwq_aligned16(W) || !stwq_aligned16(Wp) || !stwq_aligned16(s_ch) || !stwq_aligned16(s_g)) return STWQ_ERR_ALIGN;
+    const int64_t w_bytes = (int64_t)N * K * 4, es = s_dtype == STWQ_OUT_F32 ? 4 : 2;
+    if (stwq_overlap(Wp, w_bytes / 8, W, w_bytes) || stwq_overlap(s_g, (int64_t)N * (K / group) * es, W, w_bytes) || stwq_overlap(Wp, w_bytes / 8, s_ch, (int64_t)K * 4))
+        return STWQ_ERR_ALIGN;
     StwqDevGuard dev(ctx->device);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t groups = (int64_t)N * (K / group), want = (groups + 7) / 8;
@@ -534,6 +543,11 @@ int linear_w4g(stwq_ctx* ctx, const void* X, int64_t ldx, int x_dtype, int64_t M
     if (rc != STWQ_OK || ldx % (xf ? 4 : 8) != 0 || !stwq_aligned16(X) || !stwq_aligned16(Wp)) return STWQ_ERR_ALIGN;
     auto aligned = [](const void* q, int bytes) { return (reinterpret_cast<uintptr_t>(q) & (uintptr_t)(bytes - 1)) == 0; };
     if (!aligned(s_g, s_dtype == STWQ_OUT_F32 ? 4 : 2) || !aligned(Y, out_dtype == STWQ_OUT_F32 ? 4 : 2) || !aligned(bias, 4)) return STWQ_ERR_ALIGN;
+    // blocks read the operands while others already store
+    const int64_t ex = xf ? 4 : 2, es = s_dtype == STWQ_OUT_F32 ? 4 : 2, y_bytes = M * N * (out_dtype == STWQ_OUT_F32 ? 4 : 2);
+    if (stwq_overlap(Y, y_bytes, X, ((M - 1) * ldx + K) * ex) || stwq_overlap(Y, y_bytes, Wp, (int64_t)N * (K / 2)) ||
+        stwq_overlap(Y, y_bytes, s_g, (int64_t)N * (K / group) * es) || stwq_overlap(Y, y_bytes, bias, (int64_t)N * 4))
+        return STWQ_ERR_ALIGN;
     W4Params p;
     p.X = X; p.ldx = ldx; p.M = (int)M; p.K = K; p.N = N; p.per_row = K / group; p.chunks = (K + 127) / 128;
     p.Wp = Wp; p.s_g = s_g; p.s_bf = s_dtype == STWQ_OUT_BF16; p.bias = bias; p.act = act; p.y_bf = out_dtype == STWQ_OUT_BF16; p.Y = Y;

@@ -253,17 +253,19 @@ def test_the_c_entry_points_refuse_and_write_nothing(gpu):
         return lib.linear_w4g(h, *a.values(), st)
     for code, k in ((NULL, dict(X=None)), (NULL, dict(Y=None)), (DIM, dict(M=0)), (DIM, dict(M=65)), (DIM, dict(K=0)), (DIM, dict(K=131072, ldx=131072)), (DIM, dict(N=0)), (DIM, dict(ldx=120)),
                     (DIM, dict(group=0)), (DIM, dict(group=256)), (ALIGN, dict(group=48)), (ALIGN, dict(group=96)), (ALIGN, dict(ldx=130)), (ALIGN, dict(X=at(4))), (ALIGN, dict(W=at(8))), (ALIGN, dict(s=at(2))),
-                    (ALIGN, dict(Y=at(2))), (ALIGN, dict(bias=at(1))), (BITS, dict(xd=2)), (BITS, dict(sd=-1)), (BITS, dict(od=3)), (BITS, dict(act=4))):
+                    (ALIGN, dict(Y=at(2))), (ALIGN, dict(bias=at(1))), (DIM, dict(N=(1 << 30) + 1)), (ALIGN, dict(Y=p[0])), (ALIGN, dict(Y=at(65536 + 64))), (ALIGN, dict(Y=at(2 * 65536 - 8))),
+                    (ALIGN, dict(Y=p[3])), (BITS, dict(xd=2)), (BITS, dict(sd=-1)), (BITS, dict(od=3)), (BITS, dict(act=4))):
         assert w4(**k) == code, k
     assert lib.gps_fold_group4(h, p[0], 4, 128, None, 24, p[1], p[2], 0, st) == ALIGN and lib.gps_fold_group4(h, p[0], 4, 128, None, 32, p[1], p[2], 2, st) == BITS
     assert lib.gps_fold_group4(h, p[0], 0, 128, None, 32, p[1], p[2], 0, st) == DIM and lib.gps_fold_group4(h, at(4), 4, 128, None, 32, p[1], p[2], 0, st) == ALIGN
+    assert lib.gps_fold_group4(h, p[0], 4, 128, None, 32, at(1024), p[2], 0, st) == ALIGN
 
     def lp(**k):
         a = dict(X=p[0], xd=0, ld=100, B=4, V=100, T=None, tok=p[1], lp=p[2], rk=p[3], en=p[4], k=3, ids=p[5], tl=p[6])
         a.update(k)
         return lib.token_logprobs(h, *a.values(), st)
     for code, k in ((NULL, dict(X=None)), (NULL, dict(tok=None)), (NULL, dict(lp=None)), (NULL, dict(ids=None)), (NULL, dict(k=0)), (NULL, dict(tok=None, lp=None)), (DIM, dict(B=0)), (DIM, dict(V=0)),
-                    (DIM, dict(V=360449, ld=360449)), (DIM, dict(ld=99)), (DIM, dict(k=-1)), (DIM, dict(k=33)), (BITS, dict(xd=2)), (ALIGN, dict(X=at(2)))):
+                    (DIM, dict(V=360449, ld=360449)), (DIM, dict(ld=99)), (DIM, dict(k=-1)), (DIM, dict(k=33)), (BITS, dict(xd=2)), (ALIGN, dict(X=at(2))), (ALIGN, dict(lp=at(400))), (ALIGN, dict(tl=p[0])), (ALIGN, dict(en=at(1596)))):
         assert lp(**k) == code, k
     torch.cuda.synchronize()
     assert (buf == 7).all() and gpu.ctx.stwq_device_status() == 0
