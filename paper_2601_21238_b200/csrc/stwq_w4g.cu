@@ -487,7 +487,9 @@ int launch_w4(stwq_ctx* ctx, W4Params& p, size_t resident, cudaStream_t st)
 template <bool FINE, bool XF>
 int launch_w4_any(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
 {
-    const bool wide = p.N >= 32 * ctx->sm_count;          // tiles of 32 output channels for every SM
+    // Tiles of 32 output channels share the operands of X, tiles of 16 spread further. Over K = 1024 to 8192 and 1 to 16 rows, 32 against
+    // 16 took 1.22 times as long at N = 2048, 0.94 at 2560 to 4608, 0.92 to 1.0 above: 16 only while each has an SM of its own.
+    const bool wide = p.N > 16 * ctx->sm_count;
     // activations as operands in shared memory, where that leaves room for the rings: of up to 8 tokens, and of up to 16 fp32 ones, which
     // are cut into their parts once instead of once per tile
     const size_t token = (size_t)p.chunks * 128 * (XF ? 6 : 2), one = token * (p.M < 8 ? p.M : 8), both = token * (p.M < 16 ? p.M : 16);
