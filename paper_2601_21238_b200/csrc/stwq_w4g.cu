@@ -8,6 +8,7 @@
 // word of eight codes becomes four bf16 pairs in registers by a shift, a mask and one subtraction each (0x3e00 | (nibble ^ 8) is 2^-3 +
 // (code + 8) 2^-10 as bf16; less 2^-3 + 2^-7 it is code 2^-10, exactly). The 2^-10 keeps 128 codes times the largest activation
 // inside fp32; it leaves the result at the end (bits below 2^-126 are lost).
+// A second kernel, further down, takes more rows than a tile or two of eight.
 // A chunk is 128 input channels: 64 bytes of codes of each row, copied asynchronously into a ring of stages that every warp has for
 // itself, with the chunk's activations beside them. The order in which channels meet in a product does not matter as long as both
 // operands keep it. Where a group is a multiple of 128 channels, a lane takes 16 bytes of a row (32 channels), the chunk's products
@@ -20,13 +21,17 @@
 // What bounds it: with many output channels the issue of some 320 instructions per 2 KB of codes (half of them the widening, on a
 // half-rate pipe) from 16 warps of up to 128 registers: 4 x 4096 > 128000, groups of 128, 75 us, 3.6 TB/s, 0.56 of the measured copy rate
 // (65 us from L2 alone, 65 without the widening or without the products). Few channels: launch, first bytes, the exchange: 1 x 2048 >
-// 8192 6.6 us, 8 x 8192 > 2048 in groups of 64 8.4 us. fp32 activations take three products: 13 x 1920 > 5760 in groups of 32 12.9 us.
+// 8192 6.6 us, 8 x 8192 > 2048 in groups of 64 8.3 us. fp32 activations take three products: 13 x 1920 > 5760 in groups of 32 10.3 us.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
+
+#include <cstdint>
 
 #include "stwq_internal.cuh"
 #include "stwq_paged.cuh"
 #include "stwq_ptx.cuh"
 
+namespace cg = cooperative_groups;
 using namespace stwq_ptx;       // activations of the epilogue
 
 namespace {
@@ -84,6 +89,13 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// the first product of a sum
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 // Nibbles q and q + 4 of a word as a pair of bf16: the codes times 2^-10.
 __device__ __forceinline__ uint32_t codes2(uint32_t w, int q)
@@ -443,6 +455,232 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
     }
 }
 
+// Many rows: a block of eight warps takes 128 RT output channels and 8 MT tokens. The activations of a chunk come into shared memory
+// once for all its warps (fp32 ones are cut into their parts there, once); a word of codes is widened once for all its tokens. A cluster of
+// blocks splits the chunks of a tile, and its blocks add up the sums of their share of the tokens, in the order of the chunks.
+// What bounds it: 430 instructions per 16 rows, 64 tokens and chunk, half the issue slots and half of what mma.sync can do; with 32
+// tokens the widening, 2/3 of the instructions. 8192 > 16384 in groups of 128: 32 rows 46 us, 64 rows 70 to 75 (in passes of 16 rows with
+// the kernel above 62 and 115 to 125), 64 fp32 rows 173 (303). Twice the warps an SM with half the rows each (RT 1 for RT 2): 50 us for 32 rows.
+template <int RT, int MT, bool XF>
+struct ManyStage {
+    static constexpr int kCodes = RT * 8192, kRow = XF ? 512 : 256, kBytes = kCodes + MT * 8 * kRow, kStages = XF ? 2 : 4;
+    static constexpr int kOps = XF ? MT * 8 * 768 : 0, kAll = kStages * kBytes + kOps, kSum = RT * 128 + 4;    // fp32 parts; floats a token
+    static_assert(MT * 8 * kSum * 4 <= kAll, "the sums lie where the stages were");
+};
+__device__ __forceinline__ int raw_piece(int p) { return p ^ ((p >> 3) & 1); }
+
+template <int RT, int MT, bool XF, bool FINE>
+__global__ void __launch_bounds__(256, RT * MT > 8 ? 1 : RT * MT > 4 ? 2 : 3) linear_w4g_many_kernel(const W4Params p)
+{
+    using S = ManyStage<RT, MT, XF>;
+    constexpr int kTokens = MT * 8, kRows = RT * 128, kParts = XF ? 3 : 1, kPieces = S::kRow / 16, kPer = XF ? 4 : 8, kSize = XF ? 4 : 2;
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int g = lane >> 2, t = lane & 3;
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), tile = (int)blockIdx.x / ranks;
+    const int begin = p.chunks * rank / ranks, end = p.chunks * (rank + 1) / ranks;
+    const int m0 = blockIdx.y * kTokens, m_here = min(p.M - m0, kTokens);
+    char* ops = smem + S::kStages * S::kBytes;            // [part][token], as the activations of a stage lie
+    // this thread's copies: piece threadIdx.x & 3 of every 64th row of codes, piece q of every (256 / kPieces)th row of activations
+    const int piece = threadIdx.x & 3, q = threadIdx.x % kPieces, r0 = threadIdx.x / kPieces;
+    const uint8_t* codes_at = p.Wp + (int64_t)tile * kRows * (p.K >> 1);
+    uint32_t row_at[RT * 2];                              // rows behind the last output channel repeat it
+#pragma unroll
+    for (int i = 0; i < RT * 2; ++i) row_at[i] = (uint32_t)min(i * 64 + (int)(threadIdx.x >> 2), p.N - 1 - tile * kRows) * (uint32_t)(p.K >> 1) + piece * 16;
+    const char* x_at = reinterpret_cast<const char*>(p.X) + (int64_t)m0 * p.ldx * kSize;
+    auto copy = [&](int c) {
+        if (c < end) {
+            const uint32_t to = smem_u32(smem) + (uint32_t)((c - begin) % S::kStages * S::kBytes);
+            const bool in = c * 128 + piece * 32 < p.K;   // else zeros; the address stays inside the row
+#pragma unroll
+            for (int i = 0; i < RT * 2; ++i) {
+                const int row = i * 64 + (threadIdx.x >> 2);
+                copy16(to + (uint32_t)(row * 64 + code_piece<FINE>(row, piece) * 16), codes_at + row_at[i] + (in ? c * 64 : -16 * piece), in);
+            }
+            const int k = c * 128 + q * kPer;
+#pragma unroll
+            for (int i = 0; i < kTokens * kPieces / 256; ++i) {
+                const int row = i * (256 / kPieces) + r0, at = XF ? raw_piece(q) : x_piece<false, FINE>(row, q);
+                const bool here = row < m_here && k < p.K;
+                copy16(to + (uint32_t)(S::kCodes + row * S::kRow + at * 16), x_at + (here ? (int64_t)row * p.ldx + k : 0) * kSize, here);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i + 1 < S::kStages; ++i) copy(begin + i);
+    Scales<RT, FINE> scales;                              // of this warp's rows, loaded two chunks ahead
+    constexpr int kS = Scales<RT, FINE>::kN;
+    scales.enter(p, tile, warp, begin, g, t);
+    float s0[kS], s1[kS];
+    scales.load(p, warp, begin, 1, g, t, s0);
+    scales.load(p, warp, begin, 1, g, t, s1);
+    float acc[RT][MT][4];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[r][j][e] = 0.0f;
+#pragma unroll 1
+    for (int c = begin; c < end; ++c) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+        __syncthreads();                                  // the chunk is here, and all have read the one before it
+        copy(c + S::kStages - 1);
+        const char* stage = smem + (c - begin) % S::kStages * S::kBytes;
+        const char* xs = XF ? ops : stage + S::kCodes;
+        if (XF) {
+#pragma unroll
+            for (int i = 0; i < MT / 2; ++i) {
+                const int token = i * 16 + (int)(threadIdx.x >> 4), eight = threadIdx.x & 15;
+                const char* raw = stage + S::kCodes + token * 512;
+                uint4 b[3];
+                pairs_f32(lds128(raw + raw_piece(2 * eight) * 16), lds128(raw + raw_piece(2 * eight + 1) * 16), b);
+#pragma unroll
+                for (int u = 0; u < 3; ++u) *reinterpret_cast<uint4*>(ops + (u * kTokens + token) * 256 + x_piece<false, FINE>(token, eight) * 16) = b[u];
+            }
+            __syncthreads();
+        }
+        float now[kS];
+#pragma unroll
+        for (int i = 0; i < kS; ++i) {
+            now[i] = s0[i];
+            s0[i] = s1[i];
+        }
+        scales.load(p, warp, begin, 1, g, t, s1);
+        uint4 w[RT][2];
+        if (!FINE)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) w[r][h] = lds128(stage + ((warp * RT + r) * 16 + h * 8 + g) * 64 + t * 16);
+        float sum[RT][MT][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                     // 32 channels, as above
+            uint32_t a[RT][2][4];
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = (warp * RT + r) * 16 + h * 8 + g;
+                    const uint32_t v = FINE ? *reinterpret_cast<const uint32_t*>(stage + row * 64 + code_piece<FINE>(row, i) * 16 + t * 4) : word_of(w[r][h], i);
+                    const uint32_t c0 = codes2(v, 0), c1 = codes2(v, 1), c2 = codes2(v, 2), c3 = codes2(v, 3);
+                    // bf16 activations stay as they lie, in pairs of neighbours: here the codes change places
+                    a[r][0][h] = XF ? c0 : __byte_perm(c0, c1, 0x5410);
+                    a[r][0][h + 2] = XF ? c1 : __byte_perm(c2, c3, 0x5410);
+                    a[r][1][h] = XF ? c2 : __byte_perm(c0, c1, 0x7632);
+                    a[r][1][h + 2] = XF ? c3 : __byte_perm(c2, c3, 0x7632);
+                }
+            const int eight = FINE ? 4 * i + t : 4 * t + i;
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                uint4 b[kParts];
+#pragma unroll
+                for (int u = 0; u < kParts; ++u) b[u] = lds128(xs + (u * kTokens + j * 8 + g) * 256 + x_piece<false, FINE>(g, eight) * 16);
+#pragma unroll
+                for (int u = kParts - 1; u >= 0; --u)     // the smallest part first
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        if (u == kParts - 1 && (FINE || i == 0)) mma_bf16_first(sum[r][j], a[r][0], b[u].x, b[u].y);
+                        else mma_bf16(sum[r][j], a[r][0], b[u].x, b[u].y);
+                        mma_bf16(sum[r][j], a[r][1], b[u].z, b[u].w);
+                    }
+            }
+            if (FINE || i == 3)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const float lo = Scales<RT, FINE>::get(now, r, 0, i, lane), hi = Scales<RT, FINE>::get(now, r, 1, i, lane);
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) {
+                        acc[r][j][0] = fmaf(lo, sum[r][j][0], acc[r][j][0]);
+                        acc[r][j][1] = fmaf(lo, sum[r][j][1], acc[r][j][1]);
+                        acc[r][j][2] = fmaf(hi, sum[r][j][2], acc[r][j][2]);
+                        acc[r][j][3] = fmaf(hi, sum[r][j][3], acc[r][j][3]);
+                    }
+                }
+        }
+    }
+    __syncthreads();                                      // the stages are read
+    float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sums[(j * 8 + 2 * t + (e & 1)) * S::kSum + (warp * RT + r) * 16 + (e >> 1) * 8 + g] = acc[r][j][e];
+    cluster.sync();
+    for (int token = warp * ranks + rank; token < m_here; token += 8 * ranks)
+        for (int ch = lane * 4; ch < kRows; ch += 128) {
+            const int n = tile * kRows + ch;
+            if (n >= p.N) break;
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int u = 0; u < ranks; ++u) {
+                const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sums, u) + token * S::kSum + ch);
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = activate(fmaf(v[e], 1024.0f, p.bias != nullptr && n + e < p.N ? __ldg(p.bias + n + e) : 0.0f), p.act);
+            const int64_t at = (int64_t)(m0 + token) * p.N + n;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < p.N) {
+                    if (p.y_bf) reinterpret_cast<__nv_bfloat16*>(p.Y)[at + e] = __float2bfloat16_rn(v[e]);
+                    else reinterpret_cast<float*>(p.Y)[at + e] = v[e];
+                }
+        }
+    cluster.sync();                                       // no block leaves while others read its sums
+}
+
+template <int RT, int MT, bool XF, bool FINE>
+int launch_w4_many(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
+{
+    using S = ManyStage<RT, MT, XF>;
+    auto kern = linear_w4g_many_kernel<RT, MT, XF, FINE>;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(8);
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = S::kAll;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    uint16_t* fit = ctx->w4g_clusters[(RT - 1) | (XF ? 2 : 0) | (FINE ? 4 : 0) | (MT == 2 ? 0 : MT == 4 ? 8 : 16)];
+    if (!fit[0]) {
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kAll);
+        for (int r = 1; r <= 8 && e == cudaSuccess; ++r) {
+            int n = 0;
+            at[0].val.clusterDim.x = cfg.gridDim.x = (unsigned)r;
+            e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
+            fit[r] = (uint16_t)n;
+        }
+        if (e != cudaSuccess) return stwq_cuda_fail(ctx, e);
+        fit[0] = 1;
+    }
+    p.side_log = 3;                                       // eight warps side by side
+    p.tiles = (p.N + RT * 128 - 1) / (RT * 128);
+    const int passes = (p.M + MT * 8 - 1) / (MT * 8);
+    // Blocks of a cluster: a round costs its chunks and some six more for its start, its end and the exchange.
+    int ranks = 1;
+    int64_t best = INT64_MAX;
+    for (int r = 1; r <= 8 && r <= p.chunks; ++r) {
+        if (fit[r] == 0) continue;
+        const int64_t cost = (((int64_t)p.tiles * passes + fit[r] - 1) / fit[r]) * ((p.chunks + r - 1) / r + 6);
+        if (cost < best) {
+            best = cost;
+            ranks = r;
+        }
+    }
+    at[0].val.clusterDim.x = (unsigned)ranks;
+    cfg.gridDim = dim3((unsigned)(p.tiles * ranks), (unsigned)passes);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
+    ctx->launches += 1;
+    return e == cudaSuccess ? STWQ_OK : stwq_cuda_fail(ctx, e);
+}
+
 template <int RT, int MT, bool XF, bool FINE, bool RES>
 int launch_w4(stwq_ctx* ctx, W4Params& p, size_t resident, cudaStream_t st)
 {
@@ -487,14 +725,25 @@ int launch_w4(stwq_ctx* ctx, W4Params& p, size_t resident, cudaStream_t st)
 template <bool FINE, bool XF>
 int launch_w4_any(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
 {
+    const int sm = ctx->sm_count;
+    const size_t token = (size_t)p.chunks * 128 * (XF ? 6 : 2);            // bytes of a token's operands
+    // The kernel for many rows, over N = 256 to 14000 and K = 1024 to 8192 (its time over that of this one in passes of 8 or 16 rows):
+    // bf16, 64 rows 0.64 to 0.95 above N = 16 SMs, 48 rows 0.73 to 0.92 above 32 SMs, 1.0 to 1.3 between 16 and 32; 17 to 32 rows
+    // 0.74 to 0.95 above 16 SMs, where tiles of 128 output channels win up to 48 SMs, of 256 beyond. fp32 the same with a pass for every
+    // 32 rows (64 rows 0.48 to 0.97, 17 rows 0.7 to 0.97 above 24 SMs, 1.1 to 1.3 below). Fewer channels keep too few of its blocks busy: 1.1
+    // to 2.7. 9 to 16 rows: fp32 0.67 to 0.95 (1.1 where it is worst), up to 16 SMs only while K is short (0.82 to 1.0, else 1.2); bf16 0.8 to 1.3: not taken.
+    if (!XF && p.M > 32 && p.N > (p.M > 48 ? 16 : 32) * sm) return launch_w4_many<2, 8, false, FINE>(ctx, p, st);
+    if (p.M > 16 && (XF || p.M <= 32)) {
+        const int64_t work = (int64_t)p.N * ((p.M + 31) / 32);
+        if (work > 48 * sm) return launch_w4_many<2, 4, XF, FINE>(ctx, p, st);
+        if (work > (XF && p.M <= 24 ? 24 : 16) * sm) return launch_w4_many<1, 4, XF, FINE>(ctx, p, st);
+    }
+    if (XF && p.M > 8 && p.M <= 16 && (p.N > 16 * sm || token * p.M <= 144 * 1024)) return launch_w4_many<1, 2, true, FINE>(ctx, p, st);
     // Tiles of 32 output channels share the operands of X, tiles of 16 spread further. Over K = 1024 to 8192 and 1 to 16 rows, 32 against
     // 16 took 1.22 times as long at N = 2048, 0.94 at 2560 to 4608, 0.92 to 1.0 above: 16 only while each has an SM of its own.
-    const bool wide = p.N > 16 * ctx->sm_count;
-    // activations as operands in shared memory, where that leaves room for the rings: of up to 8 tokens, and of up to 16 fp32 ones, which
-    // are cut into their parts once instead of once per tile
-    const size_t token = (size_t)p.chunks * 128 * (XF ? 6 : 2), one = token * (p.M < 8 ? p.M : 8), both = token * (p.M < 16 ? p.M : 16);
-    if (XF && p.M > 8 && both <= 144 * 1024)
-        return wide ? launch_w4<2, 2, true, FINE, true>(ctx, p, both, st) : launch_w4<1, 2, true, FINE, true>(ctx, p, both, st);
+    const bool wide = p.N > 16 * sm;
+    // the activations of up to 8 tokens as operands in shared memory, where that leaves room for the rings
+    const size_t one = token * (p.M < 8 ? p.M : 8);
     if (one <= 96 * 1024 && (XF || p.M <= 8))
         return wide ? launch_w4<2, 1, XF, FINE, true>(ctx, p, one, st) : launch_w4<1, 1, XF, FINE, true>(ctx, p, one, st);
     if (XF || p.M <= 8) return wide ? launch_w4<2, 1, XF, FINE, false>(ctx, p, 0, st) : launch_w4<1, 1, XF, FINE, false>(ctx, p, 0, st);

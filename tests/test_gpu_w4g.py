@@ -283,3 +283,67 @@ def test_refusals(gpu):
     with pytest.raises(pk.StwqError) as e:
         gpu.ctx.gps_fold_group4(z(4, 128), None, z(4, 64, dt=torch.uint8), z(4, 5))
     assert e.value.code == -2
+
+
+# many rows: output channels enough for it on 148 SMs, each form of the kernel, ragged in every direction
+MANY = [("bf16", 17, 2500, 640, 64), ("bf16", 25, 3001, 1152, 128), ("bf16", 32, 5000, 32, 32), ("bf16", 32, 7333, 416, 32), ("bf16", 20, 7500, 1280, 256),
+        ("bf16", 64, 2405, 544, 32), ("bf16", 49, 4099, 768, 96), ("bf16", 40, 4801, 1024, 128), ("bf16", 33, 9000, 160, 160), ("bf16", 64, 2370, 8192, 64),
+        ("f32", 9, 2401, 320, 32), ("f32", 16, 130, 512, 128), ("f32", 13, 5760, 1920, 32), ("f32", 16, 2370, 4096, 256), ("f32", 64, 1300, 512, 128),
+        ("f32", 20, 4000, 96, 96), ("f32", 31, 3000, 1056, 32), ("f32", 33, 7200, 352, 32), ("f32", 64, 3700, 1024, 128), ("f32", 63, 8191, 64, 64)]
+
+
+@pytest.mark.parametrize("x,M,N,K,group", MANY)
+def test_many_rows(gpu, x, M, N, K, group):
+    torch = gpu.torch
+    Wp, s, g = weights(gpu, N, K, group, s_bf16=M % 2 == 0, seed=M)
+    dt = torch.bfloat16 if x == "bf16" else torch.float32
+    wide = torch.full((M + 2, K + 48), float("nan"), device=gpu.dev, dtype=dt)
+    X = wide[1:M + 1, 16:K + 16]
+    X.copy_(torch.randn((M, K), device=gpu.dev, generator=g))
+    bias = torch.randn((N,), device=gpu.dev, generator=g) if N % 2 else None
+    for out, ydt, act in ((gpu.pk.OUT_F32, torch.float32, 0), (gpu.pk.OUT_BF16, torch.bfloat16, 2)):
+        Y = torch.full((M + 1, N), 7.0, device=gpu.dev, dtype=ydt)
+        gpu.ctx.linear_w4g(X, Wp, s, bias, act, out, Y[:M])
+        check(gpu, X, Wp, s, bias, act, Y[:M], x == "f32")
+        assert (Y[M] == 7).all()
+        again = torch.empty((M, N), device=gpu.dev, dtype=ydt)
+        gpu.ctx.linear_w4g(X, Wp, s, bias, act, out, again)
+        assert torch.equal(again, Y[:M])
+
+
+@pytest.mark.parametrize("x,M,N", [("bf16", 30, 2500), ("bf16", 64, 2500), ("f32", 12, 2500), ("f32", 64, 2500), ("f32", 40, 7200)])
+@pytest.mark.parametrize("group", [32, 128])
+def test_many_rows_nan_and_inf_stay_in_their_row(gpu, x, M, N, group):
+    torch, nan, inf = gpu.torch, float("nan"), float("inf")
+    Wp, s, g = weights(gpu, N, 256, group)
+    Wp[:, 20] = 0x77                                          # channels 40, 41: code 7 in every row
+    X = torch.randn((M, 256), device=gpu.dev, generator=g).to(torch.bfloat16 if x == "bf16" else torch.float32)
+    X[1, 40], X[M - 2, 41], X[9, 40] = nan, inf, -inf
+    clean = X.clone()
+    clean[[1, 9, M - 2]] = 0
+    Y, Z = torch.empty((M, N), device=gpu.dev), torch.empty((M, N), device=gpu.dev)
+    gpu.ctx.linear_w4g(X, Wp, s, None, 0, gpu.pk.OUT_F32, Y)
+    gpu.ctx.linear_w4g(clean, Wp, s, None, 0, gpu.pk.OUT_F32, Z)
+    assert torch.isnan(Y[1]).all() and (Y[M - 2] == inf).all() and (Y[9] == -inf).all()
+    rest = [m for m in range(M) if m not in (1, 9, M - 2)]
+    assert torch.equal(Y[rest], Z[rest])
+
+
+@pytest.mark.parametrize("x,M,N,K", [("bf16", 24, 3000, 1024), ("bf16", 64, 3000, 1024), ("f32", 64, 3000, 1024), ("f32", 13, 3000, 2048)])
+def test_many_rows_captured_as_a_contexts_first_call(gpu, x, M, N, K):
+    torch = gpu.torch
+    Wp, s, g = weights(gpu, N, K, 64)
+    X = torch.randn((M, K), device=gpu.dev, generator=g).to(torch.bfloat16 if x == "bf16" else torch.float32)
+    Y, Z = torch.zeros((M, N), device=gpu.dev), torch.empty((M, N), device=gpu.dev)
+    fresh = gpu.pk.Context(0)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        fresh.linear_w4g(X, Wp, s, None, 1, gpu.pk.OUT_F32, Y)
+    X.copy_(torch.randn((M, K), device=gpu.dev, generator=g))
+    graph.replay()
+    gpu.ctx.linear_w4g(X, Wp, s, None, 1, gpu.pk.OUT_F32, Z)
+    torch.cuda.synchronize()
+    assert torch.equal(Y, Z)
+    check(gpu, X, Wp, s, None, 1, Y, x == "f32")
+    fresh.close()
