@@ -458,9 +458,10 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
 // Many rows: a block of eight warps takes 128 RT output channels and 8 MT tokens. The activations of a chunk come into shared memory
 // once for all its warps (fp32 ones are cut into their parts there, once); a word of codes is widened once for all its tokens. A cluster of
 // blocks splits the chunks of a tile, and its blocks add up the sums of their share of the tokens, in the order of the chunks.
-// What bounds it: 430 instructions per 16 rows, 64 tokens and chunk, half the issue slots and half of what mma.sync can do; with 32
-// tokens the widening, 2/3 of the instructions. 8192 > 16384 in groups of 128: 32 rows 46 us, 64 rows 70 to 75 (in passes of 16 rows with
-// the kernel above 62 and 115 to 125), 64 fp32 rows 173 (303). Twice the warps an SM with half the rows each (RT 1 for RT 2): 50 us for 32 rows.
+// What bounds it: with 64 rows some 660 instructions per 32 output channels and chunk from eight warps an SM, half of what mma.sync can
+// do, on 128 of the SMs (a tile's clusters do not fill the rest); with 32 rows the widening, half of its instructions. 8192 > 16384 in
+// groups of 128: 32 rows 46 us, 64 rows 70 to 75 (the kernel above, in passes of 16 rows: 62 and 115 to 125), 64 fp32 rows 173 (303).
+// Twice the warps an SM with half the output channels each: 50 us for 32 rows, 72 for 64.
 template <int RT, int MT, bool XF>
 struct ManyStage {
     static constexpr int kCodes = RT * 8192, kRow = XF ? 512 : 256, kBytes = kCodes + MT * 8 * kRow, kStages = XF ? 2 : 4;
