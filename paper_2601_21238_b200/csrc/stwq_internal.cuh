@@ -53,7 +53,7 @@ struct stwq_ctx {
     int attn_configured;       // so has the one-kernel attention head
     int attn_few_configured;   // and the few-query attention kernel
     uint32_t w4g_configured;   // variants of the few-row 4-bit kernel that have theirs
-    uint16_t w4g_clusters[24][9]; // [its kernel for many rows][n]: clusters of n blocks that are resident at once; [0]: the attribute is set
+    uint16_t w4g_clusters[32][9]; // [its kernel for many rows][n]: clusters of n blocks that are resident at once; [0]: the attribute is set
     void* encode_tiled;        // cuTensorMapEncodeTiled, resolved at create
 };
 

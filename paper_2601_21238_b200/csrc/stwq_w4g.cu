@@ -8,7 +8,7 @@
 // word of eight codes becomes four bf16 pairs in registers by a shift, a mask and one subtraction each (0x3e00 | (nibble ^ 8) is 2^-3 +
 // (code + 8) 2^-10 as bf16; less 2^-3 + 2^-7 it is code 2^-10, exactly). The 2^-10 keeps 128 codes times the largest activation
 // inside fp32; it leaves the result at the end (bits below 2^-126 are lost).
-// A second kernel, further down, takes more rows than a tile or two of eight.
+// A second kernel, further down, takes more rows than a tile or two of eight, and fp32 ones from four on where it is sooner done.
 // A chunk is 128 input channels: 64 bytes of codes of each row, copied asynchronously into a ring of stages that every warp has for
 // itself, with the chunk's activations beside them. The order in which channels meet in a product does not matter as long as both
 // operands keep it. Where a group is a multiple of 128 channels, a lane takes 16 bytes of a row (32 channels), the chunk's products
@@ -21,7 +21,7 @@
 // What bounds it: with many output channels the issue of some 320 instructions per 2 KB of codes (half of them the widening, on a
 // half-rate pipe) from 16 warps of up to 128 registers: 4 x 4096 > 128000, groups of 128, 75 us, 3.6 TB/s, 0.56 of the measured copy rate
 // (65 us from L2 alone, 65 without the widening or without the products). Few channels: launch, first bytes, the exchange: 1 x 2048 >
-// 8192 6.6 us, 8 x 8192 > 2048 in groups of 64 8.3 us. fp32 activations take three products: 13 x 1920 > 5760 in groups of 32 10.3 us.
+// 8192 6.6 us, 8 x 8192 > 2048 in groups of 64 8.3 us. fp32 activations take three products: 13 x 1920 > 5760 in groups of 32 10.2 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) linear_w4g_kernel(const W4P
 // Twice the warps an SM with half the output channels each: 50 us for 32 rows, 72 for 64.
 template <int RT, int MT, bool XF>
 struct ManyStage {
-    static constexpr int kCodes = RT * 8192, kRow = XF ? 512 : 256, kBytes = kCodes + MT * 8 * kRow, kStages = XF ? 2 : 4;
+    static constexpr int kCodes = RT * 8192, kRow = XF ? 512 : 256, kBytes = kCodes + MT * 8 * kRow, kStages = !XF || MT == 1 ? 4 : MT == 2 ? 3 : 2;
     static constexpr int kOps = XF ? MT * 8 * 768 : 0, kAll = kStages * kBytes + kOps, kSum = RT * 128 + 4;    // fp32 parts; floats a token
     static_assert(MT * 8 * kSum * 4 <= kAll, "the sums lie where the stages were");
 };
@@ -533,7 +533,8 @@ __global__ void __launch_bounds__(256, RT * MT > 8 ? 1 : RT * MT > 4 ? 2 : 3) li
         const char* xs = XF ? ops : stage + S::kCodes;
         if (XF) {
 #pragma unroll
-            for (int i = 0; i < MT / 2; ++i) {
+            for (int i = 0; i < (MT + 1) / 2; ++i) {
+                if (MT == 1 && threadIdx.x >= 128) break;
                 const int token = i * 16 + (int)(threadIdx.x >> 4), eight = threadIdx.x & 15;
                 const char* raw = stage + S::kCodes + token * 512;
                 uint4 b[3];
@@ -649,7 +650,7 @@ int launch_w4_many(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    uint16_t* fit = ctx->w4g_clusters[(RT - 1) | (XF ? 2 : 0) | (FINE ? 4 : 0) | (MT == 2 ? 0 : MT == 4 ? 8 : 16)];
+    uint16_t* fit = ctx->w4g_clusters[(RT - 1) | (XF ? 2 : 0) | (FINE ? 4 : 0) | (MT == 1 ? 24 : MT == 2 ? 0 : MT == 4 ? 8 : 16)];
     if (!fit[0]) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kAll);
         for (int r = 1; r <= 8 && e == cudaSuccess; ++r) {
@@ -733,6 +734,7 @@ int launch_w4_any(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
     // 0.74 to 0.95 above 16 SMs, where tiles of 128 output channels win up to 48 SMs, of 256 beyond. fp32 the same with a pass for every
     // 32 rows (64 rows 0.48 to 0.97, 17 rows 0.7 to 0.97 above 24 SMs, 1.1 to 1.3 below). Fewer channels keep too few of its blocks busy: 1.1
     // to 2.7. 9 to 16 rows: fp32 0.67 to 0.95 (1.1 where it is worst), up to 16 SMs only while K is short (0.82 to 1.0, else 1.2); bf16 0.8 to 1.3: not taken.
+    // 4 to 8 fp32 rows 0.68 to 1.0 up to 48 SMs, but 1.0 to 1.2 where its tiles are 8 to 16 and the other kernel's one for every SM; 1 to 3 rows 1.0 to 1.6.
     if (!XF && p.M > 32 && p.N > (p.M > 48 ? 16 : 32) * sm) return launch_w4_many<2, 8, false, FINE>(ctx, p, st);
     if (p.M > 16 && (XF || p.M <= 32)) {
         const int64_t work = (int64_t)p.N * ((p.M + 31) / 32);
@@ -740,6 +742,7 @@ int launch_w4_any(stwq_ctx* ctx, W4Params& p, cudaStream_t st)
         if (work > (XF && p.M <= 24 ? 24 : 16) * sm) return launch_w4_many<1, 4, XF, FINE>(ctx, p, st);
     }
     if (XF && p.M > 8 && p.M <= 16 && (p.N > 16 * sm || token * p.M <= 144 * 1024)) return launch_w4_many<1, 2, true, FINE>(ctx, p, st);
+    if (XF && p.M >= 4 && p.M <= 8 && p.N <= 48 * sm && (p.N <= 8 * sm || p.N > 16 * sm)) return launch_w4_many<1, 1, true, FINE>(ctx, p, st);
     // Tiles of 32 output channels share the operands of X, tiles of 16 spread further. Over K = 1024 to 8192 and 1 to 16 rows, 32 against
     // 16 took 1.22 times as long at N = 2048, 0.94 at 2560 to 4608, 0.92 to 1.0 above: 16 only while each has an SM of its own.
     const bool wide = p.N > 16 * sm;

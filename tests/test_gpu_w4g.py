@@ -289,7 +289,8 @@ def test_refusals(gpu):
 MANY = [("bf16", 17, 2500, 640, 64), ("bf16", 25, 3001, 1152, 128), ("bf16", 32, 5000, 32, 32), ("bf16", 32, 7333, 416, 32), ("bf16", 20, 7500, 1280, 256),
         ("bf16", 64, 2405, 544, 32), ("bf16", 49, 4099, 768, 96), ("bf16", 40, 4801, 1024, 128), ("bf16", 33, 9000, 160, 160), ("bf16", 64, 2370, 8192, 64),
         ("f32", 9, 2401, 320, 32), ("f32", 16, 130, 512, 128), ("f32", 13, 5760, 1920, 32), ("f32", 16, 2370, 4096, 256), ("f32", 64, 1300, 512, 128),
-        ("f32", 20, 4000, 96, 96), ("f32", 31, 3000, 1056, 32), ("f32", 33, 7200, 352, 32), ("f32", 64, 3700, 1024, 128), ("f32", 63, 8191, 64, 64)]
+        ("f32", 20, 4000, 96, 96), ("f32", 31, 3000, 1056, 32), ("f32", 33, 7200, 352, 32), ("f32", 64, 3700, 1024, 128), ("f32", 63, 8191, 64, 64), ("f32", 4, 2370, 1056, 32),
+        ("f32", 7, 7001, 640, 128), ("f32", 8, 5760, 1920, 96), ("f32", 5, 1184, 4096, 64), ("f32", 6, 3001, 32, 32)]
 
 
 @pytest.mark.parametrize("x,M,N,K,group", MANY)
@@ -329,7 +330,7 @@ def test_many_rows_nan_and_inf_stay_in_their_row(gpu, x, M, N, group):
     assert torch.equal(Y[rest], Z[rest])
 
 
-@pytest.mark.parametrize("x,M,N,K", [("bf16", 24, 3000, 1024), ("bf16", 64, 3000, 1024), ("f32", 64, 3000, 1024), ("f32", 13, 3000, 2048)])
+@pytest.mark.parametrize("x,M,N,K", [("bf16", 24, 3000, 1024), ("bf16", 64, 3000, 1024), ("f32", 64, 3000, 1024), ("f32", 13, 3000, 2048), ("f32", 8, 3000, 2048)])
 def test_many_rows_captured_as_a_contexts_first_call(gpu, x, M, N, K):
     torch = gpu.torch
     Wp, s, g = weights(gpu, N, K, 64)
