@@ -348,3 +348,66 @@ def test_many_rows_captured_as_a_contexts_first_call(gpu, x, M, N, K):
     assert torch.equal(Y, Z)
     check(gpu, X, Wp, s, None, 1, Y, x == "f32")
     fresh.close()
+
+
+@pytest.mark.parametrize("x,M", [("bf16", 64), ("bf16", 20), ("f32", 33), ("f32", 12)])
+def test_many_rows_offsets_beyond_2_31(gpu, x, M):
+    """Offsets in the packed weights, and then in Y, pass 32 bits: the first and the last rows against 64 bits, zeros between."""
+    torch = gpu.torch
+    g = torch.Generator(device=gpu.dev).manual_seed(M)
+    dt = torch.bfloat16 if x == "bf16" else torch.float32
+    for N, K in ((70000, 65536), (2 ** 31 // M + 300, 32)):
+        Wp = torch.zeros((N, K // 2), device=gpu.dev, dtype=torch.uint8)
+        for rows in (slice(0, 64), slice(N - 64, N)):
+            Wp[rows] = torch.randint(0, 256, (64, K // 2), device=gpu.dev, generator=g, dtype=torch.int32).to(torch.uint8)
+        s = torch.full((N, K // 32), 0.01, device=gpu.dev, dtype=torch.bfloat16)
+        X = torch.randn((M, K), device=gpu.dev, generator=g).to(dt)
+        Y = torch.empty((M, N), device=gpu.dev)
+        gpu.ctx.linear_w4g(X, Wp, s, None, 0, gpu.pk.OUT_F32, Y)
+        assert all(not Y[m, 64:-64].any() for m in range(M))
+        for rows in (slice(0, 64), slice(N - 64, N)):
+            check(gpu, X, Wp[rows], s[rows], None, 0, Y[:, rows], x == "f32")
+        del Wp, s, X, Y
+        torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("M,N", [(8, 3000), (12, 3000), (40, 3000), (64, 4000)])
+@pytest.mark.parametrize("group", [32, 128])
+def test_many_rows_large_and_small_activations(gpu, M, N, group):
+    """fp32 activations over 40 octaves and up to the largest: the parts cover all bits."""
+    torch = gpu.torch
+    Wp, s, g = weights(gpu, N, 256, group)
+    for top in (1e30, 1.0, 1e-25):
+        X = (torch.rand((M, 256), device=gpu.dev, generator=g) * 2 - 1) * torch.exp2(-40 * torch.rand((M, 256), device=gpu.dev, generator=g)) * top
+        Y = torch.empty((M, N), device=gpu.dev)
+        gpu.ctx.linear_w4g(X, Wp, s, None, 0, gpu.pk.OUT_F32, Y)
+        check(gpu, X, Wp, s, None, 0, Y, True)
+    X = torch.zeros((M, 256), device=gpu.dev)
+    X[:, 3] = 3.4028234e38
+    small = s * 0.01                                          # keeps the products finite
+    Y = torch.empty((M, N), device=gpu.dev)
+    gpu.ctx.linear_w4g(X, Wp, small, None, 0, gpu.pk.OUT_F32, Y)
+    check(gpu, X, Wp, small, None, 0, Y, True)
+
+
+def test_many_rows_beside_each_other(gpu):
+    """Clusters of several calls on two streams share the SMs: each call's bits stay what they are alone."""
+    torch = gpu.torch
+    jobs = []
+    for i, (M, N, K, dt) in enumerate([(64, 9000, 2048, torch.bfloat16), (24, 3000, 4096, torch.bfloat16), (64, 3000, 1024, torch.float32), (8, 3000, 2048, torch.float32)]):
+        Wp, s, g = weights(gpu, N, K, 64, seed=i)
+        X = torch.randn((M, K), device=gpu.dev, generator=g).to(dt)
+        alone, Y, Z = (torch.empty((M, N), device=gpu.dev) for _ in range(3))
+        gpu.ctx.linear_w4g(X, Wp, s, None, 0, gpu.pk.OUT_F32, alone)
+        jobs.append((X, Wp, s, alone, (Y, Z)))
+    other, streams = gpu.pk.Context(0), [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for turn in range(12):
+        for j in range(len(jobs)):
+            for k, ctx in enumerate((gpu.ctx, other)):
+                X, Wp, s, _, Y = jobs[(j + 2 * k + turn * k) % len(jobs)]
+                ctx.linear_w4g(X, Wp, s, None, 0, gpu.pk.OUT_F32, Y[k], stream=streams[k])
+    torch.cuda.synchronize()
+    for _, _, _, alone, Y in jobs:
+        assert torch.equal(alone, Y[0]) and torch.equal(alone, Y[1])
+    other.close()
