@@ -8,8 +8,9 @@
 // The likeliest k of V without a sort: the pass also leaves the maximum of every run of 4 vectors (64 or 32 logits) in shared
 // memory, and each four threads keep the maximum of all their runs. The k-th largest of those maxima (32 to 128 of them) is a bound
 // that at least k logits reach; the few runs that reach it (about k) are read again, their logits that reach it (about k) are
-// ranked by counting over 64-bit keys (value, then lower index), which are all different. Where too many reach the bound
-// (a constant row), the k tokens are found one after the other. With few rows a cluster of up to eight blocks takes a row: slices
+// ranked by counting over 64-bit keys (value, then lower index), which are all different. More than 64 of them (short rows, rows
+// with few logits left: a group may hold none) first meet a second bound, the k-th largest key among the maxima of 128 groups of them: 6
+// rows of 1575, half masked, k = 32: 8 us, 76 by counting over all. Where too many reach the bound (a constant row), the k tokens are found one after the other. With few rows a cluster of up to eight blocks takes a row: slices
 // that fit the registers give their candidates without a second read, and the first block joins sums and lists.
 // Bound by HBM with many rows: 4096 rows of 128000 bf16 logits 194 us, 5.4 TB/s, 0.83 of the measured copy rate (seven instructions and one
 // ex2 per logit, two more for its rank); 1000 rows of fp32 with twenty likeliest 110 us, 0.71 (3.4 rounds of blocks). Few rows by the
@@ -31,6 +32,7 @@ constexpr int kTop = 32;
 constexpr int kMaxCluster = 8;
 constexpr int kCand = 2048;                  // logits of a block that reach its bound
 constexpr int kRuns = 1024;                  // runs that do
+constexpr int kFew = 128;                    // groups of candidates for a second bound
 constexpr float kLow = -200.0f;              // octaves below which a weight is 0
 
 struct LpParams {
@@ -48,12 +50,16 @@ template <int NT>
 struct LpShared {
     float m[NT / 32], s[NT / 32], a[NT / 32];
     uint32_t n[NT / 32];
-    __align__(16) float gmax[NT / 4];        // of the runs of four threads
+    __align__(16) float gmax[NT > 128 ? NT / 4 : NT];                          // of the vectors of a group
     float bound;
-    uint32_t n_cand, n_runs;
+    uint32_t n_cand, n_runs, n_few;
     unsigned long long best[NT / 32];
     unsigned long long cand[kCand];
-    int32_t runs[kRuns];
+    unsigned long long few_max[kFew], few_bound;
+    union {                                  // one after the other
+        int32_t runs[kRuns];
+        unsigned long long few[kTop * kCand / kFew];
+    };
     float row_m[kMaxCluster], row_s[kMaxCluster], row_a[kMaxCluster];          // of the blocks of a row, in the first one
     uint32_t row_n[kMaxCluster];
     unsigned long long row_top[kMaxCluster * kTop];
@@ -250,7 +256,7 @@ __device__ __forceinline__ int place_of(const unsigned long long* keys, int n, i
 template <typename XT, int NT, bool CL, bool TOP>
 __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const LpParams p)
 {
-    constexpr int kPer = Vec<XT>::kPer, kGroups = NT / 4, kWarps = NT / 32, kAhead = CL ? 4 : 2;       // vectors in flight per thread
+    constexpr int kPer = Vec<XT>::kPer, kWarps = NT / 32, kAhead = CL ? 4 : 2;       // vectors in flight per thread
     extern __shared__ __align__(16) float run_max[];      // [runs of 4 vectors]
     __shared__ LpShared<NT> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -285,6 +291,9 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
     const float below = __fadd_rn(xt, 0.0f) == 0.0f ? -__uint_as_float(kUlp)
                         : __uint_as_float(xt > 0.0f ? __float_as_uint(xt) - kUlp : __float_as_uint(xt) + kUlp);
 
+    // threads that share a group of the bound: four, but one where 32 groups are hardly more than k (300 rows of 4768, k = 32: 18 us, 11.6;
+    // k = 5: 6.3, 7.7)
+    const int share = NT > 128 || p.k <= 16 ? 4 : 1;
     Sums<kPer> me = {-INFINITY, INFINITY, c, 0ull, 0ull, false};
     uint32_t before = 0u;
     float gmax = -INFINITY, vmax[kAhead];
@@ -326,11 +335,10 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
         next += NT * kPer;
         if (TOP) {
             vmax[u] = vm;
-            if (held) gmax = fmaxf(gmax, vm);
-            else {
+            gmax = fmaxf(gmax, vm);
+            if (!held) {
                 float rm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, 1));
                 rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, 2));
-                gmax = fmaxf(gmax, rm);
                 if ((tid & 3) == 0 && i < nvec) run_max[i >> 2] = rm;
             }
         }
@@ -342,12 +350,15 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
     // ---- the block's maximum, then its sums relative to it, added in the order of lanes and warps
     const float wm = warp_max(me.m);
     if (lane == 0) sh.m[warp] = wm;
-    gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, 1));
-    gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, 2));
-    if ((tid & 3) == 0) sh.gmax[tid >> 2] = gmax;
+    if (share == 4) {
+        gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, 1));
+        gmax = fmaxf(gmax, __shfl_xor_sync(0xffffffffu, gmax, 2));
+    }
+    if ((tid & (share - 1)) == 0) sh.gmax[tid / share] = gmax;
     if (tid == 0) {
         sh.n_cand = 0u;
         sh.n_runs = 0u;
+        sh.n_few = 0u;
     }
     __syncthreads();
     float bm = sh.m[0];                                    // the blocks' common reference
@@ -366,20 +377,22 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
             sh.n[warp] = before;
         }
     }
-    // ---- the k-th largest of the groups' maxima, ties broken by the group: four threads count for a group
+    // ---- the k-th largest of the groups' maxima, ties broken by the group: a group's threads count for it
     if (TOP) {
-        const int q = tid >> 2, from = (tid & 3) * (kGroups / 4);
+        const int q = tid / share, each = NT / (share * share), from = (tid & (share - 1)) * each;
         const float v = sh.gmax[q];
         int ahead_of = 0;
 #pragma unroll 4
-        for (int j = from; j < from + kGroups / 4; j += 4) {
+        for (int j = from; j < from + each; j += 4) {
             const float4 u = *reinterpret_cast<const float4*>(&sh.gmax[j]);
             ahead_of += (u.x > v || (u.x == v && j < q)) + (u.y > v || (u.y == v && j + 1 < q)) + (u.z > v || (u.z == v && j + 2 < q)) +
                         (u.w > v || (u.w == v && j + 3 < q));
         }
-        ahead_of += __shfl_xor_sync(0xffffffffu, ahead_of, 1);
-        ahead_of += __shfl_xor_sync(0xffffffffu, ahead_of, 2);
-        if ((tid & 3) == 0 && ahead_of == p.k - 1) sh.bound = v;
+        if (share == 4) {
+            ahead_of += __shfl_xor_sync(0xffffffffu, ahead_of, 1);
+            ahead_of += __shfl_xor_sync(0xffffffffu, ahead_of, 2);
+        }
+        if ((tid & (share - 1)) == 0 && ahead_of == p.k - 1) sh.bound = v;
     }
     __syncthreads();
     float bs = 0.0f, ba = 0.0f;
@@ -441,10 +454,33 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
         }
         __syncthreads();
         if (sh.n_runs <= kRuns && sh.n_cand <= kCand) {
-            const int n = (int)sh.n_cand;
+            int n = (int)sh.n_cand;
+            const unsigned long long* cand = sh.cand;
+            if (n > kFew / 2) {
+                // Short rows with groups hardly more than k, or many without a logit: again a bound, from the maxima of kFew groups of candidates.
+                // It is a key, so k groups reach it, with n / kFew candidates each at most.
+                unsigned long long best = 0ull;
+                if (tid < kFew) {
+                    for (int i = tid; i < n; i += kFew) best = sh.cand[i] > best ? sh.cand[i] : best;
+                    sh.few_max[tid] = best;
+                }
+                __syncthreads();
+                if (tid < kFew) {
+                    int ahead_of = 0;
+#pragma unroll 8
+                    for (int j = 0; j < kFew; ++j) ahead_of += sh.few_max[j] > best ? 1 : 0;
+                    if (ahead_of == p.k - 1) sh.few_bound = best;
+                }
+                __syncthreads();
+                for (int i = tid; i < n; i += NT)
+                    if (sh.cand[i] >= sh.few_bound) sh.few[atomicAdd(&sh.n_few, 1u)] = sh.cand[i];
+                __syncthreads();
+                n = (int)sh.n_few;
+                cand = sh.few;
+            }
             for (int first = 0; first < n; first += NT / 8) {
-                const int i = first + (tid >> 3), at = place_of(sh.cand, n, i, lane);
-                if (i < n && at < p.k && (lane & 7) == 0) top[at] = sh.cand[i];
+                const int i = first + (tid >> 3), at = place_of(cand, n, i, lane);
+                if (i < n && at < p.k && (lane & 7) == 0) top[at] = cand[i];
             }
             for (int i = n + tid; i < p.k; i += NT) top[i] = 0ull;
         } else {                                          // too many at the bound: the next largest key, k times

@@ -265,3 +265,41 @@ def test_refusals(gpu):
     refused(-4, X, None, f(4), f(4))
     refused(-3, X.t(), None, i(100), f(100))
     refused(-2, torch.zeros((1, 360449), device=gpu.dev), None, i(1), f(1))
+
+
+@pytest.mark.parametrize("V", [33, 100, 313, 511, 787, 1575, 2047, 2619, 4768, 8191])
+@pytest.mark.parametrize("k", [1, 16, 17, 32])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_the_likeliest_of_short_rows(gpu, V, k, x):
+    """Exactly those of a sort: rows with ties (bf16), with most or all but one stretch masked, with few values, constant, in order."""
+    torch = gpu.torch
+    g = torch.Generator(device=gpu.dev).manual_seed(V * 37 + k)
+    X = torch.randn((9, V), device=gpu.dev, generator=g) * 2
+    ninf = float("-inf")
+    X[1, torch.rand(V, device=gpu.dev, generator=g) < 0.5] = ninf
+    X[2, torch.rand(V, device=gpu.dev, generator=g) < 0.95] = ninf
+    X[3, :V // 3] = ninf
+    X[3, V // 3 + V // 5 + 1:] = ninf
+    X[4] = torch.randint(0, 4, (V,), device=gpu.dev, generator=g).float()
+    X[5] = 1.5
+    X[6] = torch.arange(V, device=gpu.dev) * 0.5
+    X[7] = -torch.arange(V, device=gpu.dev) * 0.5
+    X[8] = float("nan")
+    X = X.to(torch.bfloat16 if x == "bf16" else torch.float32)
+    ids, lps = torch.empty((9, k), device=gpu.dev, dtype=torch.int32), torch.empty((9, k), device=gpu.dev)
+    gpu.ctx.token_logprobs(X, None, None, None, None, None, ids, lps)
+    v = X.double().cpu().numpy()
+    v[np.isnan(v)] = -np.inf
+    for row in range(9):
+        order = np.lexsort((np.arange(V), -v[row]))
+        live = order[v[row][order] > -np.inf][:k]
+        want = np.full(k, -1)
+        want[:len(live)] = live
+        assert (ids[row].cpu().numpy() == want).all(), row
+        got = lps[row].double().cpu().numpy()
+        assert (got[len(live):] == -np.inf).all()
+        if len(live):
+            z = v[row] - v[row].max()
+            ref = z[live] - np.log(np.exp(z).sum())
+            # x - max and the final difference round once each, ln S to a few units of its own size
+            assert (np.abs(got[:len(live)] - ref) <= 2.0 ** -24 * (2 * np.abs(ref) + 16 + 4 * np.log(V))).all(), row
