@@ -441,7 +441,7 @@ extern "C" int block_norm(stwq_ctx* ctx, const void* H, int64_t ldh, int h_dtype
         return STWQ_ERR_ALIGN;
 
     BnParams p = {};
-    p.H = H; p.O = O; p.gate = gate; p.scale = scale; p.shift = shift; p.Ho = Hout; p.Y = Y;
+    p.H = H; p.O = O; p.gate = O ? gate : nullptr; p.scale = scale; p.shift = shift; p.Ho = Hout; p.Y = Y;
     p.ldh = ldh; p.ldo = ldo; p.ldc = cond ? ldc : 0; p.ldho = ldho; p.ldy = ldy; p.M = M;
     p.C = C; p.G = cond ? G : 1; p.P = P;
     p.y_dtype = Y ? y_dtype : STWQ_OUT_F32;
