@@ -136,10 +136,14 @@ struct Sums {
     uint64_t s, a;
     bool odd;                                // a logit without a weight came by
     __device__ __forceinline__ float z_of(float x) const { return finite(mc) ? fmaxf(fmaf(x, c, -mc), kLow) : octaves(x, m, c); }
-    // what sums relative to (m, mc) are multiplied by, in octaves, to stand relative to (to, toc)
+    // What sums relative to (m, mc) are multiplied by, in octaves, to stand relative to (to, toc). Where one product is kept, its sums are
+    // relative to the rounded product, and the others to the reference itself: its rounding, up to 2^-5 of an octave, is made up for.
     __device__ __forceinline__ float shift(float to, float toc) const
     {
-        return m == to ? 0.0f : finite(mc) && finite(toc) ? fmaxf(mc - toc, kLow) : octaves(m, to, c);
+        if (m == to) return 0.0f;
+        if (finite(mc) && finite(toc)) return fmaxf(mc - toc, kLow);
+        const float d = octaves(m, to, c);
+        return finite(mc) ? d - fmaf(m, c, -mc) : finite(toc) ? d + fmaf(to, c, -toc) : d;
     }
     __device__ __forceinline__ void raise(float to)       // `to` > m
     {
