@@ -524,8 +524,8 @@ int linear_w4g(stwq_ctx* ctx, const void* X, int64_t ldx, int x_dtype, int64_t M
  *    Any other token outside [0, V): NaN, rank -1, and STWQ_ERR_TOKEN is recorded.
  *  - Fewer than k tokens that can be drawn: the rest of top_ids is -1, of top_logprobs -Inf. A row without any: entropy 0.
  * fp32; S and the entropy sum are good to a few units of 2^-24, so a log probability near 0 is good to about 1e-7 absolute; none is above 0.
- * Sums have a fixed order: the same call gives the same bits (how a row is split, and with it the last bits, goes by B and V). Logits
- * more than 3.4e38 apart count as infinitely far. V <= 360448, ld >= V; outputs must not overlap the logits (STWQ_ERR_ALIGN).
+ * Sums have a fixed order: the same call gives the same bits (how a row is split, and with it the last bits, goes by B and V).
+ * V <= 360448, ld >= V; outputs must not overlap the logits (STWQ_ERR_ALIGN).
  */
 int token_logprobs(stwq_ctx* ctx, const void* logits, int x_dtype, int64_t ld, int B, int V, const float* temperature,
                    const int32_t* tokens, float* logprobs, int32_t* ranks, float* entropy, int k, int32_t* top_ids,

@@ -532,7 +532,9 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
     const float ln_s = finite(bmc) ? fmaf(-ln2, fmaf(bm, c, -bmc), ln_sums) : ln_sums;
     auto ln_p = [&](float x, bool first) {
         if (greedy) return first ? 0.0f : -INFINITY;
-        return fminf((x == bm ? 0.0f : (x - bm) / t) - ln_s, 0.0f);          // S is rounded: it may fall short of the token's own weight
+        const float d = x == bm ? 0.0f : x - bm;                             // beyond the largest number: its half, which is exact there
+        const float z = finite(d) ? d / t : (0.5f * x - 0.5f * bm) / (0.5f * t);
+        return fminf(z - ln_s, 0.0f);                                        // S is rounded: it may fall short of the token's own weight
     };
     if (tid == 0) {
         if (p.tokens != nullptr) {
