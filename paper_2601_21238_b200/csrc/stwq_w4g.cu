@@ -226,7 +226,8 @@ struct Scales {
 };
 
 // Eight activations as B operands of two products: pairs of channels (0,4), (1,5), (2,6), (3,7); fp32 ones as three such sets, the top,
-// middle and bottom 8 bits of the significands. Inf and NaN stand in the first part alone.
+// middle and bottom 8 bits of the significands. An infinity stands in the first part alone; the rest of a NaN is one again, since its
+// first 16 bits may be those of an infinity.
 __device__ __forceinline__ uint4 pairs_bf16(const uint4& x)
 {
     return make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
@@ -238,7 +239,7 @@ __device__ __forceinline__ void pairs_f32(const uint4& u, const uint4& v, uint4 
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         r[e] = __uint_as_float(x[e]) - __uint_as_float(x[e] & 0xffff0000u);
-        if (!(fabsf(__uint_as_float(x[e])) < INFINITY)) r[e] = 0.0f;
+        if (fabsf(__uint_as_float(x[e])) == INFINITY) r[e] = 0.0f;
     }
     b[0] = make_uint4(__byte_perm(x[0], x[4], 0x7632), __byte_perm(x[1], x[5], 0x7632), __byte_perm(x[2], x[6], 0x7632), __byte_perm(x[3], x[7], 0x7632));
 #pragma unroll
