@@ -502,7 +502,7 @@ int block_norm(stwq_ctx* ctx, const void* H, int64_t ldh, int h_dtype, const voi
  *    fp32 or bf16. A channel scale s_ch of the fold is divided out of X by its producer (block_norm's s_ch).
  * group a multiple of 32 that divides K, K < 131072, N <= 2^30; M <= 64: every row beyond 8 adds work that the weights' stream does not
  * hide, and beyond 64 rows the tiled GEMM of qlinear_w4 is the right call. W, s_ch, s_g of the fold, X and Wp 16-byte aligned. Outputs
- * must not overlap operands (STWQ_ERR_ALIGN).
+ * must not overlap operands or each other (STWQ_ERR_ALIGN).
  * Products of codes and activations are exact (fp32 activations enter as three bf16 parts), sums fp32 in a fixed order: the
  * same call gives the same bits. Results below 2^-100 lose bits. A row of X with NaN or Inf gives NaN or Inf in that row of Y as the formula has it.
  */

@@ -774,7 +774,10 @@ int gps_fold_group4(stwq_ctx* ctx, const float* W, int N, int K, const float* s_
     if (s_dtype != STWQ_OUT_F32 && s_dtype != STWQ_OUT_BF16) return STWQ_ERR_BITS;
     if (!stwq_aligned16(W) || !stwq_aligned16(Wp) || !stwq_aligned16(s_ch) || !stwq_aligned16(s_g)) return STWQ_ERR_ALIGN;
     const int64_t w_bytes = (int64_t)N * K * 4, es = s_dtype == STWQ_OUT_F32 ? 4 : 2;
-    if (stwq_overlap(Wp, w_bytes / 8, W, w_bytes) || stwq_overlap(s_g, (int64_t)N * (K / group) * es, W, w_bytes) || stwq_overlap(Wp, w_bytes / 8, s_ch, (int64_t)K * 4))
+    // warps read the operands while others already store
+    const int64_t s_bytes = (int64_t)N * (K / group) * es, c_bytes = (int64_t)K * 4;
+    if (stwq_overlap(Wp, w_bytes / 8, W, w_bytes) || stwq_overlap(Wp, w_bytes / 8, s_ch, c_bytes) || stwq_overlap(s_g, s_bytes, W, w_bytes) ||
+        stwq_overlap(s_g, s_bytes, s_ch, c_bytes) || stwq_overlap(s_g, s_bytes, Wp, w_bytes / 8))
         return STWQ_ERR_ALIGN;
     StwqDevGuard dev(ctx->device);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
