@@ -530,11 +530,11 @@ __global__ void __launch_bounds__(NT, CL ? 1 : 1024 / NT) logprob_kernel(const L
     const float ln2 = 0.6931471805599453f, bmc = times_c(bm, c), ln_sums = any ? logf(bs) : 0.0f;
     // S relative to bm itself: less the rounding of bm c
     const float ln_s = finite(bmc) ? fmaf(-ln2, fmaf(bm, c, -bmc), ln_sums) : ln_sums;
+    // differences may pass the largest number: halves of them, which are exact there. S is rounded and may fall short of the token's own weight.
+    const float part = fabsf(bm) > 1e30f ? 0.5f : 1.0f;
     auto ln_p = [&](float x, bool first) {
         if (greedy) return first ? 0.0f : -INFINITY;
-        const float d = x == bm ? 0.0f : x - bm;                             // beyond the largest number: its half, which is exact there
-        const float z = finite(d) ? d / t : (0.5f * x - 0.5f * bm) / (0.5f * t);
-        return fminf(z - ln_s, 0.0f);                                        // S is rounded: it may fall short of the token's own weight
+        return fminf((x == bm ? 0.0f : fmaf(part, x, -part * bm) / (part * t)) - ln_s, 0.0f);
     };
     if (tid == 0) {
         if (p.tokens != nullptr) {
