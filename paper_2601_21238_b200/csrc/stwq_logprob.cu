@@ -140,8 +140,8 @@ struct Sums {
     // relative to the rounded product, and the others to the reference itself: its rounding, up to 2^-5 of an octave, is made up for.
     __device__ __forceinline__ float shift(float to, float toc) const
     {
+        if (__builtin_expect(finite(mc) && finite(toc), 1)) return fmaxf(mc - toc, kLow);
         if (m == to) return 0.0f;
-        if (finite(mc) && finite(toc)) return fmaxf(mc - toc, kLow);
         const float d = octaves(m, to, c);
         return finite(mc) ? d - fmaf(m, c, -mc) : finite(toc) ? d + fmaf(to, c, -toc) : d;
     }
