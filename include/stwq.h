@@ -501,10 +501,11 @@ int block_norm(stwq_ctx* ctx, const void* H, int64_t ldh, int h_dtype, const voi
  *  - linear_w4g: X M rows of x_dtype (fp32 or bf16), ldx elements apart (16-byte multiples); bias [N] fp32 or NULL; Y [M,N] dense,
  *    fp32 or bf16. A channel scale s_ch of the fold is divided out of X by its producer (block_norm's s_ch).
  * group a multiple of 32 that divides K, K < 131072, N <= 2^30; M <= 64: every row beyond 8 adds work that the weights' stream does not
- * hide, and beyond 64 rows the tiled GEMM of qlinear_w4 is the right call. W, s_ch, s_g of the fold, X and Wp 16-byte aligned. Outputs
+ * hide. More rows take a call for every 64; the tiled GEMM of qlinear_w4 takes a scale per channel, that is these weights only where
+ * group = K. W, s_ch, s_g of the fold, X and Wp 16-byte aligned. Outputs
  * must not overlap operands or each other (STWQ_ERR_ALIGN).
  * Products of codes and activations are exact (fp32 activations enter as three bf16 parts), sums fp32 in a fixed order: the
- * same call gives the same bits. Results below 2^-100 lose bits. A row of X with NaN or Inf gives NaN or Inf in that row of Y as the formula has it.
+ * same call gives the same bits (how sums are split, and with it the last bits of a row, goes by M, K and N). Results below 2^-100 lose bits. A row of X with NaN or Inf gives NaN or Inf in that row of Y as the formula has it.
  */
 int gps_fold_group4(stwq_ctx* ctx, const float* W, int N, int K, const float* s_ch, int group, uint8_t* Wp, void* s_g, int s_dtype,
                     void* stream);
@@ -523,8 +524,9 @@ int linear_w4g(stwq_ctx* ctx, const void* X, int64_t ldx, int x_dtype, int64_t M
  *  - A token that is never drawn: -Inf, rank -1. Token -1 (no token: a padding row, a row sample_tokens could not draw for): 0, rank -1.
  *    Any other token outside [0, V): NaN, rank -1, and STWQ_ERR_TOKEN is recorded.
  *  - Fewer than k tokens that can be drawn: the rest of top_ids is -1, of top_logprobs -Inf. A row without any: entropy 0.
- * fp32; S and the entropy sum are good to a few units of 2^-24, so a log probability near 0 is good to about 1e-7 absolute; none is above 0.
- * Sums have a fixed order: the same call gives the same bits (how a row is split, and with it the last bits, goes by B and V).
+ * fp32; S and the entropy sum are good to a few units of 2^-24, and one or two more for each nat that the weight lies below the
+ * maximum on average, so a log probability near 0 is good to about 1e-7 absolute; none is above 0.
+ * Sums have a fixed order: the same call gives the same bits (how a row is split, and with it the last bits, goes by B, V and the alignment of its first logit).
  * V <= 360448, ld >= V; outputs must not overlap the logits (STWQ_ERR_ALIGN).
  */
 int token_logprobs(stwq_ctx* ctx, const void* logits, int x_dtype, int64_t ld, int B, int V, const float* temperature,

@@ -8,8 +8,8 @@
 // its channels stay in registers from there on. A mean and a sum of squares are one reduction each over the threads of the row; the
 // squares are those of the centred values. Vectors of C channels (weights, gate, scale, shift) come from L1 and L2.
 // Bound: HBM asks for |h| + |o| in, |h'| + |y| out. 65536 rows of 1280 (fp32 stream, bf16 branch and output) take 169 us, 6.0 TB/s, 0.91 of
-// the measured copy rate; with everything in bf16 the instructions count (some 25 per channel and lane, issue slots half busy, 16 warps of up
-// to 128 registers on an SM): 8192 rows of 1920 30 us, 4.2 TB/s; 20000 of 1024 with two weighted norms 38 us, 4.4 TB/s.
+// the measured copy rate; with everything in bf16 the phases of a row, one behind the other, which 16 warps of up to 128 registers on an SM hide
+// in part (some 25 instructions per channel and lane, issue slots half busy): 8192 rows of 1920 30 us, 4.2 TB/s; 20000 of 1024 with two weighted norms 38 us, 4.4 TB/s.
 #include <cuda_bf16.h>
 
 #include "stwq_internal.cuh"

@@ -10,11 +10,11 @@
 // that at least k logits reach; the few runs that reach it (about k) are read again, their logits that reach it (about k) are
 // ranked by counting over 64-bit keys (value, then lower index), which are all different. More than 64 of them (short rows, rows
 // with few logits left: a group may hold none) first meet a second bound, the k-th largest key among the maxima of 128 groups of them: 6
-// rows of 1575, half masked, k = 32: 8 us, 76 by counting over all. Where too many reach the bound (a constant row), the k tokens are found one after the other. With few rows a cluster of up to eight blocks takes a row: slices
+// rows of 1575, half masked, k = 32: 6.5 us, 76 by counting over all. Where too many reach the bound (a constant row), the k tokens are found one after the other. With few rows a cluster of up to eight blocks takes a row: slices
 // that fit the registers give their candidates without a second read, and the first block joins sums and lists.
-// Bound by HBM with many rows: 4096 rows of 128000 bf16 logits 194 us, 5.4 TB/s, 0.83 of the measured copy rate (seven instructions and one
-// ex2 per logit, two more for its rank); 1000 rows of fp32 with twenty likeliest 110 us, 0.71 (3.4 rounds of blocks). Few rows by the
-// chain of dependent steps: 8 rows of 128000 with twenty likeliest 11.4 us (5.7 without them), 256 of 16384 with five 8.9 us.
+// Bound by HBM with many rows: 4096 rows of 128000 bf16 logits 193 us, 5.4 TB/s, 0.83 of the measured copy rate (seven instructions and one
+// ex2 per logit, two more for its rank); 1000 rows of fp32 with twenty likeliest 108 us, 0.72 (3.4 rounds of blocks). Few rows by the
+// chain of dependent steps: 8 rows of 128000 with twenty likeliest 11.4 us (5.7 without them), 256 of 16384 with five 8.3 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 

@@ -18,8 +18,8 @@
 // The warps of a block take different chunks of the same output channels, or different channels; the sums of those that split K meet
 // in shared memory and are added in warp order. Where they fit, the activations of a block lie in shared memory as operands from the
 // start: the cutting and pairing is done once, not once per tile.
-// What bounds it: with many output channels the issue of some 320 instructions per 2 KB of codes (half of them the widening, on a
-// half-rate pipe) from 16 warps of up to 128 registers: 4 x 4096 > 128000, groups of 128, 75 us, 3.6 TB/s, 0.56 of the measured copy rate
+// What bounds it: with many output channels three things of similar length that 16 warps of up to 128 registers do not hide behind each
+// other: the copies, the widening on a half-rate pipe, the products (some 320 instructions per 2 KB of codes, issue slots 0.55 busy): 4 x 4096 > 128000, groups of 128, 75 us, 3.6 TB/s, 0.56 of the measured copy rate
 // (65 us from L2 alone, 65 without the widening or without the products). Few channels: launch, first bytes, the exchange: 1 x 2048 >
 // 8192 6.6 us, 8 x 8192 > 2048 in groups of 64 8.3 us. fp32 activations take three products: 13 x 1920 > 5760 in groups of 32 10.2 us.
 #include <cooperative_groups.h>
